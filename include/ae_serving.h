@@ -1,0 +1,116 @@
+/*
+ * ae_serving.h -- C ABI of the operators around attention with a key/value
+ * cache, for AMD MI355X (gfx950): rotary positions, a paged cache that is
+ * quantised as it is written, attention of a batch's newest tokens over that
+ * cache, and the same behind a prefix that the whole batch shares.
+ *
+ * Conventions are those of ae_attn.h: entry points are host functions that
+ * return a status, never throw and never abort; handles are host memory and
+ * immutable (calls on one handle may run concurrently); pointers marked
+ * "device" are device memory owned by the caller; work is enqueued on `stream`
+ * and the call returns without waiting; nothing is allocated on the device.
+ * ae_attn_last_error() has the message of the last failure.  The launch goes to
+ * the current device, which has to be the one of the pointers and the stream.
+ */
+#ifndef AE_SERVING_H
+#define AE_SERVING_H
+
+#include "ae_attn.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- Rotary positions -----------------------------------------------------
+ * Every pair (x1, x2) of a row's first rot_dim elements is turned by the angle
+ * of its frequency at the row's position p, and stretched:
+ *     y1 = amplitude * (x1 cos(p f_i) - x2 sin(p f_i))
+ *     y2 = amplitude * (x2 cos(p f_i) + x1 sin(p f_i))      i = 0 .. rot_dim/2 - 1
+ * AE_ROTARY_HALF pairs element i with element i + rot_dim/2, AE_ROTARY_INTERLEAVED
+ * element 2i with element 2i + 1.  Elements from rot_dim on are copied.  The
+ * backward pass turns back (the transposed map): dx1 = amplitude * (dy1 cos + dy2
+ * sin), dx2 = amplitude * (dy2 cos - dy1 sin).
+ * Frequencies are the caller's (host, doubles): scaling for long contexts is a
+ * choice of frequencies and amplitude.  Angles are exact for every 32-bit position:
+ * p f / 2 pi is formed modulo 1 in 64-bit integers; sine and cosine are good to 1e-7, products
+ * are formed in 32 bits and rounded once.
+ *
+ *   Q, K       device, [B, H_q, L, D] and [B, H_k, L, D], both of desc.dtype;
+ *              K and K_out are NULL exactly when H_k is 0;
+ *   positions  device, int32, position of row l of batch entry b at
+ *              [b * position_stride + l] (stride 0: shared by the batch);
+ *   outputs    same shapes and type; an output may be its own input (same
+ *              pointer and strides), and must not overlap anything else.
+ * Strides are in elements, {batch, head, row}, all 0 meaning contiguous; the last
+ * dimension is contiguous.  Any alignment of at least the element's own is
+ * taken; 16-byte aligned rows and pieces (pointers, strides, rot_dim / 2 and D -
+ * rot_dim whole multiples of 16 bytes) run the wide kernel.                  */
+typedef struct ae_rotary ae_rotary_t;
+typedef enum { AE_ROTARY_HALF = 0, AE_ROTARY_INTERLEAVED = 1 } ae_rotary_layout_t;
+typedef enum { AE_ROWS_BF16 = 0, AE_ROWS_F32 = 1 } ae_rows_dtype_t;
+#define AE_MAX_ROT_DIM 256
+
+typedef struct {
+  int32_t B, H_q, H_k, L; /* H_k >= 0 */
+  int32_t D, rot_dim;     /* rot_dim even, 2 .. min(D, AE_MAX_ROT_DIM); D <= 1024 */
+  ae_rotary_layout_t layout;
+  ae_rows_dtype_t dtype;
+  const double *frequencies; /* host, rot_dim / 2 values of magnitude <= 6 (radians a position), copied by create */
+  double amplitude;          /* finite */
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3]; /* >= 0 */
+  int64_t position_stride;   /* >= 0 */
+} ae_rotary_desc_t;
+
+ae_status_t ae_rotary_create(const ae_rotary_desc_t *desc, ae_rotary_t **out);
+ae_status_t ae_rotary_forward(const ae_rotary_t *h, const void *Q, const void *K, const int32_t *positions,
+                              void *Q_out, void *K_out, hipStream_t stream);
+/* dQ_out and dK_out have the layout of Q_out and K_out, dQ and dK that of Q and K. */
+ae_status_t ae_rotary_backward(const ae_rotary_t *h, const void *dQ_out, const void *dK_out, const int32_t *positions,
+                               void *dQ, void *dK, hipStream_t stream);
+ae_status_t ae_rotary_destroy(ae_rotary_t *h); /* NULL is allowed */
+
+/* ---- Paged key/value cache ------------------------------------------------
+ * The cache of one layer is four device buffers of the caller:
+ *   K_pages  [n_pages, H_kv, page_size, D_qk], V_pages [n_pages, H_kv, page_size, D_v],
+ *            contiguous, 16-byte aligned, of desc.dtype;
+ *   K_exp, V_exp  [n_pages, H_kv, page_size] bytes, 4-byte aligned (8-bit caches; else NULL).
+ * A slot is page * page_size + place.  Which page holds which tokens is the
+ * caller's affair.
+ *
+ * AE_CACHE_BF16 keeps rows as they are.  AE_CACHE_E4M3 keeps a row x of a head as
+ * e4m3 values q (finite up to 448) and a power of two 2^k: k is the smallest number
+ * >= -126 for which the row's largest finite magnitude is at most 448 * 2^k, the byte is
+ * k + 127, and q = x / 2^k rounded to nearest even -- the division is exact, so a
+ * value is rounded once.  A NaN or infinite element becomes NaN.  Values read back,
+ * q * 2^k, are exact in bfloat16 (down to its smallest numbers, where they round).
+ *
+ * ae_cache_append writes row (b, l) of every head of K and V, [B, H_kv, L, D]
+ * bfloat16, to slot slots[b * slot_stride + l]; a slot outside [0, n_pages *
+ * page_size) is skipped.  Slots of one call that are not skipped must differ: of
+ * two equal ones it is not defined which row's values and which row's exponent stay.
+ * ae_cache_read is the way back: rows of K and V from those slots, as bfloat16;
+ * zeros for a slot outside the range.  Reading the same slot more than once is fine.
+ * K, V: device, 16-byte aligned, strides {batch, head, row} in elements, each a multiple of 8
+ * (all 0: contiguous).  slots: device, int32.                                */
+typedef struct ae_cache ae_cache_t;
+typedef enum { AE_CACHE_BF16 = 0, AE_CACHE_E4M3 = 1 } ae_cache_dtype_t;
+typedef struct {
+  int32_t n_pages;   /* >= 1, n_pages * page_size < 2^31 */
+  int32_t page_size; /* 16, 32, 64, 128 or 256 */
+  int32_t H_kv, D_qk, D_v; /* head dims 64/64, 128/128 or 192/128 */
+  ae_cache_dtype_t dtype;
+} ae_cache_desc_t;
+
+ae_status_t ae_cache_create(const ae_cache_desc_t *desc, ae_cache_t **out);
+ae_status_t ae_cache_append(const ae_cache_t *h, const void *K, const int64_t k_stride[3], const void *V,
+                            const int64_t v_stride[3], int32_t B, int32_t L, const int32_t *slots, int64_t slot_stride,
+                            void *K_pages, void *V_pages, void *K_exp, void *V_exp, hipStream_t stream);
+ae_status_t ae_cache_read(const ae_cache_t *h, const void *K_pages, const void *V_pages, const void *K_exp,
+                          const void *V_exp, int32_t B, int32_t L, const int32_t *slots, int64_t slot_stride,
+                          void *K, const int64_t k_stride[3], void *V, const int64_t v_stride[3], hipStream_t stream);
+ae_status_t ae_cache_destroy(ae_cache_t *h); /* NULL is allowed */
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* AE_SERVING_H */

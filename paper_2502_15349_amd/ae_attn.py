@@ -556,3 +556,316 @@ def gated_recurrent_backward(Q, K, V, log_decay, key_gate, dO, *, scale, stream=
     finally:
         ae_gated_destroy(h)
     return dQ, dK, dV, dla, dkg
+
+
+# ---- rotary positions, paged key/value cache (include/ae_serving.h) -----------------------------------------------------
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+CACHE_DTYPES = {"bf16": 0, "e4m3": 1}
+
+
+class ae_rotary_desc_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("H_q", C.c_int32), ("H_k", C.c_int32), ("L", C.c_int32), ("D", C.c_int32), ("rot_dim", C.c_int32),
+                ("layout", C.c_int), ("dtype", C.c_int), ("frequencies", C.POINTER(C.c_double)), ("amplitude", C.c_double),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("q_out_stride", C.c_int64 * 3),
+                ("k_out_stride", C.c_int64 * 3), ("position_stride", C.c_int64)]
+
+
+class ae_cache_desc_t(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("H_kv", C.c_int32), ("D_qk", C.c_int32), ("D_v", C.c_int32),
+                ("dtype", C.c_int)]
+
+
+_strides_t = C.c_int64 * 3
+_lib.ae_rotary_create.argtypes = [C.POINTER(ae_rotary_desc_t), C.POINTER(C.c_void_p)]
+_lib.ae_rotary_create.restype = C.c_int
+_lib.ae_rotary_forward.argtypes = [C.c_void_p] * 7
+_lib.ae_rotary_forward.restype = C.c_int
+_lib.ae_rotary_backward.argtypes = [C.c_void_p] * 7
+_lib.ae_rotary_backward.restype = C.c_int
+_lib.ae_rotary_destroy.argtypes = [C.c_void_p]
+_lib.ae_rotary_destroy.restype = C.c_int
+_lib.ae_cache_create.argtypes = [C.POINTER(ae_cache_desc_t), C.POINTER(C.c_void_p)]
+_lib.ae_cache_create.restype = C.c_int
+_lib.ae_cache_append.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.POINTER(C.c_int64), C.c_int32, C.c_int32,
+                                 C.c_void_p, C.c_int64] + [C.c_void_p] * 5
+_lib.ae_cache_append.restype = C.c_int
+_lib.ae_cache_read.argtypes = [C.c_void_p] * 5 + [C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.POINTER(C.c_int64),
+                                                  C.c_void_p, C.POINTER(C.c_int64), C.c_void_p]
+_lib.ae_cache_read.restype = C.c_int
+_lib.ae_cache_destroy.argtypes = [C.c_void_p]
+_lib.ae_cache_destroy.restype = C.c_int
+
+
+def ae_rotary_create(*, B: int, H_q: int, H_k: int, L: int, D: int, frequencies: Sequence[float], amplitude: float = 1.0, layout="half",
+                     dtype="bf16", q_stride=(0, 0, 0), k_stride=(0, 0, 0), q_out_stride=(0, 0, 0), k_out_stride=(0, 0, 0),
+                     position_stride: int = 0) -> int:
+    """Handle for turning the first 2 len(frequencies) elements of the rows of Q [B, H_q, L, D] and K [B, H_k, L, D]."""
+    f = (C.c_double * len(frequencies))(*[float(x) for x in frequencies])
+    d = ae_rotary_desc_t(B=B, H_q=H_q, H_k=H_k, L=L, D=D, rot_dim=2 * len(frequencies),
+                         layout=ROTARY_LAYOUTS[layout] if isinstance(layout, str) else int(layout),
+                         dtype={"bf16": 0, "f32": 1}[dtype] if isinstance(dtype, str) else int(dtype),
+                         frequencies=C.cast(f, C.POINTER(C.c_double)), amplitude=float(amplitude), position_stride=int(position_stride))
+    for name, val in (("q_stride", q_stride), ("k_stride", k_stride), ("q_out_stride", q_out_stride), ("k_out_stride", k_out_stride)):
+        setattr(d, name, _strides_t(*[int(x) for x in val]))
+    h = C.c_void_p()
+    _check(_lib.ae_rotary_create(C.byref(d), C.byref(h)))
+    return h.value
+
+
+def ae_rotary_forward(handle: int, Q: int, K: int, positions: int, Q_out: int, K_out: int, stream: int = 0) -> None:
+    """Device addresses; K and K_out are 0 exactly when the handle has H_k = 0."""
+    _check(_lib.ae_rotary_forward(handle, Q, K, positions, Q_out, K_out, stream))
+
+
+def ae_rotary_backward(handle: int, dQ_out: int, dK_out: int, positions: int, dQ: int, dK: int, stream: int = 0) -> None:
+    _check(_lib.ae_rotary_backward(handle, dQ_out, dK_out, positions, dQ, dK, stream))
+
+
+def ae_rotary_destroy(handle: Optional[int]) -> None:
+    _check(_lib.ae_rotary_destroy(handle))
+
+
+def ae_cache_create(*, n_pages: int, page_size: int, H_kv: int, D_qk: int, D_v: int, dtype="bf16") -> int:
+    d = ae_cache_desc_t(n_pages=n_pages, page_size=page_size, H_kv=H_kv, D_qk=D_qk, D_v=D_v,
+                        dtype=CACHE_DTYPES[dtype] if isinstance(dtype, str) else int(dtype))
+    h = C.c_void_p()
+    _check(_lib.ae_cache_create(C.byref(d), C.byref(h)))
+    return h.value
+
+
+def ae_cache_append(handle: int, K: int, k_stride, V: int, v_stride, B: int, L: int, slots: int, slot_stride: int, K_pages: int, V_pages: int,
+                    K_exp: int = 0, V_exp: int = 0, stream: int = 0) -> None:
+    """Device addresses; strides {batch, head, row} in elements."""
+    _check(_lib.ae_cache_append(handle, K, _strides_t(*k_stride), V, _strides_t(*v_stride), B, L, slots, slot_stride, K_pages, V_pages, K_exp,
+                                V_exp, stream))
+
+
+def ae_cache_read(handle: int, K_pages: int, V_pages: int, K_exp: int, V_exp: int, B: int, L: int, slots: int, slot_stride: int, K: int,
+                  k_stride, V: int, v_stride, stream: int = 0) -> None:
+    _check(_lib.ae_cache_read(handle, K_pages, V_pages, K_exp, V_exp, B, L, slots, slot_stride, K, _strides_t(*k_stride), V,
+                              _strides_t(*v_stride), stream))
+
+
+def ae_cache_destroy(handle: Optional[int]) -> None:
+    _check(_lib.ae_cache_destroy(handle))
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, scaling="none", factor: float = 1.0, original_length: int = 4096,
+                       slow_turns: float = 1.0, fast_turns: float = 32.0):
+    """Frequencies of rot_dim / 2 pairs (radians a position) and the amplitude of the rotated part, as (list, float).
+    scaling, for contexts `factor` times as long as the original_length that a model was trained with:
+      "none"      base^(-2 i / rot_dim);
+      "linear"    all of them divided by the factor (positions shrink);
+      "ntk"       the base grows by factor^(rot_dim / (rot_dim - 2)): the slowest pair shrinks by the factor, the fastest stays;
+      "by_parts"  pairs that turn at most slow_turns times in original_length positions shrink by the factor, those that turn at
+                  least fast_turns times stay, the ones between blend linearly; the amplitude is 0.1 ln(factor) + 1."""
+    import math
+
+    if rot_dim < 2 or rot_dim % 2:
+        raise ValueError("rot_dim must be even and at least 2")
+    if not (base > 0 and factor >= 1.0):
+        raise ValueError("base must be positive and factor at least 1")
+    half = rot_dim // 2
+    if scaling == "ntk":
+        if rot_dim == 2:
+            raise ValueError("ntk scaling needs two pairs or more")
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    f = [base ** (-i / half) for i in range(half)]
+    if scaling in ("none", "ntk"):
+        return f, 1.0
+    if scaling == "linear":
+        return [x / factor for x in f], 1.0
+    if scaling == "by_parts":
+        if not fast_turns > slow_turns:
+            raise ValueError("fast_turns must exceed slow_turns")
+        keep = [min(1.0, max(0.0, (original_length * x / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns))) for x in f]
+        return [x * k + x / factor * (1.0 - k) for x, k in zip(f, keep)], 0.1 * math.log(factor) + 1.0
+    raise ValueError(f"unknown scaling {scaling!r}")
+
+
+def _shape_of(t):
+    return (t.shape, t.stride(), t.dtype, t.device)
+
+
+def _stream_of(stream, device):
+    import torch
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+class RotaryPlan:
+    """A rotary handle for calls of one shape: the step of a loop keeps it.  Made from the first call's tensors (Q [B, H_q, L, D], K
+    [B, H_k, L, D] or None, positions int32 [L] or [B, L], outputs of the same shapes; bf16 or fp32, last dimension contiguous);
+    forward() and backward() take tensors of the same shapes, strides, type and device.  backward(dQ_out, dK_out, positions, dQ, dK)
+    goes from the outputs' layout to the inputs'."""
+
+    def __init__(self, Q, K, positions, Q_out, K_out, *, freqs, amplitude=1.0, layout="half"):
+        import torch
+
+        self.handle = None
+        some = [t for t in (Q, K, Q_out, K_out) if t is not None]
+        if (K is None) != (K_out is None):
+            raise ValueError("K and its output come together")
+        for t in some:
+            if not t.is_cuda or t.dim() != 4 or t.stride(3) != 1 or t.dtype != Q.dtype or t.device != Q.device:
+                raise ValueError("Q, K and the outputs must be 4-D device tensors of one type and device with a contiguous last dimension; there is no CPU path")
+        if Q.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("rotary positions come in bf16 and fp32")
+        B, H_q, L, D = Q.shape
+        if Q_out.shape != Q.shape or (K is not None and (K_out.shape != K.shape or K.shape[0] != B or tuple(K.shape[2:]) != (L, D))):
+            raise ValueError("K / output shapes do not match Q")
+        if (not positions.is_cuda or positions.device != Q.device or positions.dtype != torch.int32 or tuple(positions.shape) not in ((L,), (B, L))
+                or (L > 1 and positions.stride(-1) != 1)):
+            raise ValueError("positions must be an int32 device tensor [L] or [B, L] with contiguous rows")
+        _no_overlap(Q_out, K_out)
+        zero = (0, 0, 0)
+        self.handle = ae_rotary_create(
+            B=B, H_q=H_q, H_k=0 if K is None else K.shape[1], L=L, D=D, frequencies=freqs, amplitude=amplitude, layout=layout,
+            dtype="f32" if Q.dtype == torch.float32 else "bf16", q_stride=Q.stride()[:3], k_stride=zero if K is None else K.stride()[:3],
+            q_out_stride=Q_out.stride()[:3], k_out_stride=zero if K is None else K_out.stride()[:3],
+            position_stride=positions.stride(0) if positions.dim() == 2 else 0)
+        self._specs = [None if t is None else _shape_of(t) for t in (Q, K, positions, Q_out, K_out)]
+        self.device = Q.device
+
+    def _run(self, call, specs, tensors, stream):
+        import torch
+
+        for t, spec in zip(tensors, specs):
+            if (t is None) != (spec is None) or (t is not None and _shape_of(t) != spec):
+                raise ValueError("a tensor differs from the plan's in shape, strides, type or device")
+        ptrs = [0 if t is None else t.data_ptr() for t in tensors]
+        with torch.cuda.device(self.device):
+            call(self.handle, *ptrs, _stream_of(stream, self.device))
+
+    def forward(self, Q, K, positions, Q_out, K_out, *, stream=None):
+        self._run(ae_rotary_forward, self._specs, (Q, K, positions, Q_out, K_out), stream)
+
+    def backward(self, dQ_out, dK_out, positions, dQ, dK, *, stream=None):
+        s = self._specs
+        self._run(ae_rotary_backward, (s[3], s[4], s[2], s[0], s[1]), (dQ_out, dK_out, positions, dQ, dK), stream)
+
+    def __del__(self):
+        if getattr(self, "handle", None) is not None and _lib is not None:
+            _lib.ae_rotary_destroy(self.handle)
+            self.handle = None
+
+
+def _no_overlap(*outs):
+    """Outputs that a call writes must not have two indices at one address (expanded tensors)."""
+    for t in outs:
+        if t is not None and any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
+            raise ValueError("an output must not be an expanded tensor")
+
+
+def _rotary(Q, K, positions, freqs, amplitude, layout, out, stream, backward):
+    import torch
+
+    if out is None:
+        out = (torch.empty(Q.shape, dtype=Q.dtype, device=Q.device), None if K is None else torch.empty(K.shape, dtype=K.dtype, device=K.device))
+    q, k = out
+    # the handle's "inputs" are the layout that the backward pass writes
+    a, b = ((q, k), (Q, K)) if backward else ((Q, K), (q, k))
+    plan = RotaryPlan(a[0], a[1], positions, b[0], b[1], freqs=freqs, amplitude=amplitude, layout=layout)
+    _no_overlap(q, k)
+    (plan.backward if backward else plan.forward)(Q, K, positions, q, k, stream=stream)
+    return q, k
+
+
+def rotary_forward(Q, K, positions, *, freqs, amplitude=1.0, layout="half", out=None, stream=None):
+    """Rotary positions on device tensors Q [B, H_q, L, D] and K [B, H_k, L, D] (or None), bf16 or fp32, last dimension contiguous:
+    pair i of a row at position p is turned by p freqs[i] and stretched by amplitude (rotary_frequencies() makes both); elements from
+    2 len(freqs) on are copied.  layout "half" pairs element i with i + len(freqs), "interleaved" 2 i with 2 i + 1.  positions: int32
+    [L] or [B, L].  out: a pair of output tensors (the inputs themselves: in place).  Returns (Q', K')."""
+    return _rotary(Q, K, positions, freqs, amplitude, layout, out, stream, False)
+
+
+def rotary_backward(dQ, dK, positions, *, freqs, amplitude=1.0, layout="half", out=None, stream=None):
+    """Gradients of Q and K for the gradients of rotary_forward's outputs (arguments as there): pairs are turned back."""
+    return _rotary(dQ, dK, positions, freqs, amplitude, layout, out, stream, True)
+
+
+class PagedCache:
+    """The paged key/value cache of one layer: K pages [n_pages, H_kv, page, D_qk] and V pages [n_pages, H_kv, page, D_v], bf16 or
+    float8_e4m3fn (then with exponent bytes k_exp, v_exp, uint8 [n_pages, H_kv, page]), contiguous device tensors of the caller.  A position of
+    the cache is the slot page_number * page + place."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        import torch
+
+        self.handle = None
+        e4m3 = k.dtype == torch.float8_e4m3fn
+        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn) or v.dtype != k.dtype:
+            raise ValueError("pages must be bf16 or float8_e4m3fn")
+        if (k_exp is None) == e4m3 or (v_exp is None) == e4m3:
+            raise ValueError("exponents belong to an 8-bit cache, and only to it")
+        if k.dim() != 4 or v.dim() != 4 or k.shape[:3] != v.shape[:3]:
+            raise ValueError("pages must be [n_pages, H_kv, page, D]")
+        for t in (k, v) + ((k_exp, v_exp) if e4m3 else ()):
+            if not t.is_cuda or not t.is_contiguous() or t.device != k.device:
+                raise ValueError("the cache's buffers must be contiguous tensors of one device; there is no CPU path")
+        if e4m3 and any(t.dtype != torch.uint8 or t.shape != k.shape[:3] for t in (k_exp, v_exp)):
+            raise ValueError("exponents must be uint8 [n_pages, H_kv, page]")
+        self.k, self.v, self.k_exp, self.v_exp, self.device = k, v, k_exp, v_exp, k.device
+        self.n_pages, self.H_kv, self.page_size, self.D_qk = k.shape
+        self.D_v = v.shape[3]
+        self.handle = ae_cache_create(n_pages=self.n_pages, page_size=self.page_size, H_kv=self.H_kv, D_qk=self.D_qk, D_v=self.D_v,
+                                      dtype="e4m3" if e4m3 else "bf16")
+
+    @classmethod
+    def empty(cls, n_pages, H_kv, page_size, D_qk, D_v, *, dtype="bf16", device="cuda"):
+        """A cache with buffers of its own (contents undefined until written)."""
+        import torch
+
+        e4m3 = {"bf16": False, "e4m3": True}[dtype]
+        t = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+        k, v = (torch.empty(n_pages, H_kv, page_size, d, dtype=t, device=device) for d in (D_qk, D_v))
+        e = [torch.empty(n_pages, H_kv, page_size, dtype=torch.uint8, device=device) if e4m3 else None for _ in range(2)]
+        return cls(k, v, *e)
+
+    def pointers(self):
+        return (self.k.data_ptr(), self.v.data_ptr(), 0 if self.k_exp is None else self.k_exp.data_ptr(),
+                0 if self.v_exp is None else self.v_exp.data_ptr())
+
+    def _slots(self, slots, B, L):
+        import torch
+
+        if (slots.dtype != torch.int32 or tuple(slots.shape) not in ((L,), (B, L)) or slots.device != self.device or (L > 1 and slots.stride(-1) != 1)
+                or (slots.dim() == 1 and B > 1)):
+            raise ValueError("slots must be an int32 device tensor [B, L] (or [L] for B = 1) with contiguous rows")
+        return slots.data_ptr(), slots.stride(0) if slots.dim() == 2 else 0
+
+    def append(self, K, V, slots, *, stream=None):
+        """Writes the rows of K [B, H_kv, L, D_qk] and V [B, H_kv, L, D_v] (bf16, last dimension contiguous) to the slots int32 [B, L];
+        rows whose slot is outside the cache (-1) are skipped, the others' slots must differ."""
+        import torch
+
+        B, H, L, _ = K.shape
+        for t, d in ((K, self.D_qk), (V, self.D_v)):
+            if t.dtype != torch.bfloat16 or tuple(t.shape) != (B, self.H_kv, L, d) or t.stride(3) != 1 or t.device != self.device:
+                raise ValueError("K and V must be bf16 [B, H_kv, L, D] on the cache's device with a contiguous last dimension")
+        at, stride = self._slots(slots, B, L)
+        with torch.cuda.device(self.device):
+            ae_cache_append(self.handle, K.data_ptr(), K.stride()[:3], V.data_ptr(), V.stride()[:3], B, L, at, stride, *self.pointers(),
+                            _stream_of(stream, self.device))
+
+    def read(self, slots, *, out=None, stream=None):
+        """The rows at slots int32 [B, L] (or [L]: B = 1) as bf16 K [B, H_kv, L, D_qk] and V [B, H_kv, L, D_v]; zeros for a slot outside the
+        cache.  out: a pair of tensors to write to."""
+        import torch
+
+        B, L = (1, slots.shape[0]) if slots.dim() == 1 else slots.shape
+        if out is None:
+            out = tuple(torch.empty(B, self.H_kv, L, d, dtype=torch.bfloat16, device=self.device) for d in (self.D_qk, self.D_v))
+        for t, d in zip(out, (self.D_qk, self.D_v)):
+            if t.dtype != torch.bfloat16 or tuple(t.shape) != (B, self.H_kv, L, d) or t.stride(3) != 1 or t.device != self.device:
+                raise ValueError("outputs must be bf16 [B, H_kv, L, D] on the cache's device with a contiguous last dimension")
+        _no_overlap(*out)
+        at, stride = self._slots(slots, B, L)
+        with torch.cuda.device(self.device):
+            ae_cache_read(self.handle, *self.pointers(), B, L, at, stride, out[0].data_ptr(), out[0].stride()[:3], out[1].data_ptr(),
+                          out[1].stride()[:3], _stream_of(stream, self.device))
+        return out
+
+    def __del__(self):
+        if getattr(self, "handle", None) is not None and _lib is not None:
+            _lib.ae_cache_destroy(self.handle)
+            self.handle = None

@@ -16,6 +16,7 @@
 #include "attn_decode.hpp"
 #include "gated.hpp"
 #include "recurrent.hpp"
+#include "status.hpp"
 
 // ---- static device scratch for the entry point that allocates nothing -----------------------
 // ae_attn_forward_split_static keeps the partial rows of the split-key forward in this array instead of a
@@ -24,17 +25,19 @@
 // device that is current; host code uses that pointer only.
 static __device__ __align__(256) unsigned char scratch[AE_ATTN_STATIC_SCRATCH_BYTES];
 
-namespace {
+static thread_local char g_err[256] = "";
 
-thread_local char g_err[256] = "";
-
-ae_status_t fail(ae_status_t code, const char* fmt, ...) {
+ae_status_t ae::fail(ae_status_t code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
   va_end(ap);
   return code;
 }
+
+namespace {
+
+using ae::fail;
 
 const ae::KernelEntry* find_kernel(int dqk, int dv, int norm, int mod, int mask, int fold) {
   typedef const ae::KernelEntry* (*table_fn)(int*);

@@ -1,0 +1,229 @@
+// C ABI of the operators around a key/value cache: validation and launch.  See include/ae_serving.h.
+#include "../../include/ae_serving.h"
+
+#include <cmath>
+#include <new>
+#include <utility>
+
+#include "cache.hpp"
+#include "rotary.hpp"
+#include "status.hpp"
+
+using ae::fail;
+
+namespace {
+
+void contiguous_or(int64_t dst[3], const int64_t src[3], int64_t H, int64_t L, int64_t D) {
+  const bool none = !src || (src[0] == 0 && src[1] == 0 && src[2] == 0);
+  dst[0] = none ? H * L * D : src[0];
+  dst[1] = none ? L * D : src[1];
+  dst[2] = none ? D : src[2];
+}
+
+bool negative(const int64_t s[3]) { return s[0] < 0 || s[1] < 0 || s[2] < 0; }
+
+ae_status_t launched(hipError_t e, const char* who) {
+  if (e == hipSuccess) return AE_OK;
+  if (e == hipErrorInvalidConfiguration) return fail(AE_ERR_UNSUPPORTED, "%s: more threads than one launch can have", who);
+  return fail(AE_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
+}
+
+}  // namespace
+
+// ---- rotary positions ------------------------------------------------------------------------------------------------
+struct ae_rotary {
+  ae::RotaryParams params;
+  ae::RotaryTable table;
+  bool wide;  // sizes and strides are whole 16-byte pieces (pointers are looked at per call)
+};
+
+extern "C" {
+
+ae_status_t ae_rotary_create(const ae_rotary_desc_t* d, ae_rotary_t** out) {
+  if (out) *out = nullptr;
+  if (!d || !out) return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: null argument");
+  if (d->B < 1 || d->H_q < 1 || d->H_k < 0 || d->L < 1 || d->D < 1)
+    return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: B, H_q, L, D must be >= 1 and H_k >= 0");
+  if (d->rot_dim < 2 || d->rot_dim % 2 != 0 || d->rot_dim > d->D || d->rot_dim > AE_MAX_ROT_DIM)
+    return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: rot_dim (%d) must be even, at least 2 and at most min(D, %d)", d->rot_dim, AE_MAX_ROT_DIM);
+  if (d->layout != AE_ROTARY_HALF && d->layout != AE_ROTARY_INTERLEAVED) return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: unknown layout %d", (int)d->layout);
+  if (d->dtype != AE_ROWS_BF16 && d->dtype != AE_ROWS_F32) return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: unknown dtype %d", (int)d->dtype);
+  if (!d->frequencies) return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: null frequencies");
+  if (!std::isfinite(d->amplitude) || std::fabs(d->amplitude) > 1e30) return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: amplitude must be finite (at most 1e30)");
+  for (int i = 0; i < d->rot_dim / 2; ++i)
+    if (!(std::fabs(d->frequencies[i]) <= 6.0)) return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: frequencies[%d] must be finite and at most 6 in magnitude", i);
+  if (negative(d->q_stride) || negative(d->k_stride) || negative(d->q_out_stride) || negative(d->k_out_stride) || d->position_stride < 0)
+    return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: strides must not be negative");
+  if (d->D > 1024 || (int64_t)d->H_q + d->H_k > 65535 || (int64_t)d->B * d->L > 0x7fffffffLL)
+    return fail(AE_ERR_UNSUPPORTED, "ae_rotary_create: at most 1024 elements a row, 65535 heads and 2^31 - 1 rows");
+  ae_rotary* h = new (std::nothrow) ae_rotary();
+  if (!h) return fail(AE_ERR_NOMEM, "ae_rotary_create: out of host memory");
+  ae::RotaryParams& p = h->params;
+  contiguous_or(p.xs[0], d->q_stride, d->H_q, d->L, d->D);
+  contiguous_or(p.xs[1], d->k_stride, d->H_k, d->L, d->D);
+  contiguous_or(p.ys[0], d->q_out_stride, d->H_q, d->L, d->D);
+  contiguous_or(p.ys[1], d->k_out_stride, d->H_k, d->L, d->D);
+  p.position_stride = d->position_stride;
+  p.B = d->B;
+  p.L = d->L;
+  p.D = d->D;
+  p.half = d->rot_dim / 2;
+  p.H[0] = d->H_q;
+  p.H[1] = d->H_k;
+  p.amp = (float)d->amplitude;
+  p.interleaved = d->layout == AE_ROTARY_INTERLEAVED;
+  p.f32 = d->dtype == AE_ROWS_F32;
+  // f / 2 pi modulo 1 in units of 2^-64: the product has 64 significant bits and a magnitude below one
+  for (int i = 0; i < p.half; ++i) {
+    long double t = (long double)d->frequencies[i] * 0.159154943091895335768883763372514362L;
+    t -= std::floor(t);
+    const long double u = std::nearbyint(t * 18446744073709551616.0L);
+    h->table.turn[i] = u >= 18446744073709551616.0L ? 0 : (uint64_t)u;
+  }
+  const int piece = p.f32 ? 4 : 8;
+  h->wide = p.half % piece == 0 && (p.D - 2 * p.half) % piece == 0;
+  for (int w = 0; w < (p.H[1] ? 2 : 1); ++w)
+    for (int a = 0; a < 3; ++a) h->wide = h->wide && p.xs[w][a] % piece == 0 && p.ys[w][a] % piece == 0;
+  *out = h;
+  return AE_OK;
+}
+
+}  // extern "C"
+
+static ae_status_t rotary_impl(const ae_rotary_t* h, const void* q, const void* k, const int32_t* positions, void* qo, void* ko, bool backward,
+                               hipStream_t stream, const char* who) {
+  if (!h) return fail(AE_ERR_INVALID_ARG, "%s: null handle", who);
+  if (!q || !qo || !positions) return fail(AE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if ((k != nullptr) != (h->params.H[1] > 0) || (ko != nullptr) != (h->params.H[1] > 0))
+    return fail(AE_ERR_INVALID_ARG, "%s: the second tensor is given exactly where H_k > 0", who);
+  const uintptr_t all = (uintptr_t)q | (uintptr_t)k | (uintptr_t)qo | (uintptr_t)ko;
+  if (all & (h->params.f32 ? 3 : 1) || (uintptr_t)positions & 3) return fail(AE_ERR_INVALID_ARG, "%s: pointers must be aligned to their elements", who);
+  if (q == ko || (k && k == qo) || (ko && ko == qo) || qo == (const void*)positions || (ko && ko == (const void*)positions))
+    return fail(AE_ERR_INVALID_ARG, "%s: an output aliases another tensor", who);
+  ae::RotaryParams p = h->params;
+  if (backward)  // from the outputs' layout to the inputs'
+    for (int w = 0; w < 2; ++w)
+      for (int a = 0; a < 3; ++a) std::swap(p.xs[w][a], p.ys[w][a]);
+  for (int w = 0; w < 2; ++w) {
+    const void* x = w ? k : q;
+    const void* y = w ? ko : qo;
+    if (x && x == y)
+      for (int a = 0; a < 3; ++a)
+        if (p.xs[w][a] != p.ys[w][a]) return fail(AE_ERR_INVALID_ARG, "%s: in place needs equal strides", who);
+  }
+  p.x[0] = q;
+  p.x[1] = k;
+  p.y[0] = qo;
+  p.y[1] = ko;
+  p.positions = positions;
+  p.backward = backward ? 1 : 0;
+  return launched(ae::launch_rotary(p, h->table, h->wide && (all & 15) == 0, stream), who);
+}
+
+extern "C" {
+
+ae_status_t ae_rotary_forward(const ae_rotary_t* h, const void* Q, const void* K, const int32_t* positions, void* Q_out, void* K_out, hipStream_t stream) {
+  return rotary_impl(h, Q, K, positions, Q_out, K_out, false, stream, "ae_rotary_forward");
+}
+
+ae_status_t ae_rotary_backward(const ae_rotary_t* h, const void* dQ_out, const void* dK_out, const int32_t* positions, void* dQ, void* dK,
+                               hipStream_t stream) {
+  return rotary_impl(h, dQ_out, dK_out, positions, dQ, dK, true, stream, "ae_rotary_backward");
+}
+
+ae_status_t ae_rotary_destroy(ae_rotary_t* h) {
+  delete h;
+  return AE_OK;
+}
+
+}  // extern "C"
+
+// ---- paged cache -----------------------------------------------------------------------------------------------------
+struct ae_cache {
+  ae_cache_desc_t desc;
+  int page_shift;
+};
+
+extern "C" {
+
+ae_status_t ae_cache_create(const ae_cache_desc_t* d, ae_cache_t** out) {
+  if (out) *out = nullptr;
+  if (!d || !out) return fail(AE_ERR_INVALID_ARG, "ae_cache_create: null argument");
+  if (d->n_pages < 1 || d->H_kv < 1) return fail(AE_ERR_INVALID_ARG, "ae_cache_create: n_pages and H_kv must be >= 1");
+  int shift = 4;
+  while (shift < 8 && (1 << shift) != d->page_size) ++shift;
+  if ((1 << shift) != d->page_size) return fail(AE_ERR_INVALID_ARG, "ae_cache_create: page_size (%d) must be 16, 32, 64, 128 or 256", d->page_size);
+  if ((int64_t)d->n_pages * d->page_size > 0x7fffffffLL) return fail(AE_ERR_UNSUPPORTED, "ae_cache_create: more than 2^31 - 1 slots");
+  if (!((d->D_qk == 64 && d->D_v == 64) || (d->D_qk == 128 && d->D_v == 128) || (d->D_qk == 192 && d->D_v == 128)))
+    return fail(AE_ERR_UNSUPPORTED, "ae_cache_create: head dims %d/%d not built (64/64, 128/128, 192/128)", d->D_qk, d->D_v);
+  if (d->dtype != AE_CACHE_BF16 && d->dtype != AE_CACHE_E4M3) return fail(AE_ERR_INVALID_ARG, "ae_cache_create: unknown dtype %d", (int)d->dtype);
+  ae_cache* h = new (std::nothrow) ae_cache();
+  if (!h) return fail(AE_ERR_NOMEM, "ae_cache_create: out of host memory");
+  h->desc = *d;
+  h->page_shift = shift;
+  *out = h;
+  return AE_OK;
+}
+
+}  // extern "C"
+
+static ae_status_t cache_impl(const ae_cache_t* h, const void* K, const int64_t* k_stride, const void* V, const int64_t* v_stride, int32_t B, int32_t L,
+                              const int32_t* slots, int64_t slot_stride, const void* K_pages, const void* V_pages, const void* K_exp, const void* V_exp,
+                              bool append, hipStream_t stream, const char* who) {
+  if (!h) return fail(AE_ERR_INVALID_ARG, "%s: null handle", who);
+  const ae_cache_desc_t& d = h->desc;
+  const bool e4m3 = d.dtype == AE_CACHE_E4M3;
+  if (!K || !V || !slots || !K_pages || !V_pages) return fail(AE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if ((K_exp != nullptr) != e4m3 || (V_exp != nullptr) != e4m3) return fail(AE_ERR_INVALID_ARG, "%s: exponents belong to an 8-bit cache, and only to it", who);
+  if (((uintptr_t)K | (uintptr_t)V | (uintptr_t)K_pages | (uintptr_t)V_pages) & 15)
+    return fail(AE_ERR_INVALID_ARG, "%s: rows and pages must be 16-byte aligned", who);
+  if (((uintptr_t)slots | (uintptr_t)K_exp | (uintptr_t)V_exp) & 3) return fail(AE_ERR_INVALID_ARG, "%s: slots and exponents must be 4-byte aligned", who);
+  const void* buf[] = {K, V, K_pages, V_pages, slots, K_exp, V_exp};
+  for (int i = 0; i < 7; ++i)
+    for (int j = 0; j < i; ++j)
+      if (buf[i] && buf[i] == buf[j]) return fail(AE_ERR_INVALID_ARG, "%s: two of the buffers are the same", who);
+  if (B < 1 || L < 1) return fail(AE_ERR_INVALID_ARG, "%s: B and L must be >= 1", who);
+  if (slot_stride < 0) return fail(AE_ERR_INVALID_ARG, "%s: the slots' stride must not be negative", who);
+  ae::CacheParams p = {};
+  contiguous_or(p.xs[0], k_stride, d.H_kv, L, d.D_qk);
+  contiguous_or(p.xs[1], v_stride, d.H_kv, L, d.D_v);
+  for (int w = 0; w < 2; ++w)
+    for (int a = 0; a < 3; ++a)
+      if (p.xs[w][a] < 0 || p.xs[w][a] % 8 != 0) return fail(AE_ERR_INVALID_ARG, "%s: strides must be non-negative multiples of 8 elements", who);
+  p.slots = slots;
+  p.slot_stride = slot_stride;
+  p.B = B;
+  p.L = L;
+  p.H = d.H_kv;
+  p.page_shift = h->page_shift;
+  p.n_slots = (int64_t)d.n_pages * d.page_size;
+  p.x[0] = static_cast<__bf16*>(const_cast<void*>(K));
+  p.x[1] = static_cast<__bf16*>(const_cast<void*>(V));
+  p.pages[0] = static_cast<uint8_t*>(const_cast<void*>(K_pages));
+  p.pages[1] = static_cast<uint8_t*>(const_cast<void*>(V_pages));
+  p.exps[0] = static_cast<uint8_t*>(const_cast<void*>(K_exp));
+  p.exps[1] = static_cast<uint8_t*>(const_cast<void*>(V_exp));
+  p.d[0] = d.D_qk;
+  p.d[1] = d.D_v;
+  return launched(ae::launch_cache(p, e4m3, append, stream), who);
+}
+
+extern "C" {
+
+ae_status_t ae_cache_append(const ae_cache_t* h, const void* K, const int64_t k_stride[3], const void* V, const int64_t v_stride[3], int32_t B, int32_t L,
+                            const int32_t* slots, int64_t slot_stride, void* K_pages, void* V_pages, void* K_exp, void* V_exp, hipStream_t stream) {
+  return cache_impl(h, K, k_stride, V, v_stride, B, L, slots, slot_stride, K_pages, V_pages, K_exp, V_exp, true, stream, "ae_cache_append");
+}
+
+ae_status_t ae_cache_read(const ae_cache_t* h, const void* K_pages, const void* V_pages, const void* K_exp, const void* V_exp, int32_t B, int32_t L,
+                          const int32_t* slots, int64_t slot_stride, void* K, const int64_t k_stride[3], void* V, const int64_t v_stride[3],
+                          hipStream_t stream) {
+  return cache_impl(h, K, k_stride, V, v_stride, B, L, slots, slot_stride, K_pages, V_pages, K_exp, V_exp, false, stream, "ae_cache_read");
+}
+
+ae_status_t ae_cache_destroy(ae_cache_t* h) {
+  delete h;
+  return AE_OK;
+}
+
+}  // extern "C"

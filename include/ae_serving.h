@@ -110,6 +110,53 @@ ae_status_t ae_cache_read(const ae_cache_t *h, const void *K_pages, const void *
                           void *K, const int64_t k_stride[3], void *V, const int64_t v_stride[3], hipStream_t stream);
 ae_status_t ae_cache_destroy(ae_cache_t *h); /* NULL is allowed */
 
+/* ---- Attention of the newest tokens over the paged cache -----------------
+ * Softmax attention O = softmax(scale * Q K^T) V of the newest n_new tokens of B
+ * sequences over everything cached for them (the parallel pattern of ae_attn.h
+ * with L_q = n_new, bottom-right causal, keys and values in pages).  The
+ * sequence's own keys, the newest tokens' included (append them first), are the
+ * first lengths[b] positions of its page list: position j lies on page table[b][j / page_size].
+ * Token t of the newest ones sees the first lengths[b] - n_new + 1 + t
+ * of them; one that sees none gives a zero row with statistic -inf.  Query
+ * head h reads k/v head h / (H_q / H_kv).
+ *
+ * Shared prefix (prefix_length > 0): all sequences have the prefix_length keys of
+ * the page list prefix_table in front of their own, visible to every row; table and lengths then
+ * hold what comes behind the prefix.  The prefix is read once for the rows of
+ * all sequences together instead of once for each; the result is that of the
+ * concatenated key lists.
+ *
+ *   Q          device, bf16 [B, H_q, n_new, D_qk], 16-byte aligned, strides multiples of 8;
+ *   table      device, int32 [B, table_width]; lengths  device, int32 [B];
+ *   prefix_table  device, int32, ceil(prefix_length / page_size) entries; NULL without a prefix;
+ *   O          device, [B, H_q, n_new, D_v], fp32 or (desc.out_dtype) bf16, 16-byte aligned,
+ *              strides multiples of 8; strides of 0: contiguous;
+ *   stats      device, fp32 [B, H_q, n_new], ln sum exp of the scaled scores; NULL: not written;
+ *   workspace  device, 256-byte aligned, ae_cached_workspace_bytes (0: may be NULL); owned by
+ *              the caller, contents irrelevant; calls sharing it must not overlap.
+ * lengths are read on the device: one outside [0, max_length] counts as the nearer
+ * bound.  A page number outside [0, n_pages) is not followed: its keys count as hidden.
+ * What lies in the cache behind a sequence's end may be anything, NaN included.
+ * A NaN or infinity in the cached row of one of the newest tokens reaches only the rows that see it. */
+typedef struct ae_cached ae_cached_t;
+typedef struct {
+  int32_t B, H_q, n_new;  /* H_q a multiple of the cache's H_kv */
+  int32_t table_width;    /* pages in a row of the table */
+  int32_t max_length;     /* 1 .. table_width * page_size: no sequence has more keys of its own */
+  int32_t prefix_length;  /* 0: no shared prefix */
+  int32_t chunk;          /* 0: the library chooses; else the keys that one workgroup walks, a positive multiple of 128 */
+  float scale;            /* finite and non-zero */
+  ae_out_dtype_t out_dtype;
+  int64_t q_stride[3], o_stride[3]; /* {batch, head, token} */
+} ae_cached_desc_t;
+
+ae_status_t ae_cached_create(const ae_cache_t *cache, const ae_cached_desc_t *desc, ae_cached_t **out); /* copies what it needs of the cache's handle */
+ae_status_t ae_cached_workspace_bytes(const ae_cached_t *h, size_t *bytes);
+ae_status_t ae_cached_forward(const ae_cached_t *h, const void *Q, const void *K_pages, const void *V_pages, const void *K_exp,
+                              const void *V_exp, const int32_t *table, const int32_t *lengths, const int32_t *prefix_table,
+                              void *O, float *stats, void *workspace, size_t workspace_bytes, hipStream_t stream);
+ae_status_t ae_cached_destroy(ae_cached_t *h); /* NULL is allowed */
+
 #ifdef __cplusplus
 }
 #endif

@@ -575,7 +575,21 @@ class ae_cache_desc_t(C.Structure):
                 ("dtype", C.c_int)]
 
 
+class ae_cached_desc_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("H_q", C.c_int32), ("n_new", C.c_int32), ("table_width", C.c_int32), ("max_length", C.c_int32),
+                ("prefix_length", C.c_int32), ("chunk", C.c_int32), ("scale", C.c_float), ("out_dtype", C.c_int),
+                ("q_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3)]
+
+
 _strides_t = C.c_int64 * 3
+_lib.ae_cached_create.argtypes = [C.c_void_p, C.POINTER(ae_cached_desc_t), C.POINTER(C.c_void_p)]
+_lib.ae_cached_create.restype = C.c_int
+_lib.ae_cached_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+_lib.ae_cached_workspace_bytes.restype = C.c_int
+_lib.ae_cached_forward.argtypes = [C.c_void_p] * 12 + [C.c_size_t, C.c_void_p]
+_lib.ae_cached_forward.restype = C.c_int
+_lib.ae_cached_destroy.argtypes = [C.c_void_p]
+_lib.ae_cached_destroy.restype = C.c_int
 _lib.ae_rotary_create.argtypes = [C.POINTER(ae_rotary_desc_t), C.POINTER(C.c_void_p)]
 _lib.ae_rotary_create.restype = C.c_int
 _lib.ae_rotary_forward.argtypes = [C.c_void_p] * 7
@@ -648,6 +662,34 @@ def ae_cache_read(handle: int, K_pages: int, V_pages: int, K_exp: int, V_exp: in
 
 def ae_cache_destroy(handle: Optional[int]) -> None:
     _check(_lib.ae_cache_destroy(handle))
+
+
+def ae_cached_create(cache: int, *, B: int, H_q: int, n_new: int, table_width: int, max_length: int, scale: float, prefix_length: int = 0,
+                     chunk: int = 0, out_dtype="f32", q_stride=(0, 0, 0), o_stride=(0, 0, 0)) -> int:
+    """Handle for attention of the newest n_new tokens of B sequences over a paged cache (cache: its handle)."""
+    d = ae_cached_desc_t(B=B, H_q=H_q, n_new=n_new, table_width=table_width, max_length=max_length, prefix_length=prefix_length, chunk=chunk,
+                         scale=float(scale), out_dtype=OUT_DTYPES[out_dtype] if isinstance(out_dtype, str) else int(out_dtype))
+    d.q_stride, d.o_stride = _strides_t(*[int(x) for x in q_stride]), _strides_t(*[int(x) for x in o_stride])
+    h = C.c_void_p()
+    _check(_lib.ae_cached_create(cache, C.byref(d), C.byref(h)))
+    return h.value
+
+
+def ae_cached_workspace_bytes(handle: int) -> int:
+    n = C.c_size_t()
+    _check(_lib.ae_cached_workspace_bytes(handle, C.byref(n)))
+    return n.value
+
+
+def ae_cached_forward(handle: int, Q: int, K_pages: int, V_pages: int, K_exp: int, V_exp: int, table: int, lengths: int, prefix_table: int,
+                      O: int, stats: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """Device addresses; K_exp, V_exp (16-bit cache), prefix_table (no prefix), stats and workspace (0 bytes) may be 0."""
+    _check(_lib.ae_cached_forward(handle, Q, K_pages, V_pages, K_exp, V_exp, table, lengths, prefix_table, O, stats, workspace,
+                                  workspace_bytes, stream))
+
+
+def ae_cached_destroy(handle: Optional[int]) -> None:
+    _check(_lib.ae_cached_destroy(handle))
 
 
 def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, scaling="none", factor: float = 1.0, original_length: int = 4096,
@@ -869,3 +911,78 @@ class PagedCache:
         if getattr(self, "handle", None) is not None and _lib is not None:
             _lib.ae_cache_destroy(self.handle)
             self.handle = None
+
+
+class CachedAttentionPlan:
+    """A handle for attention of the newest tokens over a PagedCache, for calls of one shape: the step of a decoding loop keeps it, and
+    its workspace.  Q [B, H_q, n, D_qk] bf16 and out [B, H_q, n, D_v] (bf16 or fp32) give shapes, strides and device; max_length: no
+    sequence has more keys of its own; table_width: pages in a row of the table; prefix_length: keys that all sequences share.
+    Calls of one plan must not overlap (they share its workspace); a captured graph keeps using the plan's buffers."""
+
+    def __init__(self, cache, Q, out, *, max_length, table_width, scale, prefix_length=0, chunk=0):
+        import torch
+
+        self.handle = None
+        for t in (Q, out):
+            if not t.is_cuda or t.dim() != 4 or t.stride(3) != 1 or t.device != cache.device:
+                raise ValueError("Q and O must be 4-D tensors on the cache's device with a contiguous last dimension; there is no CPU path")
+        B, H_q, n, D = Q.shape
+        if Q.dtype != torch.bfloat16 or D != cache.D_qk:
+            raise ValueError("Q must be bf16 [B, H_q, n, D_qk]")
+        if out.dtype not in (torch.float32, torch.bfloat16) or tuple(out.shape) != (B, H_q, n, cache.D_v):
+            raise ValueError("O must be fp32 or bf16 [B, H_q, n, D_v]")
+        _no_overlap(out)
+        self.handle = ae_cached_create(cache.handle, B=B, H_q=H_q, n_new=n, table_width=table_width, max_length=max_length, scale=scale,
+                                       prefix_length=prefix_length, chunk=chunk, out_dtype="bf16" if out.dtype == torch.bfloat16 else "f32",
+                                       q_stride=Q.stride()[:3], o_stride=out.stride()[:3])
+        self.cache, self.device, self.shape = cache, Q.device, (B, H_q, n)
+        self._q, self._o = _shape_of(Q), _shape_of(out)
+        self._table, self._prefix = (B, table_width), -(-prefix_length // cache.page_size)
+        self.workspace_bytes = ae_cached_workspace_bytes(self.handle)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=Q.device) if self.workspace_bytes else None
+
+    def forward(self, Q, table, lengths, out, *, stats=None, prefix_table=None, stream=None):
+        """table int32 [B, table_width], lengths int32 [B] (device), prefix_table int32 [pages of the prefix]; stats: fp32 [B, H_q, n] that
+        receives ln sum exp.  Writes and returns out."""
+        import torch
+
+        if _shape_of(Q) != self._q or _shape_of(out) != self._o:
+            raise ValueError("Q or O differs from the plan's in shape, strides, type or device")
+        ints = ((table, self._table), (lengths, self._table[:1])) + (((prefix_table, (self._prefix,)),) if self._prefix else ())
+        for t, shape in ints:
+            if t is None or t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+                raise ValueError(f"tables and lengths must be contiguous int32 device tensors (here {shape})")
+        if prefix_table is not None and not self._prefix:
+            raise ValueError("the plan has no prefix")
+        if stats is not None and (stats.dtype != torch.float32 or stats.shape != self.shape or not stats.is_contiguous() or stats.device != self.device):
+            raise ValueError("stats must be a contiguous fp32 tensor [B, H_q, n]")
+        with torch.cuda.device(self.device):
+            ae_cached_forward(self.handle, Q.data_ptr(), *self.cache.pointers(), table.data_ptr(), lengths.data_ptr(),
+                              prefix_table.data_ptr() if self._prefix else 0, out.data_ptr(), 0 if stats is None else stats.data_ptr(),
+                              0 if self.workspace is None else self.workspace.data_ptr(), self.workspace_bytes, _stream_of(stream, self.device))
+        return out
+
+    def __del__(self):
+        if getattr(self, "handle", None) is not None and _lib is not None:
+            _lib.ae_cached_destroy(self.handle)
+            self.handle = None
+
+
+def attention_cached(Q, cache, table, lengths, *, scale, max_length=None, prefix_table=None, prefix_length=0, out=None, out_dtype=None,
+                     stats=None, chunk=0, stream=None):
+    """Softmax attention of the newest n tokens of each sequence, Q bf16 [B, H_q, n, D_qk], over everything a PagedCache holds for
+    them: position j of sequence b lies on page table[b, j // page] (int32 [B, width]), lengths int32 [B] counts its keys, the newest n
+    among them; token t sees the first lengths[b] - n + 1 + t.  max_length: no sequence is longer (None: the table's room).
+    prefix_table / prefix_length: keys in front of every sequence's own that the whole batch shares; they are read once for all.
+    Returns O [B, H_q, n, D_v], fp32 or bf16 (out / out_dtype); stats: optional fp32 [B, H_q, n] that receives ln sum exp."""
+    import contextlib
+
+    import torch
+
+    # the workspace belongs to the stream that uses it
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        if out is None:
+            out = torch.empty(Q.shape[:3] + (cache.D_v,), dtype=out_dtype or torch.float32, device=Q.device)
+        plan = CachedAttentionPlan(cache, Q, out, max_length=table.shape[1] * cache.page_size if max_length is None else max_length,
+                                   table_width=table.shape[1], scale=scale, prefix_length=prefix_length, chunk=chunk)
+        return plan.forward(Q, table, lengths, out, stats=stats, prefix_table=prefix_table)

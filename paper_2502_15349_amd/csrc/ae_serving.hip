@@ -1,11 +1,13 @@
 // C ABI of the operators around a key/value cache: validation and launch.  See include/ae_serving.h.
 #include "../../include/ae_serving.h"
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <utility>
 
 #include "cache.hpp"
+#include "cached_attn.hpp"
 #include "rotary.hpp"
 #include "status.hpp"
 
@@ -222,6 +224,173 @@ ae_status_t ae_cache_read(const ae_cache_t* h, const void* K_pages, const void* 
 }
 
 ae_status_t ae_cache_destroy(ae_cache_t* h) {
+  delete h;
+  return AE_OK;
+}
+
+}  // extern "C"
+
+// ---- attention over the paged cache ------------------------------------------------------------------------------------
+struct ae_cached {
+  ae_cache_desc_t cache;
+  ae_cached_desc_t desc;
+  ae::CachedParams params;  // pointers filled in per call
+  ae::CachedPart own, prefix;
+  int slots;                // partial results of a row (1: written as they are)
+  size_t ws_bytes;
+};
+
+namespace {
+
+constexpr size_t kWsAlign = 256;
+size_t round_up(size_t x) { return (x + kWsAlign - 1) / kWsAlign * kWsAlign; }
+
+// How the keys of a part are cut: into chunks that make about `target` workgroups, of at least 256 keys.
+void cut_keys(ae::CachedPart& pt, int H_kv, int rows_per_wg, int64_t chunk) {
+  pt.row_tiles = (pt.rows + rows_per_wg - 1) / rows_per_wg;
+  const int64_t units = (int64_t)pt.lists * H_kv * pt.row_tiles, target = 1024;
+  if (chunk == 0) {
+    const int64_t cuts = std::max<int64_t>(1, (target + units - 1) / units);
+    chunk = std::max<int64_t>(256, ((pt.max_length + cuts - 1) / cuts + 127) / 128 * 128);
+  }
+  pt.chunk = (int)std::min<int64_t>(chunk, ((int64_t)pt.max_length + 127) / 128 * 128);
+  pt.splits = (int)(((int64_t)pt.max_length + pt.chunk - 1) / pt.chunk);
+}
+
+}  // namespace
+
+extern "C" {
+
+ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d, ae_cached_t** out) {
+  if (out) *out = nullptr;
+  if (!cache || !d || !out) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: null argument");
+  const ae_cache_desc_t& cd = cache->desc;
+  if (d->B < 1 || d->H_q < 1 || d->n_new < 1 || d->table_width < 1) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: B, H_q, n_new and table_width must be >= 1");
+  if (d->H_q % cd.H_kv != 0) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: H_q (%d) is not a multiple of H_kv (%d)", d->H_q, cd.H_kv);
+  if (d->max_length < 1 || d->max_length > (int64_t)d->table_width * cd.page_size)
+    return fail(AE_ERR_INVALID_ARG, "ae_cached_create: max_length (%d) must be between 1 and table_width * page_size", d->max_length);
+  if (d->prefix_length < 0) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: prefix_length must not be negative");
+  if (d->chunk < 0 || d->chunk % 128 != 0) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: chunk must be 0 or a positive multiple of 128");
+  if (!std::isfinite(d->scale) || d->scale == 0.f) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: scale must be finite and non-zero");
+  if (d->out_dtype != AE_OUT_F32 && d->out_dtype != AE_OUT_BF16) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: unknown out_dtype %d", (int)d->out_dtype);
+  const int64_t rows = (int64_t)d->B * d->H_q * d->n_new;
+  if (rows > 1 << 24 || d->max_length > 0x7fffff00 || d->prefix_length > 0x7fffff00 || d->chunk > 0x7fffff00)
+    return fail(AE_ERR_UNSUPPORTED, "ae_cached_create: at most 2^24 query rows and 2^31 - 256 keys");
+  ae_cached* h = new (std::nothrow) ae_cached();
+  if (!h) return fail(AE_ERR_NOMEM, "ae_cached_create: out of host memory");
+  h->cache = cd;
+  h->desc = *d;
+  ae::CachedParams& p = h->params;
+  contiguous_or(p.qs, d->q_stride, d->H_q, d->n_new, cd.D_qk);
+  contiguous_or(p.os, d->o_stride, d->H_q, d->n_new, cd.D_v);
+  for (int a = 0; a < 3; ++a)
+    if (p.qs[a] < 0 || p.os[a] < 0 || p.qs[a] % 8 != 0 || p.os[a] % 8 != 0) {
+      delete h;
+      return fail(AE_ERR_INVALID_ARG, "ae_cached_create: strides must be non-negative multiples of 8 elements");
+    }
+  p.B = d->B;
+  p.H_q = d->H_q;
+  p.H_kv = cd.H_kv;
+  p.g = d->H_q / cd.H_kv;
+  p.n = d->n_new;
+  p.page_shift = cache->page_shift;
+  p.n_pages = cd.n_pages;
+  p.c = d->scale * 1.4426950408889634f;
+  p.out_bf16 = d->out_dtype == AE_OUT_BF16;
+  const bool e4m3 = cd.dtype == AE_CACHE_E4M3;
+  auto part = [&](ae::CachedPart& pt, bool own) {
+    pt = ae::CachedPart();
+    pt.lists = own ? d->B : 1;
+    pt.rows = (own ? 1 : d->B) * d->n_new * p.g;
+    pt.max_length = own ? d->max_length : d->prefix_length;
+    pt.table_width = own ? d->table_width : 0;
+    pt.causal = own ? 1 : 0;
+    cut_keys(pt, cd.H_kv, ae::cached_rows_per_workgroup(cd.D_qk, cd.D_v, e4m3, pt.rows), d->chunk);
+  };
+  part(h->own, true);
+  if (d->prefix_length > 0) {
+    part(h->prefix, false);
+    h->own.slot0 = h->prefix.splits;
+  }
+  h->slots = h->own.splits + h->own.slot0;
+  h->ws_bytes = h->slots == 1 ? 0 : round_up((size_t)h->slots * rows * cd.D_v * 4) + round_up((size_t)h->slots * rows * 4);
+  if ((double)h->slots * rows * cd.D_v * 4 > 1e12) {
+    delete h;
+    return fail(AE_ERR_UNSUPPORTED, "ae_cached_create: the partial results would take more than 10^12 bytes");
+  }
+  *out = h;
+  return AE_OK;
+}
+
+ae_status_t ae_cached_workspace_bytes(const ae_cached_t* h, size_t* bytes) {
+  if (!h || !bytes) return fail(AE_ERR_INVALID_ARG, "ae_cached_workspace_bytes: null argument");
+  *bytes = h->ws_bytes;
+  return AE_OK;
+}
+
+ae_status_t ae_cached_forward(const ae_cached_t* h, const void* Q, const void* K_pages, const void* V_pages, const void* K_exp, const void* V_exp,
+                              const int32_t* table, const int32_t* lengths, const int32_t* prefix_table, void* O, float* stats, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream) {
+  static const char who[] = "ae_cached_forward";
+  if (!h) return fail(AE_ERR_INVALID_ARG, "%s: null handle", who);
+  const bool e4m3 = h->cache.dtype == AE_CACHE_E4M3;
+  if (!Q || !K_pages || !V_pages || !table || !lengths || !O) return fail(AE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if ((K_exp != nullptr) != e4m3 || (V_exp != nullptr) != e4m3) return fail(AE_ERR_INVALID_ARG, "%s: exponents belong to an 8-bit cache, and only to it", who);
+  if ((prefix_table != nullptr) != (h->desc.prefix_length > 0)) return fail(AE_ERR_INVALID_ARG, "%s: a prefix's table is given exactly where the handle has a prefix", who);
+  if (((uintptr_t)Q | (uintptr_t)K_pages | (uintptr_t)V_pages | (uintptr_t)O) & 15) return fail(AE_ERR_INVALID_ARG, "%s: Q, O and the pages must be 16-byte aligned", who);
+  if (((uintptr_t)table | (uintptr_t)lengths | (uintptr_t)prefix_table | (uintptr_t)K_exp | (uintptr_t)V_exp | (uintptr_t)stats) & 3)
+    return fail(AE_ERR_INVALID_ARG, "%s: tables, lengths, exponents and stats must be 4-byte aligned", who);
+  if (h->ws_bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < h->ws_bytes))
+    return fail(AE_ERR_INVALID_ARG, "%s: workspace missing, not 256-byte aligned, or smaller than %zu bytes", who, h->ws_bytes);
+  const void* in[] = {Q, K_pages, V_pages, K_exp, V_exp, table, lengths, prefix_table};
+  const void* outs[] = {O, stats, h->ws_bytes ? workspace : nullptr};
+  for (int i = 0; i < 3; ++i) {
+    for (const void* x : in)
+      if (outs[i] && outs[i] == x) return fail(AE_ERR_INVALID_ARG, "%s: an output or the workspace aliases an input", who);
+    for (int j = 0; j < i; ++j)
+      if (outs[i] && outs[i] == outs[j]) return fail(AE_ERR_INVALID_ARG, "%s: outputs and workspace alias each other", who);
+  }
+  ae::CachedParams p = h->params;
+  p.Q = static_cast<const __bf16*>(Q);
+  p.O = O;
+  p.stats = stats;
+  p.K = static_cast<const uint8_t*>(K_pages);
+  p.V = static_cast<const uint8_t*>(V_pages);
+  p.Ke = static_cast<const uint8_t*>(K_exp);
+  p.Ve = static_cast<const uint8_t*>(V_exp);
+  const size_t rows = (size_t)p.B * p.H_q * p.n;
+  p.ws_o = h->ws_bytes ? static_cast<float*>(workspace) : nullptr;
+  p.ws_lse = h->ws_bytes ? reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up((size_t)h->slots * rows * h->cache.D_v * 4)) : nullptr;
+  if (h->desc.prefix_length > 0) {
+    p.part = h->prefix;
+    p.part.table = prefix_table;
+    const ae_status_t st = launched(ae::launch_cached(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
+    if (st != AE_OK) return st;
+  }
+  p.part = h->own;
+  p.part.table = table;
+  p.part.lengths = lengths;
+  const ae_status_t st = launched(ae::launch_cached(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
+  if (st != AE_OK || !h->ws_bytes) return st;
+  ae::CachedMerge mp = {};
+  mp.ws_o = p.ws_o;
+  mp.ws_lse = p.ws_lse;
+  mp.O = O;
+  for (int a = 0; a < 3; ++a) mp.os[a] = p.os[a];
+  mp.stats = stats;
+  mp.lengths = lengths;
+  mp.B = p.B;
+  mp.H_q = p.H_q;
+  mp.n = p.n;
+  mp.d_v = h->cache.D_v;
+  mp.out_bf16 = p.out_bf16;
+  mp.prefix_slots = h->own.slot0;
+  mp.chunk = h->own.chunk;
+  mp.max_length = h->own.max_length;
+  return launched(ae::launch_cached_merge(mp, stream), who);
+}
+
+ae_status_t ae_cached_destroy(ae_cached_t* h) {
   delete h;
   return AE_OK;
 }

@@ -1,0 +1,529 @@
+// Attention of query rows over keys and values in pages: O = softmax(scale Q K^T) V per k/v head, where the rows are the newest
+// tokens of a sequence times the q heads that share the k/v head, or -- for a shared prefix -- those of all sequences.
+//
+// A wavefront walks sub-tiles of 32 keys.  Per sub-tile, with MFMA 16x16x32 (bf16, fp32 accumulators):
+//   S^T [32 keys x 16 rows] = K Q^T     two tiles of 16 keys; tile u holds the keys 8 i + 4 u + 0..3, i = 0..3
+//   O^T [D_v x 16 rows]    += V^T P^T
+// In the accumulator layout a lane holds 4 keys of one row per tile; with that choice of keys its 8 values are 8 neighbouring
+// keys, and, packed to bf16, they are the second product's B operand as they stand.  V^T comes from the transposing LDS
+// read.  Softmax with a running reference per row that moves only when a score exceeds it by more than 2^8; the row sum is of the
+// unrounded weights, in fp32.  Weights are rounded to bf16 for the second product (unbiased, 2^-9 each).
+// 8-bit keys become bf16 between LDS and the MFMA, on their row's power of two (exact, the conversion applies it);
+// 8-bit values likewise without theirs, which multiplies the weight instead (a lane's 8 values of V are of 8 rows).
+//
+// Keys and values go from the pages to LDS by global_load_lds, each wavefront its own sub-tiles into its own stages, so that
+// the walk needs no barriers; the wavefronts of a workgroup take sub-tiles in turn and their states meet at the end.
+#include "cached_attn.hpp"
+
+#include "attn_kernel.hpp"
+#include "launch.hpp"
+
+namespace ae {
+namespace {
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// a load of something that no one writes during the launch, at an address that is the same in all lanes
+__device__ __forceinline__ int32_t scalar_load(const int32_t* ptr) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uintptr_t)ptr);
+}
+
+template <int DQK_, int DV_, bool E4M3_, int RT_>
+struct CachedCfg {
+  static constexpr int DQK = DQK_, DV = DV_, RT = RT_, W = 4, THREADS = 64 * W;
+  static constexpr bool E4M3 = E4M3_;
+  static constexpr int ESZ = E4M3 ? 1 : 2, RBK = DQK * ESZ, RBV = DV * ESZ, CPRK = RBK / 16, CPRV = RBV / 16;
+  static constexpr int K_BYTES = 32 * RBK, V_BYTES = 32 * RBV, E_BYTES = E4M3 ? 256 : 0, STAGE = K_BYTES + V_BYTES + E_BYTES;
+  static constexpr int NK = K_BYTES / 1024, NV = V_BYTES / 1024, LOADS = NK + NV + (E4M3 ? 1 : 0);
+  static constexpr int STAGES = 2;
+  static constexpr int KS = DQK / 32, DB = DV / 16;
+  static constexpr int ROWS = 16 * RT;
+  static constexpr int RED_ROW = DV + 4;
+  static constexpr int RED_BYTES = W * 16 * (RED_ROW + 2) * 4;
+  static constexpr int LDS_BYTES = W * STAGES * STAGE > RED_BYTES ? W * STAGES * STAGE : RED_BYTES;
+  static_assert(LDS_BYTES <= 160 * 1024, "a workgroup must fit LDS");
+  static_assert((STAGES - 1) * LOADS < 64, "the wait count has six bits");
+};
+
+// ---- chunk swizzles: LDS position of 16-byte chunk c of tile row r is c ^ swizzle(r) -------------------------------------------
+// Row fragments: 16 lanes read one chunk of the rows 8 i + k (+ 4), i, k = 0..3.
+template <int CPR>
+__device__ __forceinline__ int row_swizzle(int r) {
+  const int f = (r & 3) | (((r >> 3) & 3) << 2);
+  return CPR % 16 == 0 ? f : CPR % 8 == 0 ? f >> 1 : f >> 2;
+}
+// Transposing reads: 16-bit, 32 lanes read 32 bytes of the rows 8 i + k, i = 0, 1, k = 0..3; 8-bit, 16 bytes of 16 rows.
+template <int CPR, bool E4M3>
+__device__ __forceinline__ int tr_swizzle(int r) {
+  if constexpr (E4M3) return CPR == 8 ? (r >> 1) & 7 : (r >> 2) & 3;
+  else return CPR == 16 ? 2 * ((r & 3) | (((r >> 3) & 1) << 2)) : 2 * (((r >> 1) & 1) | (((r >> 3) & 1) << 1));
+}
+
+// 64 lanes x 4 bytes from per-lane addresses to LDS bytes [lds_addr, lds_addr + 256)
+__device__ __forceinline__ void dma4_gather(const void* lane_ptr, uint32_t lds_addr_uniform) {
+  lds_addr_uniform = __builtin_amdgcn_readfirstlane(lds_addr_uniform);
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %1, off"
+      :
+      : "s"(lds_addr_uniform), "v"((uint64_t)(uintptr_t)lane_ptr)
+      : "memory", "m0");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmem() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ float max_over_groups(float x) {  // over the four groups of 16 lanes
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+
+// 16 bytes of e4m3 -> two fragments of 8 bf16, times a power of two
+__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+
+template <class C>
+__global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem[C::LDS_BYTES];
+  const CachedPart& pt = p.part;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ql = lane & 15, hi = lane >> 4;
+
+  // ---- workgroup -> (list, k/v head), key range, row tile ------------------------------------------------------------
+  // Row tiles that read the same keys are 8 workgroups apart: next to each other on one XCD, whose L2 has the keys for the second.
+  const int units = pt.lists * p.H_kv * pt.splits;
+  const int w8 = blockIdx.x & 7, slot = blockIdx.x >> 3;
+  const int unit = (slot / pt.row_tiles) * 8 + w8, tile = slot % pt.row_tiles;
+  if (unit >= units) return;
+  const int split = unit / (pt.lists * p.H_kv), head = unit % (pt.lists * p.H_kv);
+  const int list = head / p.H_kv, hk = head % p.H_kv;
+  int len = pt.max_length;
+  if (pt.lengths != nullptr) len = max(0, min(scalar_load(pt.lengths + list), len));
+  const int begin = split * pt.chunk, end = min(len, begin + pt.chunk);
+  if (begin >= len && (p.ws_o != nullptr || split > 0)) return;  // (nothing reads the partial result of a range past the end)
+  const int32_t* table = pt.table + (int64_t)list * pt.table_width;
+
+  // ---- the query rows: B fragments, lane = row ql, 8 elements of group hi ----------------------------------------------
+  const int row0 = tile * C::ROWS;
+  auto place = [&](int r, int& b, int& t, int& h) {
+    const int per = p.n * p.g, rr = r % per;
+    b = pt.causal ? list : r / per;
+    t = rr / p.g;
+    h = hk * p.g + rr % p.g;
+  };
+  bf16x8 qf[C::RT][C::KS];
+  int lim[C::RT];  // keys below this one are visible to the lane's row
+#pragma unroll
+  for (int rt = 0; rt < C::RT; ++rt) {
+    int b, t, h;
+    place(min(row0 + 16 * rt + ql, pt.rows - 1), b, t, h);
+    const __bf16* q = p.Q + b * p.qs[0] + h * p.qs[1] + t * p.qs[2];
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s)  // 8-bit keys: a 16-byte chunk serves two steps
+      qf[rt][s] = *reinterpret_cast<const bf16x8*>(q + (C::E4M3 ? 64 * (s / 2) + 16 * hi + 8 * (s % 2) : 32 * s + 8 * hi));
+    lim[rt] = pt.causal ? len - p.n + 1 + t : len;
+  }
+  const int all_visible = pt.causal ? len - p.n + 1 : len;  // keys below this one are visible to every row
+
+  // ---- copies --------------------------------------------------------------------------------------------------------------
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_char*)smem) + wave * (C::STAGES * C::STAGE);
+  const int page_mask = (1 << p.page_shift) - 1;
+  uint32_t koff[C::NK], voff[C::NV];  // the lane's byte offset from the first row of the half tile
+#pragma unroll
+  for (int i = 0; i < C::NK; ++i) {
+    const int pos = (i % (C::NK / 2)) * 64 + lane, r = pos / C::CPRK;
+    koff[i] = r * C::RBK + (((pos % C::CPRK) ^ row_swizzle<C::CPRK>(r + 16 * (i / (C::NK / 2)))) << 4);
+  }
+#pragma unroll
+  for (int i = 0; i < C::NV; ++i) {
+    const int pos = (i % (C::NV / 2)) * 64 + lane, r = pos / C::CPRV;
+    voff[i] = r * C::RBV + (((pos % C::CPRV) ^ tr_swizzle<C::CPRV, C::E4M3>(r + 16 * (i / (C::NV / 2)))) << 4);
+  }
+  const int n_sub = (max(end - begin, 0) + 31) / 32, n_my = (n_sub - wave + C::W - 1) / C::W;
+  // The two halves of a sub-tile (16 keys) lie in a page each.  A page number outside the cache is not followed: its keys count
+  // as hidden, and the copy takes page 0's instead, as it takes the first half's again for a half behind the last key; rows
+  // behind the last key are copied as they lie in the page.  What a hidden key holds is masked below.  Returns which halves
+  // are hidden.
+  auto issue = [&](int i, int stage) -> int {
+    const int j0 = begin + 32 * (wave + i * C::W);
+    const bool second = j0 + 16 < end;
+    const int pg0 = scalar_load(table + (j0 >> p.page_shift));
+    const int pg1 = second ? scalar_load(table + ((j0 + 16) >> p.page_shift)) : pg0;
+    const bool ok0 = (uint32_t)pg0 < (uint32_t)p.n_pages, ok1 = (uint32_t)pg1 < (uint32_t)p.n_pages;
+    const uint32_t base = lds0 + stage * C::STAGE;
+    int64_t row[2];  // first row of the half in the cache
+    row[0] = (((int64_t)(ok0 ? pg0 : 0) * p.H_kv + hk) << p.page_shift) + (j0 & page_mask);
+    row[1] = second ? (((int64_t)(ok1 ? pg1 : 0) * p.H_kv + hk) << p.page_shift) + ((j0 + 16) & page_mask) : row[0];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* kb = p.K + row[h] * C::RBK;
+      const uint8_t* vb = p.V + row[h] * C::RBV;
+#pragma unroll
+      for (int i = 0; i < C::NK / 2; ++i) dma16(kb, koff[h * (C::NK / 2) + i], base + (h * (C::NK / 2) + i) * 1024);
+#pragma unroll
+      for (int i = 0; i < C::NV / 2; ++i) dma16(vb, voff[h * (C::NV / 2) + i], base + C::K_BYTES + (h * (C::NV / 2) + i) * 1024);
+    }
+    if constexpr (C::E4M3) {  // bytes 0..31: exponents of the keys, 32..63: of the values (lanes 16.. repeat them)
+      const int k = lane & 15;
+      const uint8_t* e = (k & 8 ? p.Ve : p.Ke) + row[(k >> 2) & 1] + 4 * (k & 3);
+      dma4_gather(e, base + C::K_BYTES + C::V_BYTES);
+    }
+    return (ok0 ? 0 : 1) | (ok1 ? 0 : 2);
+  };
+
+  // ---- fragments -------------------------------------------------------------------------------------------------------------
+  const int krow = 8 * (ql >> 2) + (ql & 3);  // tile u: + 4 u (the swizzle is the same)
+  uint32_t kaddr[C::E4M3 ? C::KS / 2 : C::KS];
+#pragma unroll
+  for (int s = 0; s < (C::E4M3 ? C::KS / 2 : C::KS); ++s) kaddr[s] = lds0 + krow * C::RBK + (((4 * s + hi) ^ row_swizzle<C::CPRK>(krow)) << 4);
+  const int vrow = C::E4M3 ? 8 * hi + (ql >> 1) : 8 * hi + (ql >> 2);
+  uint32_t vaddr[C::DB];
+#pragma unroll
+  for (int d = 0; d < C::DB; ++d)
+    vaddr[d] = lds0 + C::K_BYTES + vrow * C::RBV +
+               (C::E4M3 ? ((d ^ tr_swizzle<C::CPRV, true>(vrow)) << 4) + 8 * (ql & 1)
+                        : (((2 * d + ((ql & 3) >> 1)) ^ tr_swizzle<C::CPRV, false>(vrow)) << 4) + 8 * (ql & 1));
+  auto read_v = [&](int d, uint32_t so) -> bf16x8 {
+    if constexpr (C::E4M3) {
+      const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(uintptr_t)(vaddr[d] + so));
+      return widen8(v[0], v[1], 1.f);
+    } else {
+      return read_v_frag(vaddr[d] + so, 4 * C::RBV);
+    }
+  };
+
+  f32x4 o[C::RT][C::DB];
+  float m[C::RT], l[C::RT];
+#pragma unroll
+  for (int rt = 0; rt < C::RT; ++rt) {
+    m[rt] = -INFINITY;
+    l[rt] = 0.f;
+#pragma unroll
+    for (int d = 0; d < C::DB; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  auto compute = [&](int i, int stage, int hidden) {
+    if (hidden == 3) return;
+    const int j0 = begin + 32 * (wave + i * C::W);
+    const uint32_t so = stage * C::STAGE;
+    const bool masked = hidden != 0 || j0 + 32 > min(all_visible, end);
+    float ks[2] = {1.f, 1.f}, vs[8];
+    if constexpr (C::E4M3) {
+      const uint32_t eb = lds0 + so + C::K_BYTES + C::V_BYTES;
+      typedef __attribute__((address_space(3))) const uint8_t lds_u8;
+      ks[0] = __builtin_bit_cast(float, (uint32_t)*reinterpret_cast<lds_u8*>((lds_char*)(uintptr_t)(eb + krow)) << 23);
+      ks[1] = __builtin_bit_cast(float, (uint32_t)*reinterpret_cast<lds_u8*>((lds_char*)(uintptr_t)(eb + krow + 4)) << 23);
+      const u32x2 v = *reinterpret_cast<__attribute__((address_space(3))) const u32x2*>((lds_char*)(uintptr_t)(eb + 32 + 8 * hi));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vs[e] = __builtin_bit_cast(float, ((v[e / 4] >> (8 * (e % 4))) & 0xffu) << 23);
+    }
+    f32x4 s[2][C::RT];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int rt = 0; rt < C::RT; ++rt) s[u][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (C::E4M3) {
+#pragma unroll
+      for (int s2 = 0; s2 < C::KS / 2; ++s2)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const u32x4 raw = __builtin_bit_cast(u32x4, read_k_frag(kaddr[s2] + so + u * 4 * C::RBK));
+          const bf16x8 a = widen8(raw[0], raw[1], ks[u]), b = widen8(raw[2], raw[3], ks[u]);
+#pragma unroll
+          for (int rt = 0; rt < C::RT; ++rt) {
+            s[u][rt] = mfma16(a, qf[rt][2 * s2], s[u][rt]);
+            s[u][rt] = mfma16(b, qf[rt][2 * s2 + 1], s[u][rt]);
+          }
+        }
+    } else {
+#pragma unroll
+      for (int ss = 0; ss < C::KS; ++ss)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 a = read_k_frag(kaddr[ss] + so + u * 4 * C::RBK);
+#pragma unroll
+          for (int rt = 0; rt < C::RT; ++rt) s[u][rt] = mfma16(a, qf[rt][ss], s[u][rt]);
+        }
+    }
+    // of the lane's 8 keys, those below there are in the list (and on a page of the cache); below last + 1, visible to its row
+    const int there = (hi < 2 ? hidden & 1 : hidden & 2) ? 0 : end - j0 - 8 * hi;
+    bf16x8 pb[C::RT];
+#pragma unroll
+    for (int rt = 0; rt < C::RT; ++rt) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = s[e / 4][rt][e % 4] * p.c;
+      if (masked) {
+        const int last = min(lim[rt] - j0 - 8 * hi, there) - 1;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e <= last ? x[e] : -INFINITY;
+      }
+      float mx = fmaxf(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]));
+      mx = max3(mx, x[6], x[7]);
+      if (__builtin_amdgcn_ballot_w64(mx > m[rt] + kLazyLog2) != 0) {
+        mx = fmaxf(max_over_groups(mx), m[rt]);
+        const float alpha = mx == -INFINITY ? 1.f : fast_exp2(m[rt] - mx);
+        m[rt] = mx;
+        l[rt] *= alpha;
+#pragma unroll
+        for (int d = 0; d < C::DB; ++d) o[rt][d] *= alpha;
+      }
+      const float ref = m[rt] == -INFINITY ? 0.f : m[rt];
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = fast_exp2(x[e] - ref);
+        sum += x[e];
+      }
+      l[rt] += sum;
+      if constexpr (C::E4M3) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float w = x[e] * vs[e];
+          x[e] = masked ? (x[e] == 0.f ? 0.f : w) : w;  // (an exponent byte behind the last key may be anything)
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pb[rt][e] = (__bf16)x[e];
+    }
+    if (!masked) {
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d) {
+        const bf16x8 a = read_v(d, so);
+#pragma unroll
+        for (int rt = 0; rt < C::RT; ++rt) o[rt][d] = mfma16(a, pb[rt], o[rt][d]);
+      }
+    } else {
+      // Rows that are not there are made zero: a weight of zero does not do away with a NaN.  Rows that only some of the newest tokens
+      // see and that hold a NaN or an infinity are zero in the product as well; what they do to the rows that see them is
+      // counted in two products with ones.
+      u32x4 keep;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) keep[e] = there > 2 * e + 1 ? 0xffffffffu : there > 2 * e ? 0xffffu : 0u;
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d) {
+        u32x4 a = __builtin_bit_cast(u32x4, read_v(d, so)) & keep;
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd = odd || (a[e] & 0x7f80u) == 0x7f80u || (a[e] & 0x7f800000u) == 0x7f800000u;
+        if (pt.causal && p.n > 1 && __builtin_amdgcn_ballot_w64(odd) != 0) {
+          bf16x8 up, down;
+          u32x4 fin = a;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t v = (a[e / 2] >> (16 * (e % 2))) & 0xffffu;
+            const bool special = (v & 0x7f80u) == 0x7f80u, nan = special && (v & 0x7fu) != 0;
+            up[e] = special && (nan || !(v & 0x8000u)) ? (__bf16)1.f : (__bf16)0.f;
+            down[e] = special && (nan || (v & 0x8000u)) ? (__bf16)1.f : (__bf16)0.f;
+            if (special) fin[e / 2] &= e % 2 ? 0xffffu : 0xffff0000u;
+          }
+#pragma unroll
+          for (int rt = 0; rt < C::RT; ++rt) {
+            bf16x8 sees;
+            const int last = min(lim[rt] - j0 - 8 * hi, there) - 1;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sees[e] = e <= last ? (__bf16)1.f : (__bf16)0.f;
+            o[rt][d] = mfma16(__builtin_bit_cast(bf16x8, fin), pb[rt], o[rt][d]);
+            const f32x4 n_up = mfma16(up, sees, f32x4{0.f, 0.f, 0.f, 0.f}), n_down = mfma16(down, sees, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {  // (by bits: device code is compiled for no NaN to occur)
+              const uint32_t add = n_up[r] > 0.f ? (n_down[r] > 0.f ? 0x7fc00000u : 0x7f800000u) : n_down[r] > 0.f ? 0xff800000u : 0u;
+              const uint32_t was = __builtin_bit_cast(uint32_t, (float)o[rt][d][r]);
+              if (add) o[rt][d][r] = __builtin_bit_cast(float, (was & 0x7f800000u) == 0x7f800000u && was != add ? 0x7fc00000u : add);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int rt = 0; rt < C::RT; ++rt) o[rt][d] = mfma16(__builtin_bit_cast(bf16x8, a), pb[rt], o[rt][d]);
+        }
+      }
+    }
+  };
+
+  // ---- the walk ------------------------------------------------------------------------------------------------------------------
+  int hid[C::STAGES];
+#pragma unroll
+  for (int s = 0; s < C::STAGES; ++s) hid[s] = s < n_my ? issue(s, s) : 0;
+#pragma unroll
+  for (int rt = 0; rt < C::RT; ++rt)
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) asm volatile("" ::"v"(qf[rt][s]));  // (awaited here, not inside the loop)
+  for (int i0 = 0; i0 < n_my; i0 += C::STAGES) {
+#pragma unroll
+    for (int s = 0; s < C::STAGES; ++s) {
+      const int i = i0 + s;
+      if (i < n_my) {
+        if (i + C::STAGES - 1 < n_my) wait_vmem<(C::STAGES - 1) * C::LOADS>();
+        else wait_vmem<0>();
+        compute(i, s, hid[s]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // every fragment is read before the copy overwrites the stage
+        if (i + C::STAGES < n_my) hid[s] = issue(i + C::STAGES, s);
+      }
+    }
+  }
+
+  // ---- the wavefronts' states into one, row tile by row tile --------------------------------------------------------------------
+  float* red = reinterpret_cast<float*>(smem);  // [W][16][RED_ROW], then [W][16][2]
+  float* red_ml = red + C::W * 16 * C::RED_ROW;
+#pragma unroll
+  for (int rt = 0; rt < C::RT; ++rt) {
+    if (row0 + 16 * rt >= pt.rows) break;
+    float lt = l[rt];
+    lt += __shfl_xor(lt, 16);
+    lt += __shfl_xor(lt, 32);
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < C::DB; ++d) *reinterpret_cast<f32x4*>(red + (wave * 16 + ql) * C::RED_ROW + 16 * d + 4 * hi) = o[rt][d];
+    if (hi == 0) {
+      red_ml[(wave * 16 + ql) * 2] = m[rt];
+      red_ml[(wave * 16 + ql) * 2 + 1] = lt;
+    }
+    __syncthreads();
+    constexpr int PER = C::THREADS / 16, COLS = C::DV / PER;  // threads per row, columns per thread
+    const int r = threadIdx.x / PER, c0 = (threadIdx.x % PER) * COLS;
+    if (row0 + 16 * rt + r < pt.rows) {
+      float M = -INFINITY, f[C::W], L = 0.f, acc[COLS];
+#pragma unroll
+      for (int w = 0; w < C::W; ++w) M = fmaxf(M, red_ml[(w * 16 + r) * 2]);
+      const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+      for (int w = 0; w < C::W; ++w) {
+        f[w] = fast_exp2(red_ml[(w * 16 + r) * 2] - ref);
+        L += f[w] * red_ml[(w * 16 + r) * 2 + 1];
+      }
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < C::W; ++w)
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) acc[e] += f[w] * red[(w * 16 + r) * C::RED_ROW + c0 + e];
+      // no visible key leaves the sum at +0; told from a NaN by its bits (device code is compiled for no NaN to occur)
+      const bool any = __builtin_bit_cast(uint32_t, L) != 0;
+      const float inv = any ? 1.f / L : 0.f;
+      int b, t, h;
+      place(row0 + 16 * rt + r, b, t, h);
+      const int64_t id = ((int64_t)b * p.H_q + h) * p.n + t;
+      if (p.ws_o != nullptr) {
+        const int64_t at = (int64_t)(pt.slot0 + split) * ((int64_t)p.B * p.H_q * p.n) + id;
+#pragma unroll
+        for (int e = 0; e < COLS; e += 4)
+          *reinterpret_cast<f32x4*>(p.ws_o + at * C::DV + c0 + e) = f32x4{acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv};
+        if (c0 == 0) p.ws_lse[at] = any ? M + __builtin_amdgcn_logf(L) : -INFINITY;
+      } else {
+        const int64_t at = b * p.os[0] + h * p.os[1] + t * p.os[2] + c0;
+#pragma unroll
+        for (int e = 0; e < COLS; e += 4) {
+          if (p.out_bf16) {
+            bf16x4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = (__bf16)(acc[e + k] * inv);
+            *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.O) + at + e) = v;
+          } else {
+            *reinterpret_cast<f32x4*>(static_cast<float*>(p.O) + at + e) = f32x4{acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv};
+          }
+        }
+        if (c0 == 0 && p.stats != nullptr) p.stats[id] = any ? (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f : -INFINITY;
+      }
+    }
+  }
+}
+
+// ---- partial results into one: O = sum_c 2^(lse_c - LSE) O_c ----------------------------------------------------------------
+// One wavefront per row, D_v / 64 columns a lane.
+template <int VEC>
+__global__ __launch_bounds__(256) void cached_merge_kernel(const CachedMerge p) {
+  typedef float vec __attribute__((ext_vector_type(VEC)));
+  const int64_t rows = (int64_t)p.B * p.H_q * p.n, r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= rows) return;
+  const int lane = threadIdx.x & 63;
+  const int t = (int)(r % p.n), h = (int)((r / p.n) % p.H_q), b = (int)(r / ((int64_t)p.n * p.H_q));
+  const int len = max(0, min(p.lengths[b], p.max_length));
+  const int slots = p.prefix_slots + (len + p.chunk - 1) / p.chunk;
+  float M = -INFINITY, L = 0.f;
+  vec acc = 0.f;
+  for (int c0 = 0; c0 < slots; c0 += 64) {
+    const int mine = c0 + lane;
+    const float lse = mine < slots ? p.ws_lse[(int64_t)mine * rows + r] : -INFINITY;
+    float top = lse;
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    top = fmaxf(top, M);
+    if (__builtin_bit_cast(uint32_t, top) == 0xff800000u) continue;  // no key so far
+    const float w = fast_exp2(lse - top), alpha = fast_exp2(M - top);
+    M = top;
+    L *= alpha;
+    acc *= alpha;
+    float tot = w;
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) tot += __shfl_xor(tot, s);
+    L += tot;
+    const int n = min(64, slots - c0);
+    constexpr int kBatch = 8;
+    for (int c = 0; c < n; c += kBatch) {
+      vec part[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        part[u] = *reinterpret_cast<const vec*>(p.ws_o + ((int64_t)(c0 + min(c + u, n - 1)) * rows + r) * p.d_v + VEC * lane);
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) acc += (c + u < n ? __shfl(w, (c + u) & 63) : 0.f) * part[u];
+    }
+  }
+  const bool any = __builtin_bit_cast(uint32_t, L) != 0;
+  acc *= any ? 1.f / L : 0.f;
+  const int64_t at = b * p.os[0] + h * p.os[1] + t * p.os[2] + VEC * lane;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    if (p.out_bf16) static_cast<__bf16*>(p.O)[at + e] = (__bf16)acc[e];
+    else static_cast<float*>(p.O)[at + e] = acc[e];
+  }
+  if (p.stats != nullptr && lane == 0) p.stats[r] = any ? (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <class C>
+hipError_t launch_cfg(const CachedParams& p, hipStream_t s) {
+  const int64_t units = (int64_t)p.part.lists * p.H_kv * p.part.splits, grid = (units + 7) / 8 * 8 * p.part.row_tiles;
+  if (!launch_fits(grid, C::THREADS)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((cached_attn_kernel<C>), dim3((unsigned)grid), dim3(C::THREADS), 0, s, p);
+  return hipGetLastError();
+}
+
+template <int DQK, int DV, bool E4M3>
+hipError_t launch_rows(const CachedParams& p, hipStream_t s) {
+  const int rows = cached_rows_per_workgroup(DQK, DV, E4M3, p.part.rows);
+  if (rows == 16) return launch_cfg<CachedCfg<DQK, DV, E4M3, 1>>(p, s);
+  if (rows == 32) return launch_cfg<CachedCfg<DQK, DV, E4M3, 2>>(p, s);
+  return launch_cfg<CachedCfg<DQK, DV, E4M3, 4>>(p, s);
+}
+
+template <int DQK, int DV>
+hipError_t launch_type(const CachedParams& p, bool e4m3, hipStream_t s) {
+  return e4m3 ? launch_rows<DQK, DV, true>(p, s) : launch_rows<DQK, DV, false>(p, s);
+}
+
+}  // namespace
+
+int cached_rows_per_workgroup(int, int, bool, int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+
+hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s) {
+  if (dqk == 64) return launch_type<64, 64>(p, e4m3, s);
+  if (dqk == 128) return launch_type<128, 128>(p, e4m3, s);
+  return launch_type<192, 128>(p, e4m3, s);
+}
+
+hipError_t launch_cached_merge(const CachedMerge& p, hipStream_t s) {
+  const int64_t grid = ((int64_t)p.B * p.H_q * p.n + 3) / 4;
+  if (!launch_fits(grid, 256)) return hipErrorInvalidConfiguration;
+  if (p.d_v == 64) hipLaunchKernelGGL((cached_merge_kernel<1>), dim3((unsigned)grid), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((cached_merge_kernel<2>), dim3((unsigned)grid), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+}  // namespace ae

@@ -1,0 +1,350 @@
+"""GPU parity of attention over the paged cache (ae_cached_forward) against the 64-bit definition on the values that the
+cache holds.
+
+Bounds.  A weight is rounded once to bf16 (at most 2^-8 of it) before the product with the values; scores, weights and sums are 32-bit:
+score error <= D 2^-24 scale sum |q k|, below 2e-5 for these inputs, which is also the weights' relative error.  So |O - ref| <= (2^-8 + 4e-5) *
+sum_j p_j |v_j|, and a bf16 output adds half a step, 2^-8 |O|.  The statistic is within 1e-4 (D 2^-24 scale sum |q k| plus the logarithm's own)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle.serving_oracle import attend, dequantise
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def A():
+    from paper_2502_15349_amd import ae_attn
+    return ae_attn
+
+
+def values(cache):
+    """The cache's contents in 64 bits, [n_pages, H_kv, page, D] each."""
+    if cache.k_exp is None:
+        return [t.cpu().double().numpy() for t in (cache.k, cache.v)]
+    return [dequantise(t.view(torch.uint8).cpu().numpy(), e.cpu().numpy()) for t, e in ((cache.k, cache.k_exp), (cache.v, cache.v_exp))]
+
+
+def listed(pages, table, length):
+    """Rows [H, length, D] of a page list."""
+    page = pages.shape[2]
+    need = -(-length // page)
+    return np.concatenate([pages[t] for t in table[:need]] + [np.zeros((pages.shape[1], 0, pages.shape[3]))], axis=1)[:, :length]
+
+
+def make(A, seed, n_pages, H_kv, page, dqk, dv, dtype, poison=True):
+    """A cache full of N(0, 1) rows; `poison`: what no test writes afterwards is NaN (and exponents of 255)."""
+    g = torch.Generator().manual_seed(seed)
+    c = A.PagedCache.empty(n_pages, H_kv, page, dqk, dv, dtype=dtype)
+    k, v = (torch.randn(1, H_kv, n_pages * page, d, generator=g).to(torch.bfloat16).cuda() for d in (dqk, dv))
+    c.append(k, v, torch.arange(n_pages * page, dtype=torch.int32).cuda()[None])
+    return c
+
+
+def spoil_behind(cache, tables, lengths):
+    """NaN in every row of the cache that no list holds."""
+    page = cache.page_size
+    used = torch.zeros(cache.n_pages * page, dtype=torch.bool)
+    for t, n in zip(tables, lengths):
+        for j in range(n):
+            p = int(t[j // page])
+            if 0 <= p < cache.n_pages:
+                used[p * page + j % page] = True
+    rest = ~used.view(cache.n_pages, page).cuda()
+    for t in (cache.k, cache.v):
+        if t.dtype == torch.bfloat16:
+            t.transpose(1, 2)[rest] = float("nan")
+        else:
+            t.view(torch.uint8).transpose(1, 2)[rest] = 0x7f
+    for e in (cache.k_exp, cache.v_exp):
+        if e is not None:
+            e.transpose(1, 2)[rest] = 255
+
+
+def queries(seed, B, H_q, n, D):
+    return torch.randn(B, n, H_q, D, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).cuda().transpose(1, 2)
+
+
+def check(got, stats, Q, keys, vals, scale, what):
+    """keys, vals: per sequence, [H_kv, len, D]."""
+    O, S = got.cpu().double().numpy(), None if stats is None else stats.cpu().double().numpy()
+    worst = 0.0
+    for b in range(Q.shape[0]):
+        q = Q[b].cpu().double().numpy()
+        ref, lse = attend(q, keys[b], vals[b], scale)
+        mag, _ = attend(q, keys[b], np.abs(vals[b]), scale)
+        bound = (2.0 ** -8 + 4e-5) * mag + 1e-30
+        if got.dtype == torch.bfloat16:
+            bound = bound * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref)
+        err = np.abs(O[b] - ref)
+        assert np.isfinite(O[b]).all(), (what, b)
+        worst = max(worst, float((err / bound).max()))
+        assert (err <= bound).all(), (what, b, float((err / bound).max()))
+        if S is not None:
+            empty = np.isneginf(lse)
+            assert np.array_equal(np.isneginf(S[b]), empty), (what, b)
+            assert (np.abs(S[b][~empty] - lse[~empty]) <= 1e-4).all(), (what, b)
+    print(f"{what}: largest error {worst:.3f} of the bound", flush=True)
+
+
+def tables_for(seed, n_pages, lengths, page, width, first=0):
+    """A page list per sequence; entries behind the last needed one are numbers of no page."""
+    order = torch.randperm(n_pages - first, generator=torch.Generator().manual_seed(seed)) + first
+    t, at = torch.full((len(lengths), width), -7, dtype=torch.int32), 0
+    for b, n in enumerate(lengths):
+        need = -(-n // page)
+        t[b, :need] = order[at: at + need].to(torch.int32)
+        at += need
+    return t
+
+
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("H_q,H_kv,n,page,lengths,out,chunk", [
+    (1, 1, 1, 16, [1], "f32", 0),
+    (4, 4, 1, 16, [1, 15, 16, 17, 31, 32, 33], "bf16", 0),
+    (32, 8, 1, 64, [777, 300, 64, 1], "f32", 0),
+    (8, 1, 1, 32, [1500, 129, 128, 127], "bf16", 128),
+    (6, 2, 3, 16, [3, 4, 50, 33, 160], "f32", 128),
+    (16, 2, 4, 256, [700, 4, 513], "f32", 0),
+    (64, 8, 8, 128, [333, 9], "bf16", 0),
+    (12, 12, 2, 32, [2, 34, 257], "f32", 256),
+    (7, 1, 5, 64, [90, 64, 5], "f32", 0),
+    (40, 1, 2, 16, [65, 200], "f32", 128),
+])
+def test_matches_definition(A, dqk, dv, dtype, H_q, H_kv, n, page, lengths, out, chunk):
+    B, width = len(lengths), -(-max(lengths) // page) + 2
+    n_pages = sum(-(-x // page) for x in lengths) + 1
+    c = make(A, 1, n_pages, H_kv, page, dqk, dv, dtype)
+    t = tables_for(2, n_pages, lengths, page, width)
+    spoil_behind(c, t, lengths)
+    Q = queries(3, B, H_q, n, dqk)
+    stats = torch.full((B, H_q, n), 7.0, device="cuda")
+    scale = dqk ** -0.5
+    O = A.attention_cached(Q, c, t.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), scale=scale, stats=stats, chunk=chunk,
+                           out_dtype=torch.bfloat16 if out == "bf16" else torch.float32)
+    kv = values(c)
+    rows = [[listed(x, t[b].tolist(), lengths[b]) for b in range(B)] for x in kv]
+    check(O, stats, Q, *rows, scale, f"{dqk}/{dv} {dtype} {H_q}/{H_kv} n {n} page {page}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n,chunk", [(1, 0), (3, 128)])
+def test_lengths_of_padded_batches(A, dtype, n, chunk):
+    # empty sequences, fewer keys than new tokens, lengths outside [0, max_length]
+    lengths, page, width = [0, 1, 2, 200, -5, 4000, 130], 32, 8
+    n_pages = len(lengths) * width
+    c = make(A, 4, n_pages, 2, page, 128, 128, dtype)
+    t = torch.randperm(n_pages, generator=torch.Generator().manual_seed(5)).view(len(lengths), width).to(torch.int32)
+    Q = queries(6, len(lengths), 4, n, 128)
+    stats = torch.empty(len(lengths), 4, n, device="cuda")
+    O = A.attention_cached(Q, c, t.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), scale=0.09, max_length=201, stats=stats, chunk=chunk)
+    real = [min(max(x, 0), 201) for x in lengths]
+    rows = [[listed(x, t[b].tolist(), real[b]) for b in range(len(real))] for x in values(c)]
+    check(O, stats, Q, *rows, 0.09, f"padded {dtype} n {n}")
+    assert (O[0] == 0).all() and torch.isneginf(stats[0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_pages_outside_the_cache(A, dtype):
+    # their keys are hidden; all pages of a sequence may be bad
+    page, lengths = 16, [100, 70, 40, 33]
+    c = make(A, 7, 30, 2, page, 64, 64, dtype)
+    t = tables_for(8, 29, lengths, page, 7)
+    t[t == 0] = 29  # (page 0 is what a bad number is replaced by: it holds NaN)
+    t[0, 2], t[0, 6], t[1, 0], t[1, 3], t[3, 0] = -1, 30, 2 ** 31 - 1, -2 ** 31, 99999
+    t[2, :] = -1
+    spoil_behind(c, t, lengths)
+    Q = queries(9, 4, 4, 1, 64)
+    stats = torch.empty(4, 4, 1, device="cuda")
+    O = A.attention_cached(Q, c, t.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), scale=0.125, stats=stats)
+    rows = []
+    for x in values(c):
+        per = []
+        for b, n in enumerate(lengths):
+            live = [j for j in range(n) if 0 <= int(t[b, j // page]) < 30]
+            per.append(np.stack([x[int(t[b, j // page]), :, j % page] for j in live], axis=1) if live else np.zeros((2, 0, 64)))
+        rows.append(per)
+    check(O, stats, Q, *rows, 0.125, f"bad pages {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_special_values_reach_only_the_rows_that_see_them(A, dtype):
+    # the newest tokens hold infinities (16-bit) and NaN: earlier ones of them do not see those
+    n, page, length = 4, 16, 50
+    c = make(A, 10, 5, 1, page, 64, 64, dtype)
+    t = torch.tensor([[3, 1, 4, 0]], dtype=torch.int32)
+    Q = queries(11, 1, 2, n, 64)
+    run = lambda: A.attention_cached(Q, c, t.cuda(), torch.tensor([length], dtype=torch.int32).cuda(), scale=0.125)
+    clean = run()
+    where = [(int(t[0, j // page]), 0, j % page) for j in range(length - n, length)]  # rows of the newest tokens
+    nan = float("nan") if dtype == "bf16" else 0x7f
+    V = c.v if dtype == "bf16" else c.v.view(torch.uint8)
+    K = c.k if dtype == "bf16" else c.k.view(torch.uint8)
+    V[where[1]][5] = nan
+    if dtype == "bf16":
+        V[where[2]][9], V[where[2]][10], V[where[3]][10] = float("inf"), float("-inf"), float("inf")
+    K[where[3]][0] = nan
+    O = run()
+    assert torch.equal(O[:, :, 0], clean[:, :, 0])
+    assert torch.isnan(O[0, :, 1:, 5]).all() and torch.isfinite(O[0, :, 1, :5]).all()
+    others = [d for d in range(64) if d not in (5, 9, 10)]
+    assert torch.equal(O[:, :, 1:3][..., others], clean[:, :, 1:3][..., others])
+    assert torch.isnan(O[0, :, 3]).all()
+    if dtype == "bf16":
+        assert torch.isposinf(O[0, :, 2, 9]).all() and torch.isneginf(O[0, :, 2, 10]).all()
+
+
+def test_infinity_in_the_last_row(A):
+    # a copy of the row behind the end, weighed with zero, would make it NaN
+    c = make(A, 12, 3, 1, 16, 64, 64, "bf16")
+    c.v[1, 0, 4, 7] = float("inf")  # key 20 of 21
+    Q = queries(13, 1, 1, 1, 64)
+    O = A.attention_cached(Q, c, torch.tensor([[0, 1]], dtype=torch.int32).cuda(), torch.tensor([21], dtype=torch.int32).cuda(), scale=0.125)
+    assert torch.isposinf(O[0, 0, 0, 7]) and torch.isfinite(O[0, 0, 0, :7]).all() and torch.isfinite(O[0, 0, 0, 8:]).all()
+
+
+@pytest.mark.parametrize("scale", [3.0, -0.2, 1e-4])
+def test_scales(A, scale):
+    # steep softmax (the reference moves often), a negative scale, a flat one.  Errors of the scores grow with the scale:
+    # 64 * 2^-24 * 3 * sum |q k| (about 41) = 5e-4 of a weight, inside the bound's margin over the typical 2^-9
+    c = make(A, 14, 9, 2, 64, 64, 64, "bf16")
+    t = torch.randperm(9, generator=torch.Generator().manual_seed(15)).view(1, 9).to(torch.int32)
+    Q = queries(16, 1, 6, 1, 64)
+    O = A.attention_cached(Q, c, t.cuda(), torch.tensor([570], dtype=torch.int32).cuda(), scale=scale)
+    rows = [[listed(x, t[0].tolist(), 570)] for x in values(c)]
+    check(O, None, Q, *rows, scale, f"scale {scale}")
+
+
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("H_q,H_kv,n,page,prefix,lengths,chunk", [
+    (4, 4, 1, 16, 1, [1, 2], 0),
+    (12, 12, 1, 32, 1000, [150, 1, 33, 0], 0),
+    (32, 8, 1, 64, 515, [90] * 9, 0),
+    (8, 2, 3, 16, 129, [3, 40, 17], 128),
+    (16, 1, 2, 128, 2049, [2, 130, 64, 7, 300], 256),
+    (64, 8, 1, 64, 64, [5] * 20, 0),
+])
+def test_shared_prefix(A, dqk, dv, dtype, H_q, H_kv, n, page, prefix, lengths, chunk):
+    B, width, pp = len(lengths), -(-max(lengths) // page), -(-prefix // page)
+    n_pages = pp + sum(-(-x // page) for x in lengths) + 1
+    c = make(A, 20, n_pages, H_kv, page, dqk, dv, dtype)
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(21)).to(torch.int32)
+    ptab, t, at = order[:pp].clone(), torch.full((B, width), -3, dtype=torch.int32), pp
+    for b, x in enumerate(lengths):
+        need = -(-x // page)
+        t[b, :need] = order[at: at + need]
+        at += need
+    spoil_behind(c, list(t) + [ptab], lengths + [prefix])
+    Q = queries(22, B, H_q, n, dqk)
+    stats = torch.empty(B, H_q, n, device="cuda")
+    scale = dqk ** -0.5
+    O = A.attention_cached(Q, c, t.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), scale=scale, prefix_table=ptab.cuda(), prefix_length=prefix,
+                           stats=stats, chunk=chunk)
+    kv = values(c)
+    own = [[listed(x, t[b].tolist(), lengths[b]) for b in range(B)] for x in kv]
+    pre = [listed(x, ptab.tolist(), prefix) for x in kv]
+    if min(lengths) >= n:
+        rows = [[np.concatenate((p, o), axis=1) for o in per] for p, per in zip(pre, own)]
+        check(O, stats, Q, *rows, scale, f"prefix {prefix} {dqk}/{dv} {dtype}")
+    else:  # a row without keys of its own sees the prefix alone
+        for b, x in enumerate(lengths):
+            k, v = ((np.concatenate((p, per[b]), axis=1)) for p, per in zip(pre, own))
+            qb, sb, ob = Q[b: b + 1], stats[b: b + 1], O[b: b + 1]
+            if x >= n:
+                check(ob, sb, qb, [k], [v], scale, f"prefix, sequence {b}")
+            else:
+                assert n == 1 and x == 0
+                check(ob, sb, qb, [pre[0]], [pre[1]], scale, f"prefix alone, sequence {b}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_prefix_equals_long_lists(A, dtype):
+    # the same keys, once as a shared prefix and once in every sequence's own list
+    page, prefix, B = 32, 640, 6
+    lengths = [37, 1, 64, 90, 33, 10]
+    c = make(A, 30, 20 + 6 * 3, 2, page, 128, 128, dtype)
+    ptab = torch.randperm(20, generator=torch.Generator().manual_seed(31)).to(torch.int32)
+    t = (20 + torch.arange(18).view(6, 3)).to(torch.int32)
+    Q, L = queries(32, B, 8, 1, 128), torch.tensor(lengths, dtype=torch.int32).cuda()
+    s1, s2 = torch.empty(B, 8, 1, device="cuda"), torch.empty(B, 8, 1, device="cuda")
+    a = A.attention_cached(Q, c, t.cuda(), L, scale=0.0884, prefix_table=ptab.cuda(), prefix_length=prefix, stats=s1)
+    whole = torch.cat((ptab.expand(6, 20), t), 1).contiguous().cuda()
+    b = A.attention_cached(Q, c, whole, L + prefix, scale=0.0884, stats=s2)
+    # both are within 2^-8 sum p |v| of the same result, sum p |v| <= 1.1 here
+    assert (a - b).abs().max() <= 2 * 1.1 * 2.0 ** -8 and (s1 - s2).abs().max() <= 1e-4
+
+
+def test_same_bits_twice_and_strided_output(A):
+    lengths, page = [3000, 100, 1700], 64
+    c = make(A, 40, 80, 2, page, 128, 128, "e4m3")
+    t, L = tables_for(41, 80, lengths, page, 47).cuda(), torch.tensor(lengths, dtype=torch.int32).cuda()
+    Q = queries(42, 3, 16, 2, 128)
+    buf = torch.full((3, 2, 20, 136), 5.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[:, :, 2:18, 8:136].transpose(1, 2)
+    A.attention_cached(Q, c, t, L, scale=0.0884, out=out)
+    first = out.clone()
+    assert (buf[:, :, :2] == 5).all() and (buf[:, :, 18:] == 5).all() and (buf[..., :8] == 5).all()
+    for _ in range(3):
+        again = A.attention_cached(Q, c, t, L, scale=0.0884, out_dtype=torch.bfloat16)
+        assert torch.equal(again, first)
+
+
+def test_replayed_graphs_with_growing_lengths(A):
+    # two graphs of one plan, replayed in turn while the lengths on the device grow; eager calls of another plan in between
+    page, width = 16, 40
+    c = make(A, 50, 4 * width, 2, page, 128, 128, "bf16")
+    t = torch.randperm(4 * width, generator=torch.Generator().manual_seed(51)).view(4, width).to(torch.int32).cuda()
+    L = torch.tensor([1, 100, 37, 500], dtype=torch.int32).cuda()
+    Q = queries(52, 4, 8, 1, 128)
+    outs = [torch.empty(4, 8, 1, 128, device="cuda") for _ in range(2)]
+    plan = A.CachedAttentionPlan(c, Q, outs[0], max_length=width * page, table_width=width, scale=0.0884, chunk=128)
+    plan.forward(Q, t, L, outs[0])
+    graphs = []
+    for o in outs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            plan.forward(Q, t, L, o)
+        graphs.append(g)
+    for step in range(5):
+        for g, o in zip(graphs, outs):
+            L += 7
+            g.replay()
+            eager = A.attention_cached(Q, c, t, L, scale=0.0884, chunk=128)
+            torch.cuda.synchronize()
+            assert torch.equal(o, eager), step
+
+
+def test_another_stream(A):
+    lengths, page = [900, 1300], 32
+    c = make(A, 60, 72, 4, page, 64, 64, "e4m3")
+    t, L = tables_for(61, 72, lengths, page, 41).cuda(), torch.tensor(lengths, dtype=torch.int32).cuda()
+    Q = queries(62, 2, 8, 1, 64)
+    ref = A.attention_cached(Q, c, t, L, scale=0.125)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got = A.attention_cached(Q, c, t, L, scale=0.125, stream=s)
+    s.synchronize()
+    assert torch.equal(got, ref)
+
+
+def test_cache_past_32_bits(A):
+    # pages whose byte offsets pass 2^32, a long list, few rows
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    n_pages, page = 42000, 256  # x 2 heads x 128 x 2 bytes = 5.5 GB each of K and V
+    c = A.PagedCache.empty(n_pages, 2, page, 128, 128)
+    length = 70001
+    t = torch.randperm(n_pages, generator=torch.Generator().manual_seed(70))[:274].to(torch.int32).view(1, 274)
+    t[0, 0], t[0, 1] = n_pages - 1, 33333
+    t[0, 2:] = torch.where((t[0, 2:] == n_pages - 1) | (t[0, 2:] == 33333), torch.tensor(0, dtype=torch.int32), t[0, 2:])
+    g = torch.Generator(device="cuda").manual_seed(71)
+    k, v = (torch.randn(1, 2, length, 128, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    j = torch.arange(length)
+    slots = (t[0, j // page].long() * page + j % page).to(torch.int32).cuda()
+    c.append(k, v, slots[None])
+    Q = queries(72, 1, 4, 1, 128)
+    O = A.attention_cached(Q, c, t.cuda(), torch.tensor([length], dtype=torch.int32).cuda(), scale=0.0884)
+    check(O, None, Q, [k[0].cpu().double().numpy()], [v[0].cpu().double().numpy()], 0.0884, "past 2^32")

@@ -236,6 +236,7 @@ struct ae_cached {
   ae_cached_desc_t desc;
   ae::CachedParams params;  // pointers filled in per call
   ae::CachedPart own, prefix;
+  bool wide_prefix;         // the prefix is walked by launch_prefix
   int slots;                // partial results of a row (1: written as they are)
   size_t ws_bytes;
 };
@@ -305,7 +306,9 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
     pt.max_length = own ? d->max_length : d->prefix_length;
     pt.table_width = own ? d->table_width : 0;
     pt.causal = own ? 1 : 0;
-    cut_keys(pt, cd.H_kv, ae::cached_rows_per_workgroup(cd.D_qk, cd.D_v, e4m3, pt.rows), d->chunk);
+    const bool wide = !own && pt.rows >= 192;
+    h->wide_prefix = h->wide_prefix || wide;
+    cut_keys(pt, cd.H_kv, wide ? ae::kPrefixRows : ae::cached_rows_per_workgroup(cd.D_qk, cd.D_v, e4m3, pt.rows), d->chunk);
   };
   part(h->own, true);
   if (d->prefix_length > 0) {
@@ -364,7 +367,7 @@ ae_status_t ae_cached_forward(const ae_cached_t* h, const void* Q, const void* K
   if (h->desc.prefix_length > 0) {
     p.part = h->prefix;
     p.part.table = prefix_table;
-    const ae_status_t st = launched(ae::launch_cached(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
+    const ae_status_t st = launched((h->wide_prefix ? ae::launch_prefix : ae::launch_cached)(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
     if (st != AE_OK) return st;
   }
   p.part = h->own;

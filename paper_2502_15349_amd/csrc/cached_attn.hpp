@@ -49,6 +49,8 @@ struct CachedMerge {
 
 int cached_rows_per_workgroup(int dqk, int dv, bool e4m3, int rows);
 hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);
+constexpr int kPrefixRows = 256;  // rows of a workgroup of launch_prefix
+hipError_t launch_prefix(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);
 hipError_t launch_cached_merge(const CachedMerge& p, hipStream_t s);
 
 }  // namespace ae

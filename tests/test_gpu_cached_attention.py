@@ -348,3 +348,55 @@ def test_cache_past_32_bits(A):
     Q = queries(72, 1, 4, 1, 128)
     O = A.attention_cached(Q, c, t.cuda(), torch.tensor([length], dtype=torch.int32).cuda(), scale=0.0884)
     check(O, None, Q, [k[0].cpu().double().numpy()], [v[0].cpu().double().numpy()], 0.0884, "past 2^32")
+
+
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("B,H_q,H_kv,n,page,prefix,chunk,bad", [
+    (50, 32, 8, 1, 16, 5, 0, []),          # 200 rows a k/v head, less than a tile of keys
+    (64, 32, 8, 1, 64, 700, 0, []),        # 256: one workgroup's rows
+    (65, 8, 2, 1, 32, 1024, 256, [3, 9]),  # 260: the last wavefronts have four rows; two pages are no pages
+    (40, 16, 1, 2, 16, 333, 128, [0, 20]), # 1280 rows, the last page among the bad ones, three ranges
+    (300, 1, 1, 1, 256, 2000, 0, []),
+    (23, 64, 4, 3, 128, 130, 128, [1]),    # 1104 rows; the second range has bad keys only
+])
+def test_prefix_of_many_rows(A, dqk, dv, dtype, B, H_q, H_kv, n, page, prefix, chunk, bad):
+    pp, own = -(-prefix // page), 20
+    n_pages = pp + 2 + B * 2
+    c = make(A, 80, n_pages, H_kv, page, dqk, dv, dtype)
+    order = torch.randperm(n_pages - 1, generator=torch.Generator().manual_seed(81)).to(torch.int32) + 1  # (page 0 holds NaN)
+    ptab = order[:pp].clone()
+    for i in bad:
+        ptab[i] = -1 if i % 2 else n_pages
+    width = -(-own // page)
+    t = order[pp: pp + B * width].view(B, width).clone()
+    lengths = [n + (7 * b) % (own - n) for b in range(B)]
+    spoil_behind(c, list(t) + [ptab], lengths + [prefix])
+    Q = queries(82, B, H_q, n, dqk)
+    stats = torch.empty(B, H_q, n, device="cuda")
+    scale = dqk ** -0.5
+    O = A.attention_cached(Q, c, t.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), scale=scale, prefix_table=ptab.cuda(), prefix_length=prefix,
+                           stats=stats, chunk=chunk, out_dtype=torch.bfloat16 if B == 64 else torch.float32)
+    kv = values(c)
+    live = [j for j in range(prefix) if 0 <= int(ptab[j // page]) < n_pages]
+    pre = [np.stack([x[int(ptab[j // page]), :, j % page] for j in live], axis=1) if live else np.zeros((H_kv, 0, x.shape[3])) for x in kv]
+    some = sorted({0, 1, B // 2, B - 2, B - 1})  # (the definition in 64 bits takes its time)
+    rows = [[np.concatenate((p, listed(x, t[b].tolist(), lengths[b])), axis=1) for b in some] for p, x in zip(pre, kv)]
+    check(O[some], stats[some], Q[some], *rows, scale, f"{B} x {H_q}/{H_kv} x {n} behind {prefix}, {dqk}/{dv} {dtype}")
+    # the others against the walk of few rows: the same keys as every sequence's own list
+    whole = torch.cat((ptab.expand(B, pp), t), 1).contiguous().cuda() if prefix % page == 0 else None
+    if whole is not None:
+        s2 = torch.empty_like(stats)
+        O2 = A.attention_cached(Q, c, whole, torch.tensor(lengths, dtype=torch.int32).cuda() + prefix, scale=scale, stats=s2)
+        top = float(max(np.nanmax(np.abs(np.where(np.isfinite(x), x, np.nan))) for x in kv[1:]))
+        assert (O.float() - O2).abs().max() <= 2 * (2.0 ** -8 + 2.0 ** -8) * top and (stats - s2).abs().max() <= 2e-4
+
+
+def test_negative_scale_of_many_rows(A):
+    c = make(A, 90, 12, 2, 64, 64, 64, "bf16")
+    ptab, t = torch.arange(8, dtype=torch.int32), torch.full((200, 1), 9, dtype=torch.int32)
+    Q = queries(91, 200, 4, 1, 64)
+    O = A.attention_cached(Q, c, t.cuda(), torch.full((200,), 3, dtype=torch.int32).cuda(), scale=-0.3, prefix_table=ptab.cuda(), prefix_length=500)
+    some = [0, 99, 199]
+    rows = [[np.concatenate((listed(x, ptab.tolist(), 500), listed(x, [9], 3)), axis=1) for _ in some] for x in values(c)]
+    check(O[some], None, Q[some], *rows, -0.3, "negative scale")

@@ -133,7 +133,10 @@ ae_status_t ae_cache_destroy(ae_cache_t *h); /* NULL is allowed */
  *              strides multiples of 8; strides of 0: contiguous;
  *   stats      device, fp32 [B, H_q, n_new], ln sum exp of the scaled scores; NULL: not written;
  *   workspace  device, 256-byte aligned, ae_cached_workspace_bytes (0: may be NULL); owned by
- *              the caller, contents irrelevant; calls sharing it must not overlap.
+ *              the caller.  ae_cached_init_workspace has to be enqueued once before the first
+ *              call that uses it (it clears counters, which every call leaves clear), and again
+ *              after anything else has written there, another handle's calls included.
+ *              Calls sharing it must not overlap.
  * lengths are read on the device: one outside [0, max_length] counts as the nearer
  * bound.  A page number outside [0, n_pages) is not followed: its keys count as hidden.
  * What lies in the cache behind a sequence's end may be anything, NaN included.
@@ -152,6 +155,7 @@ typedef struct {
 
 ae_status_t ae_cached_create(const ae_cache_t *cache, const ae_cached_desc_t *desc, ae_cached_t **out); /* copies what it needs of the cache's handle */
 ae_status_t ae_cached_workspace_bytes(const ae_cached_t *h, size_t *bytes);
+ae_status_t ae_cached_init_workspace(const ae_cached_t *h, void *workspace, size_t workspace_bytes, hipStream_t stream);
 ae_status_t ae_cached_forward(const ae_cached_t *h, const void *Q, const void *K_pages, const void *V_pages, const void *K_exp,
                               const void *V_exp, const int32_t *table, const int32_t *lengths, const int32_t *prefix_table,
                               void *O, float *stats, void *workspace, size_t workspace_bytes, hipStream_t stream);

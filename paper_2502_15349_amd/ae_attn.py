@@ -586,6 +586,8 @@ _lib.ae_cached_create.argtypes = [C.c_void_p, C.POINTER(ae_cached_desc_t), C.POI
 _lib.ae_cached_create.restype = C.c_int
 _lib.ae_cached_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
 _lib.ae_cached_workspace_bytes.restype = C.c_int
+_lib.ae_cached_init_workspace.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.ae_cached_init_workspace.restype = C.c_int
 _lib.ae_cached_forward.argtypes = [C.c_void_p] * 12 + [C.c_size_t, C.c_void_p]
 _lib.ae_cached_forward.restype = C.c_int
 _lib.ae_cached_destroy.argtypes = [C.c_void_p]
@@ -679,6 +681,11 @@ def ae_cached_workspace_bytes(handle: int) -> int:
     n = C.c_size_t()
     _check(_lib.ae_cached_workspace_bytes(handle, C.byref(n)))
     return n.value
+
+
+def ae_cached_init_workspace(handle: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """Once before the first call that uses the workspace (and after anything else has written there)."""
+    _check(_lib.ae_cached_init_workspace(handle, workspace, workspace_bytes, stream))
 
 
 def ae_cached_forward(handle: int, Q: int, K_pages: int, V_pages: int, K_exp: int, V_exp: int, table: int, lengths: int, prefix_table: int,
@@ -917,7 +924,8 @@ class CachedAttentionPlan:
     """A handle for attention of the newest tokens over a PagedCache, for calls of one shape: the step of a decoding loop keeps it, and
     its workspace.  Q [B, H_q, n, D_qk] bf16 and out [B, H_q, n, D_v] (bf16 or fp32) give shapes, strides and device; max_length: no
     sequence has more keys of its own; table_width: pages in a row of the table; prefix_length: keys that all sequences share.
-    Calls of one plan must not overlap (they share its workspace); a captured graph keeps using the plan's buffers."""
+    Calls of one plan must not overlap (they share its workspace, which is prepared on the stream that is current when the plan is
+    made); a captured graph keeps using the plan's buffers."""
 
     def __init__(self, cache, Q, out, *, max_length, table_width, scale, prefix_length=0, chunk=0):
         import torch
@@ -939,7 +947,11 @@ class CachedAttentionPlan:
         self._q, self._o = _shape_of(Q), _shape_of(out)
         self._table, self._prefix = (B, table_width), -(-prefix_length // cache.page_size)
         self.workspace_bytes = ae_cached_workspace_bytes(self.handle)
-        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=Q.device) if self.workspace_bytes else None
+        self.workspace = None
+        if self.workspace_bytes:
+            with torch.cuda.device(Q.device):
+                self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=Q.device)
+                ae_cached_init_workspace(self.handle, self.workspace.data_ptr(), self.workspace_bytes, _stream_of(None, Q.device))
 
     def forward(self, Q, table, lengths, out, *, stats=None, prefix_table=None, stream=None):
         """table int32 [B, table_width], lengths int32 [B] (device), prefix_table int32 [pages of the prefix]; stats: fp32 [B, H_q, n] that

@@ -235,24 +235,23 @@ struct ae_cached {
   ae_cache_desc_t cache;
   ae_cached_desc_t desc;
   ae::CachedParams params;  // pointers filled in per call
-  ae::CachedPart own, prefix;
-  bool wide_prefix;         // the prefix is walked by launch_prefix
-  int slots;                // partial results of a row (1: written as they are)
-  size_t ws_bytes;
+  bool prefix_apart;        // the prefix is walked by a launch of its own, in front
+  int slots;                // partial results of a row
+  bool counted;             // workgroups join their results: the last one of a row does
+  size_t counter_bytes, o_bytes, ws_bytes;
 };
 
 namespace {
 
-constexpr size_t kWsAlign = 256;
-size_t round_up(size_t x) { return (x + kWsAlign - 1) / kWsAlign * kWsAlign; }
+size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 
-// How the keys of a part are cut: into chunks that make about `target` workgroups, of at least 256 keys.
-void cut_keys(ae::CachedPart& pt, int H_kv, int rows_per_wg, int64_t chunk) {
+// How the keys of a part are cut: chunks that make about `target` workgroups, of at least `least` keys.
+void cut_keys(ae::CachedPart& pt, int H_kv, int rows_per_wg, int64_t chunk, int64_t target, int64_t least) {
   pt.row_tiles = (pt.rows + rows_per_wg - 1) / rows_per_wg;
-  const int64_t units = (int64_t)pt.lists * H_kv * pt.row_tiles, target = 1024;
+  const int64_t units = (int64_t)pt.lists * H_kv * pt.row_tiles;
   if (chunk == 0) {
     const int64_t cuts = std::max<int64_t>(1, (target + units - 1) / units);
-    chunk = std::max<int64_t>(256, ((pt.max_length + cuts - 1) / cuts + 127) / 128 * 128);
+    chunk = std::max<int64_t>(least, ((pt.max_length + cuts - 1) / cuts + 127) / 128 * 128);
   }
   pt.chunk = (int)std::min<int64_t>(chunk, ((int64_t)pt.max_length + 127) / 128 * 128);
   pt.splits = (int)(((int64_t)pt.max_length + pt.chunk - 1) / pt.chunk);
@@ -275,8 +274,8 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
   if (!std::isfinite(d->scale) || d->scale == 0.f) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: scale must be finite and non-zero");
   if (d->out_dtype != AE_OUT_F32 && d->out_dtype != AE_OUT_BF16) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: unknown out_dtype %d", (int)d->out_dtype);
   const int64_t rows = (int64_t)d->B * d->H_q * d->n_new;
-  if (rows > 1 << 24 || d->max_length > 0x7fffff00 || d->prefix_length > 0x7fffff00 || d->chunk > 0x7fffff00)
-    return fail(AE_ERR_UNSUPPORTED, "ae_cached_create: at most 2^24 query rows and 2^31 - 256 keys");
+  if (rows > 1 << 24 || d->max_length > 1 << 30 || d->prefix_length > 1 << 30 || d->chunk > 1 << 30)
+    return fail(AE_ERR_UNSUPPORTED, "ae_cached_create: at most 2^24 query rows and 2^30 keys");
   ae_cached* h = new (std::nothrow) ae_cached();
   if (!h) return fail(AE_ERR_NOMEM, "ae_cached_create: out of host memory");
   h->cache = cd;
@@ -298,25 +297,32 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
   p.n_pages = cd.n_pages;
   p.c = d->scale * 1.4426950408889634f;
   p.out_bf16 = d->out_dtype == AE_OUT_BF16;
-  const bool e4m3 = cd.dtype == AE_CACHE_E4M3;
-  auto part = [&](ae::CachedPart& pt, bool own) {
-    pt = ae::CachedPart();
-    pt.lists = own ? d->B : 1;
-    pt.rows = (own ? 1 : d->B) * d->n_new * p.g;
-    pt.max_length = own ? d->max_length : d->prefix_length;
-    pt.table_width = own ? d->table_width : 0;
-    pt.causal = own ? 1 : 0;
-    const bool wide = !own && pt.rows >= 192;
-    h->wide_prefix = h->wide_prefix || wide;
-    cut_keys(pt, cd.H_kv, wide ? ae::kPrefixRows : ae::cached_rows_per_workgroup(cd.D_qk, cd.D_v, e4m3, pt.rows), d->chunk);
-  };
-  part(h->own, true);
+  ae::CachedPart &own = p.part[0], &prefix = p.part[1];
+  own.lists = d->B;
+  own.rows = d->n_new * p.g;
+  own.max_length = d->max_length;
+  own.table_width = d->table_width;
+  own.causal = 1;
   if (d->prefix_length > 0) {
-    part(h->prefix, false);
-    h->own.slot0 = h->prefix.splits;
+    prefix.lists = 1;
+    prefix.rows = d->B * d->n_new * p.g;
+    prefix.max_length = d->prefix_length;
+    prefix.table_width = (d->prefix_length + cd.page_size - 1) / cd.page_size;
+    h->prefix_apart = prefix.rows > 32;
+    if (h->prefix_apart) {
+      cut_keys(prefix, cd.H_kv, ae::kPrefixRows, d->chunk, 256, 256);
+    } else {
+      cut_keys(prefix, cd.H_kv, ae::cached_rows_per_workgroup(prefix.rows), d->chunk, 512, 128);
+      p.prefix_blocks = (cd.H_kv * prefix.splits + 7) / 8 * 8 * prefix.row_tiles;
+    }
+    own.slot0 = prefix.splits;
   }
-  h->slots = h->own.splits + h->own.slot0;
-  h->ws_bytes = h->slots == 1 ? 0 : round_up((size_t)h->slots * rows * cd.D_v * 4) + round_up((size_t)h->slots * rows * 4);
+  cut_keys(own, cd.H_kv, ae::cached_rows_per_workgroup(p.prefix_blocks ? prefix.rows : own.rows), d->chunk, 768, 128);
+  h->slots = own.splits + own.slot0;
+  h->counted = own.splits > 1 || p.prefix_blocks > 0;
+  h->counter_bytes = h->counted ? round_up((size_t)d->B * cd.H_kv * own.row_tiles * 4) : 0;
+  h->o_bytes = round_up((size_t)h->slots * rows * cd.D_v * 4);
+  h->ws_bytes = h->slots == 1 ? 0 : h->counter_bytes + h->o_bytes + round_up((size_t)h->slots * rows * 4);
   if ((double)h->slots * rows * cd.D_v * 4 > 1e12) {
     delete h;
     return fail(AE_ERR_UNSUPPORTED, "ae_cached_create: the partial results would take more than 10^12 bytes");
@@ -329,6 +335,14 @@ ae_status_t ae_cached_workspace_bytes(const ae_cached_t* h, size_t* bytes) {
   if (!h || !bytes) return fail(AE_ERR_INVALID_ARG, "ae_cached_workspace_bytes: null argument");
   *bytes = h->ws_bytes;
   return AE_OK;
+}
+
+ae_status_t ae_cached_init_workspace(const ae_cached_t* h, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (!h) return fail(AE_ERR_INVALID_ARG, "ae_cached_init_workspace: null handle");
+  if (h->ws_bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < h->ws_bytes))
+    return fail(AE_ERR_INVALID_ARG, "ae_cached_init_workspace: workspace missing, not 256-byte aligned, or smaller than %zu bytes", h->ws_bytes);
+  if (!h->counter_bytes) return AE_OK;
+  return launched(ae::launch_fill_zero(static_cast<int32_t*>(workspace), (int64_t)h->counter_bytes / 4, stream), "ae_cached_init_workspace");
 }
 
 ae_status_t ae_cached_forward(const ae_cached_t* h, const void* Q, const void* K_pages, const void* V_pages, const void* K_exp, const void* V_exp,
@@ -361,36 +375,20 @@ ae_status_t ae_cached_forward(const ae_cached_t* h, const void* Q, const void* K
   p.V = static_cast<const uint8_t*>(V_pages);
   p.Ke = static_cast<const uint8_t*>(K_exp);
   p.Ve = static_cast<const uint8_t*>(V_exp);
-  const size_t rows = (size_t)p.B * p.H_q * p.n;
-  p.ws_o = h->ws_bytes ? static_cast<float*>(workspace) : nullptr;
-  p.ws_lse = h->ws_bytes ? reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up((size_t)h->slots * rows * h->cache.D_v * 4)) : nullptr;
-  if (h->desc.prefix_length > 0) {
-    p.part = h->prefix;
-    p.part.table = prefix_table;
-    const ae_status_t st = launched((h->wide_prefix ? ae::launch_prefix : ae::launch_cached)(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
+  if (h->ws_bytes) {
+    char* ws = static_cast<char*>(workspace);
+    p.counters = h->counted ? reinterpret_cast<int32_t*>(ws) : nullptr;
+    p.ws_o = reinterpret_cast<float*>(ws + h->counter_bytes);
+    p.ws_lse = reinterpret_cast<float*>(ws + h->counter_bytes + h->o_bytes);
+  }
+  p.part[0].table = table;
+  p.part[0].lengths = lengths;
+  p.part[1].table = prefix_table;
+  if (h->prefix_apart) {
+    const ae_status_t st = launched(ae::launch_prefix(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
     if (st != AE_OK) return st;
   }
-  p.part = h->own;
-  p.part.table = table;
-  p.part.lengths = lengths;
-  const ae_status_t st = launched(ae::launch_cached(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
-  if (st != AE_OK || !h->ws_bytes) return st;
-  ae::CachedMerge mp = {};
-  mp.ws_o = p.ws_o;
-  mp.ws_lse = p.ws_lse;
-  mp.O = O;
-  for (int a = 0; a < 3; ++a) mp.os[a] = p.os[a];
-  mp.stats = stats;
-  mp.lengths = lengths;
-  mp.B = p.B;
-  mp.H_q = p.H_q;
-  mp.n = p.n;
-  mp.d_v = h->cache.D_v;
-  mp.out_bf16 = p.out_bf16;
-  mp.prefix_slots = h->own.slot0;
-  mp.chunk = h->own.chunk;
-  mp.max_length = h->own.max_length;
-  return launched(ae::launch_cached_merge(mp, stream), who);
+  return launched(ae::launch_cached(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
 }
 
 ae_status_t ae_cached_destroy(ae_cached_t* h) {

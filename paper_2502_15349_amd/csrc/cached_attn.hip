@@ -34,15 +34,19 @@ struct CachedCfg {
   static constexpr bool E4M3 = E4M3_;
   static constexpr int ESZ = E4M3 ? 1 : 2, RBK = DQK * ESZ, RBV = DV * ESZ, CPRK = RBK / 16, CPRV = RBV / 16;
   static constexpr int K_BYTES = 32 * RBK, V_BYTES = 32 * RBV, E_BYTES = E4M3 ? 256 : 0, STAGE = K_BYTES + V_BYTES + E_BYTES;
-  static constexpr int NK = K_BYTES / 1024, NV = V_BYTES / 1024, LOADS = NK + NV + (E4M3 ? 1 : 0);
-  static constexpr int STAGES = 2;
+  static constexpr int NK = K_BYTES / 1024, NV = V_BYTES / 1024;
+  static constexpr int NKE = NK + (E4M3 ? 1 : 0);  // copies awaited before the scores (the exponents come with the keys)
+#ifndef AE_TUNE_CST
+#define AE_TUNE_CST 1
+#endif
+  static constexpr int STAGES = AE_TUNE_CST;
   static constexpr int KS = DQK / 32, DB = DV / 16;
   static constexpr int ROWS = 16 * RT;
   static constexpr int RED_ROW = DV + 4;
   static constexpr int RED_BYTES = W * 16 * (RED_ROW + 2) * 4;
   static constexpr int LDS_BYTES = W * STAGES * STAGE > RED_BYTES ? W * STAGES * STAGE : RED_BYTES;
   static_assert(LDS_BYTES <= 160 * 1024, "a workgroup must fit LDS");
-  static_assert((STAGES - 1) * LOADS < 64, "the wait count has six bits");
+  static_assert(STAGES * (NKE + NV) < 64, "the wait count has six bits");
 };
 
 // ---- chunk swizzles: LDS position of 16-byte chunk c of tile row r is c ^ swizzle(r) -------------------------------------------
@@ -90,26 +94,48 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) 
 
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 
+// Partial results that another workgroup of the same launch reads, on any XCD: stored past the L2 and loaded past it, value by
+// value (relaxed atomics of the whole device).  A release and an acquire of the device instead write back and invalidate an L2 that
+// the other workgroups of the XCD are reading their keys through: 32 x 32/8 x 5003 keys in ranges of 1024 took 164 us with them.
+__device__ __forceinline__ void store_shared(float* at, f32x4 v) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint64_t u = ((uint64_t)__builtin_bit_cast(uint32_t, (float)v[2 * k + 1]) << 32) | __builtin_bit_cast(uint32_t, (float)v[2 * k]);
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(at) + k, u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+__device__ __forceinline__ f32x4 load_shared(const float* at) {
+  f32x4 v;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint64_t u = __hip_atomic_load(reinterpret_cast<const uint64_t*>(at) + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    v[2 * k] = __builtin_bit_cast(float, (uint32_t)u);
+    v[2 * k + 1] = __builtin_bit_cast(float, (uint32_t)(u >> 32));
+  }
+  return v;
+}
+
+// RT = 1: 168 registers instead of 180 let a third workgroup onto a compute unit where LDS has room for it.
 template <class C>
-__global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedParams p) {
+__global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) void cached_attn_kernel(const CachedParams p) {
   __shared__ __attribute__((aligned(1024))) char smem[C::LDS_BYTES];
-  const CachedPart& pt = p.part;
+  const bool is_prefix = (int)blockIdx.x < p.prefix_blocks;
+  const CachedPart& pt = p.part[is_prefix ? 1 : 0];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ql = lane & 15, hi = lane >> 4;
 
   // ---- workgroup -> (list, k/v head), key range, row tile ------------------------------------------------------------
   // Row tiles that read the same keys are 8 workgroups apart: next to each other on one XCD, whose L2 has the keys for the second.
-  const int units = pt.lists * p.H_kv * pt.splits;
-  const int w8 = blockIdx.x & 7, slot = blockIdx.x >> 3;
-  const int unit = (slot / pt.row_tiles) * 8 + w8, tile = slot % pt.row_tiles;
-  if (unit >= units) return;
-  const int split = unit / (pt.lists * p.H_kv), head = unit % (pt.lists * p.H_kv);
+  const int heads = pt.lists * p.H_kv, block = blockIdx.x - (is_prefix ? 0 : p.prefix_blocks);
+  const int slot = block >> 3, unit = (slot / pt.row_tiles) * 8 + (block & 7), tile = slot % pt.row_tiles;
+  if (unit >= heads * pt.splits) return;
+  const int split = unit / heads, head = unit % heads;
   const int list = head / p.H_kv, hk = head % p.H_kv;
+  const int32_t* table = pt.table + (int64_t)list * pt.table_width;
   int len = pt.max_length;
   if (pt.lengths != nullptr) len = max(0, min(scalar_load(pt.lengths + list), len));
   const int begin = split * pt.chunk, end = min(len, begin + pt.chunk);
-  if (begin >= len && (p.ws_o != nullptr || split > 0)) return;  // (nothing reads the partial result of a range past the end)
-  const int32_t* table = pt.table + (int64_t)list * pt.table_width;
+  if (begin >= len && split > 0) return;  // (range 0 is always there: a list without keys has rows to write)
 
   // ---- the query rows: B fragments, lane = row ql, 8 elements of group hi ----------------------------------------------
   const int row0 = tile * C::ROWS;
@@ -152,31 +178,40 @@ __global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedPar
   // as hidden, and the copy takes page 0's instead, as it takes the first half's again for a half behind the last key; rows
   // behind the last key are copied as they lie in the page.  What a hidden key holds is masked below.  Returns which halves
   // are hidden.
-  auto issue = [&](int i, int stage) -> int {
+  int pg0, pg1;    // page numbers of the sub-tile whose keys are copied next
+  int64_t row[2];  // first rows, in the cache, of the halves of the one whose keys were copied last
+  auto fetch_pages = [&](int i) {  // (entries behind the list's end may be read, not followed)
+    const int j0 = begin + 32 * (wave + i * C::W);
+    pg0 = scalar_load(table + min(j0 >> p.page_shift, pt.table_width - 1));
+    pg1 = scalar_load(table + min((j0 + 16) >> p.page_shift, pt.table_width - 1));
+  };
+  auto issue_k = [&](int i, int stage) -> int {
     const int j0 = begin + 32 * (wave + i * C::W);
     const bool second = j0 + 16 < end;
-    const int pg0 = scalar_load(table + (j0 >> p.page_shift));
-    const int pg1 = second ? scalar_load(table + ((j0 + 16) >> p.page_shift)) : pg0;
-    const bool ok0 = (uint32_t)pg0 < (uint32_t)p.n_pages, ok1 = (uint32_t)pg1 < (uint32_t)p.n_pages;
+    const bool ok0 = (uint32_t)pg0 < (uint32_t)p.n_pages, ok1 = second ? (uint32_t)pg1 < (uint32_t)p.n_pages : ok0;
     const uint32_t base = lds0 + stage * C::STAGE;
-    int64_t row[2];  // first row of the half in the cache
     row[0] = (((int64_t)(ok0 ? pg0 : 0) * p.H_kv + hk) << p.page_shift) + (j0 & page_mask);
     row[1] = second ? (((int64_t)(ok1 ? pg1 : 0) * p.H_kv + hk) << p.page_shift) + ((j0 + 16) & page_mask) : row[0];
+    fetch_pages(i + 1);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint8_t* kb = p.K + row[h] * C::RBK;
-      const uint8_t* vb = p.V + row[h] * C::RBV;
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < C::NK / 2; ++i) dma16(kb, koff[h * (C::NK / 2) + i], base + (h * (C::NK / 2) + i) * 1024);
-#pragma unroll
-      for (int i = 0; i < C::NV / 2; ++i) dma16(vb, voff[h * (C::NV / 2) + i], base + C::K_BYTES + (h * (C::NV / 2) + i) * 1024);
-    }
+      for (int i = 0; i < C::NK / 2; ++i)
+        dma16(p.K + row[h] * C::RBK, koff[h * (C::NK / 2) + i], base + (h * (C::NK / 2) + i) * 1024);
     if constexpr (C::E4M3) {  // bytes 0..31: exponents of the keys, 32..63: of the values (lanes 16.. repeat them)
       const int k = lane & 15;
       const uint8_t* e = (k & 8 ? p.Ve : p.Ke) + row[(k >> 2) & 1] + 4 * (k & 3);
       dma4_gather(e, base + C::K_BYTES + C::V_BYTES);
     }
     return (ok0 ? 0 : 1) | (ok1 ? 0 : 2);
+  };
+  auto issue_v = [&](int stage) {
+    const uint32_t base = lds0 + stage * C::STAGE + C::K_BYTES;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < C::NV / 2; ++i)
+        dma16(p.V + row[h] * C::RBV, voff[h * (C::NV / 2) + i], base + (h * (C::NV / 2) + i) * 1024);
   };
 
   // ---- fragments -------------------------------------------------------------------------------------------------------------
@@ -210,8 +245,8 @@ __global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedPar
     for (int d = 0; d < C::DB; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  auto compute = [&](int i, int stage, int hidden) {
-    if (hidden == 3) return;
+  // One sub-tile; `keys_read` runs behind the last read of its keys, `await_values` in front of the first of its values.
+  auto compute = [&](int i, int stage, int hidden, auto&& keys_read, auto&& await_values) {
     const int j0 = begin + 32 * (wave + i * C::W);
     const uint32_t so = stage * C::STAGE;
     const bool masked = hidden != 0 || j0 + 32 > min(all_visible, end);
@@ -253,6 +288,7 @@ __global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedPar
           for (int rt = 0; rt < C::RT; ++rt) s[u][rt] = mfma16(a, qf[rt][ss], s[u][rt]);
         }
     }
+    keys_read();
     // of the lane's 8 keys, those below there are in the list (and on a page of the cache); below last + 1, visible to its row
     const int there = (hi < 2 ? hidden & 1 : hidden & 2) ? 0 : end - j0 - 8 * hi;
     bf16x8 pb[C::RT];
@@ -294,6 +330,7 @@ __global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedPar
 #pragma unroll
       for (int e = 0; e < 8; ++e) pb[rt][e] = (__bf16)x[e];
     }
+    await_values();
     if (!masked) {
 #pragma unroll
       for (int d = 0; d < C::DB; ++d) {
@@ -349,23 +386,45 @@ __global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedPar
   };
 
   // ---- the walk ------------------------------------------------------------------------------------------------------------------
+  // Keys and values of a stage are recycled apart: the next keys are requested as soon as the scores have read these, the next
+  // values behind the second product.  In flight behind a copy that is awaited (in order): whatever was requested after it.
   int hid[C::STAGES];
+  fetch_pages(0);
 #pragma unroll
-  for (int s = 0; s < C::STAGES; ++s) hid[s] = s < n_my ? issue(s, s) : 0;
+  for (int s = 0; s < C::STAGES; ++s) {
+    hid[s] = 0;
+    if (s < n_my) {
+      hid[s] = issue_k(s, s);
+      issue_v(s);
+    }
+  }
 #pragma unroll
   for (int rt = 0; rt < C::RT; ++rt)
 #pragma unroll
     for (int s = 0; s < C::KS; ++s) asm volatile("" ::"v"(qf[rt][s]));  // (awaited here, not inside the loop)
+  auto all_read = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };  // before a copy overwrites what was read
+  constexpr int PAIR = C::NKE + C::NV;
   for (int i0 = 0; i0 < n_my; i0 += C::STAGES) {
 #pragma unroll
     for (int s = 0; s < C::STAGES; ++s) {
       const int i = i0 + s;
       if (i < n_my) {
-        if (i + C::STAGES - 1 < n_my) wait_vmem<(C::STAGES - 1) * C::LOADS>();
-        else wait_vmem<0>();
-        compute(i, s, hid[s]);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // every fragment is read before the copy overwrites the stage
-        if (i + C::STAGES < n_my) hid[s] = issue(i + C::STAGES, s);
+        if (i + C::STAGES - 1 < n_my) wait_vmem<(C::STAGES - 1) * PAIR + C::NV>();
+        else wait_vmem<C::NV>();
+        const int hidden = hid[s];
+        const bool next = i + C::STAGES < n_my;
+        compute(
+            i, s, hidden,
+            [&] {
+              all_read();
+              if (next) hid[s] = issue_k(i + C::STAGES, s);
+            },
+            [&] {
+              if (next) wait_vmem<(C::STAGES - 1) * PAIR + C::NKE>();
+              else wait_vmem<0>();
+            });
+        all_read();
+        if (next) issue_v(s);
       }
     }
   }
@@ -373,6 +432,67 @@ __global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedPar
   // ---- the wavefronts' states into one, row tile by row tile --------------------------------------------------------------------
   float* red = reinterpret_cast<float*>(smem);  // [W][16][RED_ROW], then [W][16][2]
   float* red_ml = red + C::W * 16 * C::RED_ROW;
+  constexpr int PER = C::THREADS / 16, COLS = C::DV / PER;  // threads per row, columns per thread
+  const int r = threadIdx.x / PER, c0 = (threadIdx.x % PER) * COLS;
+  const int64_t all_rows = (int64_t)p.B * p.H_q * p.n;
+  float M, L, acc[COLS];  // of the thread's row: reference (log2), sum of weights, and its columns, not normalised
+  auto scale_by = [&](float f) {
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) acc[e] *= f;
+  };
+  // (M, L, acc) and the partial results of slots [s0, s1) of row `id`: the rule by which two states of an online softmax are joined
+  auto join = [&](auto sharedc, int64_t id, int s0, int s1) {
+    constexpr bool SHARED = decltype(sharedc)::value;
+    constexpr int BATCH = 4;  // partial results in flight
+    const float* po = p.ws_o + id * C::DV + c0;
+    const float* pl = p.ws_lse + id;
+    for (int s = s0; s < s1; s += BATCH) {
+      float lse[BATCH];
+      f32x4 part[BATCH][COLS / 4];
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int64_t at = (int64_t)min(s + u, s1 - 1) * all_rows;
+        lse[u] = SHARED ? __hip_atomic_load(pl + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : pl[at];
+#pragma unroll
+        for (int e = 0; e < COLS / 4; ++e) part[u][e] = SHARED ? load_shared(po + at * C::DV + 4 * e) : *reinterpret_cast<const f32x4*>(po + at * C::DV + 4 * e);
+      }
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) lse[u] = s + u < s1 ? lse[u] : -INFINITY;
+      float top = M;
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) top = fmaxf(top, lse[u]);
+      if (__builtin_bit_cast(uint32_t, top) == 0xff800000u) continue;  // no key so far
+      const float a = fast_exp2(M - top);
+      M = top;
+      L *= a;
+      scale_by(a);
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const float w = fast_exp2(lse[u] - top);
+        L += w;
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) acc[e] += w * (__builtin_bit_cast(uint32_t, w) == 0 ? 0.f : part[u][e / 4][e % 4]);
+      }
+    }
+  };
+  // no visible key leaves the sum at +0; told from a NaN by its bits (device code is compiled for no NaN to occur)
+  auto any = [&] { return __builtin_bit_cast(uint32_t, L) != 0; };
+  auto write_out = [&](int b, int t, int h, int64_t id) {
+    scale_by(any() ? 1.f / L : 0.f);
+    const int64_t at = b * p.os[0] + h * p.os[1] + t * p.os[2] + c0;
+#pragma unroll
+    for (int e = 0; e < COLS; e += 4) {
+      if (p.out_bf16) {
+        bf16x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = (__bf16)acc[e + k];
+        *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.O) + at + e) = v;
+      } else {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(p.O) + at + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+      }
+    }
+    if (c0 == 0 && p.stats != nullptr) p.stats[id] = any() ? (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f : -INFINITY;
+  };
 #pragma unroll
   for (int rt = 0; rt < C::RT; ++rt) {
     if (row0 + 16 * rt >= pt.rows) break;
@@ -387,10 +507,10 @@ __global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedPar
       red_ml[(wave * 16 + ql) * 2 + 1] = lt;
     }
     __syncthreads();
-    constexpr int PER = C::THREADS / 16, COLS = C::DV / PER;  // threads per row, columns per thread
-    const int r = threadIdx.x / PER, c0 = (threadIdx.x % PER) * COLS;
     if (row0 + 16 * rt + r < pt.rows) {
-      float M = -INFINITY, f[C::W], L = 0.f, acc[COLS];
+      float f[C::W];
+      M = -INFINITY;
+      L = 0.f;
 #pragma unroll
       for (int w = 0; w < C::W; ++w) M = fmaxf(M, red_ml[(w * 16 + r) * 2]);
       const float ref = M == -INFINITY ? 0.f : M;
@@ -405,99 +525,75 @@ __global__ __launch_bounds__(C::THREADS) void cached_attn_kernel(const CachedPar
       for (int w = 0; w < C::W; ++w)
 #pragma unroll
         for (int e = 0; e < COLS; ++e) acc[e] += f[w] * red[(w * 16 + r) * C::RED_ROW + c0 + e];
-      // no visible key leaves the sum at +0; told from a NaN by its bits (device code is compiled for no NaN to occur)
-      const bool any = __builtin_bit_cast(uint32_t, L) != 0;
-      const float inv = any ? 1.f / L : 0.f;
       int b, t, h;
       place(row0 + 16 * rt + r, b, t, h);
       const int64_t id = ((int64_t)b * p.H_q + h) * p.n + t;
-      if (p.ws_o != nullptr) {
-        const int64_t at = (int64_t)(pt.slot0 + split) * ((int64_t)p.B * p.H_q * p.n) + id;
+      if (is_prefix || p.counters != nullptr) {
+        const int64_t at = (int64_t)(pt.slot0 + split) * all_rows + id;
+        const float inv = any() ? 1.f / L : 0.f;
 #pragma unroll
         for (int e = 0; e < COLS; e += 4)
-          *reinterpret_cast<f32x4*>(p.ws_o + at * C::DV + c0 + e) = f32x4{acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv};
-        if (c0 == 0) p.ws_lse[at] = any ? M + __builtin_amdgcn_logf(L) : -INFINITY;
-      } else {
-        const int64_t at = b * p.os[0] + h * p.os[1] + t * p.os[2] + c0;
-#pragma unroll
-        for (int e = 0; e < COLS; e += 4) {
-          if (p.out_bf16) {
-            bf16x4 v;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = (__bf16)(acc[e + k] * inv);
-            *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.O) + at + e) = v;
-          } else {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(p.O) + at + e) = f32x4{acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv};
-          }
-        }
-        if (c0 == 0 && p.stats != nullptr) p.stats[id] = any ? (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f : -INFINITY;
+          store_shared(p.ws_o + at * C::DV + c0 + e, f32x4{acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv});
+        if (c0 == 0) __hip_atomic_store(p.ws_lse + at, any() ? M + __builtin_amdgcn_logf(L) : -INFINITY, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      } else {  // the only workgroup of its rows, but for a prefix that an earlier launch has walked
+        join(std::false_type{}, id, 0, pt.slot0);
+        write_out(b, t, h, id);
       }
     }
   }
+  if (p.counters == nullptr) return;
+
+  // ---- the last workgroup of a row joins its partial results -------------------------------------------------------------------------
+  // Every workgroup counts itself done for its sequences once all it stored has arrived; the one that finds all others done
+  // joins, in the slots' order (the result does not depend on who is last), and leaves the counter at zero.
+  const CachedPart& own = p.part[0];
+  const int n_seq = is_prefix ? p.B : 1;  // (of a prefix in this launch: all rows in one tile)
+  int32_t* done = reinterpret_cast<int32_t*>(smem);  // [n_seq]: this workgroup is the last one of the sequence
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if ((int)threadIdx.x < n_seq) {
+    const int b = is_prefix ? threadIdx.x : list;
+    const int keys = max(0, min(own.lengths[b], own.max_length));
+    const int expected = max(1, (keys + own.chunk - 1) / own.chunk) + (p.prefix_blocks ? p.part[1].splits : 0);
+    int32_t* counter = p.counters + (b * p.H_kv + hk) * own.row_tiles + (is_prefix ? 0 : tile);
+    const bool last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == expected - 1;
+    if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    done[threadIdx.x] = last;
+  }
+  __syncthreads();
+  for (int rt = 0; rt < C::RT; ++rt) {
+    if (row0 + 16 * rt + r >= pt.rows) break;
+    int b, t, h;
+    place(row0 + 16 * rt + r, b, t, h);
+    if (!done[is_prefix ? b : 0]) continue;
+    const int64_t id = ((int64_t)b * p.H_q + h) * p.n + t;
+    const int keys = max(0, min(own.lengths[b], own.max_length));
+    M = -INFINITY;
+    L = 0.f;
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
+    join(std::true_type{}, id, 0, own.slot0 + max(1, (keys + own.chunk - 1) / own.chunk));
+    write_out(b, t, h, id);
+  }
 }
 
-// ---- partial results into one: O = sum_c 2^(lse_c - LSE) O_c ----------------------------------------------------------------
-// One wavefront per row, D_v / 64 columns a lane.
-template <int VEC>
-__global__ __launch_bounds__(256) void cached_merge_kernel(const CachedMerge p) {
-  typedef float vec __attribute__((ext_vector_type(VEC)));
-  const int64_t rows = (int64_t)p.B * p.H_q * p.n, r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= rows) return;
-  const int lane = threadIdx.x & 63;
-  const int t = (int)(r % p.n), h = (int)((r / p.n) % p.H_q), b = (int)(r / ((int64_t)p.n * p.H_q));
-  const int len = max(0, min(p.lengths[b], p.max_length));
-  const int slots = p.prefix_slots + (len + p.chunk - 1) / p.chunk;
-  float M = -INFINITY, L = 0.f;
-  vec acc = 0.f;
-  for (int c0 = 0; c0 < slots; c0 += 64) {
-    const int mine = c0 + lane;
-    const float lse = mine < slots ? p.ws_lse[(int64_t)mine * rows + r] : -INFINITY;
-    float top = lse;
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
-    top = fmaxf(top, M);
-    if (__builtin_bit_cast(uint32_t, top) == 0xff800000u) continue;  // no key so far
-    const float w = fast_exp2(lse - top), alpha = fast_exp2(M - top);
-    M = top;
-    L *= alpha;
-    acc *= alpha;
-    float tot = w;
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) tot += __shfl_xor(tot, s);
-    L += tot;
-    const int n = min(64, slots - c0);
-    constexpr int kBatch = 8;
-    for (int c = 0; c < n; c += kBatch) {
-      vec part[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u)
-        part[u] = *reinterpret_cast<const vec*>(p.ws_o + ((int64_t)(c0 + min(c + u, n - 1)) * rows + r) * p.d_v + VEC * lane);
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) acc += (c + u < n ? __shfl(w, (c + u) & 63) : 0.f) * part[u];
-    }
-  }
-  const bool any = __builtin_bit_cast(uint32_t, L) != 0;
-  acc *= any ? 1.f / L : 0.f;
-  const int64_t at = b * p.os[0] + h * p.os[1] + t * p.os[2] + VEC * lane;
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    if (p.out_bf16) static_cast<__bf16*>(p.O)[at + e] = (__bf16)acc[e];
-    else static_cast<float*>(p.O)[at + e] = acc[e];
-  }
-  if (p.stats != nullptr && lane == 0) p.stats[r] = any ? (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f : -INFINITY;
+__global__ __launch_bounds__(256) void fill_zero_kernel(int32_t* at, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) at[i] = 0;
 }
 
 template <class C>
 hipError_t launch_cfg(const CachedParams& p, hipStream_t s) {
-  const int64_t units = (int64_t)p.part.lists * p.H_kv * p.part.splits, grid = (units + 7) / 8 * 8 * p.part.row_tiles;
-  if (!launch_fits(grid, C::THREADS)) return hipErrorInvalidConfiguration;
+  const CachedPart& pt = p.part[0];
+  const int64_t units = (int64_t)pt.lists * p.H_kv * pt.splits, grid = (units + 7) / 8 * 8 * pt.row_tiles + p.prefix_blocks;
+  if (!launch_fits(grid, C::THREADS) || grid > 0x7fffffff) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((cached_attn_kernel<C>), dim3((unsigned)grid), dim3(C::THREADS), 0, s, p);
   return hipGetLastError();
 }
 
 template <int DQK, int DV, bool E4M3>
 hipError_t launch_rows(const CachedParams& p, hipStream_t s) {
-  const int rows = cached_rows_per_workgroup(DQK, DV, E4M3, p.part.rows);
+  const int rows = cached_rows_per_workgroup(p.prefix_blocks ? p.part[1].rows : p.part[0].rows);
   if (rows == 16) return launch_cfg<CachedCfg<DQK, DV, E4M3, 1>>(p, s);
   if (rows == 32) return launch_cfg<CachedCfg<DQK, DV, E4M3, 2>>(p, s);
   return launch_cfg<CachedCfg<DQK, DV, E4M3, 4>>(p, s);
@@ -510,7 +606,7 @@ hipError_t launch_type(const CachedParams& p, bool e4m3, hipStream_t s) {
 
 }  // namespace
 
-int cached_rows_per_workgroup(int, int, bool, int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+int cached_rows_per_workgroup(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
 
 hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s) {
   if (dqk == 64) return launch_type<64, 64>(p, e4m3, s);
@@ -518,11 +614,10 @@ hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipS
   return launch_type<192, 128>(p, e4m3, s);
 }
 
-hipError_t launch_cached_merge(const CachedMerge& p, hipStream_t s) {
-  const int64_t grid = ((int64_t)p.B * p.H_q * p.n + 3) / 4;
+hipError_t launch_fill_zero(int32_t* at, int64_t n, hipStream_t s) {
+  const int64_t grid = (n + 255) / 256;
   if (!launch_fits(grid, 256)) return hipErrorInvalidConfiguration;
-  if (p.d_v == 64) hipLaunchKernelGGL((cached_merge_kernel<1>), dim3((unsigned)grid), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((cached_merge_kernel<2>), dim3((unsigned)grid), dim3(256), 0, s, p);
+  hipLaunchKernelGGL(fill_zero_kernel, dim3((unsigned)grid), dim3(256), 0, s, at, n);
   return hipGetLastError();
 }
 

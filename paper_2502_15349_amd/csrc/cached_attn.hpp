@@ -30,27 +30,20 @@ struct CachedParams {
   int B, H_q, H_kv, g, n, page_shift, n_pages;
   float c;        // scale * log2(e)
   int out_bf16;
-  float* ws_o;    // [slots, B H_q n, D_v], null: one workgroup sees all keys of a row and writes O
-  float* ws_lse;  // [slots, B H_q n]
-  CachedPart part;
+  // The parts that a launch walks: the own lists (part[0]), and in front of their workgroups the prefix's (part[1], 0 or
+  // prefix_blocks workgroups), where that has few rows.
+  CachedPart part[2];
+  int prefix_blocks;
+  // Partial results, where a row has more than one: slots [0, part[0].slot0) the prefix's, the others the own list's.
+  float* ws_o;        // [slots, B H_q n, D_v], normalised
+  float* ws_lse;      // [slots, B H_q n], log2 of the sum of weights
+  int32_t* counters;  // [B * H_kv * row tiles] of workgroups that are done, zero before and after the launch; null: no workgroup waits for others
 };
 
-struct CachedMerge {
-  const float* ws_o;
-  const float* ws_lse;
-  void* O;
-  int64_t os[3];
-  float* stats;
-  const int32_t* lengths;
-  int B, H_q, n, d_v, out_bf16;
-  int prefix_slots;             // these are all there
-  int chunk, max_length;        // own slots: ceil(length / chunk) of them are there
-};
-
-int cached_rows_per_workgroup(int dqk, int dv, bool e4m3, int rows);
+int cached_rows_per_workgroup(int rows);
 hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);
-constexpr int kPrefixRows = 256;  // rows of a workgroup of launch_prefix
+constexpr int kPrefixRows = 256;  // rows of a workgroup of launch_prefix, which walks part[1] alone
 hipError_t launch_prefix(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);
-hipError_t launch_cached_merge(const CachedMerge& p, hipStream_t s);
+hipError_t launch_fill_zero(int32_t* at, int64_t n, hipStream_t s);
 
 }  // namespace ae

@@ -35,7 +35,7 @@ struct Carry {
 template <class C, bool E4M3>
 __global__ __launch_bounds__(C::THREADS) void prefix_attn_kernel(const CachedParams p) {
   __shared__ __attribute__((aligned(1024))) char smem[C::LDS_BYTES];
-  const CachedPart& pt = p.part;
+  const CachedPart& pt = p.part[1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ql = lane & 31, half = lane >> 5;
 
@@ -308,12 +308,8 @@ __global__ __launch_bounds__(C::THREADS) void prefix_attn_kernel(const CachedPar
   const float lse2 = any ? st.m + __builtin_amdgcn_logf(l) : -INFINITY;
   const int64_t id = ((int64_t)rb * p.H_q + rh) * p.n + rt, all_rows = (int64_t)p.B * p.H_q * p.n;
   const bool live = iw0 + ql < pt.rows;
-  // every row of the wavefront has its output's place in lane `row`: partial results by row id, else by the caller's strides
-  const int64_t place = p.ws_o != nullptr ? ((int64_t)(pt.slot0 + split) * all_rows + id) * C::DV : rb * p.os[0] + rh * p.os[1] + rt * p.os[2];
-  if (half == 0 && live) {
-    if (p.ws_o != nullptr) p.ws_lse[(int64_t)(pt.slot0 + split) * all_rows + id] = lse2;
-    else if (p.stats != nullptr) p.stats[id] = any ? lse2 * 0.6931471805599453f : -INFINITY;
-  }
+  const int64_t place = ((int64_t)(pt.slot0 + split) * all_rows + id) * C::DV;  // the row's partial result
+  if (half == 0 && live) p.ws_lse[(int64_t)(pt.slot0 + split) * all_rows + id] = lse2;
   constexpr int OC = C::OC, CPRO = OC / 4, DBP = OC / 32;
   const uint32_t obuf = lds0 + wave * (32 * OC * 4);
 #pragma unroll
@@ -331,23 +327,13 @@ __global__ __launch_bounds__(C::THREADS) void prefix_attn_kernel(const CachedPar
     const f32x4 v = lds_read16(obuf + row * (OC * 4) + ((pc ^ (row & 15)) * 16));
     const uint32_t lo = __shfl((uint32_t)place, row), hi = __shfl((uint32_t)((uint64_t)place >> 32), row);
     const int64_t e = (int64_t)(((uint64_t)hi << 32) | lo) + pc * 4;
-    if (iw0 + row < pt.rows) {
-      if (p.ws_o != nullptr) *reinterpret_cast<f32x4*>(p.ws_o + e) = v;
-      else if (p.out_bf16) {
-        bf16x4 h;
-#pragma unroll
-        for (int k4 = 0; k4 < 4; ++k4) h[k4] = (__bf16)v[k4];
-        *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.O) + e) = h;
-      } else {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(p.O) + e) = v;
-      }
-    }
+    if (iw0 + row < pt.rows) *reinterpret_cast<f32x4*>(p.ws_o + e) = v;
   }
 }
 
 template <class C, bool E4M3>
 hipError_t launch_cfg(const CachedParams& p, hipStream_t s) {
-  const int64_t units = (int64_t)p.H_kv * p.part.splits, grid = (units + 7) / 8 * 8 * p.part.row_tiles;
+  const int64_t units = (int64_t)p.H_kv * p.part[1].splits, grid = (units + 7) / 8 * 8 * p.part[1].row_tiles;
   if (!launch_fits(grid, C::THREADS)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((prefix_attn_kernel<C, E4M3>), dim3((unsigned)grid), dim3(C::THREADS), 0, s, p);
   return hipGetLastError();

@@ -231,6 +231,9 @@ ae_status_t ae_cache_destroy(ae_cache_t* h) {
 }  // extern "C"
 
 // ---- attention over the paged cache ------------------------------------------------------------------------------------
+#ifndef AE_TUNE_FUSE
+#define AE_TUNE_FUSE 32
+#endif
 struct ae_cached {
   ae_cache_desc_t cache;
   ae_cached_desc_t desc;
@@ -245,12 +248,14 @@ namespace {
 
 size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 
-// How the keys of a part are cut: chunks that make about `target` workgroups, of at least `least` keys.
-void cut_keys(ae::CachedPart& pt, int H_kv, int rows_per_wg, int64_t chunk, int64_t target, int64_t least) {
+// How the keys of a part are cut: into as many chunks as keep all workgroups resident at once (`slots` of them), of at least
+// `least` keys.  A workgroup more than that starts when the others end.
+void cut_keys(ae::CachedPart& pt, int H_kv, int rows_per_wg, int64_t chunk, int64_t slots, int64_t least) {
+  pt.tile_rows = rows_per_wg;
   pt.row_tiles = (pt.rows + rows_per_wg - 1) / rows_per_wg;
   const int64_t units = (int64_t)pt.lists * H_kv * pt.row_tiles;
   if (chunk == 0) {
-    const int64_t cuts = std::max<int64_t>(1, (target + units - 1) / units);
+    const int64_t cuts = std::max<int64_t>(1, slots / units);
     chunk = std::max<int64_t>(least, ((pt.max_length + cuts - 1) / cuts + 127) / 128 * 128);
   }
   pt.chunk = (int)std::min<int64_t>(chunk, ((int64_t)pt.max_length + 127) / 128 * 128);
@@ -303,21 +308,25 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
   own.max_length = d->max_length;
   own.table_width = d->table_width;
   own.causal = 1;
+  const bool e4m3 = cd.dtype == AE_CACHE_E4M3;
+  auto slots = [&](int rows_per_wg) { return (int64_t)256 * ae::cached_residents(cd.D_qk, cd.D_v, e4m3, rows_per_wg <= 16 ? 16 : 32); };
   if (d->prefix_length > 0) {
     prefix.lists = 1;
     prefix.rows = d->B * d->n_new * p.g;
     prefix.max_length = d->prefix_length;
     prefix.table_width = (d->prefix_length + cd.page_size - 1) / cd.page_size;
-    h->prefix_apart = prefix.rows > 32;
+    h->prefix_apart = own.rows > 32 || prefix.rows > AE_TUNE_FUSE;
     if (h->prefix_apart) {
       cut_keys(prefix, cd.H_kv, ae::kPrefixRows, d->chunk, 256, 256);
-    } else {
-      cut_keys(prefix, cd.H_kv, ae::cached_rows_per_workgroup(prefix.rows), d->chunk, 512, 128);
+    } else {  // tiles of whole sequences
+      const int rpw = ae::cached_rows_per_workgroup(prefix.rows) / own.rows * own.rows;
+      cut_keys(prefix, cd.H_kv, rpw, d->chunk, slots(rpw) / 2, 128);
       p.prefix_blocks = (cd.H_kv * prefix.splits + 7) / 8 * 8 * prefix.row_tiles;
     }
     own.slot0 = prefix.splits;
   }
-  cut_keys(own, cd.H_kv, ae::cached_rows_per_workgroup(p.prefix_blocks ? prefix.rows : own.rows), d->chunk, 768, 128);
+  const int rpw = ae::cached_rows_per_workgroup(own.rows);
+  cut_keys(own, cd.H_kv, rpw, d->chunk, p.prefix_blocks ? slots(rpw) / 2 : slots(rpw), 128);
   h->slots = own.splits + own.slot0;
   h->counted = own.splits > 1 || p.prefix_blocks > 0;
   h->counter_bytes = h->counted ? round_up((size_t)d->B * cd.H_kv * own.row_tiles * 4) : 0;

@@ -15,6 +15,8 @@
 // the walk needs no barriers; the wavefronts of a workgroup take sub-tiles in turn and their states meet at the end.
 #include "cached_attn.hpp"
 
+#include <algorithm>
+
 #include "attn_kernel.hpp"
 #include "launch.hpp"
 
@@ -28,9 +30,16 @@ __device__ __forceinline__ int32_t scalar_load(const int32_t* ptr) {
   return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uintptr_t)ptr);
 }
 
+#ifndef AE_TUNE_W
+#define AE_TUNE_W 4
+#endif
+#ifndef AE_TUNE_L8
+#define AE_TUNE_L8 3
+#endif
 template <int DQK_, int DV_, bool E4M3_, int RT_>
 struct CachedCfg {
-  static constexpr int DQK = DQK_, DV = DV_, RT = RT_, W = 4, THREADS = 64 * W;
+  static constexpr int DQK = DQK_, DV = DV_, RT = RT_, W = E4M3_ && RT_ == 1 && DV_ == 128 ? AE_TUNE_W : 4, THREADS = 64 * W;
+  static constexpr int WAVES_EU = RT == 2 ? 2 : E4M3_ ? AE_TUNE_L8 : 3;
   static constexpr bool E4M3 = E4M3_;
   static constexpr int ESZ = E4M3 ? 1 : 2, RBK = DQK * ESZ, RBV = DV * ESZ, CPRK = RBK / 16, CPRV = RBV / 16;
   static constexpr int K_BYTES = 32 * RBK, V_BYTES = 32 * RBV, E_BYTES = E4M3 ? 256 : 0, STAGE = K_BYTES + V_BYTES + E_BYTES;
@@ -43,7 +52,7 @@ struct CachedCfg {
   static constexpr int KS = DQK / 32, DB = DV / 16;
   static constexpr int ROWS = 16 * RT;
   static constexpr int RED_ROW = DV + 4;
-  static constexpr int RED_BYTES = W * 16 * (RED_ROW + 2) * 4;
+  static constexpr int RED_BYTES = (W * 16 * (RED_ROW + 2) + W + ROWS + 1) * 4;
   static constexpr int LDS_BYTES = W * STAGES * STAGE > RED_BYTES ? W * STAGES * STAGE : RED_BYTES;
   static_assert(LDS_BYTES <= 160 * 1024, "a workgroup must fit LDS");
   static_assert(STAGES * (NKE + NV) < 64, "the wait count has six bits");
@@ -117,7 +126,7 @@ __device__ __forceinline__ f32x4 load_shared(const float* at) {
 
 // RT = 1: 168 registers instead of 180 let a third workgroup onto a compute unit where LDS has room for it.
 template <class C>
-__global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) void cached_attn_kernel(const CachedParams p) {
+__global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(const CachedParams p) {
   __shared__ __attribute__((aligned(1024))) char smem[C::LDS_BYTES];
   const bool is_prefix = (int)blockIdx.x < p.prefix_blocks;
   const CachedPart& pt = p.part[is_prefix ? 1 : 0];
@@ -138,7 +147,7 @@ __global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) vo
   if (begin >= len && split > 0) return;  // (range 0 is always there: a list without keys has rows to write)
 
   // ---- the query rows: B fragments, lane = row ql, 8 elements of group hi ----------------------------------------------
-  const int row0 = tile * C::ROWS;
+  const int row0 = tile * pt.tile_rows, row_end = min(pt.rows, row0 + pt.tile_rows);
   auto place = [&](int r, int& b, int& t, int& h) {
     const int per = p.n * p.g, rr = r % per;
     b = pt.causal ? list : r / per;
@@ -150,7 +159,7 @@ __global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) vo
 #pragma unroll
   for (int rt = 0; rt < C::RT; ++rt) {
     int b, t, h;
-    place(min(row0 + 16 * rt + ql, pt.rows - 1), b, t, h);
+    place(min(row0 + 16 * rt + ql, row_end - 1), b, t, h);
     const __bf16* q = p.Q + b * p.qs[0] + h * p.qs[1] + t * p.qs[2];
 #pragma unroll
     for (int s = 0; s < C::KS; ++s)  // 8-bit keys: a 16-byte chunk serves two steps
@@ -235,6 +244,7 @@ __global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) vo
     }
   };
 
+  int special = 0;  // the wavefront met NaN or infinities in values that only some of the newest tokens see
   f32x4 o[C::RT][C::DB];
   float m[C::RT], l[C::RT];
 #pragma unroll
@@ -331,6 +341,8 @@ __global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) vo
       for (int e = 0; e < 8; ++e) pb[rt][e] = (__bf16)x[e];
     }
     await_values();
+    // Rows that are not there are made zero: a weight of zero does not do away with a NaN.  Nor for the rows that only some of the
+    // newest tokens see: NaN and infinities in those count as zero here, and reach the rows that see them at the end.
     if (!masked) {
 #pragma unroll
       for (int d = 0; d < C::DB; ++d) {
@@ -338,50 +350,32 @@ __global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) vo
 #pragma unroll
         for (int rt = 0; rt < C::RT; ++rt) o[rt][d] = mfma16(a, pb[rt], o[rt][d]);
       }
-    } else {
-      // Rows that are not there are made zero: a weight of zero does not do away with a NaN.  Rows that only some of the newest tokens
-      // see and that hold a NaN or an infinity are zero in the product as well; what they do to the rows that see them is
-      // counted in two products with ones.
-      u32x4 keep;
+      return;
+    }
+    u32x4 keep;
+    const bool some_see = pt.causal && p.n > 1;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) keep[e] = there > 2 * e + 1 ? 0xffffffffu : there > 2 * e ? 0xffffu : 0u;
+    for (int e = 0; e < 4; ++e) keep[e] = there > 2 * e + 1 ? 0xffffffffu : there > 2 * e ? 0xffffu : 0u;
 #pragma unroll
-      for (int d = 0; d < C::DB; ++d) {
-        u32x4 a = __builtin_bit_cast(u32x4, read_v(d, so)) & keep;
+    for (int d = 0; d < C::DB; ++d) {
+      u32x4 a = __builtin_bit_cast(u32x4, read_v(d, so)) & keep;
+      if (some_see) {
+        uint32_t lo[4], up[4];
         bool odd = false;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) odd = odd || (a[e] & 0x7f80u) == 0x7f80u || (a[e] & 0x7f800000u) == 0x7f800000u;
-        if (pt.causal && p.n > 1 && __builtin_amdgcn_ballot_w64(odd) != 0) {
-          bf16x8 up, down;
-          u32x4 fin = a;
+        for (int e = 0; e < 4; ++e) {
+          lo[e] = (a[e] & 0x7f80u) == 0x7f80u && j0 + 8 * hi + 2 * e >= all_visible ? 0xffffu : 0u;
+          up[e] = (a[e] & 0x7f800000u) == 0x7f800000u && j0 + 8 * hi + 2 * e + 1 >= all_visible ? 0xffff0000u : 0u;
+          odd = odd || (lo[e] | up[e]) != 0;
+        }
+        if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+          special = 1;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const uint32_t v = (a[e / 2] >> (16 * (e % 2))) & 0xffffu;
-            const bool special = (v & 0x7f80u) == 0x7f80u, nan = special && (v & 0x7fu) != 0;
-            up[e] = special && (nan || !(v & 0x8000u)) ? (__bf16)1.f : (__bf16)0.f;
-            down[e] = special && (nan || (v & 0x8000u)) ? (__bf16)1.f : (__bf16)0.f;
-            if (special) fin[e / 2] &= e % 2 ? 0xffffu : 0xffff0000u;
-          }
-#pragma unroll
-          for (int rt = 0; rt < C::RT; ++rt) {
-            bf16x8 sees;
-            const int last = min(lim[rt] - j0 - 8 * hi, there) - 1;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sees[e] = e <= last ? (__bf16)1.f : (__bf16)0.f;
-            o[rt][d] = mfma16(__builtin_bit_cast(bf16x8, fin), pb[rt], o[rt][d]);
-            const f32x4 n_up = mfma16(up, sees, f32x4{0.f, 0.f, 0.f, 0.f}), n_down = mfma16(down, sees, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {  // (by bits: device code is compiled for no NaN to occur)
-              const uint32_t add = n_up[r] > 0.f ? (n_down[r] > 0.f ? 0x7fc00000u : 0x7f800000u) : n_down[r] > 0.f ? 0xff800000u : 0u;
-              const uint32_t was = __builtin_bit_cast(uint32_t, (float)o[rt][d][r]);
-              if (add) o[rt][d][r] = __builtin_bit_cast(float, (was & 0x7f800000u) == 0x7f800000u && was != add ? 0x7fc00000u : add);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int rt = 0; rt < C::RT; ++rt) o[rt][d] = mfma16(__builtin_bit_cast(bf16x8, a), pb[rt], o[rt][d]);
+          for (int e = 0; e < 4; ++e) a[e] &= ~(lo[e] | up[e]);
         }
       }
+#pragma unroll
+      for (int rt = 0; rt < C::RT; ++rt) o[rt][d] = mfma16(__builtin_bit_cast(bf16x8, a), pb[rt], o[rt][d]);
     }
   };
 
@@ -430,42 +424,69 @@ __global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) vo
   }
 
   // ---- the wavefronts' states into one, row tile by row tile --------------------------------------------------------------------
-  float* red = reinterpret_cast<float*>(smem);  // [W][16][RED_ROW], then [W][16][2]
+  float* red = reinterpret_cast<float*>(smem);  // [W][16][RED_ROW], then [W][16][2], then [W], then [ROWS + 1]
   float* red_ml = red + C::W * 16 * C::RED_ROW;
+  int32_t* red_special = reinterpret_cast<int32_t*>(red_ml + C::W * 32);
+  int32_t* done = red_special + C::W;  // this workgroup is the last one of the sequence
   constexpr int PER = C::THREADS / 16, COLS = C::DV / PER;  // threads per row, columns per thread
   const int r = threadIdx.x / PER, c0 = (threadIdx.x % PER) * COLS;
   const int64_t all_rows = (int64_t)p.B * p.H_q * p.n;
   float M, L, acc[COLS];  // of the thread's row: reference (log2), sum of weights, and its columns, not normalised
-  auto scale_by = [&](float f) {
+  auto clear = [&] {
+    M = -INFINITY;
+    L = 0.f;
 #pragma unroll
-    for (int e = 0; e < COLS; ++e) acc[e] *= f;
+    for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
   };
-  // (M, L, acc) and the partial results of slots [s0, s1) of row `id`: the rule by which two states of an online softmax are joined
-  auto join = [&](auto sharedc, int64_t id, int s0, int s1) {
-    constexpr bool SHARED = decltype(sharedc)::value;
+  // no visible key leaves the sum at +0; told from a NaN by its bits (device code is compiled for no NaN to occur)
+  auto any = [&] { return __builtin_bit_cast(uint32_t, L) != 0; };
+  auto normalise = [&] {
+    const float inv = any() ? 1.f / L : 0.f;
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) acc[e] *= inv;
+  };
+  // The states that `count` groups of 16 rows left in LDS, every `step`-th row of it from row `at` on.
+  auto combine = [&](int at, int step, int count) {
+    clear();
+    for (int w = 0; w < count; ++w) M = fmaxf(M, red_ml[(at + w * step) * 2]);
+    const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll 4
+    for (int w = 0; w < count; ++w) {
+      const float f = fast_exp2(red_ml[(at + w * step) * 2] - ref);
+      L += f * red_ml[(at + w * step) * 2 + 1];
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) acc[e] += f * red[(at + w * step) * C::RED_ROW + c0 + e];
+    }
+  };
+  // (M, L, acc) and the partial results of slots s0, s0 + step, ... below s1 of row `id`: the rule by which two states of an online
+  // softmax are joined
+  auto join = [&](int64_t id, int s0, int step, int s1) {
     constexpr int BATCH = 4;  // partial results in flight
     const float* po = p.ws_o + id * C::DV + c0;
     const float* pl = p.ws_lse + id;
-    for (int s = s0; s < s1; s += BATCH) {
+#pragma unroll 1
+    for (int s = s0; s < s1; s += BATCH * step) {
       float lse[BATCH];
       f32x4 part[BATCH][COLS / 4];
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
-        const int64_t at = (int64_t)min(s + u, s1 - 1) * all_rows;
-        lse[u] = SHARED ? __hip_atomic_load(pl + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : pl[at];
+        const int64_t at = (int64_t)min(s + u * step, s1 - 1) * all_rows;
+        lse[u] = __hip_atomic_load(pl + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
-        for (int e = 0; e < COLS / 4; ++e) part[u][e] = SHARED ? load_shared(po + at * C::DV + 4 * e) : *reinterpret_cast<const f32x4*>(po + at * C::DV + 4 * e);
+        for (int e = 0; e < COLS / 4; ++e) part[u][e] = load_shared(po + at * C::DV + 4 * e);
       }
-#pragma unroll
-      for (int u = 0; u < BATCH; ++u) lse[u] = s + u < s1 ? lse[u] : -INFINITY;
       float top = M;
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) top = fmaxf(top, lse[u]);
+      for (int u = 0; u < BATCH; ++u) {
+        lse[u] = s + u * step < s1 ? lse[u] : -INFINITY;
+        top = fmaxf(top, lse[u]);
+      }
       if (__builtin_bit_cast(uint32_t, top) == 0xff800000u) continue;  // no key so far
       const float a = fast_exp2(M - top);
       M = top;
       L *= a;
-      scale_by(a);
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) acc[e] *= a;
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
         const float w = fast_exp2(lse[u] - top);
@@ -475,10 +496,8 @@ __global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) vo
       }
     }
   };
-  // no visible key leaves the sum at +0; told from a NaN by its bits (device code is compiled for no NaN to occur)
-  auto any = [&] { return __builtin_bit_cast(uint32_t, L) != 0; };
   auto write_out = [&](int b, int t, int h, int64_t id) {
-    scale_by(any() ? 1.f / L : 0.f);
+    normalise();
     const int64_t at = b * p.os[0] + h * p.os[1] + t * p.os[2] + c0;
 #pragma unroll
     for (int e = 0; e < COLS; e += 4) {
@@ -493,9 +512,28 @@ __global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) vo
     }
     if (c0 == 0 && p.stats != nullptr) p.stats[id] = any() ? (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f : -INFINITY;
   };
+  // NaN and infinities of the newest tokens' values, to a row that sees them (by bits)
+  auto add_special = [&](int t) {
+#pragma unroll 1
+    for (int j = max(begin, all_visible); j < min(end, len - p.n + 1 + t); ++j) {
+      const int pg = table[j >> p.page_shift];
+      if ((uint32_t)pg >= (uint32_t)p.n_pages) continue;
+      const int64_t at = ((((int64_t)pg * p.H_kv + hk) << p.page_shift) + (j & page_mask)) * C::DV + c0;
+      for (int e = 0; e < COLS; ++e) {
+        uint32_t v;
+        if constexpr (C::E4M3) v = (p.V[at + e] & 0x7fu) == 0x7fu ? 0x7fc00000u : 0u;
+        else v = (uint32_t)reinterpret_cast<const uint16_t*>(p.V)[at + e] << 16;
+        if ((v & 0x7f800000u) != 0x7f800000u) continue;
+        if (v & 0x7fffffu) v = 0x7fc00000u;
+        const uint32_t was = __builtin_bit_cast(uint32_t, red[r * C::RED_ROW + c0 + e]);
+        red[r * C::RED_ROW + c0 + e] = __builtin_bit_cast(float, (was & 0x7f800000u) == 0x7f800000u && was != v ? 0x7fc00000u : v);
+      }
+    }
+  };
+  const bool counted = p.counters != nullptr;
 #pragma unroll
   for (int rt = 0; rt < C::RT; ++rt) {
-    if (row0 + 16 * rt >= pt.rows) break;
+    if (row0 + 16 * rt >= row_end) break;
     float lt = l[rt];
     lt += __shfl_xor(lt, 16);
     lt += __shfl_xor(lt, 32);
@@ -506,74 +544,77 @@ __global__ __launch_bounds__(C::THREADS, C::RT == 1 ? 3 : C::RT == 2 ? 2 : 1) vo
       red_ml[(wave * 16 + ql) * 2] = m[rt];
       red_ml[(wave * 16 + ql) * 2 + 1] = lt;
     }
+    if (lane == 0) red_special[wave] = special;
     __syncthreads();
-    if (row0 + 16 * rt + r < pt.rows) {
-      float f[C::W];
-      M = -INFINITY;
-      L = 0.f;
-#pragma unroll
-      for (int w = 0; w < C::W; ++w) M = fmaxf(M, red_ml[(w * 16 + r) * 2]);
-      const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-      for (int w = 0; w < C::W; ++w) {
-        f[w] = fast_exp2(red_ml[(w * 16 + r) * 2] - ref);
-        L += f[w] * red_ml[(w * 16 + r) * 2 + 1];
-      }
-#pragma unroll
-      for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
-#pragma unroll
-      for (int w = 0; w < C::W; ++w)
-#pragma unroll
-        for (int e = 0; e < COLS; ++e) acc[e] += f[w] * red[(w * 16 + r) * C::RED_ROW + c0 + e];
+    if (row0 + 16 * rt + r < row_end) {
       int b, t, h;
       place(row0 + 16 * rt + r, b, t, h);
       const int64_t id = ((int64_t)b * p.H_q + h) * p.n + t;
-      if (is_prefix || p.counters != nullptr) {
+      combine(r, 16, C::W);
+      if (__builtin_amdgcn_ballot_w64(lane < C::W && red_special[lane & (C::W - 1)]) != 0) {  // rare; through LDS, where a column has an address
+        for (int e = 0; e < COLS; ++e) red[r * C::RED_ROW + c0 + e] = acc[e];
+        add_special(t);
+        for (int e = 0; e < COLS; ++e) acc[e] = red[r * C::RED_ROW + c0 + e];
+      }
+      if (counted) {
         const int64_t at = (int64_t)(pt.slot0 + split) * all_rows + id;
-        const float inv = any() ? 1.f / L : 0.f;
+        normalise();
 #pragma unroll
-        for (int e = 0; e < COLS; e += 4)
-          store_shared(p.ws_o + at * C::DV + c0 + e, f32x4{acc[e] * inv, acc[e + 1] * inv, acc[e + 2] * inv, acc[e + 3] * inv});
+        for (int e = 0; e < COLS; e += 4) store_shared(p.ws_o + at * C::DV + c0 + e, f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]});
         if (c0 == 0) __hip_atomic_store(p.ws_lse + at, any() ? M + __builtin_amdgcn_logf(L) : -INFINITY, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       } else {  // the only workgroup of its rows, but for a prefix that an earlier launch has walked
-        join(std::false_type{}, id, 0, pt.slot0);
+        join(id, 0, 1, pt.slot0);
         write_out(b, t, h, id);
       }
     }
   }
-  if (p.counters == nullptr) return;
+  if (!counted) return;
 
   // ---- the last workgroup of a row joins its partial results -------------------------------------------------------------------------
   // Every workgroup counts itself done for its sequences once all it stored has arrived; the one that finds all others done
-  // joins, in the slots' order (the result does not depend on who is last), and leaves the counter at zero.
+  // joins, in an order that does not depend on who is last, and leaves the counter at zero.
   const CachedPart& own = p.part[0];
-  const int n_seq = is_prefix ? p.B : 1;  // (of a prefix in this launch: all rows in one tile)
-  int32_t* done = reinterpret_cast<int32_t*>(smem);  // [n_seq]: this workgroup is the last one of the sequence
+  // the sequences whose rows these are (a tile of a prefix in this launch has whole sequences)
+  const int per = p.n * p.g, b0 = is_prefix ? row0 / per : list, n_seq = is_prefix ? (row_end - row0) / per : 1;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
+  bool last = false;
   if ((int)threadIdx.x < n_seq) {
-    const int b = is_prefix ? threadIdx.x : list;
+    const int b = b0 + threadIdx.x;
     const int keys = max(0, min(own.lengths[b], own.max_length));
     const int expected = max(1, (keys + own.chunk - 1) / own.chunk) + (p.prefix_blocks ? p.part[1].splits : 0);
     int32_t* counter = p.counters + (b * p.H_kv + hk) * own.row_tiles + (is_prefix ? 0 : tile);
-    const bool last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == expected - 1;
+    last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == expected - 1;
     if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     done[threadIdx.x] = last;
   }
+  if (wave == 0) done[C::ROWS] = __builtin_amdgcn_ballot_w64(last) != 0;  // (the counting lanes are the first wavefront's)
   __syncthreads();
-  for (int rt = 0; rt < C::RT; ++rt) {
-    if (row0 + 16 * rt + r >= pt.rows) break;
+  if (!done[C::ROWS]) return;
+  // Sixteen rows at a time; where there are fewer, 2, 4, 8 or 16 groups of threads share a row's slots and meet in LDS.
+  const int tile_rows = row_end - row0;
+  const int groups = tile_rows > 8 ? 1 : tile_rows > 4 ? 2 : tile_rows > 2 ? 4 : tile_rows > 1 ? 8 : 16, at_once = 16 / groups;
+  const int jr = r % at_once, jg = r / at_once;
+#pragma unroll 1
+  for (int r0 = 0; r0 < tile_rows; r0 += at_once) {
     int b, t, h;
-    place(row0 + 16 * rt + r, b, t, h);
-    if (!done[is_prefix ? b : 0]) continue;
+    place(row0 + min(r0 + jr, tile_rows - 1), b, t, h);
     const int64_t id = ((int64_t)b * p.H_q + h) * p.n + t;
     const int keys = max(0, min(own.lengths[b], own.max_length));
-    M = -INFINITY;
-    L = 0.f;
+    const bool mine = r0 + jr < tile_rows && done[is_prefix ? b - b0 : 0];
+    clear();
+    if (mine) join(id, jg, groups, own.slot0 + max(1, (keys + own.chunk - 1) / own.chunk));
+    if (groups > 1) {
 #pragma unroll
-    for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
-    join(std::true_type{}, id, 0, own.slot0 + max(1, (keys + own.chunk - 1) / own.chunk));
-    write_out(b, t, h, id);
+      for (int e = 0; e < COLS; ++e) red[r * C::RED_ROW + c0 + e] = acc[e];
+      if (c0 == 0) {
+        red_ml[2 * r] = M;
+        red_ml[2 * r + 1] = L;
+      }
+      __syncthreads();
+      if (jg == 0) combine(jr, at_once, groups);
+    }
+    if (mine && jg == 0) write_out(b, t, h, id);
   }
 }
 
@@ -593,10 +634,9 @@ hipError_t launch_cfg(const CachedParams& p, hipStream_t s) {
 
 template <int DQK, int DV, bool E4M3>
 hipError_t launch_rows(const CachedParams& p, hipStream_t s) {
-  const int rows = cached_rows_per_workgroup(p.prefix_blocks ? p.part[1].rows : p.part[0].rows);
-  if (rows == 16) return launch_cfg<CachedCfg<DQK, DV, E4M3, 1>>(p, s);
-  if (rows == 32) return launch_cfg<CachedCfg<DQK, DV, E4M3, 2>>(p, s);
-  return launch_cfg<CachedCfg<DQK, DV, E4M3, 4>>(p, s);
+  const int rows = std::max(p.part[0].tile_rows, p.prefix_blocks ? p.part[1].tile_rows : 0);
+  if (rows <= 16) return launch_cfg<CachedCfg<DQK, DV, E4M3, 1>>(p, s);
+  return launch_cfg<CachedCfg<DQK, DV, E4M3, 2>>(p, s);
 }
 
 template <int DQK, int DV>
@@ -606,7 +646,14 @@ hipError_t launch_type(const CachedParams& p, bool e4m3, hipStream_t s) {
 
 }  // namespace
 
-int cached_rows_per_workgroup(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+int cached_residents(int dqk, int dv, bool e4m3, int rows_per_workgroup) {
+  const int lds = 4 * 32 * (dqk + dv) * (e4m3 ? 1 : 2) + (e4m3 ? 4 * 256 : 0);  // (CachedCfg::LDS_BYTES; 8-bit 64/64 a little more)
+  return std::min(160 * 1024 / lds, rows_per_workgroup == 16 ? 3 : 2);
+}
+
+// (Four row tiles a wavefront, 64 rows, need 512 registers, spills among them, and leave a SIMD one wavefront: 20 x 64/8 heads x 8
+// tokens x up to 4000 keys took 128 us instead of 50.)
+int cached_rows_per_workgroup(int rows) { return rows <= 16 ? 16 : 32; }
 
 hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s) {
   if (dqk == 64) return launch_type<64, 64>(p, e4m3, s);

@@ -14,7 +14,8 @@ struct CachedPart {
   int table_width, max_length;
   int lists;               // sequences, or 1
   int rows;                // query rows of a list
-  int row_tiles;           // ceil(rows / rows of a workgroup)
+  int tile_rows;           // query rows of a workgroup (of a prefix in the own keys' launch: of whole sequences)
+  int row_tiles;           // ceil(rows / tile_rows)
   int chunk, splits;       // keys of a workgroup (a multiple of 32), ceil(max_length / chunk)
   int slot0;               // first of the part's partial results
   int causal;              // the newest n tokens of the list are the queries' own
@@ -40,7 +41,9 @@ struct CachedParams {
   int32_t* counters;  // [B * H_kv * row tiles] of workgroups that are done, zero before and after the launch; null: no workgroup waits for others
 };
 
-int cached_rows_per_workgroup(int rows);
+int cached_rows_per_workgroup(int rows);  // at most
+// Workgroups of 16 or 32 rows that a compute unit holds at a time.
+int cached_residents(int dqk, int dv, bool e4m3, int rows_per_workgroup);
 hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);
 constexpr int kPrefixRows = 256;  // rows of a workgroup of launch_prefix, which walks part[1] alone
 hipError_t launch_prefix(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);

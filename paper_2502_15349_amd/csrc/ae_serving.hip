@@ -231,9 +231,6 @@ ae_status_t ae_cache_destroy(ae_cache_t* h) {
 }  // extern "C"
 
 // ---- attention over the paged cache ------------------------------------------------------------------------------------
-#ifndef AE_TUNE_FUSE
-#define AE_TUNE_FUSE 32
-#endif
 struct ae_cached {
   ae_cache_desc_t cache;
   ae_cached_desc_t desc;
@@ -248,18 +245,85 @@ namespace {
 
 size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 
-// How the keys of a part are cut: into as many chunks as keep all workgroups resident at once (`slots` of them), of at least
-// `least` keys.  A workgroup more than that starts when the others end.
-void cut_keys(ae::CachedPart& pt, int H_kv, int rows_per_wg, int64_t chunk, int64_t slots, int64_t least) {
-  pt.tile_rows = rows_per_wg;
-  pt.row_tiles = (pt.rows + rows_per_wg - 1) / rows_per_wg;
-  const int64_t units = (int64_t)pt.lists * H_kv * pt.row_tiles;
-  if (chunk == 0) {
-    const int64_t cuts = std::max<int64_t>(1, slots / units);
-    chunk = std::max<int64_t>(least, ((pt.max_length + cuts - 1) / cuts + 127) / 128 * 128);
-  }
+void cut_keys(ae::CachedPart& pt, int tile_rows, int64_t cuts, int64_t chunk) {
+  pt.tile_rows = tile_rows;
+  pt.row_tiles = (pt.rows + tile_rows - 1) / tile_rows;
+  if (chunk == 0) chunk = ((pt.max_length + cuts - 1) / cuts + 127) / 128 * 128;
   pt.chunk = (int)std::min<int64_t>(chunk, ((int64_t)pt.max_length + 127) / 128 * 128);
   pt.splits = (int)(((int64_t)pt.max_length + pt.chunk - 1) / pt.chunk);
+}
+
+// How a call is laid out -- wavefronts of a workgroup, ranges of the own keys and of the prefix, the prefix in the own keys' launch
+// or in one of its own -- by an estimate of its time, in microseconds.  A workgroup takes 5 for its start and its end and 0.25
+// + 0.8 (D_qk + D_v) / 256 for each 32 keys of a wavefront, 0.6 (D_qk + D_v) / 256 more with 32 rows; the cache is read at 5.7 TB/s; the
+// launch takes the root of the squares of what its workgroups take in their turns on the places the chip has for them, of
+// the longest one, and of the reading; the join of partial results takes 1.8 and a latency of 1 for every four a thread adds up.  A prefix in
+// a launch of its own takes 0.5 + 1.1 (D_qk + D_v) / 256 for each 64 keys and 256 rows of a workgroup, 0.37 for every MB of partial
+// results, and 3.3 for the second launch.
+// Over 4314 random calls (1 to 256 sequences, 1 to 8 new tokens, 64 to 131072 keys, all head dims and types) the choice takes 1.038 times
+// the time of the best one measured for that call (1.12 at the 90th percentile, 1.47 at most); as many ranges as keep all workgroups
+// resident, with four wavefronts, took 1.109 (1.30, 9.0).  Over 4373 calls behind a prefix (2 to 256 sequences, 100 to 32768 keys)
+// 1.047; always a launch of its own 1.19.
+struct Layout {
+  double us;
+  int waves, own_cuts, prefix_cuts;
+  bool apart;
+};
+
+Layout choose_layout(const ae_cached_desc_t& d, const ae_cache_desc_t& cd, int g) {
+  static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+  const bool e4m3 = cd.dtype == AE_CACHE_E4M3;
+  const double width = (cd.D_qk + cd.D_v) / 256.0, key_us = (cd.D_qk + cd.D_v) * (e4m3 ? 1 : 2) / 5.7e6;  // of a k/v head's key
+  const int own_rows = d.n_new * g, prefix_rows = d.B * own_rows;
+  const int own_rpw = std::min(ae::cached_rows_per_workgroup(own_rows), 32), own_tiles = (own_rows + own_rpw - 1) / own_rpw;
+  auto join = [&](int rows, double slots) {
+    const int groups = rows > 8 ? 1 : rows > 4 ? 2 : rows > 2 ? 4 : rows > 1 ? 8 : 16;
+    return (rows > 16 ? 2.0 : 1.0) * std::ceil(slots / (4 * groups));
+  };
+  const double own_read = (double)d.B * cd.H_kv * d.max_length * key_us, prefix_read = (double)cd.H_kv * d.prefix_length * key_us;
+  Layout best = {1e300, 4, 1, 1, false};
+  for (int apart = 0; apart <= (d.prefix_length > 0 ? 1 : 0); ++apart) {
+    if (d.prefix_length > 0 && !apart && own_rows > 32) continue;
+    const bool fused = d.prefix_length > 0 && !apart;
+    const int fused_rows = fused ? ae::cached_rows_per_workgroup(prefix_rows) / own_rows * own_rows : 0;
+    const bool wide = std::max(own_rpw, fused_rows) > 16;
+    for (int waves = 4; waves <= 8; waves += 4) {
+      const double start = waves == 4 ? 5.1 : 5.6, step = 0.25 + 0.8 * width + (wide ? 0.6 * width : 0.0);
+      const double places = 256.0 * ae::cached_residents(cd.D_qk, cd.D_v, e4m3, wide ? 32 : 16, waves);
+      for (int oc : kCuts) {
+        const double chunk = std::ceil(std::ceil((double)d.max_length / oc) / 128) * 128, cuts = std::ceil(d.max_length / chunk);
+        const double walk = start + std::ceil(std::min(chunk, (double)d.max_length) / (32 * waves)) * step;
+        const double groups = (double)d.B * cd.H_kv * own_tiles * cuts;
+        for (int pc : kCuts) {
+          if (d.prefix_length == 0 && pc > 1) break;
+          const double pchunk = std::ceil(std::ceil((double)d.prefix_length / pc) / 128) * 128;
+          const double pcuts = d.prefix_length ? std::ceil(d.prefix_length / pchunk) : 0;
+          double us;
+          if (!apart) {
+            double turns = groups * walk, longest = walk;
+            if (fused) {
+              const double pwalk = start + std::ceil(std::min(pchunk, (double)d.prefix_length) / (32 * waves)) * step;
+              turns += (double)cd.H_kv * ((prefix_rows + fused_rows - 1) / fused_rows) * pcuts * pwalk;
+              longest = std::max(longest, pwalk);
+            }
+            turns /= places;
+            const double read = own_read + prefix_read;
+            us = std::sqrt(turns * turns + longest * longest + read * read);
+            if (fused || cuts > 1) us += 1.8 + join(fused ? fused_rows : std::min(own_rows, own_rpw), cuts + pcuts);
+          } else {
+            const double wg = 1.0 + std::ceil(std::min(pchunk, (double)d.prefix_length) / 64) * (0.5 + 1.1 * width);
+            const double wgs = (double)cd.H_kv * ((prefix_rows + ae::kPrefixRows - 1) / ae::kPrefixRows) * pcuts;
+            us = std::max(std::ceil(wgs / 256 - 0.02), 1.0) * wg + 0.37 * pcuts * prefix_rows * cd.H_kv * (cd.D_v + 4) * 4e-6 + 3.3;
+            const double j = cuts > 1 ? 1.8 + join(std::min(own_rows, own_rpw), cuts + pcuts) : (own_rpw > 16 ? 2.0 : 1.0) * std::ceil(pcuts / 4);
+            const double turns = groups * (walk + (cuts > 1 ? 0.0 : j)) / places;
+            us += std::sqrt(turns * turns + walk * walk + own_read * own_read) + j;
+          }
+          if (us < best.us) best = {us, waves, oc, pc, apart != 0};
+        }
+      }
+    }
+  }
+  return best;
 }
 
 }  // namespace
@@ -308,25 +372,20 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
   own.max_length = d->max_length;
   own.table_width = d->table_width;
   own.causal = 1;
-  const bool e4m3 = cd.dtype == AE_CACHE_E4M3;
-  auto slots = [&](int rows_per_wg) { return (int64_t)256 * ae::cached_residents(cd.D_qk, cd.D_v, e4m3, rows_per_wg <= 16 ? 16 : 32); };
+  const Layout lay = choose_layout(*d, cd, p.g);
+  p.waves = lay.waves;
   if (d->prefix_length > 0) {
     prefix.lists = 1;
     prefix.rows = d->B * d->n_new * p.g;
     prefix.max_length = d->prefix_length;
     prefix.table_width = (d->prefix_length + cd.page_size - 1) / cd.page_size;
-    h->prefix_apart = own.rows > 32 || prefix.rows > AE_TUNE_FUSE;
-    if (h->prefix_apart) {
-      cut_keys(prefix, cd.H_kv, ae::kPrefixRows, d->chunk, 256, 256);
-    } else {  // tiles of whole sequences
-      const int rpw = ae::cached_rows_per_workgroup(prefix.rows) / own.rows * own.rows;
-      cut_keys(prefix, cd.H_kv, rpw, d->chunk, slots(rpw) / 2, 128);
-      p.prefix_blocks = (cd.H_kv * prefix.splits + 7) / 8 * 8 * prefix.row_tiles;
-    }
+    h->prefix_apart = lay.apart;
+    // (in the own keys' launch: tiles of whole sequences)
+    cut_keys(prefix, lay.apart ? ae::kPrefixRows : ae::cached_rows_per_workgroup(prefix.rows) / own.rows * own.rows, lay.prefix_cuts, d->chunk);
+    if (!lay.apart) p.prefix_blocks = (cd.H_kv * prefix.splits + 7) / 8 * 8 * prefix.row_tiles;
     own.slot0 = prefix.splits;
   }
-  const int rpw = ae::cached_rows_per_workgroup(own.rows);
-  cut_keys(own, cd.H_kv, rpw, d->chunk, p.prefix_blocks ? slots(rpw) / 2 : slots(rpw), 128);
+  cut_keys(own, ae::cached_rows_per_workgroup(own.rows), lay.own_cuts, d->chunk);
   h->slots = own.splits + own.slot0;
   h->counted = own.splits > 1 || p.prefix_blocks > 0;
   h->counter_bytes = h->counted ? round_up((size_t)d->B * cd.H_kv * own.row_tiles * 4) : 0;

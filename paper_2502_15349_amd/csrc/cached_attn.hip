@@ -30,28 +30,21 @@ __device__ __forceinline__ int32_t scalar_load(const int32_t* ptr) {
   return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uintptr_t)ptr);
 }
 
-#ifndef AE_TUNE_W
-#define AE_TUNE_W 4
-#endif
-#ifndef AE_TUNE_L8
-#define AE_TUNE_L8 3
-#endif
-template <int DQK_, int DV_, bool E4M3_, int RT_>
+template <int DQK_, int DV_, bool E4M3_, int RT_, int W_>
 struct CachedCfg {
-  static constexpr int DQK = DQK_, DV = DV_, RT = RT_, W = E4M3_ && RT_ == 1 && DV_ == 128 ? AE_TUNE_W : 4, THREADS = 64 * W;
-  static constexpr int WAVES_EU = RT == 2 ? 2 : E4M3_ ? AE_TUNE_L8 : 3;
+  static constexpr int DQK = DQK_, DV = DV_, RT = RT_, W = W_, THREADS = 64 * W;
+  // wavefronts per SIMD that the registers leave room for
+  static constexpr int WAVES_EU = RT == 2 ? 2 : W == 4 ? 3 : E4M3_ && DQK_ + DV_ <= 256 ? 4 : 2;
   static constexpr bool E4M3 = E4M3_;
   static constexpr int ESZ = E4M3 ? 1 : 2, RBK = DQK * ESZ, RBV = DV * ESZ, CPRK = RBK / 16, CPRV = RBV / 16;
   static constexpr int K_BYTES = 32 * RBK, V_BYTES = 32 * RBV, E_BYTES = E4M3 ? 256 : 0, STAGE = K_BYTES + V_BYTES + E_BYTES;
   static constexpr int NK = K_BYTES / 1024, NV = V_BYTES / 1024;
   static constexpr int NKE = NK + (E4M3 ? 1 : 0);  // copies awaited before the scores (the exponents come with the keys)
-#ifndef AE_TUNE_CST
-#define AE_TUNE_CST 1
-#endif
-  static constexpr int STAGES = AE_TUNE_CST;
+  static constexpr int STAGES = 1;
   static constexpr int KS = DQK / 32, DB = DV / 16;
   static constexpr int ROWS = 16 * RT;
   static constexpr int RED_ROW = DV + 4;
+    static constexpr int BATCH = 4;  // partial results of a thread in flight when they are joined (8 and 16: no faster)
   static constexpr int RED_BYTES = (W * 16 * (RED_ROW + 2) + W + ROWS + 1) * 4;
   static constexpr int LDS_BYTES = W * STAGES * STAGE > RED_BYTES ? W * STAGES * STAGE : RED_BYTES;
   static_assert(LDS_BYTES <= 160 * 1024, "a workgroup must fit LDS");
@@ -106,22 +99,12 @@ typedef __attribute__((ext_vector_type(2))) int i32x2;
 // Partial results that another workgroup of the same launch reads, on any XCD: stored past the L2 and loaded past it, value by
 // value (relaxed atomics of the whole device).  A release and an acquire of the device instead write back and invalidate an L2 that
 // the other workgroups of the XCD are reading their keys through: 32 x 32/8 x 5003 keys in ranges of 1024 took 164 us with them.
-__device__ __forceinline__ void store_shared(float* at, f32x4 v) {
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const uint64_t u = ((uint64_t)__builtin_bit_cast(uint32_t, (float)v[2 * k + 1]) << 32) | __builtin_bit_cast(uint32_t, (float)v[2 * k]);
-    __hip_atomic_store(reinterpret_cast<uint64_t*>(at) + k, u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
+__device__ __forceinline__ void store_shared(float* at, float x, float y) {
+  const uint64_t u = ((uint64_t)__builtin_bit_cast(uint32_t, y) << 32) | __builtin_bit_cast(uint32_t, x);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(at), u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ f32x4 load_shared(const float* at) {
-  f32x4 v;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const uint64_t u = __hip_atomic_load(reinterpret_cast<const uint64_t*>(at) + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    v[2 * k] = __builtin_bit_cast(float, (uint32_t)u);
-    v[2 * k + 1] = __builtin_bit_cast(float, (uint32_t)(u >> 32));
-  }
-  return v;
+__device__ __forceinline__ uint64_t load_shared(const float* at) {
+  return __hip_atomic_load(reinterpret_cast<const uint64_t*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // RT = 1: 168 registers instead of 180 let a third workgroup onto a compute unit where LDS has room for it.
@@ -428,7 +411,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
   float* red_ml = red + C::W * 16 * C::RED_ROW;
   int32_t* red_special = reinterpret_cast<int32_t*>(red_ml + C::W * 32);
   int32_t* done = red_special + C::W;  // this workgroup is the last one of the sequence
-  constexpr int PER = C::THREADS / 16, COLS = C::DV / PER;  // threads per row, columns per thread
+  constexpr int PER = C::THREADS / 16, COLS = C::DV / PER, PIECE = COLS < 4 ? COLS : 4;  // threads per row, columns per thread
   const int r = threadIdx.x / PER, c0 = (threadIdx.x % PER) * COLS;
   const int64_t all_rows = (int64_t)p.B * p.H_q * p.n;
   float M, L, acc[COLS];  // of the thread's row: reference (log2), sum of weights, and its columns, not normalised
@@ -461,26 +444,28 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
   // (M, L, acc) and the partial results of slots s0, s0 + step, ... below s1 of row `id`: the rule by which two states of an online
   // softmax are joined
   auto join = [&](int64_t id, int s0, int step, int s1) {
-    constexpr int BATCH = 4;  // partial results in flight
+    constexpr int BATCH = C::BATCH;
     const float* po = p.ws_o + id * C::DV + c0;
     const float* pl = p.ws_lse + id;
 #pragma unroll 1
     for (int s = s0; s < s1; s += BATCH * step) {
       float lse[BATCH];
-      f32x4 part[BATCH][COLS / 4];
+      uint64_t part[BATCH][COLS / 2];
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
-        const int64_t at = (int64_t)min(s + u * step, s1 - 1) * all_rows;
-        lse[u] = __hip_atomic_load(pl + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        lse[u] = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < COLS / 4; ++e) part[u][e] = load_shared(po + at * C::DV + 4 * e);
+        for (int e = 0; e < COLS / 2; ++e) part[u][e] = 0;
+        if (s + u * step < s1) {  // (not clamped to the last slot: these loads pass the caches)
+          const int64_t at = (int64_t)(s + u * step) * all_rows;
+          lse[u] = __hip_atomic_load(pl + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+          for (int e = 0; e < COLS / 2; ++e) part[u][e] = load_shared(po + at * C::DV + 2 * e);
+        }
       }
       float top = M;
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) {
-        lse[u] = s + u * step < s1 ? lse[u] : -INFINITY;
-        top = fmaxf(top, lse[u]);
-      }
+      for (int u = 0; u < BATCH; ++u) top = fmaxf(top, lse[u]);
       if (__builtin_bit_cast(uint32_t, top) == 0xff800000u) continue;  // no key so far
       const float a = fast_exp2(M - top);
       M = top;
@@ -492,7 +477,8 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
         const float w = fast_exp2(lse[u] - top);
         L += w;
 #pragma unroll
-        for (int e = 0; e < COLS; ++e) acc[e] += w * (__builtin_bit_cast(uint32_t, w) == 0 ? 0.f : part[u][e / 4][e % 4]);
+        for (int e = 0; e < COLS; ++e)
+          acc[e] += w * (__builtin_bit_cast(uint32_t, w) == 0 ? 0.f : __builtin_bit_cast(float, (uint32_t)(part[u][e / 2] >> (32 * (e % 2)))));
       }
     }
   };
@@ -500,14 +486,19 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     normalise();
     const int64_t at = b * p.os[0] + h * p.os[1] + t * p.os[2] + c0;
 #pragma unroll
-    for (int e = 0; e < COLS; e += 4) {
+    for (int e = 0; e < COLS; e += PIECE) {
       if (p.out_bf16) {
-        bf16x4 v;
+        typedef __attribute__((ext_vector_type(PIECE))) __bf16 piece;
+        piece v;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = (__bf16)acc[e + k];
-        *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.O) + at + e) = v;
+        for (int k = 0; k < PIECE; ++k) v[k] = (__bf16)acc[e + k];
+        *reinterpret_cast<piece*>(static_cast<__bf16*>(p.O) + at + e) = v;
       } else {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(p.O) + at + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+        typedef __attribute__((ext_vector_type(PIECE))) float piece;
+        piece v;
+#pragma unroll
+        for (int k = 0; k < PIECE; ++k) v[k] = acc[e + k];
+        *reinterpret_cast<piece*>(static_cast<float*>(p.O) + at + e) = v;
       }
     }
     if (c0 == 0 && p.stats != nullptr) p.stats[id] = any() ? (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f : -INFINITY;
@@ -560,7 +551,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
         const int64_t at = (int64_t)(pt.slot0 + split) * all_rows + id;
         normalise();
 #pragma unroll
-        for (int e = 0; e < COLS; e += 4) store_shared(p.ws_o + at * C::DV + c0 + e, f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]});
+        for (int e = 0; e < COLS; e += 2) store_shared(p.ws_o + at * C::DV + c0 + e, acc[e], acc[e + 1]);
         if (c0 == 0) __hip_atomic_store(p.ws_lse + at, any() ? M + __builtin_amdgcn_logf(L) : -INFINITY, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       } else {  // the only workgroup of its rows, but for a prefix that an earlier launch has walked
         join(id, 0, 1, pt.slot0);
@@ -632,23 +623,25 @@ hipError_t launch_cfg(const CachedParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int DQK, int DV, bool E4M3>
+template <int DQK, int DV, bool E4M3, int W>
 hipError_t launch_rows(const CachedParams& p, hipStream_t s) {
   const int rows = std::max(p.part[0].tile_rows, p.prefix_blocks ? p.part[1].tile_rows : 0);
-  if (rows <= 16) return launch_cfg<CachedCfg<DQK, DV, E4M3, 1>>(p, s);
-  return launch_cfg<CachedCfg<DQK, DV, E4M3, 2>>(p, s);
+  if (rows <= 16) return launch_cfg<CachedCfg<DQK, DV, E4M3, 1, W>>(p, s);
+  return launch_cfg<CachedCfg<DQK, DV, E4M3, 2, W>>(p, s);
 }
 
 template <int DQK, int DV>
 hipError_t launch_type(const CachedParams& p, bool e4m3, hipStream_t s) {
-  return e4m3 ? launch_rows<DQK, DV, true>(p, s) : launch_rows<DQK, DV, false>(p, s);
+  if (p.waves == 8) return e4m3 ? launch_rows<DQK, DV, true, 8>(p, s) : launch_rows<DQK, DV, false, 8>(p, s);
+  return e4m3 ? launch_rows<DQK, DV, true, 4>(p, s) : launch_rows<DQK, DV, false, 4>(p, s);
 }
 
 }  // namespace
 
-int cached_residents(int dqk, int dv, bool e4m3, int rows_per_workgroup) {
-  const int lds = 4 * 32 * (dqk + dv) * (e4m3 ? 1 : 2) + (e4m3 ? 4 * 256 : 0);  // (CachedCfg::LDS_BYTES; 8-bit 64/64 a little more)
-  return std::min(160 * 1024 / lds, rows_per_workgroup == 16 ? 3 : 2);
+int cached_residents(int dqk, int dv, bool e4m3, int rows, int waves) {
+  const int lds = waves * 32 * (dqk + dv) * (e4m3 ? 1 : 2) + (e4m3 ? waves * 256 : 0);  // (CachedCfg::LDS_BYTES; 8-bit 64/64 a little more)
+  const int waves_eu = rows > 16 ? 2 : waves == 4 ? 3 : e4m3 && dqk + dv <= 256 ? 4 : 2;
+  return std::min(160 * 1024 / lds, 4 * waves_eu / waves);
 }
 
 // (Four row tiles a wavefront, 64 rows, need 512 registers, spills among them, and leave a SIMD one wavefront: 20 x 64/8 heads x 8

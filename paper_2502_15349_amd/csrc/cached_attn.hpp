@@ -31,6 +31,7 @@ struct CachedParams {
   int B, H_q, H_kv, g, n, page_shift, n_pages;
   float c;        // scale * log2(e)
   int out_bf16;
+  int waves;      // wavefronts of a workgroup of launch_cached: 4 or 8
   // The parts that a launch walks: the own lists (part[0]), and in front of their workgroups the prefix's (part[1], 0 or
   // prefix_blocks workgroups), where that has few rows.
   CachedPart part[2];
@@ -42,8 +43,8 @@ struct CachedParams {
 };
 
 int cached_rows_per_workgroup(int rows);  // at most
-// Workgroups of 16 or 32 rows that a compute unit holds at a time.
-int cached_residents(int dqk, int dv, bool e4m3, int rows_per_workgroup);
+// Workgroups of so many rows and wavefronts that a compute unit holds at a time.
+int cached_residents(int dqk, int dv, bool e4m3, int rows, int waves);
 hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);
 constexpr int kPrefixRows = 256;  // rows of a workgroup of launch_prefix, which walks part[1] alone
 hipError_t launch_prefix(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);

@@ -736,9 +736,25 @@ def _shape_of(t):
     return (t.shape, t.stride(), t.dtype, t.device)
 
 
-def _stream_of(stream, device):
+def _enqueue(call, device, stream, *args):
+    """call(*args, raw stream) with `device` current, on `stream` (None: the device's current one).  The step of a decoding loop pays for
+    this every time: asking for a stream object takes 1.9 us, for its address 0.1, and setting the current device again 1.3."""
     import torch
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+    index = device.index
+    raw = _raw_stream(index) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        call(*args, raw)
+    else:
+        with torch.cuda.device(index):
+            call(*args, raw)
+
+
+def _raw_stream(index):
+    import torch
+
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(index) if get is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 class RotaryPlan:
@@ -776,21 +792,16 @@ class RotaryPlan:
         self.device = Q.device
 
     def _run(self, call, specs, tensors, stream):
-        import torch
-
-        for t, spec in zip(tensors, specs):
-            if (t is None) != (spec is None) or (t is not None and _shape_of(t) != spec):
-                raise ValueError("a tensor differs from the plan's in shape, strides, type or device")
-        ptrs = [0 if t is None else t.data_ptr() for t in tensors]
-        with torch.cuda.device(self.device):
-            call(self.handle, *ptrs, _stream_of(stream, self.device))
+        if [t if t is None else _shape_of(t) for t in tensors] != specs:
+            raise ValueError("a tensor differs from the plan's in shape, strides, type or device")
+        _enqueue(call, self.device, stream, self.handle, *[0 if t is None else t.data_ptr() for t in tensors])
 
     def forward(self, Q, K, positions, Q_out, K_out, *, stream=None):
         self._run(ae_rotary_forward, self._specs, (Q, K, positions, Q_out, K_out), stream)
 
     def backward(self, dQ_out, dK_out, positions, dQ, dK, *, stream=None):
         s = self._specs
-        self._run(ae_rotary_backward, (s[3], s[4], s[2], s[0], s[1]), (dQ_out, dK_out, positions, dQ, dK), stream)
+        self._run(ae_rotary_backward, [s[3], s[4], s[2], s[0], s[1]], (dQ_out, dK_out, positions, dQ, dK), stream)
 
     def __del__(self):
         if getattr(self, "handle", None) is not None and _lib is not None:
@@ -801,7 +812,7 @@ class RotaryPlan:
 def _no_overlap(*outs):
     """Outputs that a call writes must not have two indices at one address (expanded tensors)."""
     for t in outs:
-        if t is not None and any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
+        if t is not None and 0 in t.stride() and any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
             raise ValueError("an output must not be an expanded tensor")
 
 
@@ -856,6 +867,7 @@ class PagedCache:
         self.k, self.v, self.k_exp, self.v_exp, self.device = k, v, k_exp, v_exp, k.device
         self.n_pages, self.H_kv, self.page_size, self.D_qk = k.shape
         self.D_v = v.shape[3]
+        self._bf16, self._int = torch.bfloat16, torch.int32
         self.handle = ae_cache_create(n_pages=self.n_pages, page_size=self.page_size, H_kv=self.H_kv, D_qk=self.D_qk, D_v=self.D_v,
                                       dtype="e4m3" if e4m3 else "bf16")
 
@@ -875,26 +887,28 @@ class PagedCache:
                 0 if self.v_exp is None else self.v_exp.data_ptr())
 
     def _slots(self, slots, B, L):
-        import torch
-
-        if (slots.dtype != torch.int32 or tuple(slots.shape) not in ((L,), (B, L)) or slots.device != self.device or (L > 1 and slots.stride(-1) != 1)
-                or (slots.dim() == 1 and B > 1)):
+        if (slots.dtype != self._int or slots.shape not in (((L,), (B, L)) if B == 1 else ((B, L),)) or slots.device != self.device
+                or (L > 1 and slots.stride(-1) != 1)):
             raise ValueError("slots must be an int32 device tensor [B, L] (or [L] for B = 1) with contiguous rows")
         return slots.data_ptr(), slots.stride(0) if slots.dim() == 2 else 0
+
+    def _rows(self, K, V, B, L):
+        """Strides of K and V [B, H_kv, L, D]."""
+        strides = []
+        for t, d in ((K, self.D_qk), (V, self.D_v)):
+            st = t.stride()
+            if t.dtype != self._bf16 or t.shape != (B, self.H_kv, L, d) or st[3] != 1 or t.device != self.device:
+                raise ValueError("K and V must be bf16 [B, H_kv, L, D] on the cache's device with a contiguous last dimension")
+            strides.append(st[:3])
+        return strides
 
     def append(self, K, V, slots, *, stream=None):
         """Writes the rows of K [B, H_kv, L, D_qk] and V [B, H_kv, L, D_v] (bf16, last dimension contiguous) to the slots int32 [B, L];
         rows whose slot is outside the cache (-1) are skipped, the others' slots must differ."""
-        import torch
-
-        B, H, L, _ = K.shape
-        for t, d in ((K, self.D_qk), (V, self.D_v)):
-            if t.dtype != torch.bfloat16 or tuple(t.shape) != (B, self.H_kv, L, d) or t.stride(3) != 1 or t.device != self.device:
-                raise ValueError("K and V must be bf16 [B, H_kv, L, D] on the cache's device with a contiguous last dimension")
+        B, _, L, _ = K.shape
+        ks, vs = self._rows(K, V, B, L)
         at, stride = self._slots(slots, B, L)
-        with torch.cuda.device(self.device):
-            ae_cache_append(self.handle, K.data_ptr(), K.stride()[:3], V.data_ptr(), V.stride()[:3], B, L, at, stride, *self.pointers(),
-                            _stream_of(stream, self.device))
+        _enqueue(ae_cache_append, self.device, stream, self.handle, K.data_ptr(), ks, V.data_ptr(), vs, B, L, at, stride, *self.pointers())
 
     def read(self, slots, *, out=None, stream=None):
         """The rows at slots int32 [B, L] (or [L]: B = 1) as bf16 K [B, H_kv, L, D_qk] and V [B, H_kv, L, D_v]; zeros for a slot outside the
@@ -903,15 +917,13 @@ class PagedCache:
 
         B, L = (1, slots.shape[0]) if slots.dim() == 1 else slots.shape
         if out is None:
-            out = tuple(torch.empty(B, self.H_kv, L, d, dtype=torch.bfloat16, device=self.device) for d in (self.D_qk, self.D_v))
-        for t, d in zip(out, (self.D_qk, self.D_v)):
-            if t.dtype != torch.bfloat16 or tuple(t.shape) != (B, self.H_kv, L, d) or t.stride(3) != 1 or t.device != self.device:
-                raise ValueError("outputs must be bf16 [B, H_kv, L, D] on the cache's device with a contiguous last dimension")
-        _no_overlap(*out)
+            out = tuple([torch.empty((B, self.H_kv, L, d), dtype=self._bf16, device=self.device) for d in (self.D_qk, self.D_v)])
+            ks = vs = (0, 0, 0)  # (contiguous)
+        else:
+            ks, vs = self._rows(*out, B, L)
+            _no_overlap(*out)
         at, stride = self._slots(slots, B, L)
-        with torch.cuda.device(self.device):
-            ae_cache_read(self.handle, *self.pointers(), B, L, at, stride, out[0].data_ptr(), out[0].stride()[:3], out[1].data_ptr(),
-                          out[1].stride()[:3], _stream_of(stream, self.device))
+        _enqueue(ae_cache_read, self.device, stream, self.handle, *self.pointers(), B, L, at, stride, out[0].data_ptr(), ks, out[1].data_ptr(), vs)
         return out
 
     def __del__(self):
@@ -943,35 +955,31 @@ class CachedAttentionPlan:
         self.handle = ae_cached_create(cache.handle, B=B, H_q=H_q, n_new=n, table_width=table_width, max_length=max_length, scale=scale,
                                        prefix_length=prefix_length, chunk=chunk, out_dtype="bf16" if out.dtype == torch.bfloat16 else "f32",
                                        q_stride=Q.stride()[:3], o_stride=out.stride()[:3])
-        self.cache, self.device, self.shape = cache, Q.device, (B, H_q, n)
+        self.cache, self.device, self.shape, self._f32 = cache, Q.device, (B, H_q, n), torch.float32
         self._q, self._o = _shape_of(Q), _shape_of(out)
         self._table, self._prefix = (B, table_width), -(-prefix_length // cache.page_size)
         self.workspace_bytes = ae_cached_workspace_bytes(self.handle)
         self.workspace = None
         if self.workspace_bytes:
-            with torch.cuda.device(Q.device):
-                self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=Q.device)
-                ae_cached_init_workspace(self.handle, self.workspace.data_ptr(), self.workspace_bytes, _stream_of(None, Q.device))
+            self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=Q.device)
+            _enqueue(ae_cached_init_workspace, Q.device, None, self.handle, self.workspace.data_ptr(), self.workspace_bytes)
 
     def forward(self, Q, table, lengths, out, *, stats=None, prefix_table=None, stream=None):
         """table int32 [B, table_width], lengths int32 [B] (device), prefix_table int32 [pages of the prefix]; stats: fp32 [B, H_q, n] that
         receives ln sum exp.  Writes and returns out."""
-        import torch
-
         if _shape_of(Q) != self._q or _shape_of(out) != self._o:
             raise ValueError("Q or O differs from the plan's in shape, strides, type or device")
+        if (prefix_table is None) == bool(self._prefix):
+            raise ValueError("a prefix's table is given exactly where the plan has a prefix")
         ints = ((table, self._table), (lengths, self._table[:1])) + (((prefix_table, (self._prefix,)),) if self._prefix else ())
         for t, shape in ints:
-            if t is None or t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+            if t.dtype != self.cache._int or t.shape != shape or not t.is_contiguous() or t.device != self.device:
                 raise ValueError(f"tables and lengths must be contiguous int32 device tensors (here {shape})")
-        if prefix_table is not None and not self._prefix:
-            raise ValueError("the plan has no prefix")
-        if stats is not None and (stats.dtype != torch.float32 or stats.shape != self.shape or not stats.is_contiguous() or stats.device != self.device):
+        if stats is not None and (stats.dtype != self._f32 or stats.shape != self.shape or not stats.is_contiguous() or stats.device != self.device):
             raise ValueError("stats must be a contiguous fp32 tensor [B, H_q, n]")
-        with torch.cuda.device(self.device):
-            ae_cached_forward(self.handle, Q.data_ptr(), *self.cache.pointers(), table.data_ptr(), lengths.data_ptr(),
-                              prefix_table.data_ptr() if self._prefix else 0, out.data_ptr(), 0 if stats is None else stats.data_ptr(),
-                              0 if self.workspace is None else self.workspace.data_ptr(), self.workspace_bytes, _stream_of(stream, self.device))
+        _enqueue(ae_cached_forward, self.device, stream, self.handle, Q.data_ptr(), *self.cache.pointers(), table.data_ptr(), lengths.data_ptr(),
+                 0 if prefix_table is None else prefix_table.data_ptr(), out.data_ptr(), 0 if stats is None else stats.data_ptr(),
+                 0 if self.workspace is None else self.workspace.data_ptr(), self.workspace_bytes)
         return out
 
     def __del__(self):

@@ -22,7 +22,7 @@ struct RotaryParams {
   float amp;
   int backward;
   int interleaved, f32;
-  int heads_per_thread;
+  int heads_per_thread;  // (set by launch_rotary)
 };
 
 // wide: every row, pair block and stride is a whole number of 16-byte pieces

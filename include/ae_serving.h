@@ -159,6 +159,9 @@ ae_status_t ae_cached_init_workspace(const ae_cached_t *h, void *workspace, size
 ae_status_t ae_cached_forward(const ae_cached_t *h, const void *Q, const void *K_pages, const void *V_pages, const void *K_exp,
                               const void *V_exp, const int32_t *table, const int32_t *lengths, const int32_t *prefix_table,
                               void *O, float *stats, void *workspace, size_t workspace_bytes, hipStream_t stream);
+/* What create chose: wavefronts of a workgroup, keys of a range of the sequences' own lists and of the prefix (0: none),
+ * launches of a call.  Any pointer may be NULL.                              */
+ae_status_t ae_cached_query(const ae_cached_t *h, int32_t *waves, int32_t *own_chunk, int32_t *prefix_chunk, int32_t *launches);
 ae_status_t ae_cached_destroy(ae_cached_t *h); /* NULL is allowed */
 
 #ifdef __cplusplus

@@ -590,6 +590,8 @@ _lib.ae_cached_init_workspace.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.
 _lib.ae_cached_init_workspace.restype = C.c_int
 _lib.ae_cached_forward.argtypes = [C.c_void_p] * 12 + [C.c_size_t, C.c_void_p]
 _lib.ae_cached_forward.restype = C.c_int
+_lib.ae_cached_query.argtypes = [C.c_void_p] + [C.POINTER(C.c_int32)] * 4
+_lib.ae_cached_query.restype = C.c_int
 _lib.ae_cached_destroy.argtypes = [C.c_void_p]
 _lib.ae_cached_destroy.restype = C.c_int
 _lib.ae_rotary_create.argtypes = [C.POINTER(ae_rotary_desc_t), C.POINTER(C.c_void_p)]
@@ -693,6 +695,13 @@ def ae_cached_forward(handle: int, Q: int, K_pages: int, V_pages: int, K_exp: in
     """Device addresses; K_exp, V_exp (16-bit cache), prefix_table (no prefix), stats and workspace (0 bytes) may be 0."""
     _check(_lib.ae_cached_forward(handle, Q, K_pages, V_pages, K_exp, V_exp, table, lengths, prefix_table, O, stats, workspace,
                                   workspace_bytes, stream))
+
+
+def ae_cached_query(handle: int) -> dict:
+    """What create chose: wavefronts of a workgroup, keys of a range (own lists, prefix), launches of a call."""
+    v = [C.c_int32() for _ in range(4)]
+    _check(_lib.ae_cached_query(handle, *[C.byref(x) for x in v]))
+    return {k: int(x.value) for k, x in zip(("waves", "own_chunk", "prefix_chunk", "launches"), v)}
 
 
 def ae_cached_destroy(handle: Optional[int]) -> None:

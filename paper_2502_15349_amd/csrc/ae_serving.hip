@@ -459,6 +459,15 @@ ae_status_t ae_cached_forward(const ae_cached_t* h, const void* Q, const void* K
   return launched(ae::launch_cached(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
 }
 
+ae_status_t ae_cached_query(const ae_cached_t* h, int32_t* waves, int32_t* own_chunk, int32_t* prefix_chunk, int32_t* launches) {
+  if (!h) return fail(AE_ERR_INVALID_ARG, "ae_cached_query: null handle");
+  if (waves) *waves = h->params.waves;
+  if (own_chunk) *own_chunk = h->params.part[0].chunk;
+  if (prefix_chunk) *prefix_chunk = h->params.part[1].chunk;
+  if (launches) *launches = h->prefix_apart ? 2 : 1;
+  return AE_OK;
+}
+
 ae_status_t ae_cached_destroy(ae_cached_t* h) {
   delete h;
   return AE_OK;

@@ -11,24 +11,19 @@
 // 8-bit keys become bf16 between LDS and the MFMA, on their row's power of two (exact, the conversion applies it);
 // 8-bit values likewise without theirs, which multiplies the weight instead (a lane's 8 values of V are of 8 rows).
 //
-// Keys and values go from the pages to LDS by global_load_lds, each wavefront its own sub-tiles into its own stages, so that
+// Keys and values go from the pages to LDS by global_load_lds, each wavefront its own sub-tiles into LDS of its own, so that
 // the walk needs no barriers; the wavefronts of a workgroup take sub-tiles in turn and their states meet at the end.
 #include "cached_attn.hpp"
 
 #include <algorithm>
 
-#include "attn_kernel.hpp"
 #include "launch.hpp"
+#include "paged.hpp"
 
 namespace ae {
 namespace {
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
-// a load of something that no one writes during the launch, at an address that is the same in all lanes
-__device__ __forceinline__ int32_t scalar_load(const int32_t* ptr) {
-  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uintptr_t)ptr);
-}
 
 template <int DQK_, int DV_, bool E4M3_, int RT_, int W_>
 struct CachedCfg {
@@ -40,15 +35,16 @@ struct CachedCfg {
   static constexpr int K_BYTES = 32 * RBK, V_BYTES = 32 * RBV, E_BYTES = E4M3 ? 256 : 0, STAGE = K_BYTES + V_BYTES + E_BYTES;
   static constexpr int NK = K_BYTES / 1024, NV = V_BYTES / 1024;
   static constexpr int NKE = NK + (E4M3 ? 1 : 0);  // copies awaited before the scores (the exponents come with the keys)
-  static constexpr int STAGES = 1;
   static constexpr int KS = DQK / 32, DB = DV / 16;
   static constexpr int ROWS = 16 * RT;
   static constexpr int RED_ROW = DV + 4;
-    static constexpr int BATCH = 4;  // partial results of a thread in flight when they are joined (8 and 16: no faster)
+  static constexpr int BATCH = 4;  // partial results of a thread in flight when they are joined (8 and 16: no faster)
   static constexpr int RED_BYTES = (W * 16 * (RED_ROW + 2) + W + ROWS + 1) * 4;
-  static constexpr int LDS_BYTES = W * STAGES * STAGE > RED_BYTES ? W * STAGES * STAGE : RED_BYTES;
+  // One sub-tile for each wavefront.  Two (with one workgroup instead of two on a compute unit): 20 x 64/8 heads x 4 tokens x up to 4000
+  // keys 48 -> 53 us, 64 sequences behind 8192 keys 40 -> 62.
+  static constexpr int LDS_BYTES = W * STAGE > RED_BYTES ? W * STAGE : RED_BYTES;
   static_assert(LDS_BYTES <= 160 * 1024, "a workgroup must fit LDS");
-  static_assert(STAGES * (NKE + NV) < 64, "the wait count has six bits");
+  static_assert(NKE + NV < 64, "the wait count has six bits");
 };
 
 // ---- chunk swizzles: LDS position of 16-byte chunk c of tile row r is c ^ swizzle(r) -------------------------------------------
@@ -85,13 +81,6 @@ __device__ __forceinline__ void wait_vmem() {
 __device__ __forceinline__ float max_over_groups(float x) {  // over the four groups of 16 lanes
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
-}
-
-// 16 bytes of e4m3 -> two fragments of 8 bf16, times a power of two
-__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 typedef __attribute__((ext_vector_type(2))) int i32x2;
@@ -152,7 +141,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
   const int all_visible = pt.causal ? len - p.n + 1 : len;  // keys below this one are visible to every row
 
   // ---- copies --------------------------------------------------------------------------------------------------------------
-  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_char*)smem) + wave * (C::STAGES * C::STAGE);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_char*)smem) + wave * C::STAGE;
   const int page_mask = (1 << p.page_shift) - 1;
   uint32_t koff[C::NK], voff[C::NV];  // the lane's byte offset from the first row of the half tile
 #pragma unroll
@@ -177,11 +166,10 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     pg0 = scalar_load(table + min(j0 >> p.page_shift, pt.table_width - 1));
     pg1 = scalar_load(table + min((j0 + 16) >> p.page_shift, pt.table_width - 1));
   };
-  auto issue_k = [&](int i, int stage) -> int {
+  auto issue_k = [&](int i) -> int {
     const int j0 = begin + 32 * (wave + i * C::W);
     const bool second = j0 + 16 < end;
     const bool ok0 = (uint32_t)pg0 < (uint32_t)p.n_pages, ok1 = second ? (uint32_t)pg1 < (uint32_t)p.n_pages : ok0;
-    const uint32_t base = lds0 + stage * C::STAGE;
     row[0] = (((int64_t)(ok0 ? pg0 : 0) * p.H_kv + hk) << p.page_shift) + (j0 & page_mask);
     row[1] = second ? (((int64_t)(ok1 ? pg1 : 0) * p.H_kv + hk) << p.page_shift) + ((j0 + 16) & page_mask) : row[0];
     fetch_pages(i + 1);
@@ -189,21 +177,20 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < C::NK / 2; ++i)
-        dma16(p.K + row[h] * C::RBK, koff[h * (C::NK / 2) + i], base + (h * (C::NK / 2) + i) * 1024);
+        dma16(p.K + row[h] * C::RBK, koff[h * (C::NK / 2) + i], lds0 + (h * (C::NK / 2) + i) * 1024);
     if constexpr (C::E4M3) {  // bytes 0..31: exponents of the keys, 32..63: of the values (lanes 16.. repeat them)
       const int k = lane & 15;
       const uint8_t* e = (k & 8 ? p.Ve : p.Ke) + row[(k >> 2) & 1] + 4 * (k & 3);
-      dma4_gather(e, base + C::K_BYTES + C::V_BYTES);
+      dma4_gather(e, lds0 + C::K_BYTES + C::V_BYTES);
     }
     return (ok0 ? 0 : 1) | (ok1 ? 0 : 2);
   };
-  auto issue_v = [&](int stage) {
-    const uint32_t base = lds0 + stage * C::STAGE + C::K_BYTES;
+  auto issue_v = [&] {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < C::NV / 2; ++i)
-        dma16(p.V + row[h] * C::RBV, voff[h * (C::NV / 2) + i], base + (h * (C::NV / 2) + i) * 1024);
+        dma16(p.V + row[h] * C::RBV, voff[h * (C::NV / 2) + i], lds0 + C::K_BYTES + (h * (C::NV / 2) + i) * 1024);
   };
 
   // ---- fragments -------------------------------------------------------------------------------------------------------------
@@ -218,12 +205,12 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     vaddr[d] = lds0 + C::K_BYTES + vrow * C::RBV +
                (C::E4M3 ? ((d ^ tr_swizzle<C::CPRV, true>(vrow)) << 4) + 8 * (ql & 1)
                         : (((2 * d + ((ql & 3) >> 1)) ^ tr_swizzle<C::CPRV, false>(vrow)) << 4) + 8 * (ql & 1));
-  auto read_v = [&](int d, uint32_t so) -> bf16x8 {
+  auto read_v = [&](int d) -> bf16x8 {
     if constexpr (C::E4M3) {
-      const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(uintptr_t)(vaddr[d] + so));
+      const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(uintptr_t)vaddr[d]);
       return widen8(v[0], v[1], 1.f);
     } else {
-      return read_v_frag(vaddr[d] + so, 4 * C::RBV);
+      return read_v_frag(vaddr[d], 4 * C::RBV);
     }
   };
 
@@ -239,19 +226,18 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
   }
 
   // One sub-tile; `keys_read` runs behind the last read of its keys, `await_values` in front of the first of its values.
-  auto compute = [&](int i, int stage, int hidden, auto&& keys_read, auto&& await_values) {
+  auto compute = [&](int i, int hidden, auto&& keys_read, auto&& await_values) {
     const int j0 = begin + 32 * (wave + i * C::W);
-    const uint32_t so = stage * C::STAGE;
     const bool masked = hidden != 0 || j0 + 32 > min(all_visible, end);
     float ks[2] = {1.f, 1.f}, vs[8];
     if constexpr (C::E4M3) {
-      const uint32_t eb = lds0 + so + C::K_BYTES + C::V_BYTES;
+      const uint32_t eb = lds0 + C::K_BYTES + C::V_BYTES;
       typedef __attribute__((address_space(3))) const uint8_t lds_u8;
-      ks[0] = __builtin_bit_cast(float, (uint32_t)*reinterpret_cast<lds_u8*>((lds_char*)(uintptr_t)(eb + krow)) << 23);
-      ks[1] = __builtin_bit_cast(float, (uint32_t)*reinterpret_cast<lds_u8*>((lds_char*)(uintptr_t)(eb + krow + 4)) << 23);
+      ks[0] = power_of_two(*reinterpret_cast<lds_u8*>((lds_char*)(uintptr_t)(eb + krow)));
+      ks[1] = power_of_two(*reinterpret_cast<lds_u8*>((lds_char*)(uintptr_t)(eb + krow + 4)));
       const u32x2 v = *reinterpret_cast<__attribute__((address_space(3))) const u32x2*>((lds_char*)(uintptr_t)(eb + 32 + 8 * hi));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vs[e] = __builtin_bit_cast(float, ((v[e / 4] >> (8 * (e % 4))) & 0xffu) << 23);
+      for (int e = 0; e < 8; ++e) vs[e] = power_of_two((v[e / 4] >> (8 * (e % 4))) & 0xffu);
     }
     f32x4 s[2][C::RT];
 #pragma unroll
@@ -263,7 +249,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
       for (int s2 = 0; s2 < C::KS / 2; ++s2)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const u32x4 raw = __builtin_bit_cast(u32x4, read_k_frag(kaddr[s2] + so + u * 4 * C::RBK));
+          const u32x4 raw = __builtin_bit_cast(u32x4, read_k_frag(kaddr[s2] + u * 4 * C::RBK));
           const bf16x8 a = widen8(raw[0], raw[1], ks[u]), b = widen8(raw[2], raw[3], ks[u]);
 #pragma unroll
           for (int rt = 0; rt < C::RT; ++rt) {
@@ -276,7 +262,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
       for (int ss = 0; ss < C::KS; ++ss)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const bf16x8 a = read_k_frag(kaddr[ss] + so + u * 4 * C::RBK);
+          const bf16x8 a = read_k_frag(kaddr[ss] + u * 4 * C::RBK);
 #pragma unroll
           for (int rt = 0; rt < C::RT; ++rt) s[u][rt] = mfma16(a, qf[rt][ss], s[u][rt]);
         }
@@ -329,7 +315,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     if (!masked) {
 #pragma unroll
       for (int d = 0; d < C::DB; ++d) {
-        const bf16x8 a = read_v(d, so);
+        const bf16x8 a = read_v(d);
 #pragma unroll
         for (int rt = 0; rt < C::RT; ++rt) o[rt][d] = mfma16(a, pb[rt], o[rt][d]);
       }
@@ -341,7 +327,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     for (int e = 0; e < 4; ++e) keep[e] = there > 2 * e + 1 ? 0xffffffffu : there > 2 * e ? 0xffffu : 0u;
 #pragma unroll
     for (int d = 0; d < C::DB; ++d) {
-      u32x4 a = __builtin_bit_cast(u32x4, read_v(d, so)) & keep;
+      u32x4 a = __builtin_bit_cast(u32x4, read_v(d)) & keep;
       if (some_see) {
         uint32_t lo[4], up[4];
         bool odd = false;
@@ -363,47 +349,35 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
   };
 
   // ---- the walk ------------------------------------------------------------------------------------------------------------------
-  // Keys and values of a stage are recycled apart: the next keys are requested as soon as the scores have read these, the next
-  // values behind the second product.  In flight behind a copy that is awaited (in order): whatever was requested after it.
-  int hid[C::STAGES];
+  // The places of keys and values are recycled apart: the next keys are requested as soon as the scores have read these, the next
+  // values behind the second product.  What is in flight behind a copy that is awaited (they arrive in order) is known by number.
+  int hidden = 0;
   fetch_pages(0);
-#pragma unroll
-  for (int s = 0; s < C::STAGES; ++s) {
-    hid[s] = 0;
-    if (s < n_my) {
-      hid[s] = issue_k(s, s);
-      issue_v(s);
-    }
+  if (n_my > 0) {
+    hidden = issue_k(0);
+    issue_v();
   }
 #pragma unroll
   for (int rt = 0; rt < C::RT; ++rt)
 #pragma unroll
     for (int s = 0; s < C::KS; ++s) asm volatile("" ::"v"(qf[rt][s]));  // (awaited here, not inside the loop)
   auto all_read = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };  // before a copy overwrites what was read
-  constexpr int PAIR = C::NKE + C::NV;
-  for (int i0 = 0; i0 < n_my; i0 += C::STAGES) {
-#pragma unroll
-    for (int s = 0; s < C::STAGES; ++s) {
-      const int i = i0 + s;
-      if (i < n_my) {
-        if (i + C::STAGES - 1 < n_my) wait_vmem<(C::STAGES - 1) * PAIR + C::NV>();
-        else wait_vmem<C::NV>();
-        const int hidden = hid[s];
-        const bool next = i + C::STAGES < n_my;
-        compute(
-            i, s, hidden,
-            [&] {
-              all_read();
-              if (next) hid[s] = issue_k(i + C::STAGES, s);
-            },
-            [&] {
-              if (next) wait_vmem<(C::STAGES - 1) * PAIR + C::NKE>();
-              else wait_vmem<0>();
-            });
-        all_read();
-        if (next) issue_v(s);
-      }
-    }
+  for (int i = 0; i < n_my; ++i) {
+    wait_vmem<C::NV>();
+    const int now = hidden;
+    const bool next = i + 1 < n_my;
+    compute(
+        i, now,
+        [&] {
+          all_read();
+          if (next) hidden = issue_k(i + 1);
+        },
+        [&] {
+          if (next) wait_vmem<C::NKE>();
+          else wait_vmem<0>();
+        });
+    all_read();
+    if (next) issue_v();
   }
 
   // ---- the wavefronts' states into one, row tile by row tile --------------------------------------------------------------------

@@ -9,21 +9,11 @@
 // wavefront would repeat it: 64 conversions per 16 MFMAs.)
 #include "cached_attn.hpp"
 
-#include "attn_kernel.hpp"
 #include "launch.hpp"
+#include "paged.hpp"
 
 namespace ae {
 namespace {
-
-__device__ __forceinline__ int32_t scalar_load(const int32_t* ptr) {  // (nobody writes it during the launch; the same in all lanes)
-  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uintptr_t)ptr);
-}
-
-__device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi, float scale) {  // 8 e4m3 -> 8 bf16, times a power of two
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-  return u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)};
-}
 
 // 16-byte pieces of an 8-bit tile (64 rows of D bytes) that a thread carries
 template <int D, int THREADS>
@@ -159,12 +149,12 @@ __global__ __launch_bounds__(C::THREADS) void prefix_attn_kernel(const CachedPar
     }
   };
   auto write8 = [&](int stage) {
-    auto put = [&](uint32_t addr, u32x4 v) { lds_write16(addr, __builtin_bit_cast(f32x4, v)); };
+    auto put = [&](uint32_t addr, bf16x8 v) { lds_write16(addr, __builtin_bit_cast(f32x4, v)); };
 #pragma unroll
     for (int i = 0; i < NCK; ++i) {
       const int n = (int)(threadIdx.x + i * C::THREADS), r = n / CK::PER_ROW, c = 2 * (n % CK::PER_ROW);
       if (CK::EVEN || n < CK::TOTAL) {
-        const float f = __builtin_bit_cast(float, ek[i] << 23);
+        const float f = power_of_two(ek[i]);
         const uint32_t at = lds0 + stage * C::STAGE_BYTES + r * C::RB_K;
         put(at + ((c ^ kswz<C::CPR_K>(r)) << 4), widen8(rk[i][0], rk[i][1], f));
         put(at + (((c + 1) ^ kswz<C::CPR_K>(r)) << 4), widen8(rk[i][2], rk[i][3], f));
@@ -174,7 +164,7 @@ __global__ __launch_bounds__(C::THREADS) void prefix_attn_kernel(const CachedPar
     for (int i = 0; i < NCV; ++i) {
       const int n = (int)(threadIdx.x + i * C::THREADS), r = n / CV::PER_ROW, c = 2 * (n % CV::PER_ROW);
       if (CV::EVEN || n < CV::TOTAL) {
-        const float f = __builtin_bit_cast(float, ev[i] << 23);
+        const float f = power_of_two(ev[i]);
         const uint32_t at = vlds0 + stage * C::STAGE_BYTES + r * C::RB_V;
         put(at + ((c ^ (4 * vswz<C::CPR_V>(r))) << 4), widen8(rv[i][0], rv[i][1], f));
         put(at + (((c + 1) ^ (4 * vswz<C::CPR_V>(r))) << 4), widen8(rv[i][2], rv[i][3], f));

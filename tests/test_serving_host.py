@@ -92,6 +92,78 @@ def test_cache_call_refusals(A):
     A.ae_cache_destroy(None)
 
 
+CACHED = dict(B=2, H_q=8, n_new=1, table_width=4, max_length=100, scale=0.1)
+
+
+@pytest.mark.parametrize("patch,status", [
+    (dict(B=0), 1), (dict(H_q=0), 1), (dict(n_new=0), 1), (dict(table_width=0), 1), (dict(H_q=7), 1), (dict(max_length=0), 1), (dict(max_length=129), 1),
+    (dict(prefix_length=-1), 1), (dict(chunk=-128), 1), (dict(chunk=100), 1), (dict(scale=0.0), 1), (dict(scale=float("nan")), 1), (dict(scale=float("inf")), 1),
+    (dict(out_dtype=2), 1), (dict(q_stride=(1024, 128, 4)), 1), (dict(o_stride=(-8, 128, 128)), 1), (dict(B=1 << 22), 2),
+    (dict(prefix_length=(1 << 30) + 1), 2), (dict(B=1 << 20, prefix_length=1 << 20, chunk=128), 2),
+])
+def test_cached_refusals(A, patch, status):
+    c = A.ae_cache_create(**CACHE)
+    refused(A, status, A.ae_cached_create, c, **{**CACHED, **patch})
+    A.ae_cache_destroy(c)
+
+
+def test_cached_call_refusals(A):
+    refused(A, 1, A.ae_cached_create, None, **CACHED)
+    p = 1 << 20
+    for dtype, prefix, chunk in (("bf16", 0, 0), ("e4m3", 0, 0), ("bf16", 50, 0), ("e4m3", 50, 128)):
+        c = A.ae_cache_create(**CACHE, dtype=dtype)
+        h = A.ae_cached_create(c, **CACHED, prefix_length=prefix, chunk=chunk)
+        A.ae_cache_destroy(c)  # (the handle keeps what it needs of it)
+        ws = A.ae_cached_workspace_bytes(h)
+        assert (ws > 0) == (prefix > 0)
+        e = (6 * p, 7 * p) if dtype == "e4m3" else (0, 0)
+        ok = dict(Q=p, K_pages=2 * p, V_pages=3 * p, K_exp=e[0], V_exp=e[1], table=4 * p, lengths=5 * p, prefix_table=8 * p if prefix else 0, O=9 * p,
+                  stats=10 * p, workspace=11 * p if ws else 0, workspace_bytes=ws)
+        bad = [dict(Q=0), dict(K_pages=0), dict(V_pages=0), dict(table=0), dict(lengths=0), dict(O=0), dict(Q=p + 8), dict(O=9 * p + 8), dict(table=4 * p + 2),
+               dict(stats=10 * p + 1), dict(O=p), dict(O=2 * p), dict(stats=9 * p), dict(stats=5 * p), dict(prefix_table=0 if prefix else 8 * p),
+               dict(K_exp=0 if e[0] else 6 * p), dict(V_exp=0 if e[1] else 7 * p)]
+        if ws:
+            bad += [dict(workspace=0), dict(workspace=11 * p + 16), dict(workspace_bytes=ws - 1), dict(workspace=9 * p), dict(workspace=4 * p)]
+            refused(A, 1, A.ae_cached_init_workspace, h, 0, ws)
+            refused(A, 1, A.ae_cached_init_workspace, h, 11 * p, ws - 1)
+        for patch in bad:
+            refused(A, 1, A.ae_cached_forward, h, *{**ok, **patch}.values())
+        A.ae_cached_destroy(h)
+    A.ae_cached_destroy(None)
+    for call in (A.ae_cached_workspace_bytes, A.ae_cached_query):
+        refused(A, 1, call, None)
+    refused(A, 1, A.ae_cached_init_workspace, None, p, 0)
+    refused(A, 1, A.ae_cached_forward, None, *[p] * 12)
+
+
+def test_cached_layout(A):
+    c = A.ae_cache_create(n_pages=1 << 16, page_size=64, H_kv=8, D_qk=128, D_v=128)
+    try:
+        def layout(**kw):
+            h = A.ae_cached_create(c, **{**CACHED, "H_q": 32, "table_width": 1 << 14, **kw})
+            q, ws = A.ae_cached_query(h), A.ae_cached_workspace_bytes(h)
+            A.ae_cached_destroy(h)
+            return q, ws
+        # one long sequence is cut, many short ones are not; a caller's ranges are taken
+        q, ws = layout(B=1, max_length=100000)
+        assert q["own_chunk"] % 128 == 0 and q["own_chunk"] < 100000 and q["launches"] == 1 and ws > 0
+        q, ws = layout(B=256, max_length=300)
+        assert q["own_chunk"] >= 300 and ws == 0
+        assert layout(B=4, max_length=5000, chunk=640)[0]["own_chunk"] == 640
+        # rows of few sequences share the launch, those of many walk the prefix in one of their own
+        assert layout(B=4, max_length=300, prefix_length=2000)[0]["launches"] == 1
+        q, _ = layout(B=256, H_q=64, max_length=300, prefix_length=32768)
+        assert q["launches"] == 2 and q["prefix_chunk"] % 128 == 0
+        assert layout(B=4, n_new=16, max_length=300, prefix_length=2000)[0]["launches"] == 2  # (64 rows a sequence)
+        for B in (1, 7, 63, 200):  # no size is left without a layout
+            for n in (1, 3, 8, 40):
+                for L in (n, 77, 4097, 900000):
+                    q, _ = layout(B=B, n_new=n, max_length=max(n, L))
+                    assert q["waves"] in (4, 8) and q["own_chunk"] % 128 == 0
+    finally:
+        A.ae_cache_destroy(c)
+
+
 def test_frequencies(A):
     plain, one = A.rotary_frequencies(64)
     assert one == 1.0 and plain[0] == 1.0 and math.isclose(plain[-1], 10000.0 ** (-62 / 64))
@@ -115,6 +187,8 @@ def test_host_tensors_are_refused(A):
         A.rotary_forward(q, None, torch.arange(3, dtype=torch.int32), freqs=[1.0] * 32)
     with pytest.raises(ValueError):
         A.PagedCache.empty(2, 2, 16, 64, 64, device="cpu")
+    with pytest.raises(ValueError):
+        A.PagedCache(*[torch.zeros(2, 2, 16, 64, dtype=torch.float16)] * 2)
 
 
 def test_definition_of_the_quantised_rows():

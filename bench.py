@@ -139,6 +139,84 @@ def calib_mfma(A, torch, seconds):
             "nominal_peak": PEAK_BF16_TFLOPS}
 
 
+def serving_rows(torch, dev, steps, only):
+    """One decoding step of one layer per row -- rotary positions of the new tokens, their append, attention over the cache --
+    replayed from a graph, whole and operator by operator, GB/s against the HBM peak; parity of two sequences against the
+    oracle on what the cache holds."""
+    from oracle.serving_oracle import attend, dequantise
+    from paper_2502_15349_amd import ae_attn as A
+
+    def replayed(call):
+        call()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(10):
+                call()
+        t_settle = time.perf_counter()
+        while time.perf_counter() - t_settle < 0.2:
+            g.replay()
+            torch.cuda.synchronize()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        for _ in range(max(1, steps // 10)):
+            g.replay()
+        e1.record()
+        torch.cuda.synchronize()
+        return e0.elapsed_time(e1) * 1e3 / (10 * max(1, steps // 10))
+
+    rows = []
+    for name, B, H_q, H_kv, D_qk, D_v, length, prefix, dtype in (
+            ("b1_s4096", 1, 32, 8, 128, 128, 4096, 0, "bf16"), ("b16_s4096", 16, 32, 8, 128, 128, 4096, 0, "bf16"),
+            ("b16_s4096_e4m3", 16, 32, 8, 128, 128, 4096, 0, "e4m3"), ("b64_s2048_e4m3", 64, 32, 8, 128, 128, 2048, 0, "e4m3"),
+            ("b4_s131072", 4, 64, 8, 128, 128, 131072, 0, "bf16"), ("b16_s4096_192_128", 16, 16, 16, 192, 128, 4096, 0, "bf16"),
+            ("b64_s256_behind_8192", 64, 32, 8, 128, 128, 256, 8192, "bf16"), ("b256_s512_behind_16384_e4m3", 256, 64, 8, 128, 128, 512, 16384, "e4m3")):
+        if only not in name:
+            continue
+        page, g = 64, torch.Generator(device=dev).manual_seed(900 + len(rows))
+        width, pp = -(-length // page), -(-prefix // page)
+        cache = A.PagedCache.empty(B * width + pp, H_kv, page, D_qk, D_v, dtype=dtype, device=dev)
+        order = torch.randperm(B * width + pp, generator=g, device=dev).to(torch.int32)
+        ptab, table = order[:pp].contiguous(), order[pp:].view(B, width).contiguous()
+        slot = torch.arange(page, device=dev, dtype=torch.int32)
+        for lo in range(0, order.numel(), 4096):
+            pages = order[lo: lo + 4096]
+            rows_kv = [torch.randn(1, H_kv, pages.numel() * page, d, generator=g, device=dev).to(torch.bfloat16) for d in (D_qk, D_v)]
+            cache.append(*rows_kv, (pages[:, None] * page + slot).view(1, -1))
+        q, k, v = (torch.randn(B, 1, h, d, generator=g, device=dev).to(torch.bfloat16).transpose(1, 2)
+                   for h, d in ((H_q, D_qk), (H_kv, D_qk), (H_kv, D_v)))
+        qr, kr, out = torch.empty_like(q), torch.empty_like(k), torch.empty(B, H_q, 1, D_v, dtype=torch.bfloat16, device=dev)
+        pos = torch.full((B, 1), prefix + length - 1, dtype=torch.int32, device=dev)
+        lengths = torch.full((B,), length, dtype=torch.int32, device=dev)
+        slots = (table[:, (length - 1) // page] * page + (length - 1) % page).view(B, 1).contiguous()
+        freqs, amp = A.rotary_frequencies(min(D_qk, 128))
+        rot = A.RotaryPlan(q, k, pos, qr, kr, freqs=freqs, amplitude=amp)
+        plan = A.CachedAttentionPlan(cache, qr, out, max_length=length, table_width=width, prefix_length=prefix, scale=D_qk ** -0.5)
+        ops = {"rotary": lambda: rot.forward(q, k, pos, qr, kr), "append": lambda: cache.append(kr, v, slots),
+               "attention": lambda: plan.forward(qr, table, lengths, out, prefix_table=ptab if prefix else None)}
+        us = {n: round(replayed(f), 2) for n, f in ops.items()}
+        us["step"] = round(replayed(lambda: [f() for f in ops.values()]), 2)
+        byts = (B * length + prefix) * H_kv * ((D_qk + D_v) * (2 if dtype == "bf16" else 1) + (0 if dtype == "bf16" else 2))
+        flop = 2.0 * B * H_q * (length + prefix) * (D_qk + D_v)
+        err = 0.0
+        for b in {0, B - 1}:
+            t = torch.cat((ptab[: pp], table[b])).long()
+            kv = []
+            for pages, exps in ((cache.k, cache.k_exp), (cache.v, cache.v_exp)):
+                x = pages[t] if exps is None else pages.view(torch.uint8)[t]
+                x = x.cpu().double().numpy() if exps is None else dequantise(x.cpu().numpy(), exps[t].cpu().numpy())
+                x = x.transpose(1, 0, 2, 3)[:1]
+                own = x[:, pp:].reshape(1, -1, x.shape[3])[:, :length]
+                kv.append(np.concatenate((x[:, :pp].reshape(1, -1, x.shape[3])[:, :prefix], own), axis=1))
+            ref, _ = attend(qr[b, : H_q // H_kv].cpu().double().numpy(), *kv, D_qk ** -0.5)
+            err = max(err, float(np.abs(out[b, : H_q // H_kv].cpu().double().numpy() - ref).max()))
+        rows.append({"workload": "decode_step_" + name, "B": B, "H_q": H_q, "H_kv": H_kv, "D_qk": D_qk, "D_v": D_v, "length": length,
+                     "prefix": prefix, "cache": dtype, "us": us, "attention_GBps": round(byts / us["attention"] / 1e3, 1),
+                     "attention_TFLOPs": round(flop / us["attention"] / 1e6, 1), "max_abs": err, "layout": A.ae_cached_query(plan.handle)})
+        print(f"# {rows[-1]}", file=sys.stderr, flush=True)
+    return rows
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -172,7 +250,10 @@ def main():
     ap.add_argument("--gated", action="store_true",
                     help="time the recurrent pattern with per-token gates (ae_gated_forward; with --backward: ae_gated_backward; gated retention, Mamba2 SSM, "
                          "retention with a constant decay) on Table 2's recurrent shapes; GB/s against the HBM peak")
-    ap.add_argument("--only", default="", help="with --backward: only the shapes whose name contains this")
+    ap.add_argument("--serving", action="store_true",
+                    help="time one decoding step of a layer: rotary positions, append to the paged cache, attention over it, with "
+                         "and without a shared prefix; GB/s against the HBM peak")
+    ap.add_argument("--only", default="", help="with --backward or --serving: only the shapes whose name contains this")
     ap.add_argument("--calib-copy", type=int, default=0, metavar="MiB",
                     help="instead of the benchmark, run a plain device-to-device copy of this many MiB "
                          "(reference reading for the FETCH_SIZE / WRITE_SIZE counters under rocprofv3)")
@@ -196,6 +277,9 @@ def main():
         elif a.gated:
             child, name = ["--gated", "--only", a.only], f"gated_recurrent_{a.only or 'all'}"
             trace_args, pmc_args = ("--steps", "20"), ("--steps", "3")
+        elif a.serving:
+            child, name = ["--serving", "--only", a.only], f"serving_{a.only or 'all'}"
+            trace_args, pmc_args = ("--steps", "20"), ("--steps", "1")
         elif a.recurrent:
             child, name = ["--recurrent", "--only", a.only], f"recurrent_{a.only or 'all'}"
             trace_args, pmc_args = ("--steps", "20"), ("--steps", "3")
@@ -226,6 +310,9 @@ def main():
         return
     if a.calib_mfma > 0:
         print(json.dumps(calib_mfma(A, torch, a.calib_mfma)))
+        return
+    if a.serving:
+        print(json.dumps({"serving": serving_rows(torch, dev, a.steps, a.only), "peak_GBps": 8000.0, "data": "synthetic"}))
         return
     if a.decode:
         # Decoding is bound by reading K and V once: bytes / time against the 8 TB/s HBM peak.

@@ -88,16 +88,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p, const
   const int e1 = INTER ? 2 * VEC * piece : VEC * piece, e2 = INTER ? e1 + VEC : e1 + p.half;
   const int32_t pos = p.positions[b * p.position_stride + l];
   float sn[VEC], cs[VEC];
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) {
-    // the top half of pos * turn (64 bits, modulo 1): pos as an unsigned number, minus 2^32 turns' worth where it is negative
-    const uint64_t f = t.turn[VEC * piece + i];
-    const uint32_t lo = (uint32_t)f;
-    const uint32_t hi = __umulhi((uint32_t)pos, lo) + (uint32_t)pos * (uint32_t)(f >> 32) - (pos < 0 ? lo : 0u);
-    turn_sincos(hi, sn[i], cs[i]);
-    sn[i] *= p.backward ? -p.amp : p.amp;
-    cs[i] *= p.amp;
-  }
+  bool first = true;
   for (; h < h_end; h += kHeads * SIDE) {
     P x1[kHeads], x2[kHeads];
 #pragma unroll
@@ -105,6 +96,19 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p, const
       const T* x = at(h + u * SIDE < h_end ? h + u * SIDE : h, false);
       x1[u] = load_piece<T, VEC>(x + e1);
       x2[u] = load_piece<T, VEC>(x + e2);
+    }
+    if (first) {  // behind the first loads: a call of few rows is a chain of latencies
+      first = false;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        // the top half of pos * turn (64 bits, modulo 1): pos as an unsigned number, minus 2^32 turns' worth where it is negative
+        const uint64_t f = t.turn[VEC * piece + i];
+        const uint32_t lo = (uint32_t)f;
+        const uint32_t hi = __umulhi((uint32_t)pos, lo) + (uint32_t)pos * (uint32_t)(f >> 32) - (pos < 0 ? lo : 0u);
+        turn_sincos(hi, sn[i], cs[i]);
+        sn[i] *= p.backward ? -p.amp : p.amp;
+        cs[i] *= p.amp;
+      }
     }
 #pragma unroll
     for (int u = 0; u < kHeads; ++u) {

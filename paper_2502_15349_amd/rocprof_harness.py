@@ -1,7 +1,7 @@
 """rocprofv3 harness: one command that profiles a bench.py run and reports, per kernel, the launch
 durations, the matrix-pipe (MFMA) busy fraction, the HBM traffic and GB/s, and the flop cross-check.
 
-    python bench.py --profile [--workload NAME | --backward --only S | --recurrent --only S] [--profile-dir DIR]
+    python bench.py --profile [--workload NAME | --backward --only S | --recurrent --only S | --serving --only S] [--profile-dir DIR]
 
 This module never touches the GPU itself: it starts `rocprofv3 ... -- python3 bench.py <args>` child
 processes, one per pass (rocprofv3 does not split counters over passes, and trace and counter collection do
@@ -37,7 +37,7 @@ SQ_COUNTERS = ["SQ_VALU_MFMA_BUSY_CYCLES", "SQ_BUSY_CU_CYCLES", "SQ_INSTS_VALU_M
                "SQ_LDS_BANK_CONFLICT", "SQ_LDS_IDX_ACTIVE", "SQ_INSTS_LDS", "SQ_INSTS_VALU"]
 # kernels of this library (everything else in a trace -- torch's fills and copies -- is listed but not analysed)
 OURS = ("attn_fwd_kernel", "attn_fwd_wide_kernel", "attn_bwd_kernel", "attn_bwd_both_kernel", "attn_bwd_delta_kernel", "attn_decode_kernel", "attn_merge_kernel",
-        "rec_state_kernel", "rec_step_kernel", "rec_scan_kernel", "rec_fused_kernel", "gated_", "calib_mfma_kernel")
+        "cached_attn_kernel", "prefix_attn_kernel", "rotary_kernel", "cache_kernel", "rec_state_kernel", "rec_step_kernel", "rec_scan_kernel", "rec_fused_kernel", "gated_", "calib_mfma_kernel")
 N_XCD, N_SIMD = 8, 1024
 GIB = 1 << 30
 

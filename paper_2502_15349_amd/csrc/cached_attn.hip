@@ -173,11 +173,10 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     row[0] = (((int64_t)(ok0 ? pg0 : 0) * p.H_kv + hk) << p.page_shift) + (j0 & page_mask);
     row[1] = second ? (((int64_t)(ok1 ? pg1 : 0) * p.H_kv + hk) << p.page_shift) + ((j0 + 16) & page_mask) : row[0];
     fetch_pages(i + 1);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < C::NK / 2; ++i)
-        dma16(p.K + row[h] * C::RBK, koff[h * (C::NK / 2) + i], lds0 + (h * (C::NK / 2) + i) * 1024);
+    static_for<0, C::NK>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+      dma16_at<i * 1024>(p.K + row[i / (C::NK / 2)] * C::RBK, koff[i], lds0);
+    });
     if constexpr (C::E4M3) {  // bytes 0..31: exponents of the keys, 32..63: of the values (lanes 16.. repeat them)
       const int k = lane & 15;
       const uint8_t* e = (k & 8 ? p.Ve : p.Ke) + row[(k >> 2) & 1] + 4 * (k & 3);
@@ -186,11 +185,10 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     return (ok0 ? 0 : 1) | (ok1 ? 0 : 2);
   };
   auto issue_v = [&] {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < C::NV / 2; ++i)
-        dma16(p.V + row[h] * C::RBV, voff[h * (C::NV / 2) + i], lds0 + C::K_BYTES + (h * (C::NV / 2) + i) * 1024);
+    static_for<0, C::NV>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+      dma16_at<C::K_BYTES + i * 1024>(p.V + row[i / (C::NV / 2)] * C::RBV, voff[i], lds0);
+    });
   };
 
   // ---- fragments -------------------------------------------------------------------------------------------------------------
@@ -214,6 +212,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     }
   };
 
+  const float c = __builtin_fabsf(p.c);
   int special = 0;  // the wavefront met NaN or infinities in values that only some of the newest tokens see
   f32x4 o[C::RT][C::DB];
   float m[C::RT], l[C::RT];
@@ -273,16 +272,16 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     bf16x8 pb[C::RT];
 #pragma unroll
     for (int rt = 0; rt < C::RT; ++rt) {
-      float x[8];
+      float x[8];  // raw scores; c > 0 (a negative scale's sign is in the queries)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = s[e / 4][rt][e % 4] * p.c;
+      for (int e = 0; e < 8; ++e) x[e] = s[e / 4][rt][e % 4];
       if (masked) {
         const int last = min(lim[rt] - j0 - 8 * hi, there) - 1;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = e <= last ? x[e] : -INFINITY;
       }
       float mx = fmaxf(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]));
-      mx = max3(mx, x[6], x[7]);
+      mx = max3(mx, x[6], x[7]) * c;
       if (__builtin_amdgcn_ballot_w64(mx > m[rt] + kLazyLog2) != 0) {
         mx = fmaxf(max_over_groups(mx), m[rt]);
         const float alpha = mx == -INFINITY ? 1.f : fast_exp2(m[rt] - mx);
@@ -295,7 +294,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        x[e] = fast_exp2(x[e] - ref);
+        x[e] = fast_exp2(__builtin_fmaf(x[e], c, -ref));
         sum += x[e];
       }
       l[rt] += sum;
@@ -360,7 +359,10 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
 #pragma unroll
   for (int rt = 0; rt < C::RT; ++rt)
 #pragma unroll
-    for (int s = 0; s < C::KS; ++s) asm volatile("" ::"v"(qf[rt][s]));  // (awaited here, not inside the loop)
+    for (int s = 0; s < C::KS; ++s) {
+      asm volatile("" ::"v"(qf[rt][s]));  // (awaited here, not inside the loop)
+      if (p.c < 0.f) qf[rt][s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, qf[rt][s]) ^ u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u});
+    }
   auto all_read = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };  // before a copy overwrites what was read
   for (int i = 0; i < n_my; ++i) {
     wait_vmem<C::NV>();

@@ -148,7 +148,7 @@ typedef struct {
   int32_t max_length;     /* 1 .. table_width * page_size: no sequence has more keys of its own */
   int32_t prefix_length;  /* 0: no shared prefix */
   int32_t chunk;          /* 0: the library chooses; else the keys that one workgroup walks, a positive multiple of 128 */
-  float scale;            /* finite and non-zero */
+  float scale;            /* non-zero; scale * log2(e) finite */
   ae_out_dtype_t out_dtype;
   int64_t q_stride[3], o_stride[3]; /* {batch, head, token} */
 } ae_cached_desc_t;

@@ -790,7 +790,7 @@ class RotaryPlan:
         if (not positions.is_cuda or positions.device != Q.device or positions.dtype != torch.int32 or tuple(positions.shape) not in ((L,), (B, L))
                 or (L > 1 and positions.stride(-1) != 1)):
             raise ValueError("positions must be an int32 device tensor [L] or [B, L] with contiguous rows")
-        _no_overlap(Q_out, K_out)
+        self._shared = _expanded(Q_out, K_out), _expanded(Q, K)  # (expanded tensors can be read, not written)
         zero = (0, 0, 0)
         self.handle = ae_rotary_create(
             B=B, H_q=H_q, H_k=0 if K is None else K.shape[1], L=L, D=D, frequencies=freqs, amplitude=amplitude, layout=layout,
@@ -800,17 +800,19 @@ class RotaryPlan:
         self._specs = [None if t is None else _shape_of(t) for t in (Q, K, positions, Q_out, K_out)]
         self.device = Q.device
 
-    def _run(self, call, specs, tensors, stream):
+    def _run(self, call, specs, tensors, shared, stream):
+        if shared:
+            raise ValueError("an output must not be an expanded tensor")
         if [t if t is None else _shape_of(t) for t in tensors] != specs:
             raise ValueError("a tensor differs from the plan's in shape, strides, type or device")
         _enqueue(call, self.device, stream, self.handle, *[0 if t is None else t.data_ptr() for t in tensors])
 
     def forward(self, Q, K, positions, Q_out, K_out, *, stream=None):
-        self._run(ae_rotary_forward, self._specs, (Q, K, positions, Q_out, K_out), stream)
+        self._run(ae_rotary_forward, self._specs, (Q, K, positions, Q_out, K_out), self._shared[0], stream)
 
     def backward(self, dQ_out, dK_out, positions, dQ, dK, *, stream=None):
         s = self._specs
-        self._run(ae_rotary_backward, [s[3], s[4], s[2], s[0], s[1]], (dQ_out, dK_out, positions, dQ, dK), stream)
+        self._run(ae_rotary_backward, [s[3], s[4], s[2], s[0], s[1]], (dQ_out, dK_out, positions, dQ, dK), self._shared[1], stream)
 
     def __del__(self):
         if getattr(self, "handle", None) is not None and _lib is not None:
@@ -818,11 +820,14 @@ class RotaryPlan:
             self.handle = None
 
 
+def _expanded(*tensors):
+    """Whether one of them has two indices at one address."""
+    return any(t is not None and 0 in t.stride() and any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())) for t in tensors)
+
+
 def _no_overlap(*outs):
-    """Outputs that a call writes must not have two indices at one address (expanded tensors)."""
-    for t in outs:
-        if t is not None and 0 in t.stride() and any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
-            raise ValueError("an output must not be an expanded tensor")
+    if _expanded(*outs):
+        raise ValueError("an output must not be an expanded tensor")
 
 
 def _rotary(Q, K, positions, freqs, amplitude, layout, out, stream, backward):
@@ -834,7 +839,6 @@ def _rotary(Q, K, positions, freqs, amplitude, layout, out, stream, backward):
     # the handle's "inputs" are the layout that the backward pass writes
     a, b = ((q, k), (Q, K)) if backward else ((Q, K), (q, k))
     plan = RotaryPlan(a[0], a[1], positions, b[0], b[1], freqs=freqs, amplitude=amplitude, layout=layout)
-    _no_overlap(q, k)
     (plan.backward if backward else plan.forward)(Q, K, positions, q, k, stream=stream)
     return q, k
 
@@ -946,7 +950,8 @@ class CachedAttentionPlan:
     its workspace.  Q [B, H_q, n, D_qk] bf16 and out [B, H_q, n, D_v] (bf16 or fp32) give shapes, strides and device; max_length: no
     sequence has more keys of its own; table_width: pages in a row of the table; prefix_length: keys that all sequences share.
     Calls of one plan must not overlap (they share its workspace, which is prepared on the stream that is current when the plan is
-    made); a captured graph keeps using the plan's buffers."""
+    made: another stream waits for that one before its first call); a captured graph keeps using the plan's buffers, and a plan made
+    while a graph is captured is of use to that graph alone."""
 
     def __init__(self, cache, Q, out, *, max_length, table_width, scale, prefix_length=0, chunk=0):
         import torch

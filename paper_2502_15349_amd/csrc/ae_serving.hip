@@ -347,7 +347,8 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
     return fail(AE_ERR_INVALID_ARG, "ae_cached_create: max_length (%d) must be between 1 and table_width * page_size", d->max_length);
   if (d->prefix_length < 0) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: prefix_length must not be negative");
   if (d->chunk < 0 || d->chunk % 128 != 0) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: chunk must be 0 or a positive multiple of 128");
-  if (!std::isfinite(d->scale) || d->scale == 0.f) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: scale must be finite and non-zero");
+  if (!std::isfinite(d->scale * 1.4426950408889634f) || d->scale == 0.f)
+    return fail(AE_ERR_INVALID_ARG, "ae_cached_create: scale must be finite (its product with log2(e) too) and non-zero");
   if (d->out_dtype != AE_OUT_F32 && d->out_dtype != AE_OUT_BF16) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: unknown out_dtype %d", (int)d->out_dtype);
   const int64_t rows = (int64_t)d->B * d->H_q * d->n_new;
   if (rows > 1 << 24 || d->max_length > 1 << 30 || d->prefix_length > 1 << 30 || d->chunk > 1 << 30)
@@ -389,7 +390,7 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
     h->prefix_apart = lay.apart;
     // (in the own keys' launch: tiles of whole sequences)
     cut_keys(prefix, lay.apart ? ae::kPrefixRows : ae::cached_rows_per_workgroup(prefix.rows) / own.rows * own.rows, lay.prefix_cuts, d->chunk);
-    if (!lay.apart) p.prefix_blocks = (cd.H_kv * prefix.splits + 7) / 8 * 8 * prefix.row_tiles;
+    if (!lay.apart) p.prefix_blocks = (int)(((int64_t)cd.H_kv * prefix.splits + 7) / 8 * 8 * prefix.row_tiles);
     own.slot0 = prefix.splits;
   }
   cut_keys(own, ae::cached_rows_per_workgroup(own.rows), lay.own_cuts, d->chunk);
@@ -398,9 +399,9 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
   h->counter_bytes = h->counted ? round_up((size_t)d->B * cd.H_kv * own.row_tiles * 4) : 0;
   h->o_bytes = round_up((size_t)h->slots * rows * cd.D_v * 4);
   h->ws_bytes = h->slots == 1 ? 0 : h->counter_bytes + h->o_bytes + round_up((size_t)h->slots * rows * 4);
-  if ((double)h->slots * rows * cd.D_v * 4 > 1e12) {
+  if ((double)h->slots * rows * cd.D_v * 4 > 1e11) {  // (and the prefix's workgroups, fewer than partial results of 256 bytes, fit an int)
     delete h;
-    return fail(AE_ERR_UNSUPPORTED, "ae_cached_create: the partial results would take more than 10^12 bytes");
+    return fail(AE_ERR_UNSUPPORTED, "ae_cached_create: the partial results would take more than 10^11 bytes");
   }
   *out = h;
   return AE_OK;

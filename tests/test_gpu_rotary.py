@@ -153,3 +153,20 @@ def test_replayed_graph(A):
         got = qo.clone()
         eager, _ = A.rotary_forward(q, k, pos, freqs=f)
         assert torch.equal(got, eager)
+
+
+def test_expanded_tensors_are_read_and_not_written(A):
+    # a gradient that is the same for every head, as a sum over heads leaves it; and heads that share their input
+    f, amp = A.rotary_frequencies(64, scaling="by_parts", factor=4.0)
+    pos = torch.arange(33, dtype=torch.int32).cuda()
+    one = heads(11, 2, 1, 33, 64, torch.bfloat16, "bhld")
+    many = one.expand(2, 5, 33, 64)
+    for call in (A.rotary_forward, A.rotary_backward):
+        got, _ = call(many, None, pos, freqs=f, amplitude=amp)
+        ref, _ = call(many.contiguous(), None, pos, freqs=f, amplitude=amp)
+        assert torch.equal(got, ref)
+        with pytest.raises(ValueError, match="expanded"):
+            call(many.contiguous(), None, pos, freqs=f, amplitude=amp, out=(many, None))
+    plan = A.RotaryPlan(many, None, pos, torch.empty_like(got), None, freqs=f, amplitude=amp)
+    with pytest.raises(ValueError, match="expanded"):
+        plan.backward(got, None, pos, many, None)

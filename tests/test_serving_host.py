@@ -204,3 +204,11 @@ def test_definition_of_the_quantised_rows():
     import torch  # the 8-bit type's own rounding says the same
     t = torch.from_numpy(x * np.ldexp(1.0, -k)[:, None]).float().to(torch.float8_e4m3fn).view(torch.uint8).numpy()
     assert np.array_equal(t, quantise(torch.from_numpy(x * np.ldexp(1.0, -k)[:, None]).float().double().numpy() * np.ldexp(1.0, k)[:, None])[0])
+
+
+@pytest.mark.parametrize("patch,status", [(dict(scale=3e38), 1), (dict(B=64, prefix_length=1 << 28, chunk=128), 2)])
+def test_cached_limits(A, patch, status):
+    # a scale whose product with log2(e) is infinite; partial results of 2^21 ranges of 512 rows
+    c = A.ae_cache_create(**CACHE)
+    refused(A, status, A.ae_cached_create, c, **{**CACHED, **patch})
+    A.ae_cache_destroy(c)

@@ -390,13 +390,13 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
     h->prefix_apart = lay.apart;
     // (in the own keys' launch: tiles of whole sequences)
     cut_keys(prefix, lay.apart ? ae::kPrefixRows : ae::cached_rows_per_workgroup(prefix.rows) / own.rows * own.rows, lay.prefix_cuts, d->chunk);
-    if (!lay.apart) p.prefix_blocks = (int)(((int64_t)cd.H_kv * prefix.splits + 7) / 8 * 8 * prefix.row_tiles);
+    if (!lay.apart) p.prefix_blocks = (int)ae::dealt_workgroups((int64_t)cd.H_kv * prefix.splits, prefix.row_tiles);
     own.slot0 = prefix.splits;
   }
   cut_keys(own, ae::cached_rows_per_workgroup(own.rows), lay.own_cuts, d->chunk);
   h->slots = own.splits + own.slot0;
   h->counted = own.splits > 1 || p.prefix_blocks > 0;
-  h->counter_bytes = h->counted ? round_up((size_t)d->B * cd.H_kv * own.row_tiles * 4) : 0;
+  h->counter_bytes = h->counted ? round_up((size_t)d->B * cd.H_kv * own.row_tiles * ae::kCounterStride * 4) : 0;
   h->o_bytes = round_up((size_t)h->slots * rows * cd.D_v * 4);
   h->ws_bytes = h->slots == 1 ? 0 : h->counter_bytes + h->o_bytes + round_up((size_t)h->slots * rows * 4);
   if ((double)h->slots * rows * cd.D_v * 4 > 1e11) {  // (and the prefix's workgroups, fewer than partial results of 256 bytes, fit an int)

@@ -255,18 +255,21 @@ void cut_keys(ae::CachedPart& pt, int tile_rows, int64_t cuts, int64_t chunk) {
 
 // How a call is laid out -- wavefronts of a workgroup, ranges of the own keys and of the prefix, the prefix in the own keys' launch
 // or in one of its own -- by an estimate of its time, in microseconds.  With w = (D_qk + D_v) / 256:
-//   * a workgroup takes 5.1 (four wavefronts) or 5.6 (eight) for its start and its end and 0.25 + 0.8 w for each 32 keys of a
-//     wavefront, 0.6 w more with 32 rows; the cache is read at 5.7 TB/s; a launch takes the root of the squares of what its workgroups
-//     take in their turns on the places the chip has for them, of the longest one, and of the reading; the join of partial
-//     results takes 1.8 and a latency of 1 for every four that a thread adds up;
-//   * with a prefix in the launch, two more parts count, and their third powers are added: the wavefronts' work, 1.1 w per 32 keys of
-//     each on 1024 SIMDs, and 0.6 of the prefix's workgroups in whole turns of the compute units;
-//   * a prefix in a launch of its own takes 0.5 + 1.1 w for each 64 keys and 256 rows of a workgroup, 0.37 for every MB of partial results,
-//     and 3.3 for the second launch.
-// Over 4314 random calls (1 to 256 sequences, 1 to 8 new tokens, 64 to 131072 keys, all head dims and types) the choice takes 1.04 times
-// the time of the best one measured for that call (1.12 at the 90th percentile, 1.47 at most); as many ranges as keep all workgroups
-// resident, with four wavefronts, took 1.11 (1.30, 9.0).  Over 4373 calls behind a prefix (2 to 256 sequences, 100 to 32768 keys)
-// 1.04; always a launch of its own 1.19.
+//   * a workgroup takes 5.5 for its start and its end and 0.25 + 0.8 w for each 32 keys of a wavefront, 0.4 w more with 32 rows; the
+//     cache is read at 6.5 TB/s; a launch takes the root of the squares of what its workgroups take in their turns on the places the chip
+//     has for them, of the longest one, and of the reading.  Turns count partly as whole ones (a workgroup that is left over keeps the launch
+//     waiting): 0.8 of them with 32 rows, 0.5 with 16, where more workgroups fit.  The join of partial results takes 1.4 and a latency
+//     of 1 for every four that a thread adds up;
+//   * with a prefix in the launch, third powers are added, of the turns (0.14 of them whole), the reading, 0.85 of the longest workgroup, the
+//     wavefronts' work, 0.6 w per 32 keys of each on 1024 SIMDs, and 0.35 of the prefix's workgroups in whole turns of the compute units;
+//     every MB of the prefix's partial results takes 0.6, the join 6 and 0.45;
+//   * a prefix in a launch of its own takes 3.5 and 0.73 + 0.95 w for each 64 keys and 256 rows of a workgroup, 0.3 for every MB of partial
+//     results, and 3.5 for the second launch.
+// Fitted on 3218 random calls (1 to 256 sequences, 1 to 8 new tokens, 64 to 131072 keys, all head dims and types; keys that no cache
+// holds) and 2178 behind a prefix (2 to 256 sequences, 100 to 32768 keys).  On 612 other calls the choice takes 1.038 times the time of the
+// best layout measured for that call (1.11 at the 90th percentile, 1.55 at most), on 409 behind a prefix 1.041 (1.12, 1.29).  As many ranges
+// as keep all workgroups resident take 1.08 with four wavefronts (1.24, 2.0), 1.11 with eight; the best layout with a launch of its
+// own for the prefix 1.23 (1.65, 2.9).
 struct Layout {
   double us;
   int waves, own_cuts, prefix_cuts;
@@ -277,7 +280,7 @@ Layout choose_layout(const ae_cached_desc_t& d, const ae_cache_desc_t& cd, int g
   // (as they were measured; between them a number of workgroups that does not go into the compute units can cost 15 %)
   static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}, kPrefixCuts[] = {1, 2, 4, 8, 16, 32, 64};
   const bool e4m3 = cd.dtype == AE_CACHE_E4M3;
-  const double width = (cd.D_qk + cd.D_v) / 256.0, key_us = (cd.D_qk + cd.D_v) * (e4m3 ? 1 : 2) / 5.7e6;  // of a k/v head's key
+  const double width = (cd.D_qk + cd.D_v) / 256.0, key_us = (cd.D_qk + cd.D_v) * (e4m3 ? 1 : 2) / 6.5e6;  // of a k/v head's key
   const int own_rows = d.n_new * g, prefix_rows = d.B * own_rows;
   const int own_rpw = std::min(ae::cached_rows_per_workgroup(own_rows), 32), own_tiles = (own_rows + own_rpw - 1) / own_rpw;
   auto join = [&](int rows, double slots) {
@@ -287,14 +290,15 @@ Layout choose_layout(const ae_cached_desc_t& d, const ae_cache_desc_t& cd, int g
   const double own_read = (double)d.B * cd.H_kv * d.max_length * key_us, prefix_read = (double)cd.H_kv * d.prefix_length * key_us;
   Layout best = {1e300, 4, 1, 1, false};
   for (int apart = 0; apart <= (d.prefix_length > 0 ? 1 : 0); ++apart) {
-    // (in one launch with the own keys: tiles of whole sequences, which have to fit; beyond 1024 rows a launch of its own was the
-    // faster by 6 to 15 %)
-    if (d.prefix_length > 0 && !apart && (own_rows > 32 || prefix_rows > 1024)) continue;
+    // (in one launch with the own keys: tiles of whole sequences, which have to fit; not measured beyond 2048 rows)
+    if (d.prefix_length > 0 && !apart && (own_rows > 32 || prefix_rows > 2048)) continue;
     const bool fused = d.prefix_length > 0 && !apart;
     const int fused_rows = fused ? ae::cached_rows_per_workgroup(prefix_rows) / own_rows * own_rows : 0;
     const bool wide = std::max(own_rpw, fused_rows) > 16;
     for (int waves = 4; waves <= 8; waves += 4) {
-      const double start = waves == 4 ? 5.1 : 5.6, step = 0.25 + 0.8 * width + (wide ? 0.6 * width : 0.0);
+      const double start = d.prefix_length > 0 && waves == 8 ? 5.9 : 5.5, step = 0.25 + 0.8 * width + (wide ? 0.4 * width : 0.0);
+      const double whole_part = d.prefix_length > 0 ? 0.14 : wide ? 0.8 : 0.5;
+      auto turns_of = [&](double x) { return (1 - whole_part) * x + whole_part * std::ceil(x - 0.02); };
       const double places = 256.0 * ae::cached_residents(cd.D_qk, cd.D_v, e4m3, wide ? 32 : 16, waves);
       for (int oc : kCuts) {
         if (d.prefix_length > 0 && oc != 1 && oc != 3) continue;
@@ -305,24 +309,27 @@ Layout choose_layout(const ae_cached_desc_t& d, const ae_cache_desc_t& cd, int g
           if (d.prefix_length == 0 && pc > 1) break;
           const double pchunk = std::ceil(std::ceil((double)d.prefix_length / pc) / 128) * 128;
           const double pcuts = d.prefix_length ? std::ceil(d.prefix_length / pchunk) : 0;
+          const double parts = pcuts * prefix_rows * cd.H_kv * (cd.D_v + 4) * 4e-6;  // MB of the prefix's partial results
           double us;
           if (!apart && !fused) {
-            const double turns = groups * walk / places;
-            us = std::sqrt(turns * turns + walk * walk + own_read * own_read) + (cuts > 1 ? 1.8 + join(std::min(own_rows, own_rpw), cuts) : 0.0);
+            const double turns = turns_of(groups / places) * walk;
+            us = std::sqrt(turns * turns + walk * walk + own_read * own_read) + (cuts > 1 ? 1.4 + join(std::min(own_rows, own_rpw), cuts) : 0.0);
           } else if (fused) {
-            const double psteps = std::ceil(std::min(pchunk, (double)d.prefix_length) / (32 * waves)), pwalk = start + psteps * step * 0.83;
+            const double psteps = std::ceil(std::min(pchunk, (double)d.prefix_length) / (32 * waves)), pwalk = start + psteps * step;
             const double pgroups = (double)cd.H_kv * ((prefix_rows + fused_rows - 1) / fused_rows) * pcuts;
-            const double turns = (groups * walk + pgroups * pwalk) / places, longest = std::max(walk, pwalk), read = own_read + prefix_read;
-            const double busy = (groups * steps + pgroups * psteps) * waves * 1.1 * width * (wide ? 1.0 : 0.6) / 1024;
-            const double whole = 0.6 * std::ceil(pgroups / 256 - 0.02) * pwalk;
+            const double turns = turns_of((groups + pgroups) / places) * (groups * walk + pgroups * pwalk) / (groups + pgroups);
+            const double longest = 0.85 * std::max(walk, pwalk), read = own_read + prefix_read;
+            const double busy = (groups * steps + pgroups * psteps) * waves * 0.6 * width / 1024;
+            const double whole = 0.35 * std::ceil(pgroups / 256 - 0.02) * pwalk;
             auto cube = [](double x) { return x * x * x; };
-            us = std::cbrt(cube(turns) + cube(longest) + cube(read) + cube(busy) + cube(whole)) + 2.3 + join(fused_rows, cuts + pcuts);
+            us = std::cbrt(cube(turns) + cube(longest) + cube(read) + cube(busy) + cube(whole)) + 0.6 * parts + 6.0 +
+                 0.45 * join(fused_rows, cuts + pcuts);
           } else {
-            const double wg = 1.0 + std::ceil(std::min(pchunk, (double)d.prefix_length) / 64) * (0.5 + 1.1 * width);
+            const double wg = 3.5 + std::ceil(std::min(pchunk, (double)d.prefix_length) / 64) * (0.73 + 0.95 * width);
             const double wgs = (double)cd.H_kv * ((prefix_rows + ae::kPrefixRows - 1) / ae::kPrefixRows) * pcuts;
-            us = std::max(std::ceil(wgs / 256 - 0.02), 1.0) * wg + 0.37 * pcuts * prefix_rows * cd.H_kv * (cd.D_v + 4) * 4e-6 + 3.3;
-            const double j = cuts > 1 ? 1.8 + join(std::min(own_rows, own_rpw), cuts + pcuts) : (own_rpw > 16 ? 2.0 : 1.0) * std::ceil(pcuts / 4);
-            const double turns = groups * (walk + (cuts > 1 ? 0.0 : j)) / places;
+            us = std::max(std::ceil(wgs / 256 - 0.02), 1.0) * wg + 0.3 * parts + 3.5;
+            const double j = cuts > 1 ? 4.9 + 0.45 * join(std::min(own_rows, own_rpw), cuts + pcuts) : 0.45 * (own_rpw > 16 ? 2.0 : 1.0) * std::ceil(pcuts / 4);
+            const double turns = turns_of(groups / places) * (walk + (cuts > 1 ? 0.0 : j));
             us += std::sqrt(turns * turns + walk * walk + own_read * own_read) + j;
           }
           if (us < best.us) best = {us, waves, oc, pc, apart != 0};

@@ -617,9 +617,11 @@ hipError_t launch_type(const CachedParams& p, bool e4m3, hipStream_t s) {
 }  // namespace
 
 int cached_residents(int dqk, int dv, bool e4m3, int rows, int waves) {
-  const int lds = waves * 32 * (dqk + dv) * (e4m3 ? 1 : 2) + (e4m3 ? waves * 256 : 0);  // (CachedCfg::LDS_BYTES; 8-bit 64/64 a little more)
-  const int waves_eu = rows > 16 ? 2 : waves == 4 ? 3 : e4m3 && dqk + dv <= 256 ? 4 : 2;
-  return std::min(160 * 1024 / lds, 4 * waves_eu / waves);
+  const int d = dqk + dv;
+  const int lds = std::max(waves * 32 * d * (e4m3 ? 1 : 2) + (e4m3 ? waves * 256 : 0), (waves * (16 * (dv + 6) + 1) + (rows > 16 ? 32 : 16) + 1) * 4);
+  // wavefronts of a SIMD, by the registers that the kernels came to (64/64: 92 and 148; 192/128 with four wavefronts, 16 bits: 184)
+  const int simd = d <= 128 ? (rows > 16 ? 3 : 5) : rows > 16 ? 2 : waves == 4 ? (d > 256 && !e4m3 ? 2 : 3) : e4m3 && d <= 256 ? 4 : 3;
+  return std::min(160 * 1024 / lds, 4 * simd / waves);
 }
 
 // (Four row tiles a wavefront, 64 rows, need 512 registers, spills among them, and leave a SIMD one wavefront: 20 x 64/8 heads x 8

@@ -15,7 +15,7 @@
 // the walk needs no barriers; the wavefronts of a workgroup take sub-tiles in turn and their states meet at the end.
 //
 // Bound by the reading of the cache: 64 x 32/8 heads x 20000 keys of 128 + 128, keys that no cache holds: 6.1 TB/s in bf16 (857 us), 5.8 in 8 bits
-// (453 us); 64 x 5000 keys 5.9 and 5.5.  Short calls are a chain of latencies: 1 x 32/8 x 777 takes 8.8 us.
+// (453 us); 64 x 5000 keys 5.9 and 5.5.  Short calls are a chain of latencies: 1 x 32/8 x 777 takes 8.7 us.
 #include "cached_attn.hpp"
 
 #include <algorithm>

@@ -31,7 +31,8 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __
 template <int DQK_, int DV_, bool E4M3_, int RT_, int W_>
 struct CachedCfg {
   static constexpr int DQK = DQK_, DV = DV_, RT = RT_, W = W_, THREADS = 64 * W;
-  // wavefronts per SIMD that the registers leave room for
+  // Wavefronts per SIMD that the compiler is to leave room for.  (Four instead of two at 64/64 with 32 rows, where three fit anyway: eight
+  // registers spill, 11 x 32/8 x 8 tokens x 5260 keys 28 -> 35 us.)
   static constexpr int WAVES_EU = RT == 2 ? 2 : W == 4 ? 3 : E4M3_ && DQK_ + DV_ <= 256 ? 4 : 2;
   static constexpr bool E4M3 = E4M3_;
   static constexpr int ESZ = E4M3 ? 1 : 2, RBK = DQK * ESZ, RBV = DV * ESZ, CPRK = RBK / 16, CPRV = RBV / 16;

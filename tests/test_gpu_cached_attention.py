@@ -400,3 +400,53 @@ def test_negative_scale_of_many_rows(A):
     some = [0, 99, 199]
     rows = [[np.concatenate((listed(x, ptab.tolist(), 500), listed(x, [9], 3)), axis=1) for _ in some] for x in values(c)]
     check(O[some], None, Q[some], *rows, -0.3, "negative scale")
+
+
+@pytest.mark.parametrize("dqk,dv,dtype", [(64, 64, "e4m3"), (128, 128, "bf16"), (192, 128, "bf16")])
+@pytest.mark.parametrize("B,n,prefix,chunk", [(188, 1, 400, 128), (100, 2, 1290, 256), (300, 4, 700, 128)])
+def test_few_ranges_of_many_row_tiles(A, dqk, dv, dtype, B, n, prefix, chunk):
+    # one k/v head: fewer ranges of the prefix than XCDs, with many row tiles each, in the own keys' launch and in one of its own
+    H_q, page = 8, 64
+    pp = -(-prefix // page)
+    n_pages = pp + B + 1
+    c = make(A, 100, n_pages, 1, page, dqk, dv, dtype)
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(101)).to(torch.int32)
+    ptab, t = order[:pp], order[pp: pp + B].view(B, 1)
+    lengths = [n + (5 * b) % (page - n) for b in range(B)]
+    spoil_behind(c, list(t) + [ptab], lengths + [prefix])
+    Q = queries(102, B, H_q, n, dqk)
+    stats = torch.empty(B, H_q, n, device="cuda")
+    L = torch.tensor(lengths, dtype=torch.int32).cuda()
+    O = A.attention_cached(Q, c, t.cuda(), L, scale=dqk ** -0.5, prefix_table=ptab.cuda(), prefix_length=prefix, stats=stats, chunk=chunk)
+    kv = values(c)
+    some = sorted({0, 1, 31, 32, B // 2, B - 2, B - 1})
+    rows = [[np.concatenate((listed(x, ptab.tolist(), prefix), listed(x, t[b].tolist(), lengths[b])), axis=1) for b in some] for x in kv]
+    check(O[some], stats[some], Q[some], *rows, dqk ** -0.5, f"{B} x 8/1 x {n} behind {prefix}, {dqk}/{dv} {dtype}")
+    # every row was written, and the layout that the library chooses gives the same within both sides' roundings
+    O2 = A.attention_cached(Q, c, t.cuda(), L, scale=dqk ** -0.5, prefix_table=ptab.cuda(), prefix_length=prefix)
+    top = float(max(np.nanmax(np.abs(np.where(np.isfinite(x), x, np.nan))) for x in kv[1:]))
+    assert (O - O2).abs().max() <= 2 * (2.0 ** -8 + 4e-5) * top
+
+
+def test_one_handle_on_two_streams_at_once(A):
+    # handles are immutable: calls that share one, with a workspace each, may overlap
+    lengths, page = [3000, 2000, 2500], 64
+    c = make(A, 110, 128, 4, page, 128, 128, "bf16")
+    t, L = tables_for(111, 128, lengths, page, 47).cuda(), torch.tensor(lengths, dtype=torch.int32).cuda()
+    Q = [queries(112 + i, 3, 16, 2, 128).contiguous() for i in range(2)]
+    h = A.ae_cached_create(c.handle, B=3, H_q=16, n_new=2, table_width=47, max_length=3000, scale=0.09)
+    size = A.ae_cached_workspace_bytes(h)
+    assert size > 0
+    ws, O = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2)], [torch.empty(3, 16, 2, 128, device="cuda") for _ in range(2)]
+    ref = [A.attention_cached(q, c, t, L, scale=0.09, max_length=3000) for q in Q]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for w, s in zip(ws, streams):
+        A.ae_cached_init_workspace(h, w.data_ptr(), size, s.cuda_stream)
+    for _ in range(20):
+        for q, w, o, s in zip(Q, ws, O, streams):
+            A.ae_cached_forward(h, q.data_ptr(), *c.pointers(), t.data_ptr(), L.data_ptr(), 0, o.data_ptr(), 0, w.data_ptr(), size, s.cuda_stream)
+    torch.cuda.synchronize()
+    A.ae_cached_destroy(h)
+    for o, r in zip(O, ref):
+        assert torch.equal(o, r)

@@ -137,6 +137,7 @@ ae_status_t ae_cache_destroy(ae_cache_t *h); /* NULL is allowed */
  *              call that uses it (it clears counters, which every call leaves clear), and again
  *              after anything else has written there, another handle's calls included.
  *              Calls sharing it must not overlap.
+ * At most 2^24 query rows, 2^30 keys a list, and 10^11 bytes of partial results (AE_ERR_UNSUPPORTED beyond).
  * lengths are read on the device: one outside [0, max_length] counts as the nearer
  * bound.  A page number outside [0, n_pages) is not followed: its keys count as hidden.
  * What lies in the cache behind a sequence's end may be anything, NaN included.

@@ -21,6 +21,11 @@
 extern "C" {
 #endif
 
+/* Strides {0, 0, 0} mean contiguous, here as in ae_attn.h.  {AE_ONE_ROW, 0, 0} says that they really are 0: every row of the
+ * tensor is the one at its pointer (a vector expanded over batch, heads and rows).  For tensors that are read; an output is
+ * refused with it. */
+#define AE_ONE_ROW INT64_MIN
+
 /* ---- Rotary positions -----------------------------------------------------
  * Every pair (x1, x2) of a row's first rot_dim elements is turned by the angle
  * of its frequency at the row's position p, and stretched:
@@ -41,8 +46,8 @@ extern "C" {
  *              [b * position_stride + l] (stride 0: shared by the batch);
  *   outputs    same shapes and type; an output may be its own input (same
  *              pointer and strides), and must not overlap anything else.
- * Strides are in elements, {batch, head, row}, all 0 meaning contiguous; the last
- * dimension is contiguous.  Any alignment of at least the element's own is
+ * Strides are in elements, {batch, head, row}, all 0 meaning contiguous, AE_ONE_ROW
+ * and two 0 one row for all; the last dimension is contiguous.  Any alignment of at least the element's own is
  * taken; 16-byte aligned rows and pieces (pointers, strides, rot_dim / 2 and D -
  * rot_dim whole multiples of 16 bytes) run the wide kernel.                  */
 typedef struct ae_rotary ae_rotary_t;
@@ -57,7 +62,7 @@ typedef struct {
   ae_rows_dtype_t dtype;
   const double *frequencies; /* host, rot_dim / 2 values of magnitude <= 6 (radians a position), copied by create */
   double amplitude;          /* finite */
-  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3]; /* >= 0 */
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3]; /* >= 0, or AE_ONE_ROW, 0, 0 */
   int64_t position_stride;   /* >= 0 */
 } ae_rotary_desc_t;
 
@@ -91,7 +96,7 @@ ae_status_t ae_rotary_destroy(ae_rotary_t *h); /* NULL is allowed */
  * ae_cache_read is the way back: rows of K and V from those slots, as bfloat16;
  * zeros for a slot outside the range.  Reading the same slot more than once is fine.
  * K, V: device, 16-byte aligned, strides {batch, head, row} in elements, each a multiple of 8
- * (all 0: contiguous).  slots: device, int32.                                */
+ * (all 0: contiguous; AE_ONE_ROW, 0, 0: one row, for append).  slots: device, int32.                                */
 typedef struct ae_cache ae_cache_t;
 typedef enum { AE_CACHE_BF16 = 0, AE_CACHE_E4M3 = 1 } ae_cache_dtype_t;
 typedef struct {
@@ -126,7 +131,7 @@ ae_status_t ae_cache_destroy(ae_cache_t *h); /* NULL is allowed */
  * all sequences together instead of once for each; the result is that of the
  * concatenated key lists.
  *
- *   Q          device, bf16 [B, H_q, n_new, D_qk], 16-byte aligned, strides multiples of 8;
+ *   Q          device, bf16 [B, H_q, n_new, D_qk], 16-byte aligned, strides multiples of 8 (AE_ONE_ROW, 0, 0: one row);
  *   table      device, int32 [B, table_width]; lengths  device, int32 [B];
  *   prefix_table  device, int32, ceil(prefix_length / page_size) entries; NULL without a prefix;
  *   O          device, [B, H_q, n_new, D_v], fp32 or (desc.out_dtype) bf16, 16-byte aligned,

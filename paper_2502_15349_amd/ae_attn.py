@@ -741,6 +741,16 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, scaling="none", f
     raise ValueError(f"unknown scaling {scaling!r}")
 
 
+ONE_ROW = -2 ** 63  # AE_ONE_ROW
+
+
+def _row_strides(t):
+    """Element strides {batch, head, row} as the C ABI takes them, where three zeros mean contiguous: a tensor whose rows are all one
+    (expanded from a vector) says so."""
+    s = t.stride()[:3]
+    return s if any(s) or t.shape[0] * t.shape[1] * t.shape[2] <= 1 else (ONE_ROW, 0, 0)
+
+
 def _shape_of(t):
     return (t.shape, t.stride(), t.dtype, t.device)
 
@@ -794,8 +804,8 @@ class RotaryPlan:
         zero = (0, 0, 0)
         self.handle = ae_rotary_create(
             B=B, H_q=H_q, H_k=0 if K is None else K.shape[1], L=L, D=D, frequencies=freqs, amplitude=amplitude, layout=layout,
-            dtype="f32" if Q.dtype == torch.float32 else "bf16", q_stride=Q.stride()[:3], k_stride=zero if K is None else K.stride()[:3],
-            q_out_stride=Q_out.stride()[:3], k_out_stride=zero if K is None else K_out.stride()[:3],
+            dtype="f32" if Q.dtype == torch.float32 else "bf16", q_stride=_row_strides(Q), k_stride=zero if K is None else _row_strides(K),
+            q_out_stride=_row_strides(Q_out), k_out_stride=zero if K is None else _row_strides(K_out),
             position_stride=positions.stride(0) if positions.dim() == 2 else 0)
         self._specs = [None if t is None else _shape_of(t) for t in (Q, K, positions, Q_out, K_out)]
         self.device = Q.device
@@ -912,7 +922,7 @@ class PagedCache:
             st = t.stride()
             if t.dtype != self._bf16 or t.shape != (B, self.H_kv, L, d) or st[3] != 1 or t.device != self.device:
                 raise ValueError("K and V must be bf16 [B, H_kv, L, D] on the cache's device with a contiguous last dimension")
-            strides.append(st[:3])
+            strides.append(st[:3] if any(st[:3]) else _row_strides(t))
         return strides
 
     def append(self, K, V, slots, *, stream=None):
@@ -968,7 +978,7 @@ class CachedAttentionPlan:
         _no_overlap(out)
         self.handle = ae_cached_create(cache.handle, B=B, H_q=H_q, n_new=n, table_width=table_width, max_length=max_length, scale=scale,
                                        prefix_length=prefix_length, chunk=chunk, out_dtype="bf16" if out.dtype == torch.bfloat16 else "f32",
-                                       q_stride=Q.stride()[:3], o_stride=out.stride()[:3])
+                                       q_stride=_row_strides(Q), o_stride=_row_strides(out))
         self.cache, self.device, self.shape, self._f32 = cache, Q.device, (B, H_q, n), torch.float32
         self._q, self._o = _shape_of(Q), _shape_of(out)
         self._table, self._prefix = (B, table_width), -(-prefix_length // cache.page_size)

@@ -15,14 +15,20 @@ using ae::fail;
 
 namespace {
 
+// (all three are 0 afterwards exactly where every row is the same one)
 void contiguous_or(int64_t dst[3], const int64_t src[3], int64_t H, int64_t L, int64_t D) {
   const bool none = !src || (src[0] == 0 && src[1] == 0 && src[2] == 0);
+  if (!none && src[0] == AE_ONE_ROW && src[1] == 0 && src[2] == 0) {
+    dst[0] = dst[1] = dst[2] = 0;
+    return;
+  }
   dst[0] = none ? H * L * D : src[0];
   dst[1] = none ? L * D : src[1];
   dst[2] = none ? D : src[2];
 }
 
 bool negative(const int64_t s[3]) { return s[0] < 0 || s[1] < 0 || s[2] < 0; }
+bool one_row(const int64_t s[3]) { return s[0] == 0 && s[1] == 0 && s[2] == 0; }  // (of filled-in strides)
 
 ae_status_t launched(hipError_t e, const char* who) {
   if (e == hipSuccess) return AE_OK;
@@ -54,17 +60,20 @@ ae_status_t ae_rotary_create(const ae_rotary_desc_t* d, ae_rotary_t** out) {
   if (!std::isfinite(d->amplitude) || std::fabs(d->amplitude) > 1e30) return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: amplitude must be finite (at most 1e30)");
   for (int i = 0; i < d->rot_dim / 2; ++i)
     if (!(std::fabs(d->frequencies[i]) <= 6.0)) return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: frequencies[%d] must be finite and at most 6 in magnitude", i);
-  if (negative(d->q_stride) || negative(d->k_stride) || negative(d->q_out_stride) || negative(d->k_out_stride) || d->position_stride < 0)
-    return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: strides must not be negative");
   if (d->D > 1024 || (int64_t)d->H_q + d->H_k > 65535 || (int64_t)d->B * d->L > 0x7fffffffLL)
     return fail(AE_ERR_UNSUPPORTED, "ae_rotary_create: at most 1024 elements a row, 65535 heads and 2^31 - 1 rows");
+  int64_t xs[2][3], ys[2][3];
+  contiguous_or(xs[0], d->q_stride, d->H_q, d->L, d->D);
+  contiguous_or(xs[1], d->k_stride, d->H_k, d->L, d->D);
+  contiguous_or(ys[0], d->q_out_stride, d->H_q, d->L, d->D);
+  contiguous_or(ys[1], d->k_out_stride, d->H_k, d->L, d->D);
+  if (negative(xs[0]) || negative(xs[1]) || negative(ys[0]) || negative(ys[1]) || d->position_stride < 0)
+    return fail(AE_ERR_INVALID_ARG, "ae_rotary_create: strides must not be negative");
   ae_rotary* h = new (std::nothrow) ae_rotary();
   if (!h) return fail(AE_ERR_NOMEM, "ae_rotary_create: out of host memory");
   ae::RotaryParams& p = h->params;
-  contiguous_or(p.xs[0], d->q_stride, d->H_q, d->L, d->D);
-  contiguous_or(p.xs[1], d->k_stride, d->H_k, d->L, d->D);
-  contiguous_or(p.ys[0], d->q_out_stride, d->H_q, d->L, d->D);
-  contiguous_or(p.ys[1], d->k_out_stride, d->H_k, d->L, d->D);
+  std::copy(&xs[0][0], &xs[0][0] + 6, &p.xs[0][0]);
+  std::copy(&ys[0][0], &ys[0][0] + 6, &p.ys[0][0]);
   p.position_stride = d->position_stride;
   p.B = d->B;
   p.L = d->L;
@@ -109,6 +118,7 @@ static ae_status_t rotary_impl(const ae_rotary_t* h, const void* q, const void* 
   for (int w = 0; w < 2; ++w) {
     const void* x = w ? k : q;
     const void* y = w ? ko : qo;
+    if (y && one_row(p.ys[w]) && (int64_t)p.B * p.H[w] * p.L > 1) return fail(AE_ERR_INVALID_ARG, "%s: an output cannot have one row for all", who);
     if (x && x == y)
       for (int a = 0; a < 3; ++a)
         if (p.xs[w][a] != p.ys[w][a]) return fail(AE_ERR_INVALID_ARG, "%s: in place needs equal strides", who);
@@ -192,6 +202,7 @@ static ae_status_t cache_impl(const ae_cache_t* h, const void* K, const int64_t*
   for (int w = 0; w < 2; ++w)
     for (int a = 0; a < 3; ++a)
       if (p.xs[w][a] < 0 || p.xs[w][a] % 8 != 0) return fail(AE_ERR_INVALID_ARG, "%s: strides must be non-negative multiples of 8 elements", who);
+  if (!append && (int64_t)B * d.H_kv * L > 1 && (one_row(p.xs[0]) || one_row(p.xs[1]))) return fail(AE_ERR_INVALID_ARG, "%s: an output cannot have one row for all", who);
   p.slots = slots;
   p.slot_stride = slot_stride;
   p.B = B;
@@ -372,6 +383,10 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
       delete h;
       return fail(AE_ERR_INVALID_ARG, "ae_cached_create: strides must be non-negative multiples of 8 elements");
     }
+  if (rows > 1 && one_row(p.os)) {
+    delete h;
+    return fail(AE_ERR_INVALID_ARG, "ae_cached_create: an output cannot have one row for all");
+  }
   p.B = d->B;
   p.H_q = d->H_q;
   p.H_kv = cd.H_kv;

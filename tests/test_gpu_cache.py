@@ -138,3 +138,20 @@ def test_large_cache(A):
     ko, vo = c.read(slots)
     assert torch.equal(ko, k) and torch.equal(vo, v)
     assert torch.equal(c.k[n_pages - 1, :, 255], k[0, :, 0]) and torch.equal(c.v[33000, :, 0], v[0, :, 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_one_row_for_all_slots(A, dtype):
+    # a vector expanded over batch, heads and rows, as slots are cleared
+    c = filled(A, 5, 3, 16, 192, 128, dtype)
+    slots = some_slots(16, 5 * 16, 2, 21)
+    k, v = rows(17, 1, 1, 1, 192).view(192).expand(2, 3, 21, 192), torch.zeros(128, dtype=torch.bfloat16).cuda().expand(2, 3, 21, 128)
+    c.append(k, v, slots)
+    ko, vo = c.read(slots)
+    assert (vo == 0).all() and torch.equal(ko, ko[:1, :1, :1].expand_as(ko).contiguous())
+    step = 0.0 if dtype == "bf16" else 2.0 ** -4  # of the value, or of the smallest normal number, below 2^-13 of the row's largest
+    assert ((ko.float() - k.float()).abs() <= step * k.float().abs().clamp(min=2.0 ** -13 * float(k.float().abs().max()))).all()
+    other = torch.ones(5 * 16, dtype=torch.bool)
+    other[slots.cpu().long().flatten()] = False
+    for t in (c.k, c.v):
+        assert (t.view(torch.uint8).transpose(1, 2).reshape(80, -1).cpu()[other] == 0x35).all()

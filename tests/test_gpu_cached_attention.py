@@ -450,3 +450,19 @@ def test_one_handle_on_two_streams_at_once(A):
     A.ae_cached_destroy(h)
     for o, r in zip(O, ref):
         assert torch.equal(o, r)
+
+
+@pytest.mark.parametrize("B,n,prefix,launches", [(3, 2, 0, 1), (3, 2, 70, 1), (2, 17, 70, 2)])
+def test_one_row_of_queries_for_all(A, B, n, prefix, launches):
+    page, width = 16, 4
+    c = make(A, 120, B * width + 5, 2, page, 64, 64, "bf16")
+    t = torch.arange(B * width, dtype=torch.int32).view(B, width).cuda()
+    L = torch.tensor([60, 33, 47][:B], dtype=torch.int32).cuda()
+    kw = dict(prefix_length=prefix) if prefix else {}
+    tables = dict(prefix_table=(B * width + torch.arange(5, dtype=torch.int32)).cuda()) if prefix else {}
+    Q = queries(121, 1, 1, 1, 64).view(64).expand(B, 4, n, 64)
+    out = torch.empty(B, 4, n, 64, device="cuda")
+    plan = A.CachedAttentionPlan(c, Q, out, max_length=64, table_width=width, scale=0.125, **kw)
+    assert A.ae_cached_query(plan.handle)["launches"] == launches
+    plan.forward(Q, t, L, out, **tables)
+    assert torch.equal(out, A.attention_cached(Q.contiguous(), c, t, L, scale=0.125, **kw, **tables))

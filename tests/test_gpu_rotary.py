@@ -170,3 +170,19 @@ def test_expanded_tensors_are_read_and_not_written(A):
     plan = A.RotaryPlan(many, None, pos, torch.empty_like(got), None, freqs=f, amplitude=amp)
     with pytest.raises(ValueError, match="expanded"):
         plan.backward(got, None, pos, many, None)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_one_row_for_all(A, dtype):
+    # a vector expanded over batch, heads and rows: a gradient that is the same everywhere, as a sum over all rows leaves it
+    f, amp = A.rotary_frequencies(64, scaling="by_parts", factor=4.0)
+    pos = torch.arange(33, dtype=torch.int32).cuda() + 5
+    row = torch.randn(80, generator=torch.Generator().manual_seed(15)).to(dtype).cuda()
+    many, other = row.expand(2, 5, 33, 80), (row + 1).expand(3, 3, 33, 80)[:2, :1]  # (a size of one with a stride of zero)
+    for call, backward in ((A.rotary_forward, False), (A.rotary_backward, True)):
+        got = call(many, other, pos, freqs=f, amplitude=amp)
+        ref = call(many.contiguous(), other.contiguous(), pos, freqs=f, amplitude=amp)
+        assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+        check(got[0], many, pos, f, amp, "half", backward)
+        with pytest.raises(ValueError, match="expanded"):
+            call(many.contiguous(), None, pos, freqs=f, amplitude=amp, out=(many, None))

@@ -212,3 +212,86 @@ def test_cached_limits(A, patch, status):
     c = A.ae_cache_create(**CACHE)
     refused(A, status, A.ae_cached_create, c, **{**CACHED, **patch})
     A.ae_cache_destroy(c)
+
+
+class OnDevice:
+    """A host tensor that says it is on the device: the checks and the strides of a plan can be looked at without one."""
+    is_cuda = True
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def offsets(strides, shape):
+    """Element offset of every row of [B, H, L, D]."""
+    B, H, L, _ = shape
+    return [b * strides[0] + h * strides[1] + l * strides[2] for b in range(B) for h in range(H) for l in range(L)]
+
+
+def offsets_in_c(strides, shape):
+    """The same as the C ABI takes the strides."""
+    s, (_, H, L, D) = [int(x) for x in strides], shape
+    return offsets([H * L * D, L * D, D] if s == [0, 0, 0] else [0, 0, 0] if s == [-2 ** 63, 0, 0] else s, shape)
+
+
+def expanded_rows(D, dtype):
+    """Tensors with every combination of expanded dimensions, sizes of one among them."""
+    import itertools
+
+    import torch
+    for B, H, L in ((2, 4, 10), (1, 4, 10), (2, 1, 10), (2, 4, 1), (1, 1, 10), (1, 1, 1)):
+        for kept in itertools.product((False, True), repeat=3):
+            yield torch.zeros(*[n if k else 1 for n, k in zip((B, H, L), kept)], D, dtype=dtype).expand(B, H, L, D)
+        yield torch.zeros(D, dtype=dtype).expand(3, 5, 11, D)[:B, :H, :L]  # (sizes of one with a stride of zero)
+
+
+def test_rows_are_where_the_tensor_has_them(A, monkeypatch):
+    import torch
+    calls = []
+
+    def note(name, keep):
+        real = getattr(A, name)
+
+        def call(*a, **kw):
+            calls.append(keep(a, kw))
+            return real(*a, **kw)
+
+        monkeypatch.setattr(A, name, call)
+
+    note("ae_rotary_create", lambda a, kw: (kw["q_stride"], kw["k_stride"]))
+    note("ae_cached_create", lambda a, kw: (kw["q_stride"],))
+    pos = OnDevice(torch.zeros(10, dtype=torch.int32))
+    for t in expanded_rows(64, torch.bfloat16):
+        want, (B, H, L, D) = offsets(t.stride(), t.shape), t.shape
+        x, out = OnDevice(t), OnDevice(torch.zeros(t.shape, dtype=t.dtype))
+        A.RotaryPlan(x, x, OnDevice(pos.t[:L]), out, out, freqs=[1.0] * 32)
+        for s in calls.pop():
+            assert offsets_in_c(s, t.shape) == want, (t.shape, t.stride())
+        # (a plan whose call needs no workspace, hence no device: one range of keys)
+        cache = A.PagedCache(OnDevice(torch.zeros(4, H, 16, 64, dtype=torch.bfloat16)), OnDevice(torch.zeros(4, H, 16, 64, dtype=torch.bfloat16)))
+        A.CachedAttentionPlan(cache, x, out, max_length=64, table_width=4, scale=1.0)
+        assert offsets_in_c(calls.pop()[0], t.shape) == want, (t.shape, t.stride())
+        assert all(offsets_in_c(s, t.shape) == want for s in cache._rows(t, t, B, L)), (t.shape, t.stride())
+    assert not calls
+
+
+def test_one_row_for_all_is_read_only(A):
+    one, p = (A.ONE_ROW, 0, 0), 1 << 20
+    for bad in ((A.ONE_ROW, 64, 0), (A.ONE_ROW, 0, 64), (0, A.ONE_ROW, 0), (64, 0, A.ONE_ROW)):
+        refused(A, 1, A.ae_rotary_create, **ROT, q_stride=bad)
+        refused(A, 1, A.ae_rotary_create, **ROT, k_out_stride=bad)
+    for name, forward in (("q_stride", True), ("k_stride", True), ("q_out_stride", False), ("k_out_stride", False)):
+        h = A.ae_rotary_create(**ROT, **{name: one})
+        refused(A, 1, A.ae_rotary_backward if forward else A.ae_rotary_forward, h, p, 2 * p, 3 * p, 4 * p, 5 * p)
+        A.ae_rotary_destroy(h)
+    h = A.ae_cache_create(**CACHE)
+    refused(A, 1, A.ae_cache_read, h, 4 * p, 5 * p, 0, 0, 1, 4, 3 * p, 0, p, one, 2 * p, (0, 0, 0))
+    refused(A, 1, A.ae_cache_read, h, 4 * p, 5 * p, 0, 0, 1, 4, 3 * p, 0, p, (0, 0, 0), 2 * p, one)
+    refused(A, 1, A.ae_cache_append, h, p, (A.ONE_ROW, 8, 8), 2 * p, one, 1, 4, 3 * p, 0, 4 * p, 5 * p)
+    A.ae_cached_destroy(A.ae_cached_create(h, **CACHED, q_stride=one))
+    refused(A, 1, A.ae_cached_create, h, **CACHED, o_stride=one)
+    refused(A, 1, A.ae_cached_create, h, **CACHED, q_stride=(A.ONE_ROW, 128, 128))
+    A.ae_cache_destroy(h)

@@ -324,6 +324,7 @@ def attention_forward(Q, K, V, *, scale, score_mod="none", bias=0.0, gamma=None,
         out = torch.empty((B, H_q, L_q, D_v), dtype=out_dtype or torch.float32, device=Q.device)
     if out.dtype not in (torch.float32, torch.bfloat16) or out.stride(3) != 1:
         raise ValueError("O must be fp32 or bf16 with a contiguous last dimension")
+    _rows_apart(Q, K, V, out)
     h = ae_attn_create(B=B, H_q=H_q, H_kv=H_kv, L_q=L_q, L_k=L_k, D_qk=D_qk, D_v=D_v, scale=scale,
                        score_mod=score_mod, bias=bias, gamma=gamma, norm=norm, mask=mask,
                        q_stride=Q.stride()[:3], k_stride=K.stride()[:3], v_stride=V.stride()[:3],
@@ -357,6 +358,13 @@ def attention_forward(Q, K, V, *, scale, score_mod="none", bias=0.0, gamma=None,
     return out
 
 
+def _rows_apart(*tensors):
+    """Strides of zero in batch, head and row mean contiguous to the C ABI: a vector expanded over all three must not reach it."""
+    for t in tensors:
+        if not any(t.stride()[:3]) and t.shape[0] * t.shape[1] * t.shape[2] > 1:
+            raise ValueError("Q, K, V and O must not be a vector expanded over batch, heads and rows; make a contiguous copy")
+
+
 def _bias_strides(bias_tensor, B, H_q, L_q, L_k):
     """Element strides {batch, head, row} of a bias tensor [B or 1, H_q or 1, L_q, L_k]; a dimension of size 1 is
     shared (stride 0)."""
@@ -367,7 +375,11 @@ def _bias_strides(bias_tensor, B, H_q, L_q, L_k):
     if (t.dtype != torch.bfloat16 or t.dim() != 4 or t.shape[0] not in (1, B) or t.shape[1] not in (1, H_q)
             or tuple(t.shape[2:]) != (L_q, L_k) or t.stride(3) != 1 or not t.is_cuda):
         raise ValueError("bias_tensor must be a bf16 device tensor [B or 1, H_q or 1, L_q, L_k] with a contiguous last dimension")
-    return (0 if t.shape[0] == 1 else t.stride(0), 0 if t.shape[1] == 1 else t.stride(1), t.stride(2))
+    if L_q > 1 and t.stride(2) == 0:
+        raise ValueError("the rows of bias_tensor must not be expanded; make a contiguous copy")
+    # (a single row's stride is not looked at, but three zeros would mean contiguous)
+    row = t.stride(2) or -(-L_k // 8) * 8
+    return (0 if t.shape[0] == 1 else t.stride(0), 0 if t.shape[1] == 1 else t.stride(1), row)
 
 
 def attention_backward(Q, K, V, O, dO, stats, *, scale, score_mod="none", bias=0.0, gamma=None, norm="softmax",
@@ -386,6 +398,7 @@ def attention_backward(Q, K, V, O, dO, stats, *, scale, score_mod="none", bias=0
         raise ValueError("dO must be a contiguous bf16 tensor [B, H_q, L_q, D_v]")
     if stats is not None and (stats.dtype != torch.float32 or tuple(stats.shape) != (B, H_q, L_q) or not stats.is_contiguous()):
         raise ValueError("stats must be a contiguous fp32 tensor [B, H_q, L_q]")
+    _rows_apart(Q, K, V, *(() if O is None else (O,)))
     o_dtype, o_stride = ("f32", (0, 0, 0)) if O is None else ("bf16" if O.dtype == torch.bfloat16 else "f32", O.stride()[:3])
     h = ae_attn_create(B=B, H_q=H_q, H_kv=H_kv, L_q=L_q, L_k=L_k, D_qk=D_qk, D_v=D_v, scale=scale,
                        score_mod=score_mod, bias=bias, gamma=gamma, norm=norm, mask=mask, q_stride=Q.stride()[:3],

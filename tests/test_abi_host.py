@@ -502,3 +502,42 @@ def test_recurrent_segments(H, L, chunk, segments):
         want = max(want, slots * 128 * 128 * 4 + (slots * 4 + 255) // 256 * 256)
     assert A.ae_recurrent_workspace_bytes(h) == want
     A.ae_recurrent_destroy(h)
+
+
+class OnDevice:
+    """A host tensor that says it is on the device: a call's checks can be looked at without one."""
+    is_cuda = True
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+@pytest.mark.parametrize("which", ["Q", "K", "V", "O"])
+def test_vectors_expanded_over_all_rows_are_refused(which):
+    """Three strides of zero mean contiguous to the C ABI: the call would read (or write) a whole tensor behind the vector."""
+    import torch
+    from paper_2502_15349_amd import ae_attn as A
+    t = {n: torch.zeros(2, 4, 10, 64, dtype=torch.bfloat16) for n in "QKVO"}
+    t[which] = torch.zeros(64, dtype=torch.bfloat16).expand(2, 4, 10, 64)
+    Q, K, V, O = (OnDevice(t[n]) for n in "QKVO")
+    with pytest.raises(ValueError, match="expanded"):
+        A.attention_forward(Q, K, V, scale=0.1, out=O)
+    with pytest.raises(ValueError, match="expanded"):
+        A.attention_backward(Q, K, V, O, OnDevice(torch.zeros(2, 4, 10, 64, dtype=torch.bfloat16)), torch.zeros(2, 4, 10), scale=0.1)
+
+
+def test_strides_of_a_bias_tensor():
+    import torch
+    from paper_2502_15349_amd import ae_attn as A
+    strides = lambda t, L_q=10: A._bias_strides(OnDevice(t), 2, 4, L_q, 24)
+    whole = torch.zeros(2, 4, 10, 24, dtype=torch.bfloat16)
+    assert strides(whole) == (960, 240, 24) and strides(whole[:1]) == (0, 240, 24) and strides(whole[:1, :1]) == (0, 0, 24)
+    assert strides(whole[0, 0].expand(2, 4, 10, 24)) == (0, 0, 24)
+    for rows in (whole[0, 0, 0].expand(1, 1, 10, 24), whole[0, 0, 0].expand(2, 4, 10, 24), whole[:, :, :1].expand(2, 4, 10, 24)):
+        with pytest.raises(ValueError, match="expanded"):
+            strides(rows)
+    # one query row for all: not contiguous, which three zeros would mean
+    assert strides(whole[0, 0, 0].expand(2, 4, 7, 24)[:, :, :1], 1) == (0, 0, 24)

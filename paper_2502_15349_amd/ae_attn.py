@@ -8,6 +8,7 @@ Importing this module fails if the library has not been built
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -754,6 +755,16 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, scaling="none", f
     raise ValueError(f"unknown scaling {scaling!r}")
 
 
+def _memory_of(stream):
+    """What a call allocates belongs to the stream that it writes on: memory of another one may still be in use there, or be given away
+    there while this one writes it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+
+    return torch.cuda.stream(stream)
+
+
 ONE_ROW = -2 ** 63  # AE_ONE_ROW
 
 
@@ -857,7 +868,8 @@ def _rotary(Q, K, positions, freqs, amplitude, layout, out, stream, backward):
     import torch
 
     if out is None:
-        out = (torch.empty(Q.shape, dtype=Q.dtype, device=Q.device), None if K is None else torch.empty(K.shape, dtype=K.dtype, device=K.device))
+        with _memory_of(stream):
+            out = (torch.empty(Q.shape, dtype=Q.dtype, device=Q.device), None if K is None else torch.empty(K.shape, dtype=K.dtype, device=K.device))
     q, k = out
     # the handle's "inputs" are the layout that the backward pass writes
     a, b = ((q, k), (Q, K)) if backward else ((Q, K), (q, k))
@@ -870,7 +882,8 @@ def rotary_forward(Q, K, positions, *, freqs, amplitude=1.0, layout="half", out=
     """Rotary positions on device tensors Q [B, H_q, L, D] and K [B, H_k, L, D] (or None), bf16 or fp32, last dimension contiguous:
     pair i of a row at position p is turned by p freqs[i] and stretched by amplitude (rotary_frequencies() makes both); elements from
     2 len(freqs) on are copied.  layout "half" pairs element i with i + len(freqs), "interleaved" 2 i with 2 i + 1.  positions: int32
-    [L] or [B, L].  out: a pair of output tensors (the inputs themselves: in place).  Returns (Q', K')."""
+    [L] or [B, L].  out: a pair of output tensors (the inputs themselves: in place).  Returns (Q', K'); what is allocated for them belongs
+    to the stream that the call is on (stream, else the current one)."""
     return _rotary(Q, K, positions, freqs, amplitude, layout, out, stream, False)
 
 
@@ -948,12 +961,13 @@ class PagedCache:
 
     def read(self, slots, *, out=None, stream=None):
         """The rows at slots int32 [B, L] (or [L]: B = 1) as bf16 K [B, H_kv, L, D_qk] and V [B, H_kv, L, D_v]; zeros for a slot outside the
-        cache.  out: a pair of tensors to write to."""
+        cache.  out: a pair of tensors to write to (else they are allocated, on the stream that the call is on)."""
         import torch
 
         B, L = (1, slots.shape[0]) if slots.dim() == 1 else slots.shape
         if out is None:
-            out = tuple([torch.empty((B, self.H_kv, L, d), dtype=self._bf16, device=self.device) for d in (self.D_qk, self.D_v)])
+            with _memory_of(stream):
+                out = tuple([torch.empty((B, self.H_kv, L, d), dtype=self._bf16, device=self.device) for d in (self.D_qk, self.D_v)])
             ks = vs = (0, 0, 0)  # (contiguous)
         else:
             ks, vs = self._rows(*out, B, L)
@@ -1032,12 +1046,9 @@ def attention_cached(Q, cache, table, lengths, *, scale, max_length=None, prefix
     among them; token t sees the first lengths[b] - n + 1 + t.  max_length: no sequence is longer (None: the table's room).
     prefix_table / prefix_length: keys in front of every sequence's own that the whole batch shares; they are read once for all.
     Returns O [B, H_q, n, D_v], fp32 or bf16 (out / out_dtype); stats: optional fp32 [B, H_q, n] that receives ln sum exp."""
-    import contextlib
-
     import torch
 
-    # the workspace belongs to the stream that uses it
-    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+    with _memory_of(stream):  # (the workspace, too, belongs to the stream that uses it)
         if out is None:
             out = torch.empty(Q.shape[:3] + (cache.D_v,), dtype=out_dtype or torch.float32, device=Q.device)
         plan = CachedAttentionPlan(cache, Q, out, max_length=table.shape[1] * cache.page_size if max_length is None else max_length,

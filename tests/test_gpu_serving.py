@@ -184,3 +184,25 @@ def test_gradient_through_rotary_and_attention(A):
         err = np.abs(got.cpu().double().numpy() - want) / np.maximum(np.abs(want).max(axis=-1, keepdims=True), 1.0)
         # the attention's own bound, turned: two elements of a pair at most add up to sqrt(2) of it
         assert err.max() <= 1.5e-2 and err.mean() <= 1.5e-3, (err.max(), err.mean())
+
+
+def test_memory_of_outputs_on_another_stream(A):
+    # an output is allocated where it is written: given back, its memory serves that stream, not the one the caller was on
+    B, H, L, D = 2, 4, 50, 64
+    f, _ = A.rotary_frequencies(D)
+    x = torch.randn(B, H, L, D, generator=torch.Generator().manual_seed(20)).to(torch.bfloat16).to(DEV)
+    pos = torch.arange(L, dtype=torch.int32, device=DEV)
+    c = A.PagedCache.empty(8, H, 16, D, D)
+    slots = torch.arange(B * L, dtype=torch.int32, device=DEV).view(B, L)
+    c.append(x, x.clone(), slots)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for call in (lambda: A.rotary_forward(x, x, pos, freqs=f, stream=s), lambda: A.rotary_backward(x, x, pos, freqs=f, stream=s),
+                 lambda: c.read(slots, stream=s)):
+        got = call()
+        s.synchronize()
+        assert torch.equal(*got)
+        at = {t.data_ptr() for t in got}
+        del got
+        here = [torch.empty_like(x) for _ in range(8)]
+        assert not at & {t.data_ptr() for t in here}

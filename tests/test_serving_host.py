@@ -295,3 +295,54 @@ def test_one_row_for_all_is_read_only(A):
     refused(A, 1, A.ae_cached_create, h, **CACHED, o_stride=one)
     refused(A, 1, A.ae_cached_create, h, **CACHED, q_stride=(A.ONE_ROW, 128, 128))
     A.ae_cache_destroy(h)
+
+
+def allocations(monkeypatch):
+    """Records, for every torch.empty, the stream that the allocating thread had entered (None: the current one)."""
+    import contextlib
+
+    import torch
+    seen, inside, real = [], [None], torch.empty
+
+    @contextlib.contextmanager
+    def entered(stream):
+        inside.append(stream)
+        yield
+        inside.pop()
+
+    def empty(*a, **kw):
+        seen.append(inside[-1])
+        return real(*a, **kw)
+
+    monkeypatch.setattr(torch.cuda, "stream", entered)
+    monkeypatch.setattr(torch, "empty", empty)
+    return seen
+
+
+@pytest.mark.parametrize("stream", [None, "another"])
+def test_outputs_belong_to_the_stream_that_writes_them(A, monkeypatch, stream):
+    import torch
+    seen = allocations(monkeypatch)
+
+    class Plan:
+        def __init__(self, *a, **kw):
+            pass
+
+        def forward(self, *a, stream=None):
+            return stream
+
+        backward = forward
+
+    monkeypatch.setattr(A, "RotaryPlan", Plan)
+    x = torch.zeros(1, 2, 3, 64)
+    for call in (A.rotary_forward, A.rotary_backward):
+        call(x, x, torch.zeros(3, dtype=torch.int32), freqs=[1.0] * 32, stream=stream)
+        assert seen == [stream, stream]
+        seen.clear()
+    cache = A.PagedCache.__new__(A.PagedCache)
+    cache.handle, cache.device, cache._bf16, cache._int, cache.H_kv, cache.D_qk, cache.D_v = None, torch.device("cpu"), torch.bfloat16, torch.int32, 2, 64, 64
+    cache.k = cache.v = x
+    cache.k_exp = cache.v_exp = None
+    monkeypatch.setattr(A, "_enqueue", lambda *a: None)
+    cache.read(torch.zeros(3, dtype=torch.int32), stream=stream)
+    assert seen == [stream, stream]

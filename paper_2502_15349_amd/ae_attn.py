@@ -260,6 +260,16 @@ def ae_recurrent_destroy(handle: Optional[int]) -> None:
     _check(_lib.ae_recurrent_destroy(handle))
 
 
+def _memory_of(stream):
+    """What a call allocates belongs to the stream that it writes on: memory of another one may still be in use there, or be given away
+    there while this one writes it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+
+    return torch.cuda.stream(stream)
+
+
 def retention_recurrent(Q, K, V, *, scale, gamma, chunk=256, out=None, workspace=None, stream=None, h_in=None,
                         return_state=False, out_dtype=None):
     """Recurrent retention on contiguous bf16 device tensors Q, K [B, H, L, D_qk], V [B, H, L, D_v];
@@ -276,14 +286,15 @@ def retention_recurrent(Q, K, V, *, scale, gamma, chunk=256, out=None, workspace
     if K.shape != Q.shape or V.shape[:3] != Q.shape[:3]:
         raise ValueError("K / V shape does not match Q")
     if out is None:
-        out = torch.empty((B, H, L, D_v), dtype=out_dtype or torch.float32, device=Q.device)
+        with _memory_of(stream):
+            out = torch.empty((B, H, L, D_v), dtype=out_dtype or torch.float32, device=Q.device)
     if out.dtype not in (torch.float32, torch.bfloat16) or tuple(out.shape) != (B, H, L, D_v) or not out.is_contiguous():
         raise ValueError("O must be a contiguous fp32 or bf16 tensor [B, H, L, D_v]")
     h = ae_recurrent_create(B=B, H=H, L=L, D_qk=D_qk, D_v=D_v, chunk=chunk, scale=scale, gamma=gamma,
                             out_dtype="bf16" if out.dtype == torch.bfloat16 else "f32")
     try:
         s = torch.cuda.current_stream(Q.device) if stream is None else stream
-        with torch.cuda.device(Q.device):
+        with torch.cuda.device(Q.device), _memory_of(stream):
             need = ae_recurrent_workspace_bytes(h)
             if workspace is None:
                 workspace = torch.empty(need, dtype=torch.uint8, device=Q.device)
@@ -322,7 +333,8 @@ def attention_forward(Q, K, V, *, scale, score_mod="none", bias=0.0, gamma=None,
     if K.shape != (B, H_kv, L_k, D_qk):
         raise ValueError("K shape does not match Q / V")
     if out is None:
-        out = torch.empty((B, H_q, L_q, D_v), dtype=out_dtype or torch.float32, device=Q.device)
+        with _memory_of(stream):
+            out = torch.empty((B, H_q, L_q, D_v), dtype=out_dtype or torch.float32, device=Q.device)
     if out.dtype not in (torch.float32, torch.bfloat16) or out.stride(3) != 1:
         raise ValueError("O must be fp32 or bf16 with a contiguous last dimension")
     _rows_apart(Q, K, V, out)
@@ -333,7 +345,7 @@ def attention_forward(Q, K, V, *, scale, score_mod="none", bias=0.0, gamma=None,
                        window=window, kv_splits=kv_splits, bias_stride=_bias_strides(bias_tensor, B, H_q, L_q, L_k))
     try:
         s = torch.cuda.current_stream(Q.device) if stream is None else stream
-        with torch.cuda.device(Q.device):
+        with torch.cuda.device(Q.device), _memory_of(stream):
             if stats is not None and (stats.dtype != torch.float32 or tuple(stats.shape) != (B, H_q, L_q)
                                       or not stats.is_contiguous()):
                 raise ValueError("stats must be a contiguous fp32 tensor [B, H_q, L_q]")
@@ -407,7 +419,7 @@ def attention_backward(Q, K, V, O, dO, stats, *, scale, score_mod="none", bias=0
                        window=window, bias_stride=_bias_strides(bias_tensor, B, H_q, L_q, L_k))
     try:
         s = torch.cuda.current_stream(Q.device) if stream is None else stream
-        with torch.cuda.device(Q.device):
+        with torch.cuda.device(Q.device), _memory_of(stream):
             dQ = torch.empty((B, H_q, L_q, D_qk), dtype=torch.float32, device=Q.device)
             dK = torch.empty((B, H_kv, L_k, D_qk), dtype=torch.float32, device=Q.device)
             dV = torch.empty((B, H_kv, L_k, D_v), dtype=torch.float32, device=Q.device)
@@ -522,14 +534,16 @@ def gated_recurrent(Q, K, V, log_decay, key_gate=None, *, scale, h_in=None, want
             raise ValueError("gated_recurrent needs contiguous device tensors; there is no CPU path")
     B, H_qk, L, D_qk = Q.shape
     _, H, _, D_v = V.shape
-    out = torch.empty((B, H, L, D_v), dtype=out_dtype or torch.float32, device=Q.device)
-    h_out = torch.empty((B, H, D_qk, D_v), dtype=torch.float32, device=Q.device) if want_state else None
+    with _memory_of(stream):
+        out = torch.empty((B, H, L, D_v), dtype=out_dtype or torch.float32, device=Q.device)
+        h_out = torch.empty((B, H, D_qk, D_v), dtype=torch.float32, device=Q.device) if want_state else None
     h = ae_gated_create(B=B, H=H, H_qk=H_qk, L=L, D_qk=D_qk, D_v=D_v, scale=scale,
                         out_dtype="bf16" if out.dtype == torch.bfloat16 else "f32")
     try:
         s = torch.cuda.current_stream(Q.device) if stream is None else stream
         nbytes = ae_gated_workspace_bytes(h) if segmented else 0
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
+        with _memory_of(stream):
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
         with torch.cuda.device(Q.device):
             args = (h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), log_decay.data_ptr(),
                     0 if key_gate is None else key_gate.data_ptr(), 0 if h_in is None else h_in.data_ptr(),
@@ -554,13 +568,15 @@ def gated_recurrent_backward(Q, K, V, log_decay, key_gate, dO, *, scale, stream=
     B, H_qk, L, D_qk = Q.shape
     _, H, _, D_v = V.shape
     f32 = dict(dtype=torch.float32, device=Q.device)
-    dQ, dK, dV = torch.empty(Q.shape, **f32), torch.empty(K.shape, **f32), torch.empty(V.shape, **f32)
-    dla = torch.empty((B, H, L), **f32)
-    dkg = None if key_gate is None else torch.empty((B, H, L), **f32)
+    with _memory_of(stream):
+        dQ, dK, dV = torch.empty(Q.shape, **f32), torch.empty(K.shape, **f32), torch.empty(V.shape, **f32)
+        dla = torch.empty((B, H, L), **f32)
+        dkg = None if key_gate is None else torch.empty((B, H, L), **f32)
     h = ae_gated_create(B=B, H=H, H_qk=H_qk, L=L, D_qk=D_qk, D_v=D_v, scale=scale)
     try:
         nbytes = ae_gated_backward_workspace_bytes(h)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device)
+        with _memory_of(stream):
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device)
         s = torch.cuda.current_stream(Q.device) if stream is None else stream
         with torch.cuda.device(Q.device):
             ae_gated_backward(h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), log_decay.data_ptr(),
@@ -753,16 +769,6 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, scaling="none", f
         keep = [min(1.0, max(0.0, (original_length * x / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns))) for x in f]
         return [x * k + x / factor * (1.0 - k) for x, k in zip(f, keep)], 0.1 * math.log(factor) + 1.0
     raise ValueError(f"unknown scaling {scaling!r}")
-
-
-def _memory_of(stream):
-    """What a call allocates belongs to the stream that it writes on: memory of another one may still be in use there, or be given away
-    there while this one writes it."""
-    if stream is None:
-        return contextlib.nullcontext()
-    import torch
-
-    return torch.cuda.stream(stream)
 
 
 ONE_ROW = -2 ** 63  # AE_ONE_ROW

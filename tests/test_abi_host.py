@@ -541,3 +541,59 @@ def test_strides_of_a_bias_tensor():
             strides(rows)
     # one query row for all: not contiguous, which three zeros would mean
     assert strides(whole[0, 0, 0].expand(2, 4, 7, 24)[:, :, :1], 1) == (0, 0, 24)
+
+
+@pytest.mark.parametrize("call", ["forward", "split", "backward", "dbias", "recurrent", "gated", "segmented", "gated_backward"])
+@pytest.mark.parametrize("given", [True, False])
+def test_memory_belongs_to_the_stream_that_writes_it(monkeypatch, call, given):
+    """Outputs and workspaces of a call on a stream of its own are taken (and filled) there."""
+    import contextlib
+    import types
+
+    import torch
+    from paper_2502_15349_amd import ae_attn as A
+    other, seen, inside = types.SimpleNamespace(cuda_stream=7), [], [None]
+
+    @contextlib.contextmanager
+    def entered(stream):
+        inside.append(stream)
+        yield
+        inside.pop()
+
+    def recorded(real):
+        def make(*a, **kw):
+            seen.append(inside[-1])
+            return real(*a, **kw)
+        return make
+
+    zeros = torch.zeros
+    bf = lambda *n: OnDevice(zeros(*n, dtype=torch.bfloat16))
+    f32 = lambda *n: OnDevice(zeros(*n))
+    Q, K, V = bf(1, 2, 600, 128), bf(1, 2, 600, 128), bf(1, 2, 600, 128)
+    for name in ("ae_attn_forward", "ae_attn_forward_split", "ae_attn_backward", "ae_attn_backward_bias", "ae_recurrent_forward_state", "ae_gated_forward",
+                 "ae_gated_forward_segmented", "ae_gated_backward"):
+        monkeypatch.setattr(A, name, lambda *a: None)
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d: types.SimpleNamespace(cuda_stream=0))
+    monkeypatch.setattr(torch.cuda, "stream", entered)
+    monkeypatch.setattr(torch, "empty", recorded(torch.empty))
+    monkeypatch.setattr(torch, "zeros", recorded(zeros))
+    kw = dict(scale=0.1, stream=other if given else None)
+    back = (Q, K, V, bf(1, 2, 600, 128), bf(1, 2, 600, 128), f32(1, 2, 600))
+    gates = (f32(1, 2, 600), f32(1, 2, 600))
+    if call == "forward":
+        A.attention_forward(Q, K, V, **kw)
+    elif call == "split":
+        A.attention_forward(Q, K, V, kv_splits=2, **kw)
+    elif call == "backward":
+        A.attention_backward(*back, **kw)
+    elif call == "dbias":
+        A.attention_backward(*back, score_mod="bias_tensor", bias_tensor=bf(1, 2, 600, 600), want_dbias=True, mask="causal", **kw)
+    elif call == "recurrent":
+        A.retention_recurrent(Q, K, V, gamma=[0.9, 0.9], return_state=True, **kw)
+    elif call in ("gated", "segmented"):
+        A.gated_recurrent(Q, K, V, *gates, want_state=True, segmented=call == "segmented", **kw)
+    else:
+        A.gated_recurrent_backward(Q, K, V, *gates, back[4], **kw)
+    n = {"forward": 1, "split": 2, "backward": 4, "dbias": 5, "recurrent": 3, "gated": 2, "segmented": 3, "gated_backward": 6}[call]
+    assert seen == [kw["stream"]] * n

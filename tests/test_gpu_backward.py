@@ -628,3 +628,22 @@ def test_backward_decay_rates(A, dims, norm):
         # through delta, of the forward weights, less than 2^-9 each in the root mean square.
         err = np.linalg.norm(x.cpu().double().numpy() - r) / np.linalg.norm(r)
         assert err <= 3 * 2.0 ** -9, (name, err)
+
+
+def test_calls_on_another_stream_take_their_memory_there(A):
+    g = torch.Generator().manual_seed(77)
+    Q, K, V, dO = (torch.randn(1, 4, 200, 64, generator=g).to(torch.bfloat16).cuda() for _ in range(4))
+    bias = torch.randn(1, 4, 200, 200, generator=g).to(torch.bfloat16).cuda()
+    stats = torch.empty(1, 4, 200, device="cuda")
+    kw = dict(scale=0.125, score_mod="bias_tensor", bias_tensor=bias, mask="causal")
+    O = A.attention_forward(Q, K, V, stats=stats, **kw)
+    ref = (O, *A.attention_backward(Q, K, V, O, dO, stats, want_dbias=True, **kw))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        got = (A.attention_forward(Q, K, V, stream=s, **kw), *A.attention_backward(Q, K, V, O, dO, stats, want_dbias=True, stream=s, **kw))
+        s.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))
+        at = {t.data_ptr() for t in got}
+        del got
+        assert not at & {torch.empty_like(O).data_ptr() for _ in range(8)}

@@ -993,8 +993,9 @@ class CachedAttentionPlan:
     its workspace.  Q [B, H_q, n, D_qk] bf16 and out [B, H_q, n, D_v] (bf16 or fp32) give shapes, strides and device; max_length: no
     sequence has more keys of its own; table_width: pages in a row of the table; prefix_length: keys that all sequences share.
     Calls of one plan must not overlap (they share its workspace, which is prepared on the stream that is current when the plan is
-    made: another stream waits for that one before its first call); a captured graph keeps using the plan's buffers, and a plan made
-    while a graph is captured is of use to that graph alone."""
+    made: another stream waits for that one before its first call); the plan may be dropped while a call still runs, on whichever stream.
+    A captured graph keeps using the plan's buffers, so the plan has to outlive it, and a plan made while a graph is captured is of use to
+    that graph alone."""
 
     def __init__(self, cache, Q, out, *, max_length, table_width, scale, prefix_length=0, chunk=0):
         import torch
@@ -1019,6 +1020,7 @@ class CachedAttentionPlan:
         self.workspace = None
         if self.workspace_bytes:
             self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=Q.device)
+            self._streams = {_raw_stream(Q.device.index)}  # those that the allocator knows to use it
             _enqueue(ae_cached_init_workspace, Q.device, None, self.handle, self.workspace.data_ptr(), self.workspace_bytes)
 
     def forward(self, Q, table, lengths, out, *, stats=None, prefix_table=None, stream=None):
@@ -1034,10 +1036,22 @@ class CachedAttentionPlan:
                 raise ValueError(f"tables and lengths must be contiguous int32 device tensors (here {shape})")
         if stats is not None and (stats.dtype != self._f32 or stats.shape != self.shape or not stats.is_contiguous() or stats.device != self.device):
             raise ValueError("stats must be a contiguous fp32 tensor [B, H_q, n]")
+        if self.workspace is not None:
+            self._use_workspace(stream)
         _enqueue(ae_cached_forward, self.device, stream, self.handle, Q.data_ptr(), *self.cache.pointers(), table.data_ptr(), lengths.data_ptr(),
                  0 if prefix_table is None else prefix_table.data_ptr(), out.data_ptr(), 0 if stats is None else stats.data_ptr(),
                  0 if self.workspace is None else self.workspace.data_ptr(), self.workspace_bytes)
         return out
+
+    def _use_workspace(self, stream):
+        """Its memory belongs to the stream that was current when the plan was made; given back, it must not serve that one before a call on
+        another is done."""
+        import torch
+
+        raw = _raw_stream(self.device.index) if stream is None else stream.cuda_stream
+        if raw not in self._streams:
+            self.workspace.record_stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+            self._streams.add(raw)
 
     def __del__(self):
         if getattr(self, "handle", None) is not None and _lib is not None:

@@ -206,3 +206,29 @@ def test_memory_of_outputs_on_another_stream(A):
         del got
         here = [torch.empty_like(x) for _ in range(8)]
         assert not at & {t.data_ptr() for t in here}
+
+
+def test_plan_dropped_while_another_stream_uses_its_workspace(A):
+    B, H, D, page, width = 2, 4, 128, 32, 60
+    g = torch.Generator().manual_seed(21)
+    c = A.PagedCache.empty(B * width, H, page, D, D)
+    k, v = (torch.randn(1, H, B * width * page, D, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    c.append(k, v, torch.arange(B * width * page, dtype=torch.int32, device=DEV)[None])
+    t = torch.arange(B * width, dtype=torch.int32, device=DEV).view(B, width)
+    L = torch.tensor([1900, 700], dtype=torch.int32, device=DEV)
+    Q, out = torch.randn(B, H, 1, D, generator=g).to(torch.bfloat16).to(DEV), torch.empty(B, H, 1, D, device=DEV)
+    ref = A.attention_cached(Q, c, t, L, scale=0.088, chunk=128)
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        plan = A.CachedAttentionPlan(c, Q, out, max_length=width * page, table_width=width, scale=0.088, chunk=128)
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(20_000_000)  # (some milliseconds in front of the call)
+        plan.forward(Q, t, L, out, stream=s)
+        at, size = plan.workspace.data_ptr(), plan.workspace_bytes
+        del plan
+        taken = [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for _ in range(4)]
+        assert at not in {x.data_ptr() for x in taken}
+        s.synchronize()
+        assert torch.equal(out, ref)
+        out.fill_(7.0)

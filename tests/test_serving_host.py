@@ -346,3 +346,30 @@ def test_outputs_belong_to_the_stream_that_writes_them(A, monkeypatch, stream):
     monkeypatch.setattr(A, "_enqueue", lambda *a: None)
     cache.read(torch.zeros(3, dtype=torch.int32), stream=stream)
     assert seen == [stream, stream]
+
+
+def test_workspace_is_held_for_the_streams_that_use_it(A, monkeypatch):
+    import types
+
+    import torch
+    current, calls, held = [types.SimpleNamespace(cuda_stream=5)], [], []
+    monkeypatch.setattr(A, "_raw_stream", lambda index: current[0].cuda_stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: current[0])
+    monkeypatch.setattr(A, "_enqueue", lambda call, device, stream, *a: calls.append(stream))
+    x, table, L = OnDevice(torch.zeros(2, 2, 1, 64, dtype=torch.bfloat16)), torch.zeros(2, 70, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    cache = A.PagedCache(*[OnDevice(torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16))] * 2)
+    for chunk, some in ((128, True), (1152, False)):  # ranges that are joined; one range, no workspace
+        current[0] = types.SimpleNamespace(cuda_stream=5)
+        plan = A.CachedAttentionPlan(cache, x, x, max_length=1100, table_width=70, scale=1.0, chunk=chunk)
+        assert (plan.workspace is not None) == some
+        if some:
+            ws, plan.workspace = plan.workspace, types.SimpleNamespace(data_ptr=lambda: 0, record_stream=held.append)
+        other, third = types.SimpleNamespace(cuda_stream=8), types.SimpleNamespace(cuda_stream=9)
+        calls.clear()
+        for s in (None, current[0], other, other, None):
+            plan.forward(x, table, L, x, stream=s)
+        current[0] = third
+        plan.forward(x, table, L, x)
+        plan.forward(x, table, L, x, stream=other)
+        assert len(calls) == 7 and held == ([other, third] if some else [])
+        held.clear()

@@ -442,10 +442,16 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
           for (int e = 0; e < COLS / 2; ++e) part[u][e] = load_shared(po + at * C::DV + 2 * e);
         }
       }
+      // (by bits: a maximum passes over a NaN, which is the sum of a row that has met one, or an infinite score)
       float top = M;
+      bool none = __builtin_bit_cast(uint32_t, M) == 0xff800000u;
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) top = fmaxf(top, lse[u]);
-      if (__builtin_bit_cast(uint32_t, top) == 0xff800000u) continue;  // no key so far
+      for (int u = 0; u < BATCH; ++u) {
+        top = fmaxf(top, lse[u]);
+        none = none && __builtin_bit_cast(uint32_t, lse[u]) == 0xff800000u;
+      }
+      if (none) continue;  // no key so far
+      if (__builtin_bit_cast(uint32_t, top) == 0xff800000u) top = 0.f;  // nothing but NaN: any reference will do
       const float a = fast_exp2(M - top);
       M = top;
       L *= a;

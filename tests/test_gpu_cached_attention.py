@@ -466,3 +466,30 @@ def test_one_row_of_queries_for_all(A, B, n, prefix, launches):
     assert A.ae_cached_query(plan.handle)["launches"] == launches
     plan.forward(Q, t, L, out, **tables)
     assert torch.equal(out, A.attention_cached(Q.contiguous(), c, t, L, scale=0.125, **kw, **tables))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("B,n,length,chunk,prefix", [(1, 1, 600, 0, 0), (1, 1, 600, 128, 0), (2, 3, 50, 128, 0), (2, 3, 600, 128, 0), (1, 1, 20, 128, 300),
+                                                     (2, 3, 200, 128, 300), (3, 17, 40, 0, 300), (3, 17, 40, 128, 300), (3, 17, 200, 128, 300)])
+def test_bad_queries_and_keys_give_nan(A, dtype, B, n, length, chunk, prefix):
+    # NaN and infinite queries, and a NaN key that every row sees, make their rows NaN and no others, however the keys are cut
+    page, width = 16, 40
+    c = make(A, 130, B * width + 20, 2, page, 64, 64, dtype)
+    t, ptab = torch.arange(B * width, dtype=torch.int32).view(B, width).cuda(), torch.arange(B * width, B * width + 20, dtype=torch.int32).cuda()
+    L = torch.full((B,), length, dtype=torch.int32, device="cuda")
+    kw = dict(scale=0.125, chunk=chunk, **(dict(prefix_table=ptab[: -(-prefix // page)].contiguous(), prefix_length=prefix) if prefix else {}))
+    Q, stats = queries(131, B, 4, n, 64), torch.empty(B, 4, n, device="cuda")
+    clean = A.attention_cached(Q, c, t, L, **kw)
+    bad = torch.zeros(B, 4, n, dtype=torch.bool, device="cuda")
+    for b, h, i, x in ((0, 1, 0, "nan"), (B - 1, 2, n - 1, "inf"), (B - 1, 0, n // 2, "-inf")):
+        Q[b, h, i, 7] = float(x)
+        bad[b, h, i] = True
+    O = A.attention_cached(Q, c, t, L, stats=stats, **kw)
+    assert torch.isnan(O[bad]).all() and torch.isnan(stats[bad]).all()
+    assert torch.equal(O[~bad], clean[~bad]) and torch.isfinite(stats[~bad]).all()
+    # a key of the last sequence's first page, second k/v head: heads 2 and 3
+    (c.k if dtype == "bf16" else c.k.view(torch.uint8))[(B - 1) * width, 1, 3, 5] = float("nan") if dtype == "bf16" else 0x7f
+    bad[B - 1, 2:] = True
+    O = A.attention_cached(Q, c, t, L, stats=stats, **kw)
+    assert torch.isnan(O[bad]).all() and torch.isnan(stats[bad]).all()
+    assert torch.equal(O[~bad], clean[~bad]) and torch.isfinite(stats[~bad]).all()

@@ -460,10 +460,11 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
         const float w = fast_exp2(lse[u] - top);
+        const bool empty = __builtin_bit_cast(uint32_t, lse[u]) == 0xff800000u;  // (not where the weight is merely too small for 32 bits)
         L += w;
 #pragma unroll
         for (int e = 0; e < COLS; ++e)
-          acc[e] += w * (__builtin_bit_cast(uint32_t, w) == 0 ? 0.f : __builtin_bit_cast(float, (uint32_t)(part[u][e / 2] >> (32 * (e % 2)))));
+          acc[e] += w * (empty ? 0.f : __builtin_bit_cast(float, (uint32_t)(part[u][e / 2] >> (32 * (e % 2)))));
       }
     }
   };

@@ -493,3 +493,22 @@ def test_bad_queries_and_keys_give_nan(A, dtype, B, n, length, chunk, prefix):
     O = A.attention_cached(Q, c, t, L, stats=stats, **kw)
     assert torch.isnan(O[bad]).all() and torch.isnan(stats[bad]).all()
     assert torch.equal(O[~bad], clean[~bad]) and torch.isfinite(stats[~bad]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("chunk", [1024, 128])
+@pytest.mark.parametrize("H_q", [2, 16, 32])  # (how many threads add up a row's partial results)
+def test_bad_values_of_vanishing_weight(A, dtype, chunk, H_q):
+    # a NaN value whose weight is too small for 32 bits (e^-256 of the others) makes its column NaN, in the same range of keys and in another
+    page, width = 16, 32
+    c = make(A, 140, width, 1, page, 64, 64, dtype)
+    k = torch.zeros(1, 1, 512, 64, dtype=torch.bfloat16, device="cuda")
+    k[:, :, :64] = 4.0
+    c.append(k, torch.randn(1, 1, 512, 64, generator=torch.Generator().manual_seed(141)).to(torch.bfloat16).cuda(), torch.arange(512, dtype=torch.int32).cuda())
+    t, L = torch.arange(width, dtype=torch.int32).view(1, width).cuda(), torch.tensor([500], dtype=torch.int32).cuda()
+    Q = torch.ones(1, H_q, 1, 64, dtype=torch.bfloat16, device="cuda")
+    clean = A.attention_cached(Q, c, t, L, scale=1.0, chunk=chunk)
+    (c.v if dtype == "bf16" else c.v.view(torch.uint8))[20, 0, 3, 9] = float("nan") if dtype == "bf16" else 0x7f  # key 323
+    O = A.attention_cached(Q, c, t, L, scale=1.0, chunk=chunk)
+    others = [d for d in range(64) if d != 9]
+    assert torch.isnan(O[..., 9]).all() and torch.equal(O[..., others], clean[..., others]) and torch.isfinite(clean).all()

@@ -512,3 +512,83 @@ def test_bad_values_of_vanishing_weight(A, dtype, chunk, H_q):
     O = A.attention_cached(Q, c, t, L, scale=1.0, chunk=chunk)
     others = [d for d in range(64) if d != 9]
     assert torch.isnan(O[..., 9]).all() and torch.equal(O[..., others], clean[..., others]) and torch.isfinite(clean).all()
+
+
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("B,H_q,H_kv,n,page,prefix,chunk,bad,scale", [
+    (7, 16, 2, 5, 16, 333, 0, [0, 3, 20], 0.1),      # pages that are no pages in the first tile of 64 keys, two of its four, and the last page
+    (7, 16, 2, 5, 32, 1000, 256, [1, 8, 31], -0.1),  # in the first tile, in front of the second range, the last page; a negative scale
+    (5, 12, 1, 3, 16, 64, 0, [], 0.1),               # one whole tile
+    (3, 40, 1, 1, 16, 65, 0, [4], 0.1),              # the second tile's only key is hidden
+    (9, 40, 1, 1, 32, 129, 128, [4], -0.1),          # the second range has no other key
+    (9, 40, 1, 1, 16, 400, 128, [0, 1, 2, 3, 12, 13, 14, 15], 0.1),  # whole tiles, the first one of a range among them
+    (260, 8, 1, 1, 16, 200, 0, [5], 0.1),            # 2080 rows
+    (4, 64, 8, 6, 64, 700, 0, [0], -0.1),
+    (2, 34, 2, 2, 16, 5, 0, [], 0.1),                # a few keys
+    (2, 34, 2, 2, 32, 70, 0, [0, 1, 2], 0.1),        # no key at all
+])
+def test_prefix_in_a_launch_of_its_own(A, dqk, dv, dtype, B, H_q, H_kv, n, page, prefix, chunk, bad, scale):
+    pp, own = -(-prefix // page), n + 30
+    width = -(-own // page)
+    n_pages = pp + 1 + B * width
+    c = make(A, 150, n_pages, H_kv, page, dqk, dv, dtype)
+    order = torch.randperm(n_pages - 1, generator=torch.Generator().manual_seed(151)).to(torch.int32) + 1  # (page 0 holds NaN)
+    ptab, t = order[:pp].clone(), order[pp: pp + B * width].view(B, width).clone()
+    for i in bad:
+        ptab[i] = -1 if i % 2 else n_pages
+    lengths = [n + (7 * b) % (own - n) for b in range(B)]
+    spoil_behind(c, list(t) + [ptab], lengths + [prefix])
+    Q, stats, out = queries(152, B, H_q, n, dqk), torch.empty(B, H_q, n, device="cuda"), torch.empty(B, H_q, n, dv, device="cuda")
+    plan = A.CachedAttentionPlan(c, Q, out, max_length=max(lengths), table_width=width, scale=scale, prefix_length=prefix, chunk=chunk)
+    assert A.ae_cached_query(plan.handle)["launches"] == 2
+    plan.forward(Q, t.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), out, stats=stats, prefix_table=ptab.cuda())
+    kv = values(c)
+    live = [j for j in range(prefix) if 0 <= int(ptab[j // page]) < n_pages]
+    pre = [np.stack([x[int(ptab[j // page]), :, j % page] for j in live], axis=1) if live else np.zeros((H_kv, 0, x.shape[3])) for x in kv]
+    some = sorted({0, 1, B // 2, B - 2, B - 1})
+    rows = [[np.concatenate((p, listed(x, t[b].tolist(), lengths[b])), axis=1) for b in some] for p, x in zip(pre, kv)]
+    check(out[some], stats[some], Q[some], *rows, scale, f"{B} x {H_q}/{H_kv} x {n} behind {prefix}, page {page}, {dqk}/{dv} {dtype}")
+
+
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("H_q,H_kv,n,page,chunk,prefix", [(4, 4, 40, 16, 0, 0), (6, 2, 130, 32, 128, 0), (3, 1, 700, 64, 256, 0), (2, 1, 33, 16, 0, 90)])
+def test_many_new_tokens(A, dqk, dv, dtype, H_q, H_kv, n, page, chunk, prefix):
+    # a prompt's piece: tokens whose visible keys end in different tiles; a sequence that has no more keys than those, and one that has fewer
+    lengths = [n, n + 77, 2 * n + 301] + ([] if prefix else [n // 2])
+    B, width, pp = len(lengths), -(-max(lengths) // page), -(-prefix // page)
+    n_pages = pp + sum(-(-x // page) for x in lengths) + 1
+    c = make(A, 160, n_pages, H_kv, page, dqk, dv, dtype)
+    t, ptab = tables_for(161, n_pages, lengths, page, width, first=pp), torch.arange(pp, dtype=torch.int32)
+    spoil_behind(c, list(t) + [ptab], lengths + [prefix])
+    Q, stats = queries(162, B, H_q, n, dqk), torch.empty(B, H_q, n, device="cuda")
+    kw = dict(prefix_table=ptab.cuda(), prefix_length=prefix) if prefix else {}
+    O = A.attention_cached(Q, c, t.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), scale=dqk ** -0.5, chunk=chunk, stats=stats, **kw)
+    kv = values(c)
+    rows = [[np.concatenate((listed(x, ptab.tolist(), prefix), listed(x, t[b].tolist(), lengths[b])), axis=1) for b in range(B)] for x in kv]
+    check(O, stats, Q, *rows, dqk ** -0.5, f"{n} new tokens, {dqk}/{dv} {dtype} {H_q}/{H_kv} page {page} chunk {chunk} prefix {prefix}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n,length,chunk", [(40, 40, 0), (40, 95, 128), (130, 300, 128), (130, 300, 0), (700, 900, 0)])
+def test_special_values_among_many_new_tokens(A, dtype, n, length, chunk):
+    # NaN in values and keys of new tokens in different tiles of keys: rows that do not see them keep their bits
+    page = 16
+    c = make(A, 170, -(-length // page) + 1, 2, page, 64, 64, dtype)
+    t = torch.randperm(c.n_pages - 1, generator=torch.Generator().manual_seed(171)).to(torch.int32).view(1, -1) + 1
+    Q, L = queries(172, 1, 4, n, 64), torch.tensor([length], dtype=torch.int32).cuda()
+    run = lambda: A.attention_cached(Q, c, t.cuda(), L, scale=0.125, chunk=chunk)
+    clean = run()
+    nan = float("nan") if dtype == "bf16" else 0x7f
+    K, V = (x if dtype == "bf16" else x.view(torch.uint8) for x in (c.k, c.v))
+    first = length - n  # key of the first new token
+    seen = torch.zeros(4, n, 64, dtype=torch.bool)
+    for i, head, d in ((1, 0, 5), (n // 2, 1, 9), (n // 2 + 1, 0, 33), (n - 2, 0, 60)):
+        V[int(t[0, (first + i) // page]), head, (first + i) % page, d] = nan
+        seen[2 * head: 2 * head + 2, i:, d] = True
+    i = n - 5
+    K[int(t[0, (first + i) // page]), 1, (first + i) % page, 0] = nan
+    seen[2:, i:] = True
+    O = run()[0].cpu()
+    assert torch.isnan(O[seen]).all() and torch.equal(O[~seen], clean[0].cpu()[~seen])

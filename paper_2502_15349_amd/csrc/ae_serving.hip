@@ -277,7 +277,7 @@ void cut_keys(ae::CachedPart& pt, int tile_rows, int64_t cuts, int64_t chunk) {
 //   * a prefix in a launch of its own takes 3.5 and 0.73 + 0.95 w for each 64 keys and 256 rows of a workgroup, 0.3 for every MB of partial
 //     results, and 3.5 for the second launch.
 // Fitted on 3218 random calls (1 to 256 sequences, 1 to 8 new tokens, 64 to 131072 keys, all head dims and types; keys that no cache
-// holds) and 2178 behind a prefix (2 to 256 sequences, 100 to 32768 keys).  On 612 other calls the choice takes 1.038 times the time of the
+// holds) and 2178 behind a prefix (2 to 256 sequences, 100 to 32768 keys, own lists of 1 to 1024).  On 612 other calls the choice takes 1.038 times the time of the
 // best layout measured for that call (1.11 at the 90th percentile, 1.55 at most), on 409 behind a prefix 1.041 (1.12, 1.29).  As many ranges
 // as keep all workgroups resident take 1.08 with four wavefronts (1.24, 2.0), 1.11 with eight; the best layout with a launch of its
 // own for the prefix 1.23 (1.65, 2.9).
@@ -312,6 +312,8 @@ Layout choose_layout(const ae_cached_desc_t& d, const ae_cache_desc_t& cd, int g
       auto turns_of = [&](double x) { return (1 - whole_part) * x + whole_part * std::ceil(x - 0.02); };
       const double places = 256.0 * ae::cached_residents(cd.D_qk, cd.D_v, e4m3, wide ? 32 : 16, waves);
       for (int oc : kCuts) {
+        // (behind a prefix: as they were measured, on own lists of at most 1024 keys.  Too few for much longer ones: 4 x 8/1 heads x 131072
+        // keys of 128 + 128 take 48 us, behind 2000 more 255, and 81 in ranges of 1024 by the caller's choice)
         if (d.prefix_length > 0 && oc != 1 && oc != 3) continue;
         const double chunk = std::ceil(std::ceil((double)d.max_length / oc) / 128) * 128, cuts = std::ceil(d.max_length / chunk);
         const double steps = std::ceil(std::min(chunk, (double)d.max_length) / (32 * waves)), walk = start + steps * step;

@@ -7,8 +7,8 @@
 // 448 = 1.75 * 2^8, so k + 127 = E - 8 + (M > 0.75 * 128), at least 1.  Magnitudes are compared as integers, which
 // leaves infinities and NaN aside without a comparison of floats.
 //
-// Bound by memory; the rows of keys and of values share a launch.  4 x 8 heads x 4096 rows of 128 + 128, 8-bit, written and read back: 45 us
-// together, 4.5 TB/s.
+// Bound by memory; the rows of keys and of values share a launch.  4 x 8 heads x 4096 rows of 128 + 128, written and read back: 45 us
+// together in 8 bits (4.5 TB/s) and 46 in 16 (5.9, some of it from the last level of cache, which still holds rows just written).
 #include "cache.hpp"
 
 #include "launch.hpp"

@@ -7,7 +7,7 @@
 // In the accumulator layout a lane holds 4 keys of one row per tile; with that choice of keys its 8 values are 8 neighbouring
 // keys, and, packed to bf16, they are the second product's B operand as they stand.  V^T comes from the transposing LDS
 // read.  Softmax with a running reference per row that moves only when a score exceeds it by more than 2^8; the row sum is of the
-// unrounded weights, in fp32.  Weights are rounded to bf16 for the second product (unbiased, 2^-9 each).
+// unrounded weights, in fp32.  Weights are rounded to bf16 for the second product (unbiased, at most 2^-8 of each).
 // 8-bit keys become bf16 between LDS and the MFMA, on their row's power of two (exact, the conversion applies it);
 // 8-bit values likewise without theirs, which multiplies the weight instead (a lane's 8 values of V are of 8 rows).
 //

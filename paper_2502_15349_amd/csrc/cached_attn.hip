@@ -568,9 +568,11 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
   if (wave == 0) done[C::ROWS] = __builtin_amdgcn_ballot_w64(last) != 0;  // (the counting lanes are the first wavefront's)
   __syncthreads();
   if (!done[C::ROWS]) return;
-  // Sixteen rows at a time; where there are fewer, 2, 4, 8 or 16 groups of threads share a row's slots and meet in LDS.
-  const int tile_rows = row_end - row0;
-  const int groups = tile_rows > 8 ? 1 : tile_rows > 4 ? 2 : tile_rows > 2 ? 4 : tile_rows > 1 ? 8 : 16, at_once = 16 / groups;
+  // Sixteen rows at a time; where there are fewer, 2, 4, 8 or 16 groups of threads share a row's slots and meet in LDS.  With a prefix in
+  // the launch the last workgroup of a row may be of either part, and their sums must be the same: the prefix's tile decides for both.
+  // (Four groups for the own list's few rows, whose sums the prefix's workgroups then form one after the other: 1 to 2 us slower.)
+  const int tile_rows = row_end - row0, rule_rows = p.prefix_blocks ? p.part[1].tile_rows : tile_rows;
+  const int groups = rule_rows > 8 ? 1 : rule_rows > 4 ? 2 : rule_rows > 2 ? 4 : rule_rows > 1 ? 8 : 16, at_once = 16 / groups;
   const int jr = r % at_once, jg = r / at_once;
 #pragma unroll 1
   for (int r0 = 0; r0 < tile_rows; r0 += at_once) {

@@ -592,3 +592,26 @@ def test_special_values_among_many_new_tokens(A, dtype, n, length, chunk):
     seen[2:, i:] = True
     O = run()[0].cpu()
     assert torch.isnan(O[seen]).all() and torch.equal(O[~seen], clean[0].cpu()[~seen])
+
+
+@pytest.mark.parametrize("dqk,dv,dtype", [(64, 64, "bf16"), (128, 128, "e4m3")])
+@pytest.mark.parametrize("B,H_q,H_kv", [(16, 8, 2), (40, 2, 2), (16, 6, 2), (10, 12, 2), (6, 24, 2)])
+def test_same_bits_whoever_is_last(A, dqk, dv, dtype, B, H_q, H_kv):
+    # in the launch that walks the prefix too, a workgroup of either kind may be the last of a sequence, which joins the partial results: with
+    # a page of own keys those of the prefix are, with thousands of hidden ones behind it those of the own list (their ranges come
+    # later and outnumber the places)
+    page, prefix, long = 16, 8192, 40000
+    pp, width = prefix // page, long // page
+    c = make(A, 180, pp + B, H_kv, page, dqk, dv, dtype)
+    order = torch.randperm(pp + B, generator=torch.Generator().manual_seed(181)).to(torch.int32).cuda()
+    ptab, t = order[:pp].contiguous(), torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+    t[:, 0] = order[pp:]
+    Q, out, stats = queries(182, B, H_q, 1, dqk), torch.empty(B, H_q, 1, dv, device="cuda"), torch.empty(B, H_q, 1, device="cuda")
+    plan = A.CachedAttentionPlan(c, Q, out, max_length=long, table_width=width, scale=dqk ** -0.5, prefix_length=prefix, chunk=1024)
+    assert A.ae_cached_query(plan.handle)["launches"] == 1
+    got = []
+    for n in (page, long, page, long, page, long):
+        plan.forward(Q, t, torch.full((B,), n, dtype=torch.int32, device="cuda"), out, stats=stats, prefix_table=ptab)
+        got.append((out.clone(), stats.clone()))
+    for o, s in got[1:]:
+        assert torch.equal(o, got[0][0]) and torch.equal(s, got[0][1])

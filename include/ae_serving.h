@@ -148,7 +148,8 @@ ae_status_t ae_cache_destroy(ae_cache_t *h); /* NULL is allowed */
  * lengths are read on the device: one outside [0, max_length] counts as the nearer
  * bound.  A page number outside [0, n_pages) is not followed: its keys count as hidden.
  * What lies in the cache behind a sequence's end may be anything, NaN included.
- * A NaN or infinity in a query row makes that row alone NaN; one in a cached row reaches the rows that see it and no others.
+ * A NaN or infinity in a query row reaches that row alone (NaN, but for a row whose every score is -infinity: it counts as one without
+ * keys); one in a cached row reaches the rows that see it and no others.
  *
  * Precision: scores, their softmax, sums, accumulators and partial results are fp32.  A weight is rounded once to bfloat16 (at most
  * 2^-8 of it, unbiased; 8-bit caches: after its product with the value row's power of two) for the product with the values, while

@@ -1080,3 +1080,222 @@ def attention_cached(Q, cache, table, lengths, *, scale, max_length=None, prefix
         plan = CachedAttentionPlan(cache, Q, out, max_length=table.shape[1] * cache.page_size if max_length is None else max_length,
                                    table_width=table.shape[1], scale=scale, prefix_length=prefix_length, chunk=chunk)
         return plan.forward(Q, table, lengths, out, stats=stats, prefix_table=prefix_table)
+
+
+# ---- span attention (include/ae_span.h) -----------------------------------------------------------------------------------
+SPAN_MASKS = {"none": 0, "causal": 1, "sliding_window": 2, "spans": 3}
+
+
+class ae_span_desc_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("H_q", C.c_int32), ("H_kv", C.c_int32), ("L_q", C.c_int32), ("L_k", C.c_int32), ("D_qk", C.c_int32),
+                ("D_v", C.c_int32), ("scale", C.c_float), ("cap", C.c_float), ("slopes", C.POINTER(C.c_float)), ("mask", C.c_int),
+                ("window", C.c_int32), ("out_dtype", C.c_int), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
+                ("v_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3)]
+
+
+_lib.ae_span_create.argtypes = [C.POINTER(ae_span_desc_t), C.POINTER(C.c_void_p)]
+_lib.ae_span_create.restype = C.c_int
+_lib.ae_span_forward.argtypes = [C.c_void_p] * 6 + [C.c_int64] + [C.c_void_p] * 3
+_lib.ae_span_forward.restype = C.c_int
+_lib.ae_span_backward_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+_lib.ae_span_backward_workspace_bytes.restype = C.c_int
+_lib.ae_span_backward.argtypes = ([C.c_void_p] * 6 + [C.c_int64] + [C.c_void_p] * 2 + [C.POINTER(C.c_int64)] + [C.c_void_p] * 4
+                                  + [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p])
+_lib.ae_span_backward.restype = C.c_int
+_lib.ae_span_destroy.argtypes = [C.c_void_p]
+_lib.ae_span_destroy.restype = C.c_int
+_lib.ae_span_documents.argtypes = ([C.c_int32] * 3 + [C.c_void_p, C.c_int64] * 2 + [C.c_int, C.c_int32] + [C.c_void_p] * 3)
+_lib.ae_span_documents.restype = C.c_int
+
+
+def _float_array(values):
+    """(pointer, what it points into) of host floats; null for None."""
+    if values is None:
+        return C.POINTER(C.c_float)(), None
+    keep = (C.c_float * len(values))(*[float(x) for x in values])
+    return C.cast(keep, C.POINTER(C.c_float)), keep
+
+
+def ae_span_create(*, B: int, H_q: int, H_kv: int, L_q: int, L_k: int, D_qk: int, D_v: int, scale: float, cap: float = 0.0,
+                   slopes: Optional[Sequence[float]] = None, mask="causal", window: int = 0, out_dtype="f32", q_stride=(0, 0, 0),
+                   k_stride=(0, 0, 0), v_stride=(0, 0, 0), o_stride=(0, 0, 0)) -> int:
+    """Handle for softmax attention over a span of keys per query row; slopes: H_q host floats."""
+    if slopes is not None and len(slopes) != H_q:
+        raise ValueError("slopes must hold a number for every query head")
+    at, keep = _float_array(slopes)
+    d = ae_span_desc_t(B=B, H_q=H_q, H_kv=H_kv, L_q=L_q, L_k=L_k, D_qk=D_qk, D_v=D_v, scale=float(scale), cap=float(cap), slopes=at,
+                       mask=SPAN_MASKS[mask] if isinstance(mask, str) else int(mask), window=int(window),
+                       out_dtype=OUT_DTYPES[out_dtype] if isinstance(out_dtype, str) else int(out_dtype))
+    for name, val in (("q_stride", q_stride), ("k_stride", k_stride), ("v_stride", v_stride), ("o_stride", o_stride)):
+        setattr(d, name, _strides_t(*[int(x) for x in val]))
+    h = C.c_void_p()
+    _check(_lib.ae_span_create(C.byref(d), C.byref(h)))
+    return h.value
+
+
+def ae_span_forward(handle: int, Q: int, K: int, V: int, key_begin: int, key_end: int, span_stride: int, O: int, stats: int = 0,
+                    stream: int = 0) -> None:
+    """Device addresses; key_begin and key_end are 0 but for the mask "spans", stats may be 0."""
+    _check(_lib.ae_span_forward(handle, Q, K, V, key_begin, key_end, span_stride, O, stats, stream))
+
+
+def ae_span_backward_workspace_bytes(handle: int) -> int:
+    n = C.c_size_t()
+    _check(_lib.ae_span_backward_workspace_bytes(handle, C.byref(n)))
+    return n.value
+
+
+def ae_span_backward(handle: int, Q: int, K: int, V: int, key_begin: int, key_end: int, span_stride: int, O: int, dO: int, do_stride, stats: int,
+                     dQ: int, dK: int, dV: int, grad_dtype, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(_lib.ae_span_backward(handle, Q, K, V, key_begin, key_end, span_stride, O, dO, _strides_t(*do_stride), stats, dQ, dK, dV,
+                                 OUT_DTYPES[grad_dtype] if isinstance(grad_dtype, str) else int(grad_dtype), workspace, workspace_bytes, stream))
+
+
+def ae_span_destroy(handle: Optional[int]) -> None:
+    _check(_lib.ae_span_destroy(handle))
+
+
+def ae_span_documents(B: int, L: int, n_docs: int, offsets: int, offset_stride: int, prefix: int, prefix_stride: int, mask, window: int,
+                      key_begin: int, key_end: int, stream: int = 0) -> None:
+    """Device addresses; prefix may be 0."""
+    _check(_lib.ae_span_documents(B, L, n_docs, offsets, offset_stride, prefix, prefix_stride,
+                                  SPAN_MASKS[mask] if isinstance(mask, str) else int(mask), window, key_begin, key_end, stream))
+
+
+class SpanAttentionPlan:
+    """A handle for span attention, for calls of one shape: the layers of a model keep it.  Q [B, H_q, L_q, D_qk], K [B, H_kv, L_k, D_qk],
+    V [B, H_kv, L_k, D_v] (bf16) and out [B, H_q, L_q, D_v] (bf16 or fp32), last dimension contiguous, give shapes, strides and device.
+    cap: scores are bent to cap tanh(s / cap) (0: not); slopes: a host number per query head, times the distance between query and key
+    taken off the score; mask: "none", "causal", "sliding_window" (window keys) or "spans", the key span of every query row given with each call
+    (document_spans makes them for packed documents).  Calls of one plan may run at the same time."""
+
+    def __init__(self, Q, K, V, out, *, scale, cap=0.0, slopes=None, mask="causal", window=0):
+        import torch
+
+        self.handle = None
+        for t in (Q, K, V, out):
+            if not t.is_cuda or t.dim() != 4 or t.stride(3) != 1 or t.device != Q.device:
+                raise ValueError("Q, K, V and O must be 4-D tensors of one device with a contiguous last dimension; there is no CPU path")
+        if any(t.dtype != torch.bfloat16 for t in (Q, K, V)) or out.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("Q, K and V must be bf16, O fp32 or bf16")
+        B, H_q, L_q, D_qk = Q.shape
+        _, H_kv, L_k, D_v = V.shape
+        if tuple(K.shape) != (B, H_kv, L_k, D_qk) or V.shape[0] != B or tuple(out.shape) != (B, H_q, L_q, D_v):
+            raise ValueError("K, V or O does not match Q in shape")
+        _rows_apart(Q, K, V, out)
+        _no_overlap(out)
+        self.handle = ae_span_create(B=B, H_q=H_q, H_kv=H_kv, L_q=L_q, L_k=L_k, D_qk=D_qk, D_v=D_v, scale=scale, cap=cap, slopes=slopes, mask=mask,
+                                     window=window, out_dtype="bf16" if out.dtype == torch.bfloat16 else "f32", q_stride=Q.stride()[:3],
+                                     k_stride=K.stride()[:3], v_stride=V.stride()[:3], o_stride=out.stride()[:3])
+        self.device, self._given, self._rows = Q.device, mask in ("spans", 3), (B, H_q, L_q)
+        self._specs = [_shape_of(t) for t in (Q, K, V, out)]
+        self._grad_shapes = [tuple(t.shape) for t in (Q, K, V)]
+        self._types = (torch.bfloat16, torch.float32, torch.int32, torch.uint8)
+        self.workspace_bytes = ae_span_backward_workspace_bytes(self.handle)
+
+    def _spans(self, spans):
+        if (spans is not None) != self._given:
+            raise ValueError('spans are given exactly with mask "spans"')
+        if spans is None:
+            return 0, 0, 0
+        begin, end = spans
+        B, _, L_q = self._rows
+        for t in (begin, end):
+            if (t.dtype != self._types[2] or t.device != self.device or tuple(t.shape) not in ((L_q,), (B, L_q)) or t.shape != begin.shape
+                    or (L_q > 1 and t.stride(-1) != 1) or t.stride() != begin.stride()):
+                raise ValueError("spans must be a pair of int32 device tensors [L_q] or [B, L_q] of the same strides, with contiguous rows")
+        return begin.data_ptr(), end.data_ptr(), begin.stride(0) if begin.dim() == 2 else 0
+
+    def _check_stats(self, stats):
+        if stats.dtype != self._types[1] or tuple(stats.shape) != self._rows or not stats.is_contiguous() or stats.device != self.device:
+            raise ValueError("stats must be a contiguous fp32 tensor [B, H_q, L_q]")
+        return stats.data_ptr()
+
+    def forward(self, Q, K, V, out, *, spans=None, stats=None, stream=None):
+        """Writes and returns out; spans: (begin, end), int32 [B, L_q] or [L_q]; stats: fp32 [B, H_q, L_q] that receives ln sum exp."""
+        if [_shape_of(t) for t in (Q, K, V, out)] != self._specs:
+            raise ValueError("a tensor differs from the plan's in shape, strides, type or device")
+        _enqueue(ae_span_forward, self.device, stream, self.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), *self._spans(spans), out.data_ptr(),
+                 0 if stats is None else self._check_stats(stats))
+        return out
+
+    def backward(self, Q, K, V, out, dO, stats, dQ, dK, dV, *, spans=None, stream=None):
+        """Gradients for those of the output, dO bf16 [B, H_q, L_q, D_v] (last dimension contiguous); out and stats are what forward() wrote; dQ, dK,
+        dV: contiguous, all fp32 or all bf16.  The workspace is allocated on the stream that the call is on."""
+        import torch
+
+        if [_shape_of(t) for t in (Q, K, V, out)] != self._specs:
+            raise ValueError("a tensor differs from the plan's in shape, strides, type or device")
+        if dO.dtype != self._types[0] or dO.shape != out.shape or dO.device != self.device or dO.stride(3) != 1:
+            raise ValueError("dO must be a bf16 device tensor of O's shape with a contiguous last dimension")
+        _rows_apart(dO)
+        for t, shape in zip((dQ, dK, dV), self._grad_shapes):
+            if tuple(t.shape) != shape or t.dtype != dQ.dtype or t.dtype not in self._types[:2] or not t.is_contiguous() or t.device != self.device:
+                raise ValueError("dQ, dK and dV must be contiguous device tensors of the shapes of Q, K and V, all fp32 or all bf16")
+        given, at = self._spans(spans), self._check_stats(stats)
+        if stream is None:
+            ws = torch.empty(self.workspace_bytes, dtype=self._types[3], device=self.device)
+        else:
+            with _memory_of(stream):
+                ws = torch.empty(self.workspace_bytes, dtype=self._types[3], device=self.device)
+        _enqueue(ae_span_backward, self.device, stream, self.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), *given, out.data_ptr(), dO.data_ptr(),
+                 dO.stride()[:3], at, dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), 1 if dQ.dtype == self._types[0] else 0, ws.data_ptr(),
+                 self.workspace_bytes)
+        return dQ, dK, dV
+
+    def __del__(self):
+        if getattr(self, "handle", None) is not None and _lib is not None:
+            _lib.ae_span_destroy(self.handle)
+            self.handle = None
+
+
+def span_attention_forward(Q, K, V, *, scale, cap=0.0, slopes=None, mask="causal", window=0, spans=None, out=None, out_dtype=None, stats=None,
+                           stream=None):
+    """Softmax attention on bf16 device tensors Q [B, H_q, L_q, D_qk], K, V [B, H_kv, L_k, D] (last dimension contiguous), every query row over a span of
+    keys; scores scale q k, capped by cap tanh(s / cap) where cap > 0, less slopes[h] |i + L_k - L_q - j| where slopes (H_q host
+    numbers) are given.  mask: "none", "causal", "sliding_window" with window, or "spans" with spans = (begin, end), int32 [B, L_q] or [L_q]: row i
+    sees begin <= j < end.  Returns O [B, H_q, L_q, D_v], fp32 or bf16 (out / out_dtype); stats: optional fp32 [B, H_q, L_q] that receives
+    ln sum exp, which span_attention_backward needs."""
+    import torch
+
+    if out is None:
+        with _memory_of(stream):
+            out = torch.empty(Q.shape[:3] + V.shape[3:], dtype=out_dtype or torch.float32, device=Q.device)
+    plan = SpanAttentionPlan(Q, K, V, out, scale=scale, cap=cap, slopes=slopes, mask=mask, window=window)
+    return plan.forward(Q, K, V, out, spans=spans, stats=stats, stream=stream)
+
+
+def span_attention_backward(Q, K, V, O, dO, stats, *, scale, cap=0.0, slopes=None, mask="causal", window=0, spans=None, grad_dtype=None, stream=None):
+    """Gradients (dQ, dK, dV) of sum(O * dO) for span_attention_forward (arguments as there; O and stats are what it gave), fp32, or bf16 with
+    grad_dtype=torch.bfloat16."""
+    import torch
+
+    plan = SpanAttentionPlan(Q, K, V, O, scale=scale, cap=cap, slopes=slopes, mask=mask, window=window)
+    with _memory_of(stream):
+        grads = [torch.empty(t.shape, dtype=grad_dtype or torch.float32, device=Q.device) for t in (Q, K, V)]
+    return plan.backward(Q, K, V, O, dO, stats, *grads, spans=spans, stream=stream)
+
+
+def document_spans(offsets, L, *, mask="causal", window=0, prefix=None, out=None, stream=None):
+    """The spans of documents packed in rows of L tokens, as (begin, end), int32 [B, L]: document d of row b is the tokens
+    offsets[b, d] <= i < offsets[b, d + 1] (int32 device tensor [B, n_docs + 1], or [n_docs + 1] for one row; never falling; tokens outside see
+    nothing).  mask: "none" (a token sees its document), "causal" (up to itself) or "sliding_window" (of that the nearest window keys); prefix: int32
+    [B, n_docs] or [n_docs], so many first tokens of a document are seen by all of it."""
+    import torch
+
+    rows = offsets.dim()
+    if not offsets.is_cuda or offsets.dtype != torch.int32 or rows not in (1, 2) or offsets.shape[-1] < 2 or offsets.stride(-1) != 1:
+        raise ValueError("offsets must be an int32 device tensor [B, n_docs + 1] or [n_docs + 1] with contiguous rows; there is no CPU path")
+    B, n = offsets.shape[0] if rows == 2 else 1, offsets.shape[-1] - 1
+    if prefix is not None and (prefix.dtype != torch.int32 or tuple(prefix.shape) not in (((n,), (B, n)) if B == 1 else ((B, n),)) or prefix.device != offsets.device
+                               or (n > 1 and prefix.stride(-1) != 1)):
+        raise ValueError("prefix must be an int32 device tensor [B, n_docs] (or [n_docs] for one row) with contiguous rows")
+    if out is None:
+        with _memory_of(stream):
+            out = tuple([torch.empty((B, L), dtype=torch.int32, device=offsets.device) for _ in range(2)])
+    if any(t.dtype != torch.int32 or tuple(t.shape) != (B, L) or not t.is_contiguous() or t.device != offsets.device for t in out):
+        raise ValueError("the outputs must be contiguous int32 device tensors [B, L]")
+    _enqueue(ae_span_documents, offsets.device, stream, B, L, n, offsets.data_ptr(), offsets.stride(0) if rows == 2 else 0,
+             0 if prefix is None else prefix.data_ptr(), prefix.stride(0) if prefix is not None and prefix.dim() == 2 else 0, mask, window,
+             out[0].data_ptr(), out[1].data_ptr())
+    return out

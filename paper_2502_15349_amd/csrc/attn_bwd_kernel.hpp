@@ -75,6 +75,22 @@ struct BwdParams {
   int cut;  // a group's workgroups go to 2^cut XCDs in turn (see group_cut)
 };
 
+// Span attention (VAR of a configuration: 0 none, else BWD_SPAN with BWD_CAP and BWD_SLOPE): every query row sees the keys of its span.  The
+// decay table holds the slopes times log2(e).
+enum : int { BWD_SPAN = 1, BWD_CAP = 2, BWD_SLOPE = 4 };
+// What 32 query rows see: the first key that some row does, the first behind the last one, and the keys [last_lo, least_hi) that all of
+// them do.  (A row that sees none counts in least_hi alone, as 0; first is 2^31 - 1 where all rows are such.)
+struct SpanBlock {
+  int32_t first, behind, last_lo, least_hi;
+};
+struct BwdSpanParams : BwdParams {
+  const int32_t *begin, *end;  // [B, L_q], cut to the keys that there are (0, 0: none)
+  const SpanBlock* blocks;     // [B, ceil(L_q / 32)]
+  CapParams cap;
+  int64_t dos[3];              // element strides {batch, head, row} of dO
+  int grad_bf16;               // dQ, dK and dV are bf16
+};
+
 // Chunk swizzle of the backward tiles.  A tile row is read both ways -- 128-bit row
 // fragments, 16 lanes = 16 consecutive rows at a time, and 64-bit transposing loads, 32
 // lanes = 4 consecutive rows x 4 chunks at a time -- so the XOR pattern takes 16 values
@@ -96,8 +112,11 @@ __device__ __forceinline__ bool factor_hidden(float f) { return __builtin_bit_ca
 enum : int { BWD_DQ = 0, BWD_DKV = 1 };  // the query-side kernel (dQ), the key-side kernel (dK and dV)
 
 // ---- one wavefront per 32 own rows ---------------------------------------------------------------------------------
-template <int DQK_, int DV_, int NORM_, bool CAUSAL_, int OUT_, bool BIAS_ = false>
+template <int DQK_, int DV_, int NORM_, bool CAUSAL_, int OUT_, bool BIAS_ = false, int VAR_ = 0>
 struct BwdCfg {
+  static constexpr bool SPAN = VAR_ != 0, CAPPED = (VAR_ & BWD_CAP) != 0, SLOPED = (VAR_ & BWD_SLOPE) != 0;
+  typedef std::conditional_t<SPAN, BwdSpanParams, BwdParams> P;
+  static_assert(!SPAN || (NORM_ == NORM_SOFTMAX && !CAUSAL_ && !BIAS_), "spans: softmax, no other mask, no bias tensor");
   static constexpr bool BIAS = BIAS_;  // S' = scale * S + bias[b, h_q, i, j]
   static constexpr int DQK = DQK_, DV = DV_, NORM = NORM_, OUT = OUT_;
   static constexpr bool CAUSAL = CAUSAL_, KV_SIDE = OUT_ == BWD_DKV;
@@ -112,7 +131,8 @@ struct BwdCfg {
   static constexpr int Y1_BYTES = TILE * RB1, Y2_BYTES = TILE * RB2, STAGE_BYTES = Y1_BYTES + Y2_BYTES;
   // per stage: bias*log2(e) - lse*log2(e) and delta of the tile's rows (key side: they belong to the registers' rows;
   // on the query side they belong to the lane's own row and stay in registers)
-  static constexpr int ROW_BYTES = KV_SIDE ? 2 * TILE * 4 : 0;
+  // (spans: and the first key and the first behind the last one that those rows see)
+  static constexpr int ROW_BYTES = KV_SIDE ? (SPAN ? 4 : 2) * TILE * 4 : 0;
   // bias tensor: per stage the block of it that the tile meets, 16 KB: [128 own queries][64 keys] on the query
   // side, [64 queries][128 own keys] on the key side
   static constexpr int BIAS_BYTES = BIAS_ ? 16384 : 0;
@@ -134,6 +154,88 @@ struct BwdCfg {
   static_assert((TILE * CPR1 / 64) % WAVES == 0 && (TILE * CPR2 / 64) % WAVES == 0, "every wave copies the same number of blocks");
 };
 
+// dO of a q head: contiguous, but for spans
+template <class C>
+__device__ __forceinline__ const __bf16* do_rows(const typename C::P& p, int b, int hq) {
+  if constexpr (C::SPAN) return p.dO + b * p.dos[0] + hq * p.dos[1];
+  else return p.dO + ((int64_t)b * p.H_q + hq) * p.L_q * C::DV;
+}
+template <class C>
+__device__ __forceinline__ const __bf16* do_row(const typename C::P& p, int b, int hq, int i) {
+  if constexpr (C::SPAN) return p.dO + b * p.dos[0] + hq * p.dos[1] + i * p.dos[2];
+  else return p.dO + (((int64_t)b * p.H_q + hq) * p.L_q + i) * C::DV;
+}
+template <class C>
+__device__ __forceinline__ int64_t do_stride(const typename C::P& p) {
+  if constexpr (C::SPAN) return p.dos[2];
+  else return C::DV;
+}
+// (through the scalar cache: an earlier launch wrote it)
+__device__ __forceinline__ SpanBlock load_block(const SpanBlock* at) {
+  typedef __attribute__((ext_vector_type(4))) int i32x4;
+  const i32x4 v = *reinterpret_cast<const __attribute__((address_space(4))) i32x4*>((uintptr_t)uniform_ptr(at));
+  return {v[0], v[1], v[2], v[3]};
+}
+// Tiles of TILE other rows that own rows [own0, own0 + OWN) need: queries whose span has one of these keys (key side), keys of their
+// spans (query side).  Spans need not be sorted; the walk takes the tiles between the first and the last one.  Every wave forms them.
+template <class C>
+__device__ __forceinline__ void span_walk(const BwdSpanParams& p, int b, int own0, int& t_first, int& t_end) {
+  const int nb = (p.L_q + 31) / 32;
+  const SpanBlock* blocks = p.blocks + (int64_t)b * nb;
+  int first = 0x7fffffff, behind = 0;
+  if constexpr (C::KV_SIDE) {
+    for (int k = threadIdx.x & 63; k < nb; k += 64) {
+      const SpanBlock s = blocks[k];
+      if (s.first < own0 + C::OWN && s.behind > own0) {
+        first = min(first, 32 * k);
+        behind = 32 * k + 32;
+      }
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      first = min(first, __shfl_xor(first, s));
+      behind = max(behind, __shfl_xor(behind, s));
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    behind = __builtin_amdgcn_readfirstlane(behind);
+  } else {
+#pragma unroll
+    for (int k = 0; k < C::OWN / 32; ++k)
+      if (own0 / 32 + k < nb) {
+        const SpanBlock s = load_block(blocks + own0 / 32 + k);
+        first = min(first, s.first);
+        behind = max(behind, s.behind);
+      }
+  }
+  t_end = (behind + C::TILE - 1) / C::TILE;
+  t_first = behind > 0 ? first / C::TILE : 0;
+}
+// Whether any own row of a wave (from ow0 on) meets a row of the 32 other rows from o0 on, and whether all meet all.  s: what these (key
+// side) or the own rows (query side) see.
+template <class C>
+__device__ __forceinline__ void span_visibility(const BwdSpanParams& p, const SpanBlock& s, int ow0, int o0, bool& any, bool& full) {
+  if constexpr (C::KV_SIDE) {
+    any = o0 < p.L_q && s.first < ow0 + 32 && s.behind > ow0;
+    full = o0 + 31 < p.L_q && s.last_lo <= ow0 && s.least_hi >= min(ow0 + 32, p.L_k);
+  } else {
+    any = s.first < o0 + 32 && s.behind > o0;
+    full = s.last_lo <= o0 && s.least_hi >= o0 + 32;
+  }
+}
+// Four neighbouring values of a result, whose element `to` they are of the fp32 tensor at `base`; spans: of the bf16 tensor there.
+template <class C>
+__device__ __forceinline__ void store_result(const typename C::P& p, float* base, float* to, f32x4 v) {
+  if constexpr (C::SPAN)
+    if (p.grad_bf16) {
+      bf16x4 h;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = (__bf16)v[e];
+      *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(base) + (to - base)) = h;
+      return;
+    }
+  *reinterpret_cast<f32x4*>(to) = v;
+}
+
 __device__ __forceinline__ bf16x8 read_tr_frag(uint32_t addr_lo, uint32_t addr_hi) {
   const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)addr_lo);
   const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)addr_hi);
@@ -149,7 +251,7 @@ __device__ __forceinline__ bf16x8 pack8(const float (&x)[16], int t) {
 }
 
 template <class C>
-__device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayTable& dt, int block, uint32_t lds0) {
+__device__ __forceinline__ void bwd_single_walk(const typename C::P& p, const DecayTable& dt, int block, uint32_t lds0) {
   const uint32_t rows0 = lds0 + 2 * C::STAGE_BYTES;
   const uint32_t bias0 = rows0 + 2 * C::ROW_BYTES;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -178,7 +280,7 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
   const __bf16* x1 = C::KV_SIDE ? p.K + b * p.ks[0] + hk * p.ks[1] + (int64_t)own_c * p.ks[2]
                                 : p.Q + b * p.qs[0] + ho * p.qs[1] + (int64_t)own_c * p.qs[2];
   const __bf16* x2 = C::KV_SIDE ? p.V + b * p.vs[0] + hk * p.vs[1] + (int64_t)own_c * p.vs[2]
-                                : p.dO + (((int64_t)b * p.H_q + ho) * p.L_q + own_c) * C::DV;
+                                : do_row<C>(p, b, ho, own_c);
   bf16x8 xb1[C::T1], xb2[C::T2];
 #pragma unroll
   for (int t = 0; t < C::T1; ++t) xb1[t] = *reinterpret_cast<const bf16x8*>(x1 + (2 * t + half) * 8);
@@ -196,6 +298,16 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
       dl_own = p.delta[r];
     }
   }
+  // Spans, query side: the keys of the lane's own row; slopes: log2(e) times that of the q head at hand
+  int span_lo = 0, span_hi = 0;
+  float sl = 0.f;
+  if constexpr (C::SPAN && !C::KV_SIDE) {
+    if (own < p.L_q) {
+      span_lo = p.begin[(int64_t)b * p.L_q + own];
+      span_hi = p.end[(int64_t)b * p.L_q + own];
+    }
+  }
+  if constexpr (C::SLOPED) sl = dt.log2_gamma[C::KV_SIDE ? hk * p.g : ho];
   // Abs-sum family, no normalization: log2 of the decay rate of the q head at hand (0: no decay), and, for sub-tiles whose entries are
   // all visible, what the decay factor of register 4 q + e is of the largest one (register 0 on the key side, 15 on the query side).
   // An exponential and a dozen instructions of index and visibility per entry took the vector unit longer than the products take:
@@ -235,6 +347,11 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
       if (t_first > t_end) t_first = t_end;
     }
   }
+  SpanBlock own_block{0x7fffffff, 0, 0, 0};  // spans, query side: what the wave's own rows see
+  if constexpr (C::SPAN) {
+    span_walk<C>(p, b, own0, t_first, t_end);
+    if (!C::KV_SIDE && ow0 < p.L_q) own_block = load_block(p.blocks + (int64_t)b * ((p.L_q + 31) / 32) + ow0 / 32);
+  }
   const int nt = t_end - t_first;
   const int total = C::KV_SIDE ? nt * p.g : nt;
 
@@ -244,8 +361,8 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
     const int hq = C::KV_SIDE ? hk * p.g + n / nt : ho;
     const int r0 = (t_first + (C::KV_SIDE ? n % nt : n)) * C::TILE;
     const __bf16* y1 = C::KV_SIDE ? p.Q + b * p.qs[0] + hq * p.qs[1] : p.K + b * p.ks[0] + hk * p.ks[1];
-    const __bf16* y2 = C::KV_SIDE ? p.dO + ((int64_t)b * p.H_q + hq) * p.L_q * C::DV : p.V + b * p.vs[0] + hk * p.vs[1];
-    const int64_t s1 = C::KV_SIDE ? p.qs[2] : p.ks[2], s2 = C::KV_SIDE ? (int64_t)C::DV : p.vs[2];
+    const __bf16* y2 = C::KV_SIDE ? do_rows<C>(p, b, hq) : p.V + b * p.vs[0] + hk * p.vs[1];
+    const int64_t s1 = C::KV_SIDE ? p.qs[2] : p.ks[2], s2 = C::KV_SIDE ? do_stride<C>(p) : p.vs[2];
     const uint32_t base = lds0 + stage * C::STAGE_BYTES;
 #pragma unroll
     for (int i = 0; i < C::TILE * C::CPR1 / 64 / C::WAVES; ++i) {
@@ -292,6 +409,12 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
   auto load_rowq = [&](int n) -> float {
     float v = 0.f;
     if constexpr (C::KV_SIDE && C::ROWS) {
+      if constexpr (C::SPAN) {
+        if (wave >= 2) {  // waves 2 and 3: the rows' spans, as they are
+          const int i = (t_first + n % nt) * C::TILE + lane;
+          if (i < p.L_q) v = __builtin_bit_cast(float, (wave == 2 ? p.begin : p.end)[(int64_t)b * p.L_q + i]);
+        }
+      }
       if (wave < 2 && lane < C::TILE) {
         const int hq = hk * p.g + n / nt;
         const int i = (t_first + n % nt) * C::TILE + lane;
@@ -305,7 +428,7 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
   };
   auto store_rowq = [&](float v, int stage) {
     if constexpr (C::KV_SIDE && C::ROWS) {
-      if (wave < 2 && lane < C::TILE) {
+      if (wave < (C::SPAN ? 4 : 2) && lane < C::TILE) {
         if (wave == 0) v = C::ABS ? fast_rcp(fmaxf(fabsf(v), 1.f)) : v == -INFINITY ? -INFINITY : p.b2 - v * 1.4426950408889634f;
         *reinterpret_cast<__attribute__((address_space(3))) float*>(
             (lds_char*)(uintptr_t)(rows0 + stage * C::ROW_BYTES + wave * C::TILE * 4 + lane * 4)) = v;
@@ -362,6 +485,11 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
     constexpr int STAGE = decltype(stagec)::value, SUB = decltype(subc)::value;
     // anything visible to this wave's rows?  everything?
     bool any = o0 < L_oth, full = o0 + 31 < L_oth;
+    if constexpr (C::SPAN) {
+      SpanBlock sb = own_block;
+      if constexpr (C::KV_SIDE) sb = load_block(p.blocks + (int64_t)b * ((p.L_q + 31) / 32) + min(o0, p.L_q - 1) / 32);
+      span_visibility<C>(p, sb, ow0, o0, any, full);
+    }
     if constexpr (C::CAUSAL) {
       const int wd = p.window;
       if constexpr (C::KV_SIDE) {  // own = keys j, other = queries i: visible iff i + off - window < j <= i + off
@@ -421,8 +549,15 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
       for (int t = 0; t < C::T2; ++t) dp = mfma(read_k_frag(ar2[t] + kRow2), xb2[t], dp);
     }
     float x[16];
+    if constexpr (C::CAPPED) cap_scores<16>(s, p.cap);  // (kept: the cap's derivative follows from them)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(s[r], p.c2, C::NORM == NORM_SOFTMAX ? nl4[r / 4][r % 4] : p.b2);
+    for (int r = 0; r < 16; ++r)
+      x[r] = C::CAPPED ? s[r] + nl4[r / 4][r % 4] : __builtin_fmaf(s[r], p.c2, C::NORM == NORM_SOFTMAX ? nl4[r / 4][r % 4] : p.b2);
+    if constexpr (C::SLOPED) {
+      const float d0 = (float)(C::KV_SIDE ? o0 + off - own + 4 * half : own + off - o0 - 4 * half);  // query less key, register 0
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(-sl, __builtin_fabsf(C::KV_SIDE ? d0 + (float)key_offset(r) : d0 - (float)key_offset(r)), x[r]);
+    }
     if constexpr (C::BIAS) {
       // register r = 4 q4 + e is (query, key) = (own row, key 8 q4 + 4 half + e of the sub-tile) on the query side,
       // (query 8 q4 + 4 half + e of the sub-tile, own key) on the key side
@@ -456,10 +591,23 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
     float f[C::LIN ? 16 : 1];  // decay factors
     if (!full) {  // a hidden entry gets the exponent (or the factors) that make its weight exactly 0
       sched_fence();  // (keeps this a branch: most sub-tiles skip it)
+      f32x4 lo4[4], hi4[4];  // spans, key side: of the 16 rows
+      if constexpr (C::SPAN && C::KV_SIDE) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          lo4[q] = lds_read16(lds0 + kRq + 2 * C::TILE * 4 + (8 * q + 4 * half) * 4);
+          hi4[q] = lds_read16(lds0 + kRq + 3 * C::TILE * 4 + (8 * q + 4 * half) * 4);
+        }
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int oth = o0 + key_offset(r) + 4 * half;
         bool vis = oth < L_oth;
+        if constexpr (C::SPAN) {
+          const float lo = lo4[r / 4][r % 4], hi = hi4[r / 4][r % 4];
+          if constexpr (C::KV_SIDE) vis = vis && own >= __builtin_bit_cast(int, lo) && own < __builtin_bit_cast(int, hi);
+          else vis = oth >= span_lo && oth < span_hi;
+        }
         if constexpr (C::CAUSAL)
           vis = vis && (C::KV_SIDE ? own <= oth + off && oth + off - p.window < own : oth <= own + off && own + off - p.window < oth);
         x[r] = vis ? x[r] : C::LIN ? 0.f : -INFINITY;
@@ -485,6 +633,7 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
         pv = fast_exp2(x[r]);
         if constexpr (C::HAS2) w2[r] = pv;
         pv = pv * (dp[r] - dl4[r / 4][r % 4]);
+        if constexpr (C::CAPPED) pv *= cap_slope(s[r], p.cap.inv);
       } else if constexpr (C::NORM == NORM_SIGMOID) {
         pv = fast_rcp(1.f + fast_exp2(-x[r]));
         if constexpr (C::HAS2) w2[r] = pv;
@@ -558,6 +707,8 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
     const int r0 = (t_first + (C::KV_SIDE ? n % nt : n)) * C::TILE;
     if constexpr (C::KV_SIDE && C::LIN)
       if (n % nt == 0) set_decay(hk * p.g + n / nt);
+    if constexpr (C::KV_SIDE && C::SLOPED)
+      if (n % nt == 0) sl = dt.log2_gamma[hk * p.g + n / nt];
     subtile(stagec, std::integral_constant<int, 0>{}, r0);
     subtile(stagec, std::integral_constant<int, 1>{}, r0 + 32);
     if (n + 1 < total) store_rowq(rowq_next, STAGE ^ 1);
@@ -576,6 +727,7 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
 #pragma unroll
   for (int t = 0; t < C::T2; ++t) asm volatile("" ::"v"(xb2[t]));
   asm volatile("" ::"v"(nl_own), "v"(dl_own));
+  if constexpr (C::SPAN) asm volatile("" ::"v"(span_lo), "v"(span_hi));
   for (int n = 0; n < total; n += 2) {
     tile(std::integral_constant<int, 0>{}, n);
     if (n + 1 < total) tile(std::integral_constant<int, 1>{}, n + 1);
@@ -590,17 +742,25 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
 #pragma unroll
     for (int db = 0; db < C::DB; ++db)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4*>(o + 32 * db + 8 * q + 4 * half) =
-            f32x4{g[db][4 * q] * f, g[db][4 * q + 1] * f, g[db][4 * q + 2] * f, g[db][4 * q + 3] * f};
+      for (int q = 0; q < 4; ++q) {
+        if constexpr (C::SPAN)
+          store_result<C>(p, C::KV_SIDE ? p.dK : p.dQ, o + 32 * db + 8 * q + 4 * half,
+                          f32x4{g[db][4 * q] * f, g[db][4 * q + 1] * f, g[db][4 * q + 2] * f, g[db][4 * q + 3] * f});
+        else
+          *reinterpret_cast<f32x4*>(o + 32 * db + 8 * q + 4 * half) =
+              f32x4{g[db][4 * q] * f, g[db][4 * q + 1] * f, g[db][4 * q + 2] * f, g[db][4 * q + 3] * f};
+      }
     if constexpr (C::HAS2) {
       float* o2 = p.dV + (((int64_t)b * p.H_kv + hk) * p.L_k + own) * C::DV;
 #pragma unroll
       for (int db = 0; db < C::DB2; ++db)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<f32x4*>(o2 + 32 * db + 8 * q + 4 * half) =
-              f32x4{g2[db][4 * q], g2[db][4 * q + 1], g2[db][4 * q + 2], g2[db][4 * q + 3]};
+          if constexpr (C::SPAN)
+            store_result<C>(p, p.dV, o2 + 32 * db + 8 * q + 4 * half, f32x4{g2[db][4 * q], g2[db][4 * q + 1], g2[db][4 * q + 2], g2[db][4 * q + 3]});
+          else
+            *reinterpret_cast<f32x4*>(o2 + 32 * db + 8 * q + 4 * half) =
+                f32x4{g2[db][4 * q], g2[db][4 * q + 1], g2[db][4 * q + 2], g2[db][4 * q + 3]};
     }
   }
 }
@@ -624,8 +784,11 @@ __device__ __forceinline__ void bwd_single_walk(const BwdParams& p, const DecayT
 // Deeper rings, more products in front of the weights, raised wave priority: no difference.  The query side's copies all
 // go with role 1, which has less to do there (role 0 or both: 2 % more).  Against two workgroups per CU where those
 // fit (64/64; 128/128 query side, 4 x 32/8 x 2048 212) the pair takes longer (128/128 query side 250): the choice in bwd_launch.hpp.
-template <int DQK_, int DV_, int NORM_, bool CAUSAL_, int OUT_, bool BIAS_ = false>
+template <int DQK_, int DV_, int NORM_, bool CAUSAL_, int OUT_, bool BIAS_ = false, int VAR_ = 0>
 struct BwdPairCfg {
+  static constexpr bool SPAN = VAR_ != 0, CAPPED = (VAR_ & BWD_CAP) != 0, SLOPED = (VAR_ & BWD_SLOPE) != 0;
+  typedef std::conditional_t<SPAN, BwdSpanParams, BwdParams> P;
+  static_assert(!SPAN || (NORM_ == NORM_SOFTMAX && !CAUSAL_ && !BIAS_), "spans: softmax, no other mask, no bias tensor");
   static constexpr bool BIAS = BIAS_;
   static constexpr int DQK = DQK_, DV = DV_, NORM = NORM_, OUT = OUT_;
   static constexpr bool CAUSAL = CAUSAL_, KV_SIDE = OUT_ == BWD_DKV;
@@ -639,7 +802,7 @@ struct BwdPairCfg {
   static constexpr int RB1 = DQK * 2, RB2 = DV * 2, CPR1 = DQK / 8, CPR2 = DV / 8;
   static constexpr int Y1_BYTES = TILE * RB1, Y2_BYTES = TILE * RB2, BIAS_BYTES = BIAS_ ? 8192 : 0;
   static constexpr int STAGE_BYTES = Y1_BYTES + Y2_BYTES + BIAS_BYTES;
-  static constexpr int ROW_BYTES = ROWQ ? 512 : 0;  // per stage: [64] statistic, [64] delta (32 of each are used)
+  static constexpr int ROW_BYTES = ROWQ ? (SPAN ? 1024 : 512) : 0;  // per stage: [64] statistic, [64] delta, spans: [64] begin, [64] end (32 of each are used)
   static constexpr int STAGES = 5 * (STAGE_BYTES + ROW_BYTES) + 2 * 4 * 4096 <= 160 * 1024 ? 5 : 4, LOOK = STAGES - 2;
   static constexpr int ROWS0 = STAGES * STAGE_BYTES, E0 = ROWS0 + STAGES * ROW_BYTES, E_PAIR = KV_SIDE ? 4096 : 2048, E_BYTES = 4 * E_PAIR;
   static constexpr int LDS_BYTES = E0 + 2 * E_BYTES;
@@ -680,7 +843,7 @@ __device__ __forceinline__ void lds_store16(uint32_t addr, u32x4 v) {
 }
 
 template <class C>
-__device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTable& dt, int block, uint32_t lds0) {
+__device__ __forceinline__ void bwd_pair_walk(const typename C::P& p, const DecayTable& dt, int block, uint32_t lds0) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w4 = wave & 3;
   const int ln = lane & 31, half = lane >> 5;
   const int off = p.L_k - p.L_q;
@@ -716,6 +879,11 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
       if (t_first > t_end) t_first = t_end;
     }
   }
+  SpanBlock span_block{0x7fffffff, 0, 0, 0};  // spans: what the wave's own rows see (query side), the queries of the tile at hand (key side)
+  if constexpr (C::SPAN) {
+    span_walk<C>(p, b, own0, t_first, t_end);
+    if (!C::KV_SIDE && ow0 < p.L_q) span_block = load_block(p.blocks + (int64_t)b * ((p.L_q + 31) / 32) + ow0 / 32);
+  }
   const int N = (t_end - t_first) * (C::KV_SIDE ? p.g : 1);
   struct Pos {  // a position of the walk: tile t of q head h
     int t, h;
@@ -737,7 +905,7 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
     constexpr int NCQ = C::COPIER == 2 ? 2 : 1, Q0 = C::COPIER == 2 ? ROLE : 0;  // copy k is group k NCQ + Q0
 
     // ---- copies ----
-    const int64_t s1 = C::KV_SIDE ? p.qs[2] : p.ks[2], s2 = C::KV_SIDE ? (int64_t)C::DV : p.vs[2];
+    const int64_t s1 = C::KV_SIDE ? p.qs[2] : p.ks[2], s2 = C::KV_SIDE ? do_stride<C>(p) : p.vs[2];
     const int tail = (L_oth - 1) % C::TILE;  // the last tile's last row: rows past it repeat it
     constexpr int PER1 = C::copy_period(C::CPR1), PER2 = C::copy_period(C::CPR2);
     auto copy_offset = [&](auto cprc, int Q, int64_t stride, int last) {  // the lane's byte offset from the tile's first row, group Q
@@ -767,7 +935,7 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
     const __bf16 *y1, *y2;
     auto head_start = [&]() {
       y1 = (C::KV_SIDE ? p.Q + b * p.qs[0] + ahead.h * p.qs[1] : p.K + b * p.ks[0] + hk * p.ks[1]) + (int64_t)t_first * C::TILE * s1;
-      y2 = (C::KV_SIDE ? p.dO + ((int64_t)b * p.H_q + ahead.h) * p.L_q * C::DV : p.V + b * p.vs[0] + hk * p.vs[1]) + (int64_t)t_first * C::TILE * s2;
+      y2 = (C::KV_SIDE ? do_rows<C>(p, b, ahead.h) : p.V + b * p.vs[0] + hk * p.vs[1]) + (int64_t)t_first * C::TILE * s2;
     };
     head_start();
     const int h_last = h_first + (C::KV_SIDE ? p.g : 1) - 1;
@@ -829,6 +997,13 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
           if constexpr (ROLE == 0 || C::COPIER == 1) dma4(p.lse + row0, (uint32_t)i * 4u, rows);
           if constexpr (ROLE == 1 || C::COPIER == 0) dma4(p.delta + row0, (uint32_t)i * 4u, rows + 256);
         }
+        if constexpr (C::SPAN)
+          if (NC > 0 && w4 == 1) {
+            const int i = min(ahead.t * C::TILE + lane, p.L_q - 1);
+            const uint32_t rows = lds0 + C::ROWS0 + ST * C::ROW_BYTES;
+            if constexpr (ROLE == 0 || C::COPIER == 1) dma4(p.begin + (int64_t)b * p.L_q, (uint32_t)i * 4u, rows + 512);
+            if constexpr (ROLE == 1 || C::COPIER == 0) dma4(p.end + (int64_t)b * p.L_q, (uint32_t)i * 4u, rows + 768);
+          }
       }
     };
     auto all_copies = [&](auto copyc) {
@@ -849,6 +1024,7 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
     // anything of the tile visible to this wave's rows?  everything?
     auto visibility = [&](int o0, bool& any, bool& full) {
       any = o0 < L_oth, full = o0 + 31 < L_oth;
+      if constexpr (C::SPAN) span_visibility<C>(p, span_block, ow0, o0, any, full);
       if constexpr (C::CAUSAL) {
         const int wd = p.window;
         if constexpr (C::KV_SIDE) {  // own = keys j, other = queries i: visible iff i + off - window < j <= i + off
@@ -861,6 +1037,10 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
       }
     };
     Pos here{t_first, h_first};  // the tile this role works on
+    auto take_block = [&]() {
+      if constexpr (C::SPAN && C::KV_SIDE) span_block = load_block(p.blocks + (int64_t)b * ((p.L_q + 31) / 32) + min(here.t, (p.L_q - 1) / 32));
+    };
+    take_block();
 
     // Iteration i of the walk: tiles i and i + 1 have landed (of this wave's copies only the youngest LOOK - 2 tiles'
     // may be in flight), dS' and the weights of tile i - 1 are written (of role 0's LDS operations only the reads of
@@ -889,6 +1069,7 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
     auto next_tile = [&]() {
       advance_copies();
       advance(here);
+      take_block();
       e_lane += e_flip;
       e_flip = 0u - e_flip;
     };
@@ -920,7 +1101,7 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
       const __bf16* x1 = C::KV_SIDE ? p.K + b * p.ks[0] + hk * p.ks[1] + (int64_t)own_c * p.ks[2]
                                     : p.Q + b * p.qs[0] + ho * p.qs[1] + (int64_t)own_c * p.qs[2];
       const __bf16* x2 = C::KV_SIDE ? p.V + b * p.vs[0] + hk * p.vs[1] + (int64_t)own_c * p.vs[2]
-                                    : p.dO + (((int64_t)b * p.H_q + ho) * p.L_q + own_c) * C::DV;
+                                    : do_row<C>(p, b, ho, own_c);
       bf16x8 xb1[T1], xb2[T2];
 #pragma unroll
       for (int t = 0; t < T1; ++t) xb1[t] = *reinterpret_cast<const bf16x8*>(x1 + (2 * t + half) * 8);
@@ -929,6 +1110,15 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
       // query side: the row quantities of the lane's own row (the statistic is converted behind the first copies)
       constexpr bool OWN_ROW = !C::KV_SIDE && C::ROWS;
       float nl_own = OWN_ROW ? (C::ABS ? 0.f : -INFINITY) : C::LIN ? 1.f : -INFINITY, dl_own = 0.f;
+      int span_lo = 0, span_hi = 0;  // spans, query side: the keys of the lane's own row
+      float sl = 0.f;                // slopes: log2(e) times that of the q head at hand
+      if constexpr (C::SPAN && !C::KV_SIDE) {
+        if (own < p.L_q) {
+          span_lo = p.begin[(int64_t)b * p.L_q + own];
+          span_hi = p.end[(int64_t)b * p.L_q + own];
+        }
+      }
+      if constexpr (C::SLOPED) sl = dt.log2_gamma[h_first];
       if constexpr (OWN_ROW) {
         if (own < p.L_q) {
           nl_own = p.lse[((int64_t)b * p.H_q + ho) * p.L_q + own];
@@ -1000,8 +1190,15 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
         static_for<0, T1 + AHEAD>(product);
         if constexpr (C::LIN) read_rows(nl4, nl_own, 0);  // (here: 16 registers less during the products)
         float x[16];
+        if constexpr (C::CAPPED) cap_scores<16>(s, p.cap);  // (kept: the cap's derivative follows from them)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(s[r], p.c2, C::NORM == NORM_SOFTMAX ? nl4[r / 4][r % 4] : p.b2);
+        for (int r = 0; r < 16; ++r)
+          x[r] = C::CAPPED ? s[r] + nl4[r / 4][r % 4] : __builtin_fmaf(s[r], p.c2, C::NORM == NORM_SOFTMAX ? nl4[r / 4][r % 4] : p.b2);
+        if constexpr (C::SLOPED) {
+          const float d0 = (float)(C::KV_SIDE ? o0 + off - own + 4 * half : own + off - o0 - 4 * half);  // query less key, register 0
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(-sl, __builtin_fabsf(C::KV_SIDE ? d0 + (float)key_offset(r) : d0 - (float)key_offset(r)), x[r]);
+        }
         if constexpr (C::BIAS) {
           // register r = 4 q4 + e is (query, key) = (own row, key 8 q4 + 4 half + e of the tile) on the query side,
           // (query 8 q4 + 4 half + e of the tile, own key) on the key side
@@ -1035,10 +1232,20 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
         float f[C::LIN ? 16 : 1];
         if (!full) {  // a hidden entry gets the exponent (or the factors) that make its weight exactly 0
           sched_fence();  // (keeps this a branch: most tiles skip it)
+          f32x4 lo4[4], hi4[4];  // spans, key side: of the 16 rows
+          if constexpr (C::SPAN && C::KV_SIDE) {
+            read_rows(lo4, 0.f, 512);
+            read_rows(hi4, 0.f, 768);
+          }
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int oth = o0 + key_offset(r) + 4 * half;
             bool vis = oth < L_oth;
+            if constexpr (C::SPAN) {
+              const float lo = lo4[r / 4][r % 4], hi = hi4[r / 4][r % 4];
+              if constexpr (C::KV_SIDE) vis = vis && own >= __builtin_bit_cast(int, lo) && own < __builtin_bit_cast(int, hi);
+              else vis = oth >= span_lo && oth < span_hi;
+            }
             if constexpr (C::CAUSAL)
               vis = vis && (C::KV_SIDE ? own <= oth + off && oth + off - p.window < own : oth <= own + off && own + off - p.window < oth);
             x[r] = vis ? x[r] : C::LIN ? 0.f : -INFINITY;
@@ -1087,6 +1294,7 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
           const float dl = dl4[r / 4][r % 4], d = dp[r];
           if constexpr (C::NORM == NORM_SOFTMAX) {
             w[r] = pv[r] * (d - dl);
+            if constexpr (C::CAPPED) w[r] *= cap_slope(s[r], p.cap.inv);
           } else if constexpr (C::NORM == NORM_SIGMOID) {
             w[r] = d * pv[r] * (1.f - pv[r]);
           } else if constexpr (C::LIN) {
@@ -1134,6 +1342,10 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
       for (int t = 0; t < T2; ++t) pin(xb2[t]);
       pin(nl_own);
       pin(dl_own);
+      if constexpr (C::SPAN) {
+        pin(span_lo);
+        pin(span_hi);
+      }
       if constexpr (OWN_ROW) nl_own = convert_stat(nl_own);
       if (N > 0) {
         first_tiles_landed();
@@ -1149,6 +1361,8 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
           sched_fence();
           if constexpr (C::LIN && C::KV_SIDE)
             if (here.t == t_first && n + 1 < N) set_decay(here.h);
+          if constexpr (C::SLOPED && C::KV_SIDE)
+            if (here.t == t_first && n + 1 < N) sl = dt.log2_gamma[here.h];
         });
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // iteration N
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (no copy outlives the workgroup's LDS)
@@ -1274,7 +1488,8 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           if (8 * k < rows)
-            *reinterpret_cast<f32x4*>(db < DB ? o1 + 8 * k * C::DQK + 32 * db : o2 + 8 * k * C::DV + 32 * (db - DB)) = v[db % 2][k];
+            store_result<C>(p, db >= DB ? p.dV : C::KV_SIDE ? p.dK : p.dQ, db < DB ? o1 + 8 * k * C::DQK + 32 * db : o2 + 8 * k * C::DV + 32 * (db - DB),
+                            v[db % 2][k]);
       });
     }
   };
@@ -1284,7 +1499,7 @@ __device__ __forceinline__ void bwd_pair_walk(const BwdParams& p, const DecayTab
 
 // ---- the kernels ----------------------------------------------------------------------------------------------------
 template <class C>
-__device__ __forceinline__ void bwd_walk(const BwdParams& p, const DecayTable& dt, int block, uint32_t lds0) {
+__device__ __forceinline__ void bwd_walk(const typename C::P& p, const DecayTable& dt, int block, uint32_t lds0) {
   if constexpr (C::PAIR) bwd_pair_walk<C>(p, dt, block, lds0);
   else bwd_single_walk<C>(p, dt, block, lds0);
 }
@@ -1294,7 +1509,7 @@ constexpr int bwd_waves_per_simd() { return C::PAIR || C::OCC2 ? 2 : 1; }
 
 // One side.
 template <class C>
-__global__ __launch_bounds__(C::THREADS, bwd_waves_per_simd<C>()) void attn_bwd_kernel(const BwdParams p, const DecayTable dt) {
+__global__ __launch_bounds__(C::THREADS, bwd_waves_per_simd<C>()) void attn_bwd_kernel(const typename C::P p, const DecayTable dt) {
   __shared__ __attribute__((aligned(1024))) char smem[C::LDS_BYTES];
   bwd_walk<C>(p, dt, blockIdx.x, (uint32_t)(uintptr_t)((lds_char*)smem));
 }
@@ -1309,7 +1524,7 @@ struct BwdBoth {
 };
 template <class K, class Q>
 __global__ __launch_bounds__((BwdBoth<K, Q>::THREADS), (BwdBoth<K, Q>::WAVES_PER_SIMD))
-void attn_bwd_both_kernel(const BwdParams p, const DecayTable dt, int key_blocks) {
+void attn_bwd_both_kernel(const typename K::P p, const DecayTable dt, int key_blocks) {
   __shared__ __attribute__((aligned(1024))) char smem[BwdBoth<K, Q>::LDS_BYTES];
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_char*)smem);
   // (wavefronts beyond those of the walk end here: a barrier counts those that are left)

@@ -44,6 +44,7 @@
 #include <type_traits>
 
 #include "launch.hpp"
+#include "span.hpp"
 
 namespace ae {
 
@@ -59,6 +60,8 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 enum : int { NORM_SOFTMAX = 0, NORM_SIGMOID = 1, NORM_ABSSUM = 2, NORM_ABS_OF_SUM = 3, NORM_NONE = 4 };
 enum : int { MOD_PLAIN = 0, MOD_DECAY = 1, MOD_RELU = 2, MOD_BIAS_T = 3 };  // PLAIN carries a runtime bias (0 for "none"); BIAS_T: an additive bias tensor
+enum : int { MOD_CAP = 4, MOD_SLOPE = 5, MOD_CAP_SLOPE = 6 };  // with MASK_SPAN: scores capped by a tanh, biased by distance, both
+enum : int { MASK_SPAN = 3 };
 
 constexpr int kMaxDecayHeads = 256;
 
@@ -97,6 +100,12 @@ struct Params {
   int state_b0;
 };
 
+// MASK_SPAN kernels.  The decay table holds the slopes times log2(e).
+struct SpanParams : Params {
+  SpanRows span;
+  CapParams cap;
+};
+
 struct DecayTable {
   float log2_gamma[kMaxDecayHeads];
 };
@@ -114,7 +123,7 @@ inline int group_cut(int64_t n_groups) {
   return cut;
 }
 
-// MASK_: 0 none, 1 causal, 2 causal with a sliding window (Params::window keys per query)
+// MASK_: 0 none, 1 causal, 2 causal with a sliding window (Params::window keys per query), 3 a span of keys for every query row
 // FOLD_ (softmax and sigmoid without a bias tensor): the exponent comes out of the scoring MFMA ready to use.
 // Q is multiplied by |scale| * log2(e) when loaded and rounded to bf16 again (the paper's own form: its
 // modification scales q, Section 4.1), and the constant term of the exponent -- minus the running reference
@@ -129,7 +138,12 @@ struct Cfg {
   static constexpr bool FOLD = FOLD_ != 0;
   static_assert(!FOLD || ((NORM_ == NORM_SOFTMAX || NORM_ == NORM_SIGMOID) && MOD_ == MOD_PLAIN), "FOLD: softmax or sigmoid, no bias tensor");
   static constexpr int MASK = MASK_;
-  static constexpr bool CAUSAL = MASK_ != 0, WINDOW = MASK_ == 2;
+  static constexpr bool CAUSAL = MASK_ == 1 || MASK_ == 2, WINDOW = MASK_ == 2, SPAN = MASK_ == MASK_SPAN;
+  static constexpr bool ROTATED = WINDOW || SPAN;  // (see the walk over the key tiles)
+  static constexpr bool CAPPED = MOD_ == MOD_CAP || MOD_ == MOD_CAP_SLOPE, SLOPED = MOD_ == MOD_SLOPE || MOD_ == MOD_CAP_SLOPE;
+  static constexpr bool FINAL = CAPPED || SLOPED;  // the modified scores, in powers of two, are formed in front of mask and row maximum
+  static_assert(!FINAL || (SPAN && NORM_ == NORM_SOFTMAX), "capped and distance-biased scores: softmax over spans");
+  typedef std::conditional_t<SPAN, SpanParams, Params> P;
   static constexpr int SUB_N = 32;    // keys per compute sub-tile
   static constexpr int BLOCK_N = 64;  // keys per LDS tile (two sub-tiles)
   static constexpr int BLOCK_M = 32 * WAVES;
@@ -168,7 +182,7 @@ struct Cfg {
 #define AE_TUNE_PF 8
 #endif
   static constexpr int PF = (4 * (DV / 32 + DQK / 16)) % AE_TUNE_PF == 0 && AE_TUNE_PF <= DQK / 16 && AE_TUNE_PF <= 2 * (DV / 32) &&
-                                    DQK + DV <= 320 && MASK_ != 2 && MOD_ != MOD_BIAS_T
+                                    DQK + DV <= 320 && !ROTATED && MOD_ != MOD_BIAS_T
                                 ? AE_TUNE_PF : 4;
   // A copy instruction that finds the CU's vector memory queue full blocks the wave
   // that issues it, and with it everything behind it in program order.  Where the
@@ -442,7 +456,7 @@ template <class C>
 __device__ __forceinline__ void post_done(const Params& p, const RowState<C>& st, float mx, bool& moved, float& xm) {
   if constexpr (C::NORM == NORM_SOFTMAX) {
     mx = max_halves(mx);
-    xm = C::MOD == MOD_BIAS_T ? mx * p.b2 : __builtin_fmaf(mx, p.c, p.b2);  // c > 0
+    xm = C::FINAL ? mx : C::MOD == MOD_BIAS_T ? mx * p.b2 : __builtin_fmaf(mx, p.c, p.b2);  // c > 0
     moved = xm > st.m + kLazyLog2;
   }
 }
@@ -473,6 +487,10 @@ __device__ __forceinline__ uint32_t finish_pair(const Params& p, int q, const f3
     x0 = fast_exp2(__builtin_fmaf(x0, p.b2, k0));
     x1 = fast_exp2(__builtin_fmaf(x1, p.b2, k0));
     acc += x0 + x1;
+  } else if constexpr (C::FINAL) {
+    x0 = fast_exp2(x0 + k0);
+    x1 = fast_exp2(x1 + k0);
+    acc += x0 + x1;
   } else if constexpr (C::NORM == NORM_SOFTMAX) {
     x0 = fast_exp2(__builtin_fmaf(x0, p.c, k0));
     x1 = fast_exp2(__builtin_fmaf(x1, p.c, k0));
@@ -496,7 +514,7 @@ __device__ __forceinline__ uint32_t finish_pair(const Params& p, int q, const f3
 // Softmax exponent offset for the current reference maximum.
 template <class C>
 __device__ __forceinline__ float finish_k0(const Params& p, const RowState<C>& st) {
-  if constexpr (C::NORM == NORM_SOFTMAX) return (C::MOD == MOD_BIAS_T ? 0.f : p.b2) - ((st.m == -INFINITY) ? 0.f : st.m);
+  if constexpr (C::NORM == NORM_SOFTMAX) return (C::MOD == MOD_BIAS_T || C::FINAL ? 0.f : p.b2) - ((st.m == -INFINITY) ? 0.f : st.m);
   return 0.f;
 }
 template <class C>
@@ -622,7 +640,7 @@ struct Sched {
 template <class C>
 struct KeyLoop {
   using S = Sched<C>;
-  const Params& p;
+  const typename C::P& p;
   const bf16x8 (&qf)[C::T];
   RowState<C>& st;
   u32x4 (&pk)[2];
@@ -655,6 +673,8 @@ struct KeyLoop {
   int bias_j0 = -1;               // sub-tile whose copy was requested last
   int bias_newer = 0;
   u32x2 bcur[4] = {};             // the sub-tile at hand, per lane
+  // Spans: the keys of this lane's row, [lo, hi); all rows of the wave see the keys of [all_lo, all_hi)
+  int lo = 0, hi = 0, all_lo = 0, all_hi = 0;
 
   __device__ __forceinline__ void copy_bias(int j0) const {
     const int lane = threadIdx.x & 63;
@@ -817,15 +837,21 @@ struct KeyLoop {
   __device__ __forceinline__ void vector_phase(f32x16& s, int j0) {
     const int half = (threadIdx.x & 63) >> 5;
     // wave-uniform: does the sub-tile cross the causal diagonal or the end of the keys?
-    const bool masked = !FAST && ((j0 + C::SUB_N > p.L_k) || (C::CAUSAL && (j0 + C::SUB_N - 1 > iw0 + off)));
+    const bool masked = !FAST && (C::SPAN ? j0 + C::SUB_N > all_hi : (j0 + C::SUB_N > p.L_k) || (C::CAUSAL && (j0 + C::SUB_N - 1 > iw0 + off)));
     // register r is visible  <=>  key_offset(r) <= jlim
-    const int jlim = min(C::CAUSAL ? i + off : p.L_k - 1, p.L_k - 1) - j0 - 4 * half;
+    const int jlim = (C::SPAN ? hi - 1 : min(C::CAUSAL ? i + off : p.L_k - 1, p.L_k - 1)) - j0 - 4 * half;
     // sliding window: the sub-tile reaches below the window of the wave's last row; visible <=> key_offset(r) >= jlo
-    const bool masked_lo = !FAST && C::WINDOW && (j0 < iw0 + 31 + off - p.window + 1);
-    const int jlo = i + off - p.window + 1 - j0 - 4 * half;
+    const bool masked_lo = !FAST && (C::SPAN ? j0 < all_lo : C::WINDOW && (j0 < iw0 + 31 + off - p.window + 1));
+    const int jlo = (C::SPAN ? lo : i + off - p.window + 1) - j0 - 4 * half;
     const float dbase = C::MOD == MOD_DECAY ? g2 * (float)(i + off - j0 - 4 * half) : 0.f;
     float mx = -INFINITY, xm = 0.f, acc = 0.f;
     bool moved = false;
+    if constexpr (C::CAPPED) cap_scores<16>(s, p.cap);
+    if constexpr (C::SLOPED) {
+      const float d0 = (float)(i + off - j0 - 4 * half);  // distance of register 0's key
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(-g2, __builtin_fabsf(d0 - (float)key_offset(r)), C::CAPPED ? s[r] : s[r] * p.c);
+    }
     if (masked) mask_raw<C>(s, jlim, -INFINITY);
     if (masked_lo) mask_raw_below<C>(s, jlo, -INFINITY);
     if constexpr (C::FOLD) {
@@ -915,7 +941,7 @@ __device__ __forceinline__ bool place_in_group(int w, int n_groups, int per_grou
 }
 
 template <class C>
-__global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, const DecayTable dt) {
+__global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::P p, const DecayTable dt) {
   __shared__ __attribute__((aligned(1024))) char smem[C::LDS_BYTES];
 
   // ---- workgroup -> (batch, kv head, q head, q tile) ------------------------
@@ -936,7 +962,7 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, co
   const int b = group / p.H_kv, hkv = group % p.H_kv;
   const int hq = hkv * p.g + (t_in % p.g);
   const int qt_lin = t_in / p.g;
-  const int qtile = C::CAUSAL ? (p.n_qtiles - 1 - qt_lin) : qt_lin;
+  const int qtile = C::CAUSAL || C::SPAN ? (p.n_qtiles - 1 - qt_lin) : qt_lin;
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // scalar: keeps per-wave branches uniform
@@ -971,13 +997,51 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, co
   for (int db = 0; db < C::DB; ++db) st.o[db] = zero16();
 
   float g2 = 0.f;
-  if constexpr (C::MOD == MOD_DECAY) g2 = dt.log2_gamma[hq];
+  if constexpr (C::MOD == MOD_DECAY || C::SLOPED) g2 = dt.log2_gamma[hq];
 
   // keys the workgroup walks, and the prefix of them this wave can see
   int kmax = p.L_k, kmax_w = p.L_k;
   if (C::CAUSAL) {
     kmax = max(0, min(p.L_k, i_wg + C::BLOCK_M + off));
     kmax_w = max(0, min(p.L_k, iw0 + 32 + off));
+  }
+  // Spans: the lane's own row's; the keys that some row of the wave sees, [lo_w, kmax_w), and that all do, [all_lo, all_hi); the first and the
+  // last one that a row of the workgroup sees, [lo_wg, kmax), and the last beginning of a row's.  Rows that see nothing count in
+  // all_hi alone (0), rows behind the last one not at all.
+  int span_lo = 0, span_hi = 0, lo_w = 0, all_lo = 0, all_hi = 0, lo_wg = 0, last_lo = 0;
+  if constexpr (C::SPAN) {
+    constexpr int kNone = 0x7fffffff;
+    span_of(p.span, b, min(i, p.L_q - 1), off, p.L_k, span_lo, span_hi);
+    const bool sees = span_lo < span_hi;
+    lo_w = sees ? span_lo : kNone;
+    kmax_w = span_hi;
+    all_lo = span_lo;
+    all_hi = span_hi;
+    // (two lanes hold a row of the wave; the workgroup's other rows are read again, by every wave, which needs no barrier)
+    lo_wg = lo_w;
+    kmax = span_hi;
+    last_lo = span_lo;
+#pragma unroll
+    for (int k = 0; k < C::BLOCK_M / 64; ++k) {
+      int lo, hi;
+      span_of(p.span, b, min(i_wg + 64 * k + lane, p.L_q - 1), off, p.L_k, lo, hi);
+      lo_wg = min(lo_wg, lo < hi ? lo : kNone);
+      kmax = max(kmax, hi);
+      last_lo = max(last_lo, lo);
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      lo_w = min(lo_w, __shfl_xor(lo_w, s));
+      kmax_w = max(kmax_w, __shfl_xor(kmax_w, s));
+      all_lo = max(all_lo, __shfl_xor(all_lo, s));
+      all_hi = min(all_hi, __shfl_xor(all_hi, s));
+      lo_wg = min(lo_wg, __shfl_xor(lo_wg, s));
+      kmax = max(kmax, __shfl_xor(kmax, s));
+      last_lo = max(last_lo, __shfl_xor(last_lo, s));
+    }
+    auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
+    scalar(lo_w), scalar(kmax_w), scalar(all_lo), scalar(all_hi), scalar(lo_wg), scalar(kmax), scalar(last_lo);
+    if (lo_wg == kNone) lo_wg = 0;
   }
   if (iw0 >= p.L_q) kmax_w = 0;  // a wave past the last query row only helps with the copies
   int n_tiles = (kmax + C::BLOCK_N - 1) / C::BLOCK_N;  // LDS tiles (workgroup): tiles [jt0, n_tiles) are walked
@@ -1005,8 +1069,13 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, co
     jtm = max(jt0, min(jtm, n_tiles));
     u_first = max(0, iw0 + off - p.window + 1) / C::SUB_N;
   }
+  if constexpr (C::SPAN) {  // the same walk: first the tiles behind every row's first key
+    jt0 = lo_wg / C::BLOCK_N;
+    jtm = max(jt0, min((last_lo + C::BLOCK_N - 1) / C::BLOCK_N, n_tiles));
+    u_first = lo_w / C::SUB_N;
+  }
   const int n_walk = max(n_tiles - jt0, 0), n_lead = n_tiles - jtm;  // positions in the walk; those before the rotation
-  auto tile_at = [&](int pos) { return C::WINDOW ? (pos < n_lead ? jtm + pos : jt0 + (pos - n_lead)) : jt0 + pos; };
+  auto tile_at = [&](int pos) { return C::ROTATED ? (pos < n_lead ? jtm + pos : jt0 + (pos - n_lead)) : jt0 + pos; };
   // LDS: STAGES stages of a K buffer and a V buffer; tile j lives in stage j % STAGES.
   const uint32_t lds0 = (uint32_t)(uintptr_t)((lds_char*)smem);
   const uint32_t vlds0 = lds0 + C::K_BYTES;
@@ -1174,7 +1243,7 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, co
     // every wave has read its rows before tile 1 overwrites them
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     copy_slice(One{}, Zero{}, n_walk > 1 ? tile_at(1) : tile_at(0), 1);
-    if (C::WINDOW || n_vis > 2 * jt0) score_block<C>(kaddr, 0, qf, s_a, cinit);
+    if (C::ROTATED || n_vis > 2 * jt0) score_block<C>(kaddr, 0, qf, s_a, cinit);
   }
 
   // ---- key loop ------------------------------------------------------------------------
@@ -1210,6 +1279,12 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, co
       }
       kl.bscr = lds0 + C::TILE_BYTES + wave * 4096;  // behind the K/V stages
     }
+    if constexpr (C::SPAN) {
+      kl.lo = span_lo;
+      kl.hi = span_hi;
+      kl.all_lo = all_lo;
+      kl.all_hi = all_hi;
+    }
     if constexpr (C::MOD == MOD_DECAY) {
       kl.fact = g2 <= 0.f && g2 >= -4.f;  // per head, hence uniform over the workgroup
       kl.a8 = fast_exp2(-8.f * g2);
@@ -1217,12 +1292,12 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, co
       kl.b2 = fast_exp2(-2.f * g2);
       kl.b3 = fast_exp2(-3.f * g2);
     }
-    if (C::WINDOW || n_vis > 2 * jt0) static_for<0, C::PF>([&](auto nc) { kl.template fetch<decltype(nc)::value>(); });
+    if (C::ROTATED || n_vis > 2 * jt0) static_for<0, C::PF>([&](auto nc) { kl.template fetch<decltype(nc)::value>(); });
     const bool trailing = wave >= C::WAVES / 2;  // second wave of its SIMD
     int buf = 0;
 
     // The vector phase of a sub-tile, or all-zero weights for one in front of the wave's window.
-    auto vector_or_zero = [&](auto fastc, bool real, int j0) {
+    auto vector_or_zero = [&](auto fastc, bool real, int j0) __attribute__((always_inline)) {
       if (real) {
         kl.template vector_phase<decltype(fastc)::value>(s_a, j0);
       } else {
@@ -1232,18 +1307,18 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, co
       }
     };
     // One step of the walk: position pos, tile jt = tile_at(pos).
-    auto iteration = [&](auto fastc, int pos) {
+    auto iteration = [&](auto fastc, int pos) __attribute__((always_inline)) {
       constexpr bool FAST = decltype(fastc)::value;
       const int nb = next_buf(buf), stage = next_buf(nb);
       kl.dk = kl.dv = (uint32_t)((nb - buf) * C::STAGE_BYTES);
       const int jt = FAST ? pos + jtm : tile_at(pos);
       const int u = 2 * jt;
       // sub-tiles the wave runs its phases for / has weights of its own in / scores ahead
-      const bool vis0 = FAST || C::WINDOW || u < n_vis, vis1 = FAST || C::WINDOW || u + 1 < n_vis;
-      const bool real0 = FAST || !C::WINDOW || (u >= u_first && u < n_vis);
-      const bool real1 = FAST || !C::WINDOW || (u + 1 >= u_first && u + 1 < n_vis);
-      const bool sc0 = FAST || C::WINDOW || u + 1 < n_vis;
-      const bool sc1 = FAST || (C::WINDOW ? pos + 1 < n_walk : u + 2 < n_vis);
+      const bool vis0 = FAST || C::ROTATED || u < n_vis, vis1 = FAST || C::ROTATED || u + 1 < n_vis;
+      const bool real0 = FAST || !C::ROTATED || (u >= u_first && u < n_vis);
+      const bool real1 = FAST || !C::ROTATED || (u + 1 >= u_first && u + 1 < n_vis);
+      const bool sc0 = FAST || C::ROTATED || u + 1 < n_vis;
+      const bool sc1 = FAST || (C::ROTATED ? pos + 1 < n_walk : u + 2 < n_vis);
       const bool more = FAST || pos + 2 < n_walk;  // there is a tile two positions on to copy
       auto copy = [&](auto nsl, auto part) {
         if constexpr (FAST) copy_whole(nsl, part, stage);
@@ -1259,7 +1334,7 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, co
       // Vector phase of sub-tile j0 with the copy slice that goes in front of it.  With a bias tensor the
       // sub-tile's bias values are taken first and the next ones requested, ahead of the slice: `newer` copy
       // instructions follow the request before the next vector phase and may stay in flight then.
-      auto vector_with_copy = [&](bool vis, bool real, int j0, int newer, auto&& copy_fn) {
+      auto vector_with_copy = [&](bool vis, bool real, int j0, int newer, auto&& copy_fn) __attribute__((always_inline)) {
         if constexpr (C::MOD == MOD_BIAS_T) {
           if (vis && real) {
             kl.take_bias(j0);
@@ -1315,6 +1390,7 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const Params p, co
     // edge of a window), and the tile two positions on is a whole tile before the rotation.
     int m1 = min((n_vis - 1) / 2, min(p.L_k / C::BLOCK_N, n_tiles) - 2);
     if (C::CAUSAL) m1 = min(m1, (iw0 + off + 1) / C::BLOCK_N);
+    if (C::SPAN) m1 = min(m1, all_hi / C::BLOCK_N);
     const int n_fast = max(m1 - jtm, 0);
 
     if (trailing) phase_barrier();

@@ -2,7 +2,8 @@
  * ae_serving.h -- C ABI of the operators around attention with a key/value
  * cache, for AMD MI355X (gfx950): rotary positions, a paged cache that is
  * quantised as it is written, attention of a batch's newest tokens over that
- * cache, and the same behind a prefix that the whole batch shares.
+ * cache, the same behind a prefix that the whole batch shares, the weights that
+ * cached entries gather from it, and their eviction by weight.
  *
  * Conventions are those of ae_attn.h: entry points are host functions that
  * return a status, never throw and never abort; handles are host memory and
@@ -174,6 +175,12 @@ typedef struct {
 } ae_cached_desc_t;
 
 ae_status_t ae_cached_create(const ae_cache_t *cache, const ae_cached_desc_t *desc, ae_cached_t **out); /* copies what it needs of the cache's handle */
+/* The same with modified scores: s = scale q k becomes cap tanh(s / cap) where cap > 0 (with cap and scale / cap in the range of
+ * 32-bit numbers; 0: no cap), less slopes[h] times the distance between the token's place and the key's in the list (a prefix in front of it)
+ * where slopes (host, [H_q] finite numbers, copied; H_q <= 256; max_length + prefix_length <= 2^24) are given.  They are formed in fp32: a capped score
+ * has a relative error of 2e-7 up to 0.6 of the cap and an absolute one of 2e-7 of the cap beyond.  A prefix is walked in the own keys' launch here: AE_ERR_UNSUPPORTED where a
+ * sequence has more than 32 rows for a k/v head (n_new * H_q / H_kv) or the batch more than 2048; name the prefix's pages in every list then. */
+ae_status_t ae_cached_create_scored(const ae_cache_t *cache, const ae_cached_desc_t *desc, float cap, const float *slopes, ae_cached_t **out);
 ae_status_t ae_cached_workspace_bytes(const ae_cached_t *h, size_t *bytes);
 ae_status_t ae_cached_init_workspace(const ae_cached_t *h, void *workspace, size_t workspace_bytes, hipStream_t stream);
 ae_status_t ae_cached_forward(const ae_cached_t *h, const void *Q, const void *K_pages, const void *V_pages, const void *K_exp,
@@ -183,6 +190,60 @@ ae_status_t ae_cached_forward(const ae_cached_t *h, const void *Q, const void *K
  * launches of a call.  Any pointer may be NULL.                              */
 ae_status_t ae_cached_query(const ae_cached_t *h, int32_t *waves, int32_t *own_chunk, int32_t *prefix_chunk, int32_t *launches);
 ae_status_t ae_cached_destroy(ae_cached_t *h); /* NULL is allowed */
+
+/* ---- What cached entries receive, and which of them stay ------------------
+ * Every entry of a sequence's list has, for each k/v head, a weight -- the sum of the probabilities that the query rows of that
+ * head have given it so far -- and the position of its token:
+ *   weights    device, fp32  [B, H_kv, capacity]     positions  device, int32 [B, H_kv, capacity]
+ * indexed like the list: entry j lies on page table[b][j / page_size].  lengths as in ae_cached_forward.
+ *
+ * ae_weigh_forward, behind the attention of the newest n_new tokens (ae_cached_forward with its stats, or with those of
+ * ae_cached_create_scored with a cap; the prefix of a call is not weighed, its part of the statistic is):
+ *     weights_out[j] = weights[j] (0 for the newest n_new entries) + sum over rows i that see j of exp(s_ij - stats_i)
+ * and, unless both are NULL, positions[j] = new_positions[b][j - (lengths[b] - n_new)] for the newest.  Entries from lengths[b] on are left as
+ * they are.  weights_out may be weights itself.  An entry on a page number outside the cache receives nothing; a row with the
+ * statistic -inf gives nothing.  Sums are fp32, in an order that does not change.
+ *   Q, stats   as in ae_cached_forward; new_positions  device, int32, [B, n_new], batch entries new_stride apart (0: shared).   */
+typedef struct ae_weigh ae_weigh_t;
+typedef struct {
+  int32_t B, H_q, n_new;
+  int32_t table_width, max_length; /* as in ae_cached_desc_t */
+  int64_t capacity;                /* >= max_length */
+  float scale, cap;                /* of the attention */
+  int64_t q_stride[3];
+} ae_weigh_desc_t;
+
+ae_status_t ae_weigh_create(const ae_cache_t *cache, const ae_weigh_desc_t *desc, ae_weigh_t **out);
+ae_status_t ae_weigh_forward(const ae_weigh_t *h, const void *Q, const void *K_pages, const void *K_exp, const int32_t *table,
+                             const int32_t *lengths, const float *stats, const float *weights, float *weights_out, int32_t *positions,
+                             const int32_t *new_positions, int64_t new_stride, hipStream_t stream);
+ae_status_t ae_weigh_destroy(ae_weigh_t *h); /* NULL is allowed */
+
+/* ae_evict_forward keeps min(lengths[b], keep) entries of every list, for each k/v head its own: first those whose position is among the newest
+ * `recent` of the list (greater than its greatest less recent) or below `sinks`, then those with the most weight; equal ones go to the front of the list, a
+ * NaN counts as less than any number.  Kept entries from place `keep` on move, in their order, to the free places below it, in theirs, with
+ * their rows of K and V (and exponents), weights and positions; the others stay where they are.  lengths_out[b] is the new length; what lies
+ * behind it, in the cache too, is left as it was.  The order of a list is then no longer that of its tokens: attention with slopes
+ * does not fit an evicted cache.
+ * weights_out and positions_out may be the inputs themselves, lengths_out not.  The pages of the lists must be the sequences' own: a page in
+ * two lists (or twice in one) would be rewritten for both.  An entry on a page number outside the cache is counted like the others, and a row
+ * that would come from or go to one is not copied.  workspace: device, 4-byte aligned, ae_evict_workspace_bytes, needs no
+ * initialisation; calls that share it must not overlap.  Two launches (one where max_length <= keep).                       */
+typedef struct ae_evict ae_evict_t;
+typedef struct {
+  int32_t B;
+  int32_t table_width, max_length; /* as in ae_cached_desc_t */
+  int64_t capacity;                /* >= max_length */
+  int32_t keep;                    /* >= 1 */
+  int32_t recent, sinks;           /* >= 0 */
+} ae_evict_desc_t;
+
+ae_status_t ae_evict_create(const ae_cache_t *cache, const ae_evict_desc_t *desc, ae_evict_t **out);
+ae_status_t ae_evict_workspace_bytes(const ae_evict_t *h, size_t *bytes);
+ae_status_t ae_evict_forward(const ae_evict_t *h, void *K_pages, void *V_pages, void *K_exp, void *V_exp, const int32_t *table,
+                             const int32_t *lengths, const float *weights, const int32_t *positions, float *weights_out, int32_t *positions_out,
+                             int32_t *lengths_out, void *workspace, size_t workspace_bytes, hipStream_t stream);
+ae_status_t ae_evict_destroy(ae_evict_t *h); /* NULL is allowed */
 
 #ifdef __cplusplus
 }

@@ -62,3 +62,31 @@ def attend(q, keys, values, scale):
             w = np.exp(x - m)
             O[h, t], S[h, t] = w @ values[h // g, :end] / w.sum(), m + np.log(w.sum())
     return O, S
+
+
+def received(q, keys, stats, scale, cap=0.0):
+    """What the cached entries of one sequence receive: q [H_q, n, D], keys [H_kv, len, D], stats [H_q, n]; [H_kv, len] sums over a head's rows of
+    exp(s - stat), token t of the newest n seeing the first len - n + 1 + t keys."""
+    q, keys, stats = (np.asarray(t, np.float64) for t in (q, keys, stats))
+    H_q, n, _ = q.shape
+    g, length = H_q // keys.shape[0], keys.shape[1]
+    got = np.zeros(keys.shape[:2])
+    for h in range(H_q):
+        for t in range(n):
+            end = length - n + 1 + t
+            if end > 0 and stats[h, t] != -np.inf:
+                x = scale * keys[h // g, :end] @ q[h, t]
+                got[h // g, :end] += np.exp((cap * np.tanh(x / cap) if cap else x) - stats[h, t])
+    return got
+
+
+def kept_entries(weights, positions, keep, recent=0, sinks=0):
+    """Eviction from one list: the entry that each of its first min(len, keep) places holds afterwards."""
+    length = len(weights)
+    count = min(length, keep)
+    newest = max(map(int, positions), default=0)
+    safe = [int(p) > newest - recent or int(p) < sinks for p in positions]
+    order = sorted(range(length), key=lambda i: (not safe[i], 0 if safe[i] else np.isnan(weights[i]), 0.0 if safe[i] or np.isnan(weights[i]) else -weights[i], i))
+    stay = set(order[:count])
+    behind = iter(sorted(i for i in stay if i >= count))
+    return [i if i in stay else next(behind) for i in range(count)]

@@ -611,9 +611,35 @@ class ae_cached_desc_t(C.Structure):
                 ("q_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3)]
 
 
+class ae_weigh_desc_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("H_q", C.c_int32), ("n_new", C.c_int32), ("table_width", C.c_int32), ("max_length", C.c_int32),
+                ("capacity", C.c_int64), ("scale", C.c_float), ("cap", C.c_float), ("q_stride", C.c_int64 * 3)]
+
+
+class ae_evict_desc_t(C.Structure):
+    _fields_ = [("B", C.c_int32), ("table_width", C.c_int32), ("max_length", C.c_int32), ("capacity", C.c_int64), ("keep", C.c_int32),
+                ("recent", C.c_int32), ("sinks", C.c_int32)]
+
+
 _strides_t = C.c_int64 * 3
+_lib.ae_weigh_create.argtypes = [C.c_void_p, C.POINTER(ae_weigh_desc_t), C.POINTER(C.c_void_p)]
+_lib.ae_weigh_create.restype = C.c_int
+_lib.ae_weigh_forward.argtypes = [C.c_void_p] * 11 + [C.c_int64, C.c_void_p]
+_lib.ae_weigh_forward.restype = C.c_int
+_lib.ae_weigh_destroy.argtypes = [C.c_void_p]
+_lib.ae_weigh_destroy.restype = C.c_int
+_lib.ae_evict_create.argtypes = [C.c_void_p, C.POINTER(ae_evict_desc_t), C.POINTER(C.c_void_p)]
+_lib.ae_evict_create.restype = C.c_int
+_lib.ae_evict_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+_lib.ae_evict_workspace_bytes.restype = C.c_int
+_lib.ae_evict_forward.argtypes = [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p]
+_lib.ae_evict_forward.restype = C.c_int
+_lib.ae_evict_destroy.argtypes = [C.c_void_p]
+_lib.ae_evict_destroy.restype = C.c_int
 _lib.ae_cached_create.argtypes = [C.c_void_p, C.POINTER(ae_cached_desc_t), C.POINTER(C.c_void_p)]
 _lib.ae_cached_create.restype = C.c_int
+_lib.ae_cached_create_scored.argtypes = [C.c_void_p, C.POINTER(ae_cached_desc_t), C.c_float, C.POINTER(C.c_float), C.POINTER(C.c_void_p)]
+_lib.ae_cached_create_scored.restype = C.c_int
 _lib.ae_cached_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
 _lib.ae_cached_workspace_bytes.restype = C.c_int
 _lib.ae_cached_init_workspace.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
@@ -698,14 +724,30 @@ def ae_cache_destroy(handle: Optional[int]) -> None:
     _check(_lib.ae_cache_destroy(handle))
 
 
+def _float_array(values):
+    """(pointer, what it points into) of host floats; null for None."""
+    if values is None:
+        return C.POINTER(C.c_float)(), None
+    keep = (C.c_float * len(values))(*[float(x) for x in values])
+    return C.cast(keep, C.POINTER(C.c_float)), keep
+
+
 def ae_cached_create(cache: int, *, B: int, H_q: int, n_new: int, table_width: int, max_length: int, scale: float, prefix_length: int = 0,
-                     chunk: int = 0, out_dtype="f32", q_stride=(0, 0, 0), o_stride=(0, 0, 0)) -> int:
-    """Handle for attention of the newest n_new tokens of B sequences over a paged cache (cache: its handle)."""
+                     chunk: int = 0, out_dtype="f32", q_stride=(0, 0, 0), o_stride=(0, 0, 0), cap: float = 0.0,
+                     slopes: Optional[Sequence[float]] = None) -> int:
+    """Handle for attention of the newest n_new tokens of B sequences over a paged cache (cache: its handle); cap, slopes (H_q host floats):
+    with modified scores (ae_cached_create_scored)."""
+    if slopes is not None and len(slopes) != H_q:
+        raise ValueError("slopes must hold a number for every query head")
     d = ae_cached_desc_t(B=B, H_q=H_q, n_new=n_new, table_width=table_width, max_length=max_length, prefix_length=prefix_length, chunk=chunk,
                          scale=float(scale), out_dtype=OUT_DTYPES[out_dtype] if isinstance(out_dtype, str) else int(out_dtype))
     d.q_stride, d.o_stride = _strides_t(*[int(x) for x in q_stride]), _strides_t(*[int(x) for x in o_stride])
     h = C.c_void_p()
-    _check(_lib.ae_cached_create(cache, C.byref(d), C.byref(h)))
+    if cap == 0 and slopes is None:
+        _check(_lib.ae_cached_create(cache, C.byref(d), C.byref(h)))
+    else:
+        at, keep = _float_array(slopes)
+        _check(_lib.ae_cached_create_scored(cache, C.byref(d), float(cap), at, C.byref(h)))
     return h.value
 
 
@@ -736,6 +778,51 @@ def ae_cached_query(handle: int) -> dict:
 
 def ae_cached_destroy(handle: Optional[int]) -> None:
     _check(_lib.ae_cached_destroy(handle))
+
+
+def ae_weigh_create(cache: int, *, B: int, H_q: int, n_new: int, table_width: int, max_length: int, capacity: int, scale: float, cap: float = 0.0,
+                    q_stride=(0, 0, 0)) -> int:
+    """Handle for the weights that cached entries receive from the newest n_new tokens of B sequences (cache: its handle)."""
+    d = ae_weigh_desc_t(B=B, H_q=H_q, n_new=n_new, table_width=table_width, max_length=max_length, capacity=capacity, scale=float(scale), cap=float(cap))
+    d.q_stride = _strides_t(*[int(x) for x in q_stride])
+    h = C.c_void_p()
+    _check(_lib.ae_weigh_create(cache, C.byref(d), C.byref(h)))
+    return h.value
+
+
+def ae_weigh_forward(handle: int, Q: int, K_pages: int, K_exp: int, table: int, lengths: int, stats: int, weights: int, weights_out: int,
+                     positions: int, new_positions: int, new_stride: int, stream: int = 0) -> None:
+    """Device addresses; K_exp (16-bit cache) and positions with new_positions may be 0."""
+    _check(_lib.ae_weigh_forward(handle, Q, K_pages, K_exp, table, lengths, stats, weights, weights_out, positions, new_positions, new_stride, stream))
+
+
+def ae_weigh_destroy(handle: Optional[int]) -> None:
+    _check(_lib.ae_weigh_destroy(handle))
+
+
+def ae_evict_create(cache: int, *, B: int, table_width: int, max_length: int, capacity: int, keep: int, recent: int = 0, sinks: int = 0) -> int:
+    """Handle for the eviction of the entries of B lists (cache: its handle)."""
+    d = ae_evict_desc_t(B=B, table_width=table_width, max_length=max_length, capacity=capacity, keep=keep, recent=recent, sinks=sinks)
+    h = C.c_void_p()
+    _check(_lib.ae_evict_create(cache, C.byref(d), C.byref(h)))
+    return h.value
+
+
+def ae_evict_workspace_bytes(handle: int) -> int:
+    n = C.c_size_t()
+    _check(_lib.ae_evict_workspace_bytes(handle, C.byref(n)))
+    return n.value
+
+
+def ae_evict_forward(handle: int, K_pages: int, V_pages: int, K_exp: int, V_exp: int, table: int, lengths: int, weights: int, positions: int,
+                     weights_out: int, positions_out: int, lengths_out: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """Device addresses; K_exp and V_exp are 0 for a 16-bit cache."""
+    _check(_lib.ae_evict_forward(handle, K_pages, V_pages, K_exp, V_exp, table, lengths, weights, positions, weights_out, positions_out,
+                                 lengths_out, workspace, workspace_bytes, stream))
+
+
+def ae_evict_destroy(handle: Optional[int]) -> None:
+    _check(_lib.ae_evict_destroy(handle))
 
 
 def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, scaling="none", factor: float = 1.0, original_length: int = 4096,
@@ -998,12 +1085,14 @@ class CachedAttentionPlan:
     """A handle for attention of the newest tokens over a PagedCache, for calls of one shape: the step of a decoding loop keeps it, and
     its workspace.  Q [B, H_q, n, D_qk] bf16 and out [B, H_q, n, D_v] (bf16 or fp32) give shapes, strides and device; max_length: no
     sequence has more keys of its own; table_width: pages in a row of the table; prefix_length: keys that all sequences share.
+    cap: scores are bent to cap tanh(s / cap) (0: not); slopes: a host number per query head, times the distance in the list between the token and the
+    key taken off the score (not for an evicted cache, whose lists are no longer in the tokens' order).
     Calls of one plan must not overlap (they share its workspace, which is prepared on the stream that is current when the plan is
     made: another stream waits for that one before its first call); the plan may be dropped while a call still runs, on whichever stream.
     A captured graph keeps using the plan's buffers, so the plan has to outlive it, and a plan made while a graph is captured is of use to
     that graph alone."""
 
-    def __init__(self, cache, Q, out, *, max_length, table_width, scale, prefix_length=0, chunk=0):
+    def __init__(self, cache, Q, out, *, max_length, table_width, scale, prefix_length=0, chunk=0, cap=0.0, slopes=None):
         import torch
 
         self.handle = None
@@ -1018,7 +1107,7 @@ class CachedAttentionPlan:
         _no_overlap(out)
         self.handle = ae_cached_create(cache.handle, B=B, H_q=H_q, n_new=n, table_width=table_width, max_length=max_length, scale=scale,
                                        prefix_length=prefix_length, chunk=chunk, out_dtype="bf16" if out.dtype == torch.bfloat16 else "f32",
-                                       q_stride=_row_strides(Q), o_stride=_row_strides(out))
+                                       q_stride=_row_strides(Q), o_stride=_row_strides(out), cap=cap, slopes=slopes)
         self.cache, self.device, self.shape, self._f32 = cache, Q.device, (B, H_q, n), torch.float32
         self._q, self._o = _shape_of(Q), _shape_of(out)
         self._table, self._prefix = (B, table_width), -(-prefix_length // cache.page_size)
@@ -1066,20 +1155,148 @@ class CachedAttentionPlan:
 
 
 def attention_cached(Q, cache, table, lengths, *, scale, max_length=None, prefix_table=None, prefix_length=0, out=None, out_dtype=None,
-                     stats=None, chunk=0, stream=None):
+                     stats=None, chunk=0, stream=None, cap=0.0, slopes=None):
     """Softmax attention of the newest n tokens of each sequence, Q bf16 [B, H_q, n, D_qk], over everything a PagedCache holds for
     them: position j of sequence b lies on page table[b, j // page] (int32 [B, width]), lengths int32 [B] counts its keys, the newest n
     among them; token t sees the first lengths[b] - n + 1 + t.  max_length: no sequence is longer (None: the table's room).
     prefix_table / prefix_length: keys in front of every sequence's own that the whole batch shares; they are read once for all.
-    Returns O [B, H_q, n, D_v], fp32 or bf16 (out / out_dtype); stats: optional fp32 [B, H_q, n] that receives ln sum exp."""
+    cap, slopes: capped and distance-biased scores (CachedAttentionPlan).  Returns O [B, H_q, n, D_v], fp32 or bf16 (out / out_dtype); stats: optional fp32 [B, H_q, n] that receives ln sum exp."""
     import torch
 
     with _memory_of(stream):  # (the workspace, too, belongs to the stream that uses it)
         if out is None:
             out = torch.empty(Q.shape[:3] + (cache.D_v,), dtype=out_dtype or torch.float32, device=Q.device)
         plan = CachedAttentionPlan(cache, Q, out, max_length=table.shape[1] * cache.page_size if max_length is None else max_length,
-                                   table_width=table.shape[1], scale=scale, prefix_length=prefix_length, chunk=chunk)
+                                   table_width=table.shape[1], scale=scale, prefix_length=prefix_length, chunk=chunk, cap=cap, slopes=slopes)
         return plan.forward(Q, table, lengths, out, stats=stats, prefix_table=prefix_table)
+
+
+def _check_entries(cache, spec, *tensors):
+    """Arrays beside the lists of a cache: contiguous [B, H_kv, capacity] of the given types on its device."""
+    for t, dtype in tensors:
+        if t.dtype != dtype or tuple(t.shape) != spec or not t.is_contiguous() or t.device != cache.device:
+            raise ValueError(f"weights (fp32) and positions (int32) must be contiguous device tensors {list(spec)}")
+
+
+def _check_ints(cache, *tensors):
+    for t, shape in tensors:
+        if t.dtype != cache._int or tuple(t.shape) != shape or not t.is_contiguous() or t.device != cache.device:
+            raise ValueError(f"tables and lengths must be contiguous int32 device tensors (here {shape})")
+
+
+class CacheWeightsPlan:
+    """A handle for the weights that cached entries receive, for calls of one shape: a decoding loop that will evict keeps one and calls
+    it behind each attention over the cache.  Q [B, H_q, n, D_qk] bf16 as for the attention, weights [B, H_kv, capacity] fp32 give shapes, strides
+    and device; max_length, table_width, scale and cap are the attention's (slopes do not fit a cache that is evicted).  Calls of one plan may
+    run at the same time, on weights of their own."""
+
+    def __init__(self, cache, Q, weights, *, max_length, table_width, scale, cap=0.0):
+        import torch
+
+        self.handle = None
+        if not Q.is_cuda or Q.dim() != 4 or Q.dtype != torch.bfloat16 or Q.shape[3] != cache.D_qk or Q.stride(3) != 1 or Q.device != cache.device:
+            raise ValueError("Q must be bf16 [B, H_q, n, D_qk] on the cache's device with a contiguous last dimension; there is no CPU path")
+        B, H_q, n, _ = Q.shape
+        self._f32 = torch.float32
+        self._entries = (B, cache.H_kv, weights.shape[-1])
+        _check_entries(cache, self._entries, (weights, torch.float32))
+        self.handle = ae_weigh_create(cache.handle, B=B, H_q=H_q, n_new=n, table_width=table_width, max_length=max_length, capacity=weights.shape[-1],
+                                      scale=scale, cap=cap, q_stride=_row_strides(Q))
+        self.cache, self.device, self.shape, self._q, self._table = cache, Q.device, (B, H_q, n), _shape_of(Q), (B, table_width)
+
+    def forward(self, Q, table, lengths, stats, weights, positions=None, new_positions=None, *, out=None, stream=None):
+        """stats: fp32 [B, H_q, n], what the attention over the cache wrote; weights: fp32 [B, H_kv, capacity], updated in place or, with `out`, written
+        there; positions int32 [B, H_kv, capacity] receive new_positions (int32 [B, n] or [n]) at the newest tokens' entries.  Returns the weights."""
+        out = weights if out is None else out
+        if _shape_of(Q) != self._q:
+            raise ValueError("Q differs from the plan's in shape, strides, type or device")
+        B, _, n = self.shape
+        _check_ints(self.cache, (table, self._table), (lengths, (B,)))
+        _check_entries(self.cache, self._entries, (weights, self._f32), (out, self._f32), *(((positions, self.cache._int),) if positions is not None else ()))
+        if stats.dtype != self._f32 or tuple(stats.shape) != self.shape or not stats.is_contiguous() or stats.device != self.device:
+            raise ValueError("stats must be a contiguous fp32 tensor [B, H_q, n]")
+        if (positions is None) != (new_positions is None):
+            raise ValueError("positions and the new ones come together")
+        new = 0, 0
+        if new_positions is not None:
+            if (new_positions.dtype != self.cache._int or tuple(new_positions.shape) not in ((n,), (B, n)) or new_positions.device != self.device
+                    or (n > 1 and new_positions.stride(-1) != 1)):
+                raise ValueError("new positions must be an int32 device tensor [B, n] or [n] with contiguous rows")
+            new = new_positions.data_ptr(), new_positions.stride(0) if new_positions.dim() == 2 else 0
+        K, _, K_exp, _ = self.cache.pointers()
+        _enqueue(ae_weigh_forward, self.device, stream, self.handle, Q.data_ptr(), K, K_exp, table.data_ptr(), lengths.data_ptr(), stats.data_ptr(),
+                 weights.data_ptr(), out.data_ptr(), 0 if positions is None else positions.data_ptr(), *new)
+        return out
+
+    def __del__(self):
+        if getattr(self, "handle", None) is not None and _lib is not None:
+            _lib.ae_weigh_destroy(self.handle)
+            self.handle = None
+
+
+class CacheEvictionPlan:
+    """A handle for the eviction of cached entries by weight, for lists of one shape, with its workspace.  weights [B, H_kv, capacity] fp32 gives
+    shapes and device.  Of every list `keep` entries stay, for each k/v head its own: those of the newest `recent` positions and of positions below `sinks`
+    first, then those with the most weight (equal ones from the list's front).  Calls of one plan must not overlap; of a captured graph, the
+    plan has to outlive it."""
+
+    def __init__(self, cache, weights, *, keep, max_length, table_width, recent=0, sinks=0):
+        import torch
+
+        self.handle = None
+        if not weights.is_cuda or weights.dim() != 3:
+            raise ValueError("weights must be a device tensor [B, H_kv, capacity]; there is no CPU path")
+        B, _, capacity = weights.shape
+        self._f32, self._entries = torch.float32, (B, cache.H_kv, capacity)
+        _check_entries(cache, self._entries, (weights, torch.float32))
+        self.handle = ae_evict_create(cache.handle, B=B, table_width=table_width, max_length=max_length, capacity=capacity, keep=keep, recent=recent,
+                                      sinks=sinks)
+        self.cache, self.device, self._table = cache, cache.device, (B, table_width)
+        self.workspace_bytes = ae_evict_workspace_bytes(self.handle)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+        self._streams = {_raw_stream(self.device.index)}
+
+    def forward(self, table, lengths, weights, positions, lengths_out, *, weights_out=None, positions_out=None, stream=None):
+        """Evicts in the cache's pages, which have to be the sequences' own, and writes the entries that stay to weights and positions (or to weights_out and
+        positions_out) and the new lengths to lengths_out (int32 [B], not lengths itself).  Returns lengths_out."""
+        weights_out, positions_out = weights if weights_out is None else weights_out, positions if positions_out is None else positions_out
+        B = self._table[0]
+        _check_ints(self.cache, (table, self._table), (lengths, (B,)), (lengths_out, (B,)))
+        _check_entries(self.cache, self._entries, (weights, self._f32), (weights_out, self._f32), (positions, self.cache._int),
+                       (positions_out, self.cache._int))
+        self._use_workspace(stream)
+        _enqueue(ae_evict_forward, self.device, stream, self.handle, *self.cache.pointers(), table.data_ptr(), lengths.data_ptr(), weights.data_ptr(),
+                 positions.data_ptr(), weights_out.data_ptr(), positions_out.data_ptr(), lengths_out.data_ptr(), self.workspace.data_ptr(),
+                 self.workspace_bytes)
+        return lengths_out
+
+    _use_workspace = CachedAttentionPlan._use_workspace
+
+    def __del__(self):
+        if getattr(self, "handle", None) is not None and _lib is not None:
+            _lib.ae_evict_destroy(self.handle)
+            self.handle = None
+
+
+def cache_weights(Q, cache, table, lengths, stats, weights, positions=None, new_positions=None, *, scale, cap=0.0, max_length=None, out=None, stream=None):
+    """Adds to weights (fp32 [B, H_kv, capacity]; with `out`, written there) what the newest n tokens of each sequence, Q bf16 [B, H_q, n, D_qk], give the
+    cached entries of their lists: per k/v head the sum of the query rows' probabilities.  table, lengths, scale, cap as in attention_cached, which
+    gives stats [B, H_q, n].  Entries of the newest tokens start from nothing, and their positions (int32, like weights) are taken from new_positions."""
+    plan = CacheWeightsPlan(cache, Q, weights, max_length=min(table.shape[1] * cache.page_size, weights.shape[-1]) if max_length is None else max_length,
+                            table_width=table.shape[1], scale=scale, cap=cap)
+    return plan.forward(Q, table, lengths, stats, weights, positions, new_positions, out=out, stream=stream)
+
+
+def cache_evict(cache, table, lengths, weights, positions, *, keep, recent=0, sinks=0, max_length=None, lengths_out=None, stream=None):
+    """Keeps `keep` entries of every list (CacheEvictionPlan), in place in the cache's pages, weights and positions; returns the new lengths, int32 [B]."""
+    import torch
+
+    with _memory_of(stream):
+        if lengths_out is None:
+            lengths_out = torch.empty_like(lengths)
+        plan = CacheEvictionPlan(cache, weights, keep=keep, recent=recent, sinks=sinks, table_width=table.shape[1],
+                                 max_length=min(table.shape[1] * cache.page_size, weights.shape[-1]) if max_length is None else max_length)
+        return plan.forward(table, lengths, weights, positions, lengths_out)
 
 
 # ---- span attention (include/ae_span.h) -----------------------------------------------------------------------------------
@@ -1106,14 +1323,6 @@ _lib.ae_span_destroy.argtypes = [C.c_void_p]
 _lib.ae_span_destroy.restype = C.c_int
 _lib.ae_span_documents.argtypes = ([C.c_int32] * 3 + [C.c_void_p, C.c_int64] * 2 + [C.c_int, C.c_int32] + [C.c_void_p] * 3)
 _lib.ae_span_documents.restype = C.c_int
-
-
-def _float_array(values):
-    """(pointer, what it points into) of host floats; null for None."""
-    if values is None:
-        return C.POINTER(C.c_float)(), None
-    keep = (C.c_float * len(values))(*[float(x) for x in values])
-    return C.cast(keep, C.POINTER(C.c_float)), keep
 
 
 def ae_span_create(*, B: int, H_q: int, H_kv: int, L_q: int, L_k: int, D_qk: int, D_v: int, scale: float, cap: float = 0.0,

@@ -7,6 +7,7 @@
 #include <utility>
 
 #include "cache.hpp"
+#include "cache_weights.hpp"
 #include "cached_attn.hpp"
 #include "rotary.hpp"
 #include "status.hpp"
@@ -246,6 +247,7 @@ struct ae_cached {
   ae_cache_desc_t cache;
   ae_cached_desc_t desc;
   ae::CachedParams params;  // pointers filled in per call
+  ae::ScoredParams* scored; // modified scores: cap and slopes (the rest is params); else null
   bool prefix_apart;        // the prefix is walked by a launch of its own, in front
   int slots;                // partial results of a row
   bool counted;             // workgroups join their results: the last one of a row does
@@ -287,7 +289,7 @@ struct Layout {
   bool apart;
 };
 
-Layout choose_layout(const ae_cached_desc_t& d, const ae_cache_desc_t& cd, int g) {
+Layout choose_layout(const ae_cached_desc_t& d, const ae_cache_desc_t& cd, int g, bool may_part) {
   // (as they were measured; between them a number of workgroups that does not go into the compute units can cost 15 %)
   static const int kCuts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}, kPrefixCuts[] = {1, 2, 4, 8, 16, 32, 64};
   const bool e4m3 = cd.dtype == AE_CACHE_E4M3;
@@ -300,7 +302,7 @@ Layout choose_layout(const ae_cached_desc_t& d, const ae_cache_desc_t& cd, int g
   };
   const double own_read = (double)d.B * cd.H_kv * d.max_length * key_us, prefix_read = (double)cd.H_kv * d.prefix_length * key_us;
   Layout best = {1e300, 4, 1, 1, false};
-  for (int apart = 0; apart <= (d.prefix_length > 0 ? 1 : 0); ++apart) {
+  for (int apart = 0; apart <= (d.prefix_length > 0 && may_part ? 1 : 0); ++apart) {
     // (in one launch with the own keys: tiles of whole sequences, which have to fit; not measured beyond 2048 rows)
     if (d.prefix_length > 0 && !apart && (own_rows > 32 || prefix_rows > 2048)) continue;
     const bool fused = d.prefix_length > 0 && !apart;
@@ -355,9 +357,8 @@ Layout choose_layout(const ae_cached_desc_t& d, const ae_cache_desc_t& cd, int g
 
 }  // namespace
 
-extern "C" {
-
-ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d, ae_cached_t** out) {
+// (scored: of the modified scores, which the handle takes over on success; null: plain ones)
+static ae_status_t cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d, ae_cached_t** out, ae::ScoredParams* scored) {
   if (out) *out = nullptr;
   if (!cache || !d || !out) return fail(AE_ERR_INVALID_ARG, "ae_cached_create: null argument");
   const ae_cache_desc_t& cd = cache->desc;
@@ -404,7 +405,11 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
   own.max_length = d->max_length;
   own.table_width = d->table_width;
   own.causal = 1;
-  const Layout lay = choose_layout(*d, cd, p.g);
+  const Layout lay = choose_layout(*d, cd, p.g, scored == nullptr);
+  if (lay.us >= 1e300) {
+    delete h;
+    return fail(AE_ERR_UNSUPPORTED, "ae_cached_create_scored: a prefix comes with at most 32 rows for a k/v head of a sequence and 2048 of the batch");
+  }
   p.waves = lay.waves;
   if (d->prefix_length > 0) {
     prefix.lists = 1;
@@ -427,8 +432,49 @@ ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* d,
     delete h;
     return fail(AE_ERR_UNSUPPORTED, "ae_cached_create: the partial results would take more than 10^11 bytes");
   }
+  h->scored = scored;
   *out = h;
   return AE_OK;
+}
+
+// Whether a cap is one, and its constants (0: none).
+static ae_status_t check_cap(float scale, float cap, ae::CapParams* out, const char* who) {
+  *out = {};
+  if (cap == 0.f) return AE_OK;
+  if (!(cap > 0.f) || !std::isfinite(cap)) return fail(AE_ERR_INVALID_ARG, "%s: cap must be 0 or positive and finite", who);
+  *out = ae::cap_params(scale, cap);
+  const float all[] = {out->k, out->unit, out->e, out->inv};
+  for (float x : all)
+    if (!std::isnormal(x)) return fail(AE_ERR_INVALID_ARG, "%s: cap and scale / cap must be in the range of 32-bit numbers", who);
+  return AE_OK;
+}
+
+extern "C" {
+
+ae_status_t ae_cached_create(const ae_cache_t* cache, const ae_cached_desc_t* desc, ae_cached_t** out) { return cached_create(cache, desc, out, nullptr); }
+
+ae_status_t ae_cached_create_scored(const ae_cache_t* cache, const ae_cached_desc_t* d, float cap, const float* slopes, ae_cached_t** out) {
+  static const char who[] = "ae_cached_create_scored";
+  if (out) *out = nullptr;
+  if (!cache || !d || !out) return fail(AE_ERR_INVALID_ARG, "%s: null argument", who);
+  ae::CapParams bend;
+  const ae_status_t st = check_cap(std::fabs(d->scale), cap, &bend, who);  // (the sign is on the queries)
+  if (st != AE_OK) return st;
+  if (slopes) {
+    if (d->H_q > ae::kMaxSlopeHeads) return fail(AE_ERR_UNSUPPORTED, "%s: slopes come with at most %d query heads", who, ae::kMaxSlopeHeads);
+    if ((int64_t)d->max_length + d->prefix_length > (1 << 24)) return fail(AE_ERR_UNSUPPORTED, "%s: slopes come with at most 2^24 keys", who);
+    for (int k = 0; k < d->H_q; ++k)
+      if (!std::isfinite(slopes[k] * 1.4426950408889634f * (1 << 24))) return fail(AE_ERR_INVALID_ARG, "%s: slopes[%d] must be finite, and 2^24 times it", who, k);
+  }
+  ae::ScoredParams* scored = new (std::nothrow) ae::ScoredParams();
+  if (!scored) return fail(AE_ERR_NOMEM, "%s: out of host memory", who);
+  scored->cap = bend;
+  scored->capped = cap != 0.f;
+  if (slopes)
+    for (int k = 0; k < d->H_q; ++k) scored->slopes[k] = slopes[k] * 1.4426950408889634f;
+  const ae_status_t made = cached_create(cache, d, out, scored);
+  if (made != AE_OK) delete scored;
+  return made;
 }
 
 ae_status_t ae_cached_workspace_bytes(const ae_cached_t* h, size_t* bytes) {
@@ -488,6 +534,11 @@ ae_status_t ae_cached_forward(const ae_cached_t* h, const void* Q, const void* K
     const ae_status_t st = launched(ae::launch_prefix(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
     if (st != AE_OK) return st;
   }
+  if (h->scored) {
+    ae::ScoredParams q = *h->scored;
+    static_cast<ae::CachedParams&>(q) = p;
+    return launched(ae::launch_scored(q, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
+  }
   return launched(ae::launch_cached(p, h->cache.D_qk, h->cache.D_v, e4m3, stream), who);
 }
 
@@ -501,6 +552,206 @@ ae_status_t ae_cached_query(const ae_cached_t* h, int32_t* waves, int32_t* own_c
 }
 
 ae_status_t ae_cached_destroy(ae_cached_t* h) {
+  if (h) delete h->scored;
+  delete h;
+  return AE_OK;
+}
+
+}  // extern "C"
+
+// ---- weights of cached entries, eviction -------------------------------------------------------------------------------
+struct ae_weigh {
+  ae_cache_desc_t cache;
+  ae::WeighParams params;  // pointers filled in per call
+};
+struct ae_evict {
+  ae_cache_desc_t cache;
+  ae::EvictParams params;
+  size_t ws_bytes;
+};
+
+// Whether two arrays of so many bytes are the same or apart.
+static bool same_or_apart(const void* a, const void* b, uint64_t bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x == y || (x < y ? y - x : x - y) >= bytes;
+}
+
+// What both have in common: the lists and the arrays beside them.
+static ae_status_t check_lists(const ae_cache_desc_t& cd, int32_t B, int32_t table_width, int32_t max_length, int64_t capacity, const char* who) {
+  if (B < 1 || table_width < 1) return fail(AE_ERR_INVALID_ARG, "%s: B and table_width must be >= 1", who);
+  if (max_length < 1 || max_length > (int64_t)table_width * cd.page_size)
+    return fail(AE_ERR_INVALID_ARG, "%s: max_length (%d) must be between 1 and table_width * page_size", who, max_length);
+  if (capacity < max_length) return fail(AE_ERR_INVALID_ARG, "%s: capacity must be at least max_length", who);
+  if (max_length > 1 << 30 || (int64_t)B * cd.H_kv > 1 << 24) return fail(AE_ERR_UNSUPPORTED, "%s: at most 2^30 entries a list and 2^24 lists", who);
+  return AE_OK;
+}
+
+extern "C" {
+
+ae_status_t ae_weigh_create(const ae_cache_t* cache, const ae_weigh_desc_t* d, ae_weigh_t** out) {
+  static const char who[] = "ae_weigh_create";
+  if (out) *out = nullptr;
+  if (!cache || !d || !out) return fail(AE_ERR_INVALID_ARG, "%s: null argument", who);
+  const ae_cache_desc_t& cd = cache->desc;
+  ae_status_t st = check_lists(cd, d->B, d->table_width, d->max_length, d->capacity, who);
+  if (st != AE_OK) return st;
+  if (d->H_q < 1 || d->n_new < 1) return fail(AE_ERR_INVALID_ARG, "%s: H_q and n_new must be >= 1", who);
+  if (d->H_q % cd.H_kv != 0) return fail(AE_ERR_INVALID_ARG, "%s: H_q (%d) is not a multiple of H_kv (%d)", who, d->H_q, cd.H_kv);
+  if (!std::isfinite(d->scale * 1.4426950408889634f) || d->scale == 0.f)
+    return fail(AE_ERR_INVALID_ARG, "%s: scale must be finite (its product with log2(e) too) and non-zero", who);
+  if ((int64_t)d->B * d->H_q * d->n_new > 1 << 24) return fail(AE_ERR_UNSUPPORTED, "%s: at most 2^24 query rows", who);
+  ae::CapParams cap;
+  st = check_cap(d->scale, d->cap, &cap, who);
+  if (st != AE_OK) return st;
+  int64_t qs[3];
+  contiguous_or(qs, d->q_stride, d->H_q, d->n_new, cd.D_qk);
+  for (int a = 0; a < 3; ++a)
+    if (qs[a] < 0 || qs[a] % 8 != 0) return fail(AE_ERR_INVALID_ARG, "%s: strides must be non-negative multiples of 8 elements", who);
+  ae_weigh* h = new (std::nothrow) ae_weigh();
+  if (!h) return fail(AE_ERR_NOMEM, "%s: out of host memory", who);
+  h->cache = cd;
+  ae::WeighParams& p = h->params;
+  std::copy(qs, qs + 3, p.qs);
+  p.capacity = d->capacity;
+  p.B = d->B;
+  p.H_q = d->H_q;
+  p.H_kv = cd.H_kv;
+  p.g = d->H_q / cd.H_kv;
+  p.n = d->n_new;
+  p.page_shift = cache->page_shift;
+  p.n_pages = cd.n_pages;
+  p.table_width = d->table_width;
+  p.max_length = d->max_length;
+  p.c = d->scale * 1.4426950408889634f;
+  p.capped = d->cap != 0.f;
+  p.cap = cap;
+  *out = h;
+  return AE_OK;
+}
+
+ae_status_t ae_weigh_forward(const ae_weigh_t* h, const void* Q, const void* K_pages, const void* K_exp, const int32_t* table, const int32_t* lengths,
+                             const float* stats, const float* weights, float* weights_out, int32_t* positions, const int32_t* new_positions,
+                             int64_t new_stride, hipStream_t stream) {
+  static const char who[] = "ae_weigh_forward";
+  if (!h) return fail(AE_ERR_INVALID_ARG, "%s: null handle", who);
+  const bool e4m3 = h->cache.dtype == AE_CACHE_E4M3;
+  if (!Q || !K_pages || !table || !lengths || !stats || !weights || !weights_out) return fail(AE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if ((K_exp != nullptr) != e4m3) return fail(AE_ERR_INVALID_ARG, "%s: exponents belong to an 8-bit cache, and only to it", who);
+  if ((positions != nullptr) != (new_positions != nullptr)) return fail(AE_ERR_INVALID_ARG, "%s: positions and the new ones come together", who);
+  if (((uintptr_t)Q | (uintptr_t)K_pages) & 15) return fail(AE_ERR_INVALID_ARG, "%s: Q and the pages must be 16-byte aligned", who);
+  if (((uintptr_t)K_exp | (uintptr_t)table | (uintptr_t)lengths | (uintptr_t)stats | (uintptr_t)weights | (uintptr_t)weights_out | (uintptr_t)positions |
+       (uintptr_t)new_positions) & 3)
+    return fail(AE_ERR_INVALID_ARG, "%s: tables, lengths, stats, weights and positions must be 4-byte aligned", who);
+  if (new_stride < 0) return fail(AE_ERR_INVALID_ARG, "%s: the new positions' stride must not be negative", who);
+  const void* in[] = {Q, K_pages, K_exp, table, lengths, stats, new_positions};
+  for (const void* x : in)
+    if (x && (x == weights_out || x == positions)) return fail(AE_ERR_INVALID_ARG, "%s: an output aliases an input", who);
+  const uint64_t bytes = 4 * (uint64_t)h->params.B * h->params.H_kv * h->params.capacity;
+  if (!same_or_apart(weights, weights_out, bytes)) return fail(AE_ERR_INVALID_ARG, "%s: weights_out overlaps the weights", who);
+  for (const float* x : {weights, (const float*)weights_out})
+    if (positions && ((const void*)x == positions || !same_or_apart(x, positions, bytes)))
+      return fail(AE_ERR_INVALID_ARG, "%s: weights and positions alias each other", who);
+  ae::WeighParams p = h->params;
+  p.Q = static_cast<const __bf16*>(Q);
+  p.K = static_cast<const uint8_t*>(K_pages);
+  p.Ke = static_cast<const uint8_t*>(K_exp);
+  p.table = table;
+  p.lengths = lengths;
+  p.stats = stats;
+  p.weights = weights;
+  p.weights_out = weights_out;
+  p.positions = positions;
+  p.new_positions = new_positions;
+  p.new_stride = new_stride;
+  return launched(ae::launch_weigh(p, h->cache.D_qk, e4m3, stream), who);
+}
+
+ae_status_t ae_weigh_destroy(ae_weigh_t* h) {
+  delete h;
+  return AE_OK;
+}
+
+ae_status_t ae_evict_create(const ae_cache_t* cache, const ae_evict_desc_t* d, ae_evict_t** out) {
+  static const char who[] = "ae_evict_create";
+  if (out) *out = nullptr;
+  if (!cache || !d || !out) return fail(AE_ERR_INVALID_ARG, "%s: null argument", who);
+  const ae_cache_desc_t& cd = cache->desc;
+  const ae_status_t st = check_lists(cd, d->B, d->table_width, d->max_length, d->capacity, who);
+  if (st != AE_OK) return st;
+  if (d->keep < 1 || d->recent < 0 || d->sinks < 0) return fail(AE_ERR_INVALID_ARG, "%s: keep must be >= 1, recent and sinks >= 0", who);
+  ae_evict* h = new (std::nothrow) ae_evict();
+  if (!h) return fail(AE_ERR_NOMEM, "%s: out of host memory", who);
+  h->cache = cd;
+  ae::EvictParams& p = h->params;
+  p.capacity = d->capacity;
+  p.B = d->B;
+  p.H_kv = cd.H_kv;
+  p.page_shift = cache->page_shift;
+  p.n_pages = cd.n_pages;
+  p.table_width = d->table_width;
+  p.max_length = d->max_length;
+  p.keep = d->keep;
+  p.recent = d->recent;
+  p.sinks = d->sinks;
+  p.most_moves = ae::evict_most_moves(d->max_length, d->keep);
+  const int size = cd.dtype == AE_CACHE_E4M3 ? 1 : 2;
+  p.row_k = cd.D_qk * size;
+  p.row_v = cd.D_v * size;
+  h->ws_bytes = (size_t)d->B * cd.H_kv * (1 + 2 * (size_t)p.most_moves) * 4;
+  *out = h;
+  return AE_OK;
+}
+
+ae_status_t ae_evict_workspace_bytes(const ae_evict_t* h, size_t* bytes) {
+  if (!h || !bytes) return fail(AE_ERR_INVALID_ARG, "ae_evict_workspace_bytes: null argument");
+  *bytes = h->ws_bytes;
+  return AE_OK;
+}
+
+ae_status_t ae_evict_forward(const ae_evict_t* h, void* K_pages, void* V_pages, void* K_exp, void* V_exp, const int32_t* table, const int32_t* lengths,
+                             const float* weights, const int32_t* positions, float* weights_out, int32_t* positions_out, int32_t* lengths_out,
+                             void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  static const char who[] = "ae_evict_forward";
+  if (!h) return fail(AE_ERR_INVALID_ARG, "%s: null handle", who);
+  const bool e4m3 = h->cache.dtype == AE_CACHE_E4M3;
+  if (!K_pages || !V_pages || !table || !lengths || !weights || !positions || !weights_out || !positions_out || !lengths_out || !workspace)
+    return fail(AE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if ((K_exp != nullptr) != e4m3 || (V_exp != nullptr) != e4m3) return fail(AE_ERR_INVALID_ARG, "%s: exponents belong to an 8-bit cache, and only to it", who);
+  if (((uintptr_t)K_pages | (uintptr_t)V_pages) & 15) return fail(AE_ERR_INVALID_ARG, "%s: the pages must be 16-byte aligned", who);
+  if (((uintptr_t)table | (uintptr_t)lengths | (uintptr_t)weights | (uintptr_t)positions | (uintptr_t)weights_out | (uintptr_t)positions_out |
+       (uintptr_t)lengths_out | (uintptr_t)workspace | (uintptr_t)K_exp | (uintptr_t)V_exp) & 3)
+    return fail(AE_ERR_INVALID_ARG, "%s: tables, lengths, weights, positions, exponents and the workspace must be 4-byte aligned", who);
+  if (workspace_bytes < h->ws_bytes) return fail(AE_ERR_INVALID_ARG, "%s: the workspace holds %zu bytes, %zu are needed", who, workspace_bytes, h->ws_bytes);
+  const void* outs[] = {K_pages, V_pages, K_exp, V_exp, weights_out, positions_out, lengths_out, workspace};
+  const void* ins[] = {table, lengths, weights, positions};
+  for (int i = 0; i < 8; ++i) {
+    for (int k = 0; k < i; ++k)
+      if (outs[i] && outs[i] == outs[k]) return fail(AE_ERR_INVALID_ARG, "%s: two outputs alias each other", who);
+    for (const void* x : ins)
+      if (outs[i] && outs[i] == x && !(x == weights && outs[i] == weights_out) && !(x == positions && outs[i] == positions_out))
+        return fail(AE_ERR_INVALID_ARG, "%s: an output aliases an input", who);
+  }
+  const uint64_t bytes = 4 * (uint64_t)h->params.B * h->params.H_kv * h->params.capacity;
+  if (!same_or_apart(weights, weights_out, bytes) || !same_or_apart(positions, positions_out, bytes) || !same_or_apart(weights, positions_out, bytes) ||
+      !same_or_apart(positions, weights_out, bytes) || !same_or_apart(weights_out, positions_out, bytes))
+    return fail(AE_ERR_INVALID_ARG, "%s: weights and positions overlap each other", who);
+  ae::EvictParams p = h->params;
+  p.K = static_cast<uint8_t*>(K_pages);
+  p.V = static_cast<uint8_t*>(V_pages);
+  p.Ke = static_cast<uint8_t*>(K_exp);
+  p.Ve = static_cast<uint8_t*>(V_exp);
+  p.table = table;
+  p.lengths = lengths;
+  p.weights = weights;
+  p.positions = positions;
+  p.weights_out = weights_out;
+  p.positions_out = positions_out;
+  p.lengths_out = lengths_out;
+  p.moves = static_cast<int32_t*>(workspace);
+  return launched(ae::launch_evict(p, stream), who);
+}
+
+ae_status_t ae_evict_destroy(ae_evict_t* h) {
   delete h;
   return AE_OK;
 }

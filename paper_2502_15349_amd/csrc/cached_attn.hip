@@ -28,8 +28,11 @@ namespace {
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-template <int DQK_, int DV_, bool E4M3_, int RT_, int W_>
+// SCORED_: scores capped by a tanh, biased by the distance, or both (ScoredParams says which: the reading of the cache hides the choice)
+template <int DQK_, int DV_, bool E4M3_, int RT_, int W_, bool SCORED_ = false>
 struct CachedCfg {
+  static constexpr bool SCORED = SCORED_;
+  typedef std::conditional_t<SCORED, ScoredParams, CachedParams> P;
   static constexpr int DQK = DQK_, DV = DV_, RT = RT_, W = W_, THREADS = 64 * W;
   // Wavefronts per SIMD that the compiler is to leave room for.  (Four instead of two at 64/64 with 32 rows, where three fit anyway: eight
   // registers spill, 11 x 32/8 x 8 tokens x 5260 keys 28 -> 35 us.)
@@ -102,7 +105,7 @@ __device__ __forceinline__ uint64_t load_shared(const float* at) {
 
 // (WAVES_EU bounds the registers so that the wavefronts that LDS has room for are resident.)
 template <class C>
-__global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(const CachedParams p) {
+__global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(const typename C::P p) {
   __shared__ __attribute__((aligned(1024))) char smem[C::LDS_BYTES];
   const bool is_prefix = (int)blockIdx.x < p.prefix_blocks;
   const CachedPart& pt = p.part[is_prefix ? 1 : 0];
@@ -131,6 +134,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
   };
   bf16x8 qf[C::RT][C::KS];
   int lim[C::RT];  // keys below this one are visible to the lane's row
+  float slope[C::RT], at[C::RT];  // SCORED: of the lane's row, times log2(e); the row's own place, counted like the keys of this list
 #pragma unroll
   for (int rt = 0; rt < C::RT; ++rt) {
     int b, t, h;
@@ -140,6 +144,11 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     for (int s = 0; s < C::KS; ++s)  // 8-bit keys: a 16-byte chunk serves two steps
       qf[rt][s] = *reinterpret_cast<const bf16x8*>(q + (C::E4M3 ? 64 * (s / 2) + 16 * hi + 8 * (s % 2) : 32 * s + 8 * hi));
     lim[rt] = pt.causal ? len - p.n + 1 + t : len;
+    if constexpr (C::SCORED) {
+      const CachedPart& own = p.part[0];
+      slope[rt] = p.slopes[h];
+      at[rt] = (float)(pt.causal ? len - p.n + t : len + max(0, min(own.lengths[b], own.max_length)) - p.n + t);
+    }
   }
   const int all_visible = pt.causal ? len - p.n + 1 : len;  // keys below this one are visible to every row
 
@@ -278,13 +287,25 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
       float x[8];  // raw scores; c > 0 (a negative scale's sign is in the queries)
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = s[e / 4][rt][e % 4];
+      if constexpr (C::SCORED) {  // in powers of two from here on
+        if (p.capped) {
+          cap_scores<8>(x, p.cap);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= c;
+        }
+        const float d0 = at[rt] - (float)(j0 + 8 * hi);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(-slope[rt], d0 - (float)e, x[e]);
+      }
       if (masked) {
         const int last = min(lim[rt] - j0 - 8 * hi, there) - 1;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = e <= last ? x[e] : -INFINITY;
       }
       float mx = fmaxf(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]));
-      mx = max3(mx, x[6], x[7]) * c;
+      mx = max3(mx, x[6], x[7]);
+      if constexpr (!C::SCORED) mx *= c;
       if (__builtin_amdgcn_ballot_w64(mx > m[rt] + kLazyLog2) != 0) {
         mx = fmaxf(max_over_groups(mx), m[rt]);
         const float alpha = mx == -INFINITY ? 1.f : fast_exp2(m[rt] - mx);
@@ -297,7 +318,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        x[e] = fast_exp2(__builtin_fmaf(x[e], c, -ref));
+        x[e] = fast_exp2(C::SCORED ? x[e] - ref : __builtin_fmaf(x[e], c, -ref));
         sum += x[e];
       }
       l[rt] += sum;
@@ -358,6 +379,10 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
   if (n_my > 0) {
     hidden = issue_k(0);
     issue_v();
+  }
+  if constexpr (C::SCORED) {
+#pragma unroll
+    for (int rt = 0; rt < C::RT; ++rt) asm volatile("" ::"v"(slope[rt]), "v"(at[rt]));
   }
 #pragma unroll
   for (int rt = 0; rt < C::RT; ++rt)
@@ -603,7 +628,7 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(int32_t* at, int64_t n) 
 }
 
 template <class C>
-hipError_t launch_cfg(const CachedParams& p, hipStream_t s) {
+hipError_t launch_cfg(const typename C::P& p, hipStream_t s) {
   const CachedPart& pt = p.part[0];
   const int64_t grid = dealt_workgroups((int64_t)pt.lists * p.H_kv * pt.splits, pt.row_tiles) + p.prefix_blocks;
   if (!launch_fits(grid, C::THREADS) || grid > 0x7fffffff) return hipErrorInvalidConfiguration;
@@ -611,17 +636,25 @@ hipError_t launch_cfg(const CachedParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int DQK, int DV, bool E4M3, int W>
-hipError_t launch_rows(const CachedParams& p, hipStream_t s) {
+template <int DQK, int DV, bool E4M3, int W, class P>
+hipError_t launch_rows(const P& p, hipStream_t s) {
+  constexpr bool SCORED = std::is_same_v<P, ScoredParams>;
   const int rows = std::max(p.part[0].tile_rows, p.prefix_blocks ? p.part[1].tile_rows : 0);
-  if (rows <= 16) return launch_cfg<CachedCfg<DQK, DV, E4M3, 1, W>>(p, s);
-  return launch_cfg<CachedCfg<DQK, DV, E4M3, 2, W>>(p, s);
+  if (rows <= 16) return launch_cfg<CachedCfg<DQK, DV, E4M3, 1, W, SCORED>>(p, s);
+  return launch_cfg<CachedCfg<DQK, DV, E4M3, 2, W, SCORED>>(p, s);
 }
 
-template <int DQK, int DV>
-hipError_t launch_type(const CachedParams& p, bool e4m3, hipStream_t s) {
+template <int DQK, int DV, class P>
+hipError_t launch_type(const P& p, bool e4m3, hipStream_t s) {
   if (p.waves == 8) return e4m3 ? launch_rows<DQK, DV, true, 8>(p, s) : launch_rows<DQK, DV, false, 8>(p, s);
   return e4m3 ? launch_rows<DQK, DV, true, 4>(p, s) : launch_rows<DQK, DV, false, 4>(p, s);
+}
+
+template <class P>
+hipError_t launch_dims(const P& p, int dqk, int dv, bool e4m3, hipStream_t s) {
+  if (dqk == 64) return launch_type<64, 64>(p, e4m3, s);
+  if (dqk == 128) return launch_type<128, 128>(p, e4m3, s);
+  return launch_type<192, 128>(p, e4m3, s);
 }
 
 }  // namespace
@@ -638,11 +671,8 @@ int cached_residents(int dqk, int dv, bool e4m3, int rows, int waves) {
 // tokens x up to 4000 keys took 128 us instead of 50.)
 int cached_rows_per_workgroup(int rows) { return rows <= 16 ? 16 : 32; }
 
-hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s) {
-  if (dqk == 64) return launch_type<64, 64>(p, e4m3, s);
-  if (dqk == 128) return launch_type<128, 128>(p, e4m3, s);
-  return launch_type<192, 128>(p, e4m3, s);
-}
+hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s) { return launch_dims(p, dqk, dv, e4m3, s); }
+hipError_t launch_scored(const ScoredParams& p, int dqk, int dv, bool e4m3, hipStream_t s) { return launch_dims(p, dqk, dv, e4m3, s); }
 
 hipError_t launch_fill_zero(int32_t* at, int64_t n, hipStream_t s) {
   const int64_t grid = (n + 255) / 256;

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "span.hpp"
+
 namespace ae {
 
 // One set of key lists that the kernel walks: the sequences' own pages, or the shared prefix.  Rows are the query rows of one k/v
@@ -42,6 +44,14 @@ struct CachedParams {
   int32_t* counters;  // [B * H_kv * row tiles], kCounterStride apart, of workgroups that are done, zero before and after the launch; null: no workgroup waits for others
 };
 
+// With scores capped by a tanh (capped != 0) or biased by the distance (slopes, times log2(e); 0: not).
+constexpr int kMaxSlopeHeads = 256;
+struct ScoredParams : CachedParams {
+  CapParams cap;
+  int capped;
+  float slopes[kMaxSlopeHeads];
+};
+
 // Workgroups of `units` pieces of work with `tiles` row tiles each, dealt to the XCDs (which take the workgroups of a launch in turn):
 // tiles of a unit read the same keys and go to one XCD, one after the other, so that its L2 has them for the second; the tiles of
 // what is left over from whole rounds of eight units are spread over all XCDs.  (161 sequences x 8 tokens x 8/1 heads, 64/64, behind
@@ -71,6 +81,7 @@ int cached_rows_per_workgroup(int rows);  // at most
 // Workgroups of so many rows and wavefronts that a compute unit holds at a time.
 int cached_residents(int dqk, int dv, bool e4m3, int rows, int waves);
 hipError_t launch_cached(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);
+hipError_t launch_scored(const ScoredParams& p, int dqk, int dv, bool e4m3, hipStream_t s);
 constexpr int kPrefixRows = 256;  // rows of a workgroup of launch_prefix, which walks part[1] alone
 hipError_t launch_prefix(const CachedParams& p, int dqk, int dv, bool e4m3, hipStream_t s);
 hipError_t launch_fill_zero(int32_t* at, int64_t n, hipStream_t s);

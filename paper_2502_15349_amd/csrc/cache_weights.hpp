@@ -36,8 +36,9 @@ struct EvictParams {
   int64_t capacity;
   int B, H_kv, page_shift, n_pages, table_width, max_length, keep, recent, sinks, most_moves;
   int row_k, row_v;  // bytes of a row
+  int one_launch;    // rows are moved by the workgroup that selects
 };
 inline int evict_most_moves(int max_length, int keep) { return keep < max_length - keep ? keep : max_length > keep ? max_length - keep : 0; }
-hipError_t launch_evict(const EvictParams& p, hipStream_t s);
+hipError_t launch_evict(EvictParams p, hipStream_t s);
 
 }  // namespace ae

@@ -203,7 +203,8 @@ ae_status_t ae_cached_destroy(ae_cached_t *h); /* NULL is allowed */
  * and, unless both are NULL, positions[j] = new_positions[b][j - (lengths[b] - n_new)] for the newest.  Entries from lengths[b] on are left as
  * they are.  weights_out may be weights itself.  An entry on a page number outside the cache receives nothing; a row with the
  * statistic -inf gives nothing.  Sums are fp32, in an order that does not change.
- *   Q, stats   as in ae_cached_forward; new_positions  device, int32, [B, n_new], batch entries new_stride apart (0: shared).   */
+ *   Q, stats   as in ae_cached_forward; new_positions  device, int32, [B, n_new], batch entries new_stride apart (0: shared).
+ * At most 2^24 query rows, n_new (H_q / H_kv)^2 < 2^32 (AE_ERR_UNSUPPORTED beyond).                                             */
 typedef struct ae_weigh ae_weigh_t;
 typedef struct {
   int32_t B, H_q, n_new;
@@ -228,7 +229,7 @@ ae_status_t ae_weigh_destroy(ae_weigh_t *h); /* NULL is allowed */
  * weights_out and positions_out may be the inputs themselves, lengths_out not.  The pages of the lists must be the sequences' own: a page in
  * two lists (or twice in one) would be rewritten for both.  An entry on a page number outside the cache is counted like the others, and a row
  * that would come from or go to one is not copied.  workspace: device, 4-byte aligned, ae_evict_workspace_bytes, needs no
- * initialisation; calls that share it must not overlap.  Two launches (one where max_length <= keep).                       */
+ * initialisation; calls that share it must not overlap.  One launch or two.                                                */
 typedef struct ae_evict ae_evict_t;
 typedef struct {
   int32_t B;

@@ -92,7 +92,7 @@ ae_status_t ae_span_create(const ae_span_desc_t* d, ae_span_t** out) {
   if (d->cap != 0.f) {
     if (!(d->cap > 0.f) || !std::isfinite(d->cap)) return fail(AE_ERR_INVALID_ARG, "%s: cap must be 0 or positive and finite", who);
     cap = ae::cap_params(d->scale, d->cap);
-    const float all[] = {cap.k, cap.unit, cap.e, cap.inv};
+    const float all[] = {cap.k, cap.unit, cap.e, cap.poly[4]};
     for (float x : all)
       if (!std::isnormal(x)) return fail(AE_ERR_INVALID_ARG, "%s: cap and scale / cap must be in the range of 32-bit numbers", who);
   }

@@ -549,10 +549,10 @@ __device__ __forceinline__ void bwd_single_walk(const typename C::P& p, const De
       for (int t = 0; t < C::T2; ++t) dp = mfma(read_k_frag(ar2[t] + kRow2), xb2[t], dp);
     }
     float x[16];
-    if constexpr (C::CAPPED) cap_scores<16>(s, p.cap);  // (kept: the cap's derivative follows from them)
+    if constexpr (C::CAPPED) cap_tanh<16>(s, p.cap);  // (kept: the cap's derivative follows from them)
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      x[r] = C::CAPPED ? s[r] + nl4[r / 4][r % 4] : __builtin_fmaf(s[r], p.c2, C::NORM == NORM_SOFTMAX ? nl4[r / 4][r % 4] : p.b2);
+      x[r] = C::CAPPED ? __builtin_fmaf(s[r], p.cap.unit, nl4[r / 4][r % 4]) : __builtin_fmaf(s[r], p.c2, C::NORM == NORM_SOFTMAX ? nl4[r / 4][r % 4] : p.b2);
     if constexpr (C::SLOPED) {
       const float d0 = (float)(C::KV_SIDE ? o0 + off - own + 4 * half : own + off - o0 - 4 * half);  // query less key, register 0
 #pragma unroll
@@ -633,7 +633,7 @@ __device__ __forceinline__ void bwd_single_walk(const typename C::P& p, const De
         pv = fast_exp2(x[r]);
         if constexpr (C::HAS2) w2[r] = pv;
         pv = pv * (dp[r] - dl4[r / 4][r % 4]);
-        if constexpr (C::CAPPED) pv *= cap_slope(s[r], p.cap.inv);
+        if constexpr (C::CAPPED) pv *= cap_slope(s[r]);
       } else if constexpr (C::NORM == NORM_SIGMOID) {
         pv = fast_rcp(1.f + fast_exp2(-x[r]));
         if constexpr (C::HAS2) w2[r] = pv;
@@ -1190,10 +1190,10 @@ __device__ __forceinline__ void bwd_pair_walk(const typename C::P& p, const Deca
         static_for<0, T1 + AHEAD>(product);
         if constexpr (C::LIN) read_rows(nl4, nl_own, 0);  // (here: 16 registers less during the products)
         float x[16];
-        if constexpr (C::CAPPED) cap_scores<16>(s, p.cap);  // (kept: the cap's derivative follows from them)
+        if constexpr (C::CAPPED) cap_tanh<16>(s, p.cap);  // (kept: the cap's derivative follows from them)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          x[r] = C::CAPPED ? s[r] + nl4[r / 4][r % 4] : __builtin_fmaf(s[r], p.c2, C::NORM == NORM_SOFTMAX ? nl4[r / 4][r % 4] : p.b2);
+          x[r] = C::CAPPED ? __builtin_fmaf(s[r], p.cap.unit, nl4[r / 4][r % 4]) : __builtin_fmaf(s[r], p.c2, C::NORM == NORM_SOFTMAX ? nl4[r / 4][r % 4] : p.b2);
         if constexpr (C::SLOPED) {
           const float d0 = (float)(C::KV_SIDE ? o0 + off - own + 4 * half : own + off - o0 - 4 * half);  // query less key, register 0
 #pragma unroll
@@ -1294,7 +1294,7 @@ __device__ __forceinline__ void bwd_pair_walk(const typename C::P& p, const Deca
           const float dl = dl4[r / 4][r % 4], d = dp[r];
           if constexpr (C::NORM == NORM_SOFTMAX) {
             w[r] = pv[r] * (d - dl);
-            if constexpr (C::CAPPED) w[r] *= cap_slope(s[r], p.cap.inv);
+            if constexpr (C::CAPPED) w[r] *= cap_slope(s[r]);
           } else if constexpr (C::NORM == NORM_SIGMOID) {
             w[r] = d * pv[r] * (1.f - pv[r]);
           } else if constexpr (C::LIN) {

@@ -456,7 +456,7 @@ template <class C>
 __device__ __forceinline__ void post_done(const Params& p, const RowState<C>& st, float mx, bool& moved, float& xm) {
   if constexpr (C::NORM == NORM_SOFTMAX) {
     mx = max_halves(mx);
-    xm = C::FINAL ? mx : C::MOD == MOD_BIAS_T ? mx * p.b2 : __builtin_fmaf(mx, p.c, p.b2);  // c > 0
+    xm = C::MOD == MOD_BIAS_T ? mx * p.b2 : __builtin_fmaf(mx, p.c, p.b2);  // c > 0
     moved = xm > st.m + kLazyLog2;
   }
 }
@@ -486,10 +486,6 @@ __device__ __forceinline__ uint32_t finish_pair(const Params& p, int q, const f3
   if constexpr (C::NORM == NORM_SOFTMAX && C::MOD == MOD_BIAS_T) {
     x0 = fast_exp2(__builtin_fmaf(x0, p.b2, k0));
     x1 = fast_exp2(__builtin_fmaf(x1, p.b2, k0));
-    acc += x0 + x1;
-  } else if constexpr (C::FINAL) {
-    x0 = fast_exp2(x0 + k0);
-    x1 = fast_exp2(x1 + k0);
     acc += x0 + x1;
   } else if constexpr (C::NORM == NORM_SOFTMAX) {
     x0 = fast_exp2(__builtin_fmaf(x0, p.c, k0));
@@ -830,6 +826,39 @@ struct KeyLoop {
     }
   }
 
+  // Capped and distance-biased scores, as exponents relative to the row's reference (to zero while it has none): where one is above it by
+  // more than kLazyLog2 the reference moves, and the exponents, the sum and the output with it.  Under a slope the scores rise from tile to tile
+  // (by 46 powers of two in 32 keys at a slope of one), so there it moves kAhead powers of two beyond them, which spares most of the moves that would follow:
+  // weights of 2^-40 leave 86 more in 32 bits, and a common factor of all weights of a row is no error.
+  static constexpr float kAhead = C::SLOPED ? 40.f : 0.f;
+  __device__ __forceinline__ void final_weights(f32x16& s, float& acc) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) mx = max3(mx, s[2 * q], s[2 * q + 1]);
+    mx = max_halves(mx);
+    const bool unset = st.m == -INFINITY, moved = unset ? mx > -INFINITY : mx > kLazyLog2;
+    if (__builtin_amdgcn_ballot_w64(moved) != 0) {
+      const float d = moved ? mx + kAhead : 0.f, alpha = moved && !unset ? fast_exp2(-d) : 1.f;  // (a row without a reference has nothing to rescale)
+      if (moved) st.m = unset ? d : st.m + d;
+      st.l *= alpha;
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st.o[db][r] *= alpha;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] -= d;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float x0 = fast_exp2(s[2 * q]), x1 = fast_exp2(s[2 * q + 1]);
+      acc += x0 + x1;
+      bf16x2 pr;
+      pr[0] = (__bf16)x0;
+      pr[1] = (__bf16)x1;
+      pk[q / 4][q % 4] = __builtin_bit_cast(uint32_t, pr);
+    }
+  }
+
   // Vector phase: the raw scores in s (sub-tile u, starting at key j0 = 32u) become
   // packed weights in pk; the row state follows.
   // FAST: the caller knows that no key of the sub-tile is hidden from any row of the wave.
@@ -846,16 +875,33 @@ struct KeyLoop {
     const float dbase = C::MOD == MOD_DECAY ? g2 * (float)(i + off - j0 - 4 * half) : 0.f;
     float mx = -INFINITY, xm = 0.f, acc = 0.f;
     bool moved = false;
-    if constexpr (C::CAPPED) cap_scores<16>(s, p.cap);
-    if constexpr (C::SLOPED) {
+    if constexpr (C::FINAL) {
+      // exponents relative to the row's reference, which so comes along in the last multiply-add
+      const float k0 = finish_k0<C>(p, st);
       const float d0 = (float)(i + off - j0 - 4 * half);  // distance of register 0's key
+      auto form = [&](auto&& term) {
+        if constexpr (C::CAPPED) {
+          cap_scores<16>(s, p.cap, term);
+        } else {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(-g2, __builtin_fabsf(d0 - (float)key_offset(r)), C::CAPPED ? s[r] : s[r] * p.c);
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], p.c, term(r));
+        }
+      };
+      if constexpr (!C::SLOPED) {
+        form([&](int) { return k0; });
+      } else if (j0 + C::SUB_N - 1 <= iw0 + off) {  // no key behind a row of the wave: distances need no magnitude
+        const float base = __builtin_fmaf(-g2, d0, k0);
+        form([&](int r) { return __builtin_fmaf(g2, (float)key_offset(r), base); });
+      } else {
+        form([&](int r) { return __builtin_fmaf(-g2, __builtin_fabsf(d0 - (float)key_offset(r)), k0); });
+      }
     }
     if (masked) mask_raw<C>(s, jlim, -INFINITY);
     if (masked_lo) mask_raw_below<C>(s, jlo, -INFINITY);
     if constexpr (C::FOLD) {
       folded_weights(s, acc);
+    } else if constexpr (C::FINAL) {
+      final_weights(s, acc);
     } else {
     if (C::MOD == MOD_DECAY && fact) {
       // one exponential per lane and sub-tile instead of one per score
@@ -1012,35 +1058,49 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
   if constexpr (C::SPAN) {
     constexpr int kNone = 0x7fffffff;
     span_of(p.span, b, min(i, p.L_q - 1), off, p.L_k, span_lo, span_hi);
-    const bool sees = span_lo < span_hi;
-    lo_w = sees ? span_lo : kNone;
-    kmax_w = span_hi;
-    all_lo = span_lo;
-    all_hi = span_hi;
-    // (two lanes hold a row of the wave; the workgroup's other rows are read again, by every wave, which needs no barrier)
-    lo_wg = lo_w;
-    kmax = span_hi;
-    last_lo = span_lo;
+    if (p.span.kind != SPAN_GIVEN) {  // begin and end never fall from row to row, and the first rows may see nothing
+      auto bounds = [&](int r0, int r1, int& lo_first, int& hi_last, int& lo_last, int& hi_first) {
+        r1 = min(r1, p.L_q - 1);
+        int unused;
+        span_of(p.span, b, min(r0, r1), off, p.L_k, unused, hi_first);
+        span_of(p.span, b, r1, off, p.L_k, lo_last, hi_last);
+        span_of(p.span, b, min(max(r0, -off), r1), off, p.L_k, lo_first, unused);
+        if (lo_first >= unused) lo_first = kNone;
+      };
+      int unused;
+      bounds(iw0, iw0 + 31, lo_w, kmax_w, all_lo, all_hi);
+      bounds(i_wg, i_wg + C::BLOCK_M - 1, lo_wg, kmax, last_lo, unused);
+    } else {
+      const bool sees = span_lo < span_hi;
+      lo_w = sees ? span_lo : kNone;
+      kmax_w = span_hi;
+      all_lo = span_lo;
+      all_hi = span_hi;
+      // (two lanes hold a row of the wave; the workgroup's other rows are read again, by every wave, which needs no barrier)
+      lo_wg = lo_w;
+      kmax = span_hi;
+      last_lo = span_lo;
 #pragma unroll
-    for (int k = 0; k < C::BLOCK_M / 64; ++k) {
-      int lo, hi;
-      span_of(p.span, b, min(i_wg + 64 * k + lane, p.L_q - 1), off, p.L_k, lo, hi);
-      lo_wg = min(lo_wg, lo < hi ? lo : kNone);
-      kmax = max(kmax, hi);
-      last_lo = max(last_lo, lo);
-    }
+      for (int k = 0; k < C::BLOCK_M / 64; ++k) {
+        int lo, hi;
+        span_of(p.span, b, min(i_wg + 64 * k + lane, p.L_q - 1), off, p.L_k, lo, hi);
+        lo_wg = min(lo_wg, lo < hi ? lo : kNone);
+        kmax = max(kmax, hi);
+        last_lo = max(last_lo, lo);
+      }
 #pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-      lo_w = min(lo_w, __shfl_xor(lo_w, s));
-      kmax_w = max(kmax_w, __shfl_xor(kmax_w, s));
-      all_lo = max(all_lo, __shfl_xor(all_lo, s));
-      all_hi = min(all_hi, __shfl_xor(all_hi, s));
-      lo_wg = min(lo_wg, __shfl_xor(lo_wg, s));
-      kmax = max(kmax, __shfl_xor(kmax, s));
-      last_lo = max(last_lo, __shfl_xor(last_lo, s));
+      for (int s = 1; s < 64; s *= 2) {
+        lo_w = min(lo_w, __shfl_xor(lo_w, s));
+        kmax_w = max(kmax_w, __shfl_xor(kmax_w, s));
+        all_lo = max(all_lo, __shfl_xor(all_lo, s));
+        all_hi = min(all_hi, __shfl_xor(all_hi, s));
+        lo_wg = min(lo_wg, __shfl_xor(lo_wg, s));
+        kmax = max(kmax, __shfl_xor(kmax, s));
+        last_lo = max(last_lo, __shfl_xor(last_lo, s));
+      }
+      auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
+      scalar(lo_w), scalar(kmax_w), scalar(all_lo), scalar(all_hi), scalar(lo_wg), scalar(kmax), scalar(last_lo);
     }
-    auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
-    scalar(lo_w), scalar(kmax_w), scalar(all_lo), scalar(all_hi), scalar(lo_wg), scalar(kmax), scalar(last_lo);
     if (lo_wg == kNone) lo_wg = 0;
   }
   if (iw0 >= p.L_q) kmax_w = 0;  // a wave past the last query row only helps with the copies
@@ -1419,7 +1479,12 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
       inv = l > 0.f ? 1.f / l : 0.f;
       // weights are 2^(x*log2e - m): sum_j exp(x_j) = 2^m * l  (FOLD leaves a constant bias out of m: every
       // weight of the row carries it, so only the statistic sees it)
-      stat = l > 0.f ? (st.m + (C::FOLD ? p.b2 : 0.f) + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+      float m = st.m + (C::FOLD ? p.b2 : 0.f), f = l;
+      if constexpr (C::SLOPED) {  // (a reference far beyond the scores: the powers of two that the sum holds go with it, exactly)
+        m += (float)__builtin_amdgcn_frexp_expf(l);
+        f = __builtin_amdgcn_frexp_mantf(l);
+      }
+      stat = l > 0.f ? (m + __builtin_amdgcn_logf(f)) * 0.6931471805599453f : -INFINITY;
     } else if constexpr (C::NORM == NORM_ABSSUM) {
       inv = 1.f / fmaxf(l, 1.f);
     } else {

@@ -5,7 +5,12 @@
 // A wavefront takes 32 keys, which stay in registers, and goes through the query rows of its k/v head 16 at a time: S^T [32 keys x 16
 // rows] = K Q^T by MFMA 16x16x32 with the keys in the order of cached_attn.hip, so that a lane holds 8 neighbouring keys of one
 // row.  The weights are summed in its registers over the row tiles and over the 16 lanes of a group at the end, in a fixed order; every
-// entry is written once, by one wavefront.
+// entry is written once, by one wavefront.  One tile of rows comes straight from memory, more through LDS, 64 rows at a time, where the four wavefronts
+// of a workgroup share them (each for itself: the L2 serves 2 GB for 500 tokens of 4 x 16/16 heads x 8000 keys of 128, 237 us instead of 138 in 8 bits with a cap).
+//
+// Bound by the reading of the keys for a few rows (16 x 32/8 x 2048, one token: 12.9 us, 3.2 TB/s; 8 tokens 15.4), by vector instructions for many (an
+// exponential, a multiply-add, an addition and, with a cap, eight more for every score; 500 tokens as above: 98 us, 0.65 PFLOP/s; capped 138).  64 keys a wavefront, with half
+// the reads of the rows: 106 and 147, and a third slower where there are fewer keys than compute units take (1 x 32/8 x 200 of 3000: 21.6 -> 32.4).
 #include "cache_weights.hpp"
 
 #include "cached_attn.hpp"
@@ -18,27 +23,39 @@ namespace {
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 constexpr int kWeighKeys = 128;  // of a workgroup: four wavefronts of 32
+constexpr int kWeighRows = 64;  // query rows in LDS at a time (twice: the next ones arrive meanwhile)
 
-template <int DQK, bool E4M3>
+// SHARED: rows go through LDS.
+template <int DQK, bool E4M3, bool SHARED>
 __global__ __launch_bounds__(256) void weigh_kernel(const WeighParams p) {
   constexpr int KS = DQK / 32, RB = DQK * (E4M3 ? 1 : 2);
+  // Rows in LDS are 16 bytes apart from each other's end: 16 rows' chunks of 16 bytes lie in different banks.
+  constexpr int PITCH = 2 * DQK + 16, CHUNKS = DQK / 8, COPIES = kWeighRows * CHUNKS / 256;
+  __shared__ __attribute__((aligned(16))) char row_lds[SHARED ? 2 * kWeighRows * PITCH : 16];
+  __shared__ float nl_lds[SHARED ? 2 * kWeighRows : 1];
+  __shared__ int lim_lds[SHARED ? 2 * kWeighRows : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ql = lane & 15, hi = lane >> 4;
   int head, tile;
   if (!dealt_to(blockIdx.x, p.B * p.H_kv, (p.max_length + kWeighKeys - 1) / kWeighKeys, head, tile)) return;
   const int b = head / p.H_kv, hk = head % p.H_kv;
   const int len = max(0, min(scalar_load(p.lengths + b), p.max_length));
+  if (tile * kWeighKeys >= len) return;
   const int j0 = tile * kWeighKeys + 32 * wave;
-  if (j0 >= len) return;
+  if (!SHARED && j0 >= len) return;
 
-  // ---- keys: A fragments, straight from the pages (the two halves of 16 lie on a page each; one outside the cache is hidden) ----
+  // ---- keys: A fragments, straight from the pages (the two halves of 16 lie on a page each; one outside the cache is hidden, one behind the list's
+  // end is the one in front of it) ----
   const int32_t* table = p.table + (int64_t)b * p.table_width;
   const int mask = (1 << p.page_shift) - 1;
-  const bool second = j0 + 16 < len;
-  const int pg0 = scalar_load(table + (j0 >> p.page_shift)), pg1 = second ? scalar_load(table + ((j0 + 16) >> p.page_shift)) : pg0;
-  const bool ok0 = (uint32_t)pg0 < (uint32_t)p.n_pages, ok1 = (uint32_t)pg1 < (uint32_t)p.n_pages;
-  const int64_t row0 = (((int64_t)(ok0 ? pg0 : 0) * p.H_kv + hk) << p.page_shift) + (j0 & mask);
-  const int64_t row1 = second ? (((int64_t)(ok1 ? pg1 : 0) * p.H_kv + hk) << p.page_shift) + ((j0 + 16) & mask) : row0;
-  const int64_t krow = (ql < 8 ? row0 : row1) + 8 * ((ql >> 2) & 1) + (ql & 3);  // of tile u: + 4 u
+  bool hidden[2];
+  auto page_row = [&](int n) -> int64_t {
+    const int j = min(j0 + 16 * n, (len - 1) & ~15);
+    const int pg = scalar_load(table + (j >> p.page_shift));
+    hidden[n] = (uint32_t)pg >= (uint32_t)p.n_pages;
+    return (((int64_t)(hidden[n] ? 0 : pg) * p.H_kv + hk) << p.page_shift) + (j & mask);
+  };
+  const int64_t lower = page_row(0), upper = page_row(1);
+  const int64_t krow = (ql < 8 ? lower : upper) + 8 * ((ql >> 2) & 1) + (ql & 3);  // of tile u: + 4 u
   bf16x8 kf[2][KS];
   if constexpr (E4M3) {
     u32x4 raw[2][KS / 2];
@@ -63,36 +80,28 @@ __global__ __launch_bounds__(256) void weigh_kernel(const WeighParams p) {
       for (int s = 0; s < KS; ++s) kf[u][s] = *reinterpret_cast<const bf16x8*>(p.K + (krow + 4 * u) * RB + 64 * s + 16 * hi);
   }
 
-  // ---- query rows: B fragments, lane = row ql of the tile ----
+  // ---- the lane's own entry, in the end ----
   const int rows = p.n * p.g, first_new = len - p.n;  // (less than 0: the first rows see nothing)
-  // rows of earlier tokens see none of these keys
-  const int rt0 = (int)((int64_t)max(0, j0 - first_new) * p.g / 16);
-  bf16x8 qn[KS];  // the next tile's
-  float nl_next = 0.f;
-  int lim_next = 0;  // keys below it are visible to the row
-  auto fetch = [&](int rt) {
-    const int r = min(16 * rt + ql, rows - 1), t = r / p.g, h = hk * p.g + r % p.g;
-    const __bf16* q = p.Q + b * p.qs[0] + h * p.qs[1] + t * p.qs[2];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qn[s] = *reinterpret_cast<const bf16x8*>(q + (E4M3 ? 64 * (s / 2) + 16 * hi + 8 * (s % 2) : 32 * s + 8 * hi));
-    const float lse = p.stats[((int64_t)b * p.H_q + h) * p.n + t];
-    nl_next = lse * -1.4426950408889634f;
-    // (a row that there is not, or one with the statistic -infinity, sees nothing, whatever the keys hold)
-    lim_next = 16 * rt + ql < rows && __builtin_bit_cast(uint32_t, lse) != 0xff800000u ? first_new + 1 + t : -1;
+  const int j = j0 + 8 * hi + (ql >> 1);              // (bits 3, 2, 1 of the lane: 4, 2, 1 keys)
+  const bool writes = (ql & 1) == 0 && j < len, is_new = j >= first_new;
+  const int64_t at = ((int64_t)b * p.H_kv + hk) * p.capacity + j;
+  const float was = writes && !is_new ? p.weights[at] : 0.f;
+
+  // ---- query rows: B fragments, lane = row ql of the tile; row r is token r / g, q head r % g of the group ----
+  const __bf16* q0 = p.Q + b * p.qs[0] + (int64_t)hk * p.g * p.qs[1];
+  const float* lse0 = p.stats + ((int64_t)b * p.H_q + hk * p.g) * p.n;
+  auto q_chunk = [&](int s) { return E4M3 ? 64 * (s / 2) + 16 * hi + 8 * (s % 2) : 32 * s + 8 * hi; };  // first element of the lane's piece of step s
+  // what a row takes off its exponents, and the keys that it sees: those below the limit (a row that there is not, or one with the statistic
+  // -infinity, sees nothing, whatever the keys hold)
+  auto row_state = [&](bool there, int t, int h, float& nl, int& lim) {
+    const float lse = lse0[h * p.n + t];
+    nl = lse * -1.4426950408889634f;
+    lim = there && __builtin_bit_cast(uint32_t, lse) != 0xff800000u ? first_new + 1 + t : -1;
   };
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  const int n_rt = (rows + 15) / 16;
-  if (rt0 < n_rt) fetch(rt0);
-  for (int rt = rt0; rt < n_rt; ++rt) {
-    bf16x8 qf[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = qn[s];
-    const float nl = nl_next;
-    const int last = lim_next - 1 - j0 - 8 * hi;  // of the lane's 8 keys those up to it are visible
-    const bool masked = __builtin_amdgcn_ballot_w64(last < 7) != 0;
-    if (rt + 1 < n_rt) fetch(rt + 1);
+  auto tile_of_rows = [&](const bf16x8 (&qf)[KS], float nl, int lim) {
     f32x4 sc[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -104,19 +113,79 @@ __global__ __launch_bounds__(256) void weigh_kernel(const WeighParams p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = sc[e / 4][e % 4];
     if (p.capped) {
-      cap_scores<8>(x, p.cap);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += nl;
+      cap_scores<8>(x, p.cap, [&](int) { return nl; });
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(x[e], p.c, nl);
     }
-    if (masked) {
+    const int last = lim - 1 - j0 - 8 * hi;  // of the lane's 8 keys those up to it are visible
+    if (__builtin_amdgcn_ballot_w64(last < 7) != 0) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = e <= last ? x[e] : -INFINITY;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] += __builtin_amdgcn_exp2f(x[e]);
+  };
+  // rows of earlier tokens see none of the keys
+  if constexpr (SHARED) {
+    const int c0 = (int)((int64_t)max(0, tile * kWeighKeys - first_new) * p.g / kWeighRows), n_c = (rows + kWeighRows - 1) / kWeighRows;
+    u32x4 got[COPIES];
+    float nl = 0.f;
+    int lim = -1;
+    auto place = [&](int r, int& t, int& h) {
+      r = min(r, rows - 1);
+      t = p.g == 1 ? r : (int)__umulhi((uint32_t)r, p.g_inverse);  // (exact: r g < 2^32)
+      h = r - t * p.g;
+    };
+    auto request = [&](int c) {
+      int t, h;
+#pragma unroll
+      for (int i = 0; i < COPIES; ++i) {
+        const int n = 256 * i + threadIdx.x;
+        place(kWeighRows * c + n / CHUNKS, t, h);
+        got[i] = *reinterpret_cast<const u32x4*>(q0 + h * p.qs[1] + t * p.qs[2] + n % CHUNKS * 8);
+      }
+      if (threadIdx.x < kWeighRows) {
+        const int r = kWeighRows * c + threadIdx.x;
+        place(r, t, h);
+        row_state(r < rows, t, h, nl, lim);
+      }
+    };
+    request(c0);
+    for (int c = c0; c < n_c; ++c) {
+      const int buf = c & 1;
+      char* to = row_lds + buf * kWeighRows * PITCH;
+#pragma unroll
+      for (int i = 0; i < COPIES; ++i) {
+        const int n = 256 * i + threadIdx.x;
+        *reinterpret_cast<u32x4*>(to + n / CHUNKS * PITCH + n % CHUNKS * 16) = got[i];
+      }
+      if (threadIdx.x < kWeighRows) {
+        nl_lds[buf * kWeighRows + threadIdx.x] = nl;
+        lim_lds[buf * kWeighRows + threadIdx.x] = lim;
+      }
+      __syncthreads();  // (the other buffer was read in front of it)
+      if (c + 1 < n_c) request(c + 1);
+      const int tiles = min(kWeighRows / 16, (rows - kWeighRows * c + 15) / 16);
+      if (j0 >= len) continue;
+      for (int rt = 0; rt < tiles; ++rt) {
+        bf16x8 qf[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(to + (16 * rt + ql) * PITCH + q_chunk(s) * 2);
+        tile_of_rows(qf, nl_lds[buf * kWeighRows + 16 * rt + ql], lim_lds[buf * kWeighRows + 16 * rt + ql]);
+      }
+    }
+  } else {  // one tile
+    const bool there = ql < rows;
+    const int r = there ? ql : rows - 1, t = r / p.g, h = r % p.g;
+    const __bf16* q = q0 + h * p.qs[1] + t * p.qs[2];
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + q_chunk(s));
+    float nl;
+    int lim;
+    row_state(there, t, h, nl, lim);
+    tile_of_rows(qf, nl, lim);
   }
 
   // ---- over the 16 lanes of a group: halves are exchanged, so that a pair of lanes ends with one key ----
@@ -138,23 +207,24 @@ __global__ __launch_bounds__(256) void weigh_kernel(const WeighParams p) {
     acc[0] = keep + __shfl_xor(give, 2);
   }
   acc[0] += __shfl_xor(acc[0], 1);
-  const int j = j0 + 8 * hi + (ql >> 1);  // (bits 3, 2, 1 of the lane: 4, 2, 1 keys)
-  if ((ql & 1) == 0 && j < len) {
-    const int64_t at = ((int64_t)b * p.H_kv + hk) * p.capacity + j;
-    const bool is_new = j >= first_new;
-    const float was = is_new ? 0.f : p.weights[at];
-    p.weights_out[at] = was + ((hi < 2 ? ok0 : ok1) ? acc[0] : 0.f);
+  if (writes) {
+    p.weights_out[at] = was + ((hi < 2 ? hidden[0] : hidden[1]) ? 0.f : acc[0]);
     if (is_new && p.positions != nullptr) p.positions[at] = p.new_positions[b * p.new_stride + (j - first_new)];
   }
 }
 
-template <int DQK>
-hipError_t launch_weigh_dim(const WeighParams& p, bool e4m3, hipStream_t s) {
+template <int DQK, bool SHARED>
+hipError_t launch_weigh_cfg(const WeighParams& p, bool e4m3, hipStream_t s) {
   const int64_t grid = dealt_workgroups((int64_t)p.B * p.H_kv, (p.max_length + kWeighKeys - 1) / kWeighKeys);
   if (!launch_fits(grid, 256) || grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-  if (e4m3) hipLaunchKernelGGL((weigh_kernel<DQK, true>), dim3((unsigned)grid), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((weigh_kernel<DQK, false>), dim3((unsigned)grid), dim3(256), 0, s, p);
+  if (e4m3) hipLaunchKernelGGL((weigh_kernel<DQK, true, SHARED>), dim3((unsigned)grid), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((weigh_kernel<DQK, false, SHARED>), dim3((unsigned)grid), dim3(256), 0, s, p);
   return hipGetLastError();
+}
+template <int DQK>
+hipError_t launch_weigh_dim(const WeighParams& p, bool e4m3, hipStream_t s) {
+  if ((int64_t)p.n * p.g > 16) return launch_weigh_cfg<DQK, true>(p, e4m3, s);
+  return launch_weigh_cfg<DQK, false>(p, e4m3, s);
 }
 
 }  // namespace

@@ -288,15 +288,14 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = s[e / 4][rt][e % 4];
       if constexpr (C::SCORED) {  // in powers of two from here on
+        const float base = -slope[rt] * (at[rt] - (float)(j0 + 8 * hi));  // (no key is behind its token)
+        auto far = [&](int e) { return __builtin_fmaf(slope[rt], (float)e, base); };
         if (p.capped) {
-          cap_scores<8>(x, p.cap);
+          cap_scores<8>(x, p.cap, far);
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= c;
+          for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(x[e], c, far(e));
         }
-        const float d0 = at[rt] - (float)(j0 + 8 * hi);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(-slope[rt], d0 - (float)e, x[e]);
       }
       if (masked) {
         const int last = min(lim[rt] - j0 - 8 * hi, there) - 1;

@@ -112,7 +112,10 @@ __device__ __forceinline__ bool factor_hidden(float f) { return __builtin_bit_ca
 enum : int { BWD_DQ = 0, BWD_DKV = 1 };  // the query-side kernel (dQ), the key-side kernel (dK and dV)
 
 // ---- one wavefront per 32 own rows ---------------------------------------------------------------------------------
-template <int DQK_, int DV_, int NORM_, bool CAUSAL_, int OUT_, bool BIAS_ = false, int VAR_ = 0>
+// SPLIT_ (spans): a workgroup owns 64 rows; wavefronts 0 and 1 take the first 32 other rows of every tile for them, 2 and 3 the second 32, and hand
+// their results over at the end.  Walks are half as long, for twice the copies of the other side's tiles: for calls of few workgroups (see
+// launch_span_var).
+template <int DQK_, int DV_, int NORM_, bool CAUSAL_, int OUT_, bool BIAS_ = false, int VAR_ = 0, bool SPLIT_ = false>
 struct BwdCfg {
   static constexpr bool SPAN = VAR_ != 0, CAPPED = (VAR_ & BWD_CAP) != 0, SLOPED = (VAR_ & BWD_SLOPE) != 0;
   typedef std::conditional_t<SPAN, BwdSpanParams, BwdParams> P;
@@ -120,7 +123,9 @@ struct BwdCfg {
   static constexpr bool BIAS = BIAS_;  // S' = scale * S + bias[b, h_q, i, j]
   static constexpr int DQK = DQK_, DV = DV_, NORM = NORM_, OUT = OUT_;
   static constexpr bool CAUSAL = CAUSAL_, KV_SIDE = OUT_ == BWD_DKV;
-  static constexpr int WAVES = 4, THREADS = 256, OWN = 128;  // own rows per workgroup
+  static constexpr bool SPLIT = SPLIT_;
+  static_assert(!SPLIT || SPAN, "");
+  static constexpr int WAVES = 4, THREADS = 256, OWN = SPLIT ? 64 : 128;  // own rows per workgroup
   static constexpr bool PAIR = false;
   static constexpr int T1 = DQK / 16, T2 = DV / 16;
   static constexpr int DB = DQK / 32;  // 32-row blocks of the transposed result dQ^T / dK^T
@@ -151,8 +156,13 @@ struct BwdCfg {
   // one workgroup per CU: the LDS fragments of a step are read as a batch ahead of its MFMAs
   static constexpr bool BATCH = !OCC2 && DQK + DV <= 320;  // (beyond that the batches do not fit 512 registers)
   static_assert(LDS_BYTES <= 160 * 1024, "a workgroup must fit LDS");
+  static_assert(!SPLIT || 8192 * (DB + DB2) <= LDS_BYTES, "the results of two wavefronts go through LDS");
   static_assert((TILE * CPR1 / 64) % WAVES == 0 && (TILE * CPR2 / 64) % WAVES == 0, "every wave copies the same number of blocks");
 };
+
+__device__ __forceinline__ void lds_store16(uint32_t addr, u32x4 v) {
+  *reinterpret_cast<__attribute__((address_space(3))) u32x4*>((lds_char*)(uintptr_t)addr) = v;
+}
 
 // dO of a q head: contiguous, but for spans
 template <class C>
@@ -272,7 +282,7 @@ __device__ __forceinline__ void bwd_single_walk(const typename C::P& p, const De
   const int b = group / p.H_kv, hk = group % p.H_kv;
   int ot = C::KV_SIDE ? item : n_own_tiles - 1 - item / p.g;
   const int ho = C::KV_SIDE ? hk : hk * p.g + item % p.g;  // ho: k/v head (key side) or q head (query side)
-  const int own0 = ot * C::OWN, ow0 = own0 + wave * 32;  // first own row of the workgroup / of this wave
+  const int own0 = ot * C::OWN, ow0 = own0 + (C::SPLIT ? wave & 1 : wave) * 32;  // first own row of the workgroup / of this wave
   const int own = ow0 + ln;                              // this lane's own row (column of S, dP, G^T)
   const int own_c = own < L_own ? own : L_own - 1;
 
@@ -709,8 +719,8 @@ __device__ __forceinline__ void bwd_single_walk(const typename C::P& p, const De
       if (n % nt == 0) set_decay(hk * p.g + n / nt);
     if constexpr (C::KV_SIDE && C::SLOPED)
       if (n % nt == 0) sl = dt.log2_gamma[hk * p.g + n / nt];
-    subtile(stagec, std::integral_constant<int, 0>{}, r0);
-    subtile(stagec, std::integral_constant<int, 1>{}, r0 + 32);
+    if (!C::SPLIT || wave < 2) subtile(stagec, std::integral_constant<int, 0>{}, r0);
+    if (!C::SPLIT || wave >= 2) subtile(stagec, std::integral_constant<int, 1>{}, r0 + 32);
     if (n + 1 < total) store_rowq(rowq_next, STAGE ^ 1);
   };
 
@@ -731,6 +741,30 @@ __device__ __forceinline__ void bwd_single_walk(const typename C::P& p, const De
   for (int n = 0; n < total; n += 2) {
     tile(std::integral_constant<int, 0>{}, n);
     if (n + 1 < total) tile(std::integral_constant<int, 1>{}, n + 1);
+  }
+
+  if constexpr (C::SPLIT) {
+    constexpr int NB = C::DB + C::DB2;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (every wave is done with the tiles)
+    const uint32_t to = lds0 + ((wave & 1) * NB * 4 * 64 + lane) * 16;
+    auto each = [&](auto&& f) {
+      static_for<0, NB>([&](auto kc) {
+        constexpr int k = decltype(kc)::value;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if constexpr (k < C::DB) f(g[k], q, to + (4 * k + q) * 1024);
+          else f(g2[k - C::DB], q, to + (4 * k + q) * 1024);
+        }
+      });
+    };
+    if (wave >= 2) each([&](f32x16& v, int q, uint32_t at) { lds_store16(at, __builtin_bit_cast(u32x4, f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]})); });
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (wave >= 2) return;
+    each([&](f32x16& v, int q, uint32_t at) {
+      const f32x4 x = lds_read16(at);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * q + e] += x[e];
+    });
   }
 
   // ---- results: register r of block db is column own, row d = 32 db + 8 (r/4) + 4 half + r%4 ----
@@ -837,9 +871,6 @@ __device__ __forceinline__ float lds_read4(uint32_t addr) {
 }
 __device__ __forceinline__ void lds_store4(uint32_t addr, float v) {
   *reinterpret_cast<__attribute__((address_space(3))) float*>((lds_char*)(uintptr_t)addr) = v;
-}
-__device__ __forceinline__ void lds_store16(uint32_t addr, u32x4 v) {
-  *reinterpret_cast<__attribute__((address_space(3))) u32x4*>((lds_char*)(uintptr_t)addr) = v;
 }
 
 template <class C>

@@ -53,13 +53,13 @@ constexpr int64_t short_window() { return DQK == 128 && DV == 128 ? 128 : 0; }
 // The workgroups of a side: whole sets of `together` groups (or parts of groups) per XCD (the kernels' mapping): sets x together x
 // 8 XCDs x workgroups per group or part.
 inline int64_t side_rounds(const BwdParams& p) { return (((int64_t)p.B * p.H_kv << p.cut) + 7) / 8; }
-inline int64_t side_per_group(const BwdParams& p, bool key_side) {
-  const int64_t n = (int64_t)(((key_side ? p.L_k : p.L_q) + 127) / 128) * (key_side ? 1 : p.g);  // (all kernels own 128 rows per workgroup)
+inline int64_t side_per_group(const BwdParams& p, bool key_side, int own = 128) {
+  const int64_t n = (int64_t)(((key_side ? p.L_k : p.L_q) + own - 1) / own) * (key_side ? 1 : p.g);
   return (n + (1 << p.cut) - 1) >> p.cut;
 }
-inline int64_t side_blocks(const BwdParams& p, bool key_side) {
+inline int64_t side_blocks(const BwdParams& p, bool key_side, int own = 128) {
   const int64_t tg = p.together[key_side ? 1 : 0];
-  return tg < 1 ? -1 : (side_rounds(p) + tg - 1) / tg * tg * 8 * side_per_group(p, key_side);
+  return tg < 1 ? -1 : (side_rounds(p) + tg - 1) / tg * tg * 8 * side_per_group(p, key_side, own);
 }
 
 // The keys that the query side's workgroups of an XCD walk together.

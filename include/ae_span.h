@@ -56,6 +56,7 @@ typedef struct {
   int32_t window;                 /* AE_SPAN_WINDOW: >= 1 */
   ae_out_dtype_t out_dtype;       /* of O */
   int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+  int32_t kv_splits;              /* of ae_span_forward_split: ranges that a row's keys are cut into, 0 .. 256; 0: the library chooses */
 } ae_span_desc_t;
 
 typedef struct ae_span ae_span_t;
@@ -75,6 +76,14 @@ ae_status_t ae_span_create(const ae_span_desc_t *desc, ae_span_t **out);
  * of the cap and an absolute one of 2e-7 of the cap beyond.                                                             */
 ae_status_t ae_span_forward(const ae_span_t *h, const void *Q, const void *K, const void *V, const int32_t *key_begin,
                             const int32_t *key_end, int64_t span_stride, void *O, float *stats, hipStream_t stream);
+
+/* The same with the keys that 256 rows see cut into ranges, for calls of few workgroups (few rows and heads, many keys): each range's rows go to the workspace, and a
+ * second launch combines them, in a fixed order.  workspace: device, 16-byte aligned, ae_span_workspace_bytes (0, where keys are not cut: may be
+ * NULL, and the call is ae_span_forward), needs no initialisation.  Calls that share it must not overlap.               */
+ae_status_t ae_span_workspace_bytes(const ae_span_t *h, size_t *bytes);
+ae_status_t ae_span_forward_split(const ae_span_t *h, const void *Q, const void *K, const void *V, const int32_t *key_begin,
+                                  const int32_t *key_end, int64_t span_stride, void *O, float *stats, void *workspace, size_t workspace_bytes,
+                                  hipStream_t stream);
 
 /* Gradients of sum(O * dO):
  *   P = exp(s' - stats), dV = P^T dO, dP = dO V^T, dS = P (dP - dO . O) (1 - tanh^2(s / cap)), dQ = scale dS K, dK = scale dS^T Q,

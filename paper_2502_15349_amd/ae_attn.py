@@ -1307,13 +1307,17 @@ class ae_span_desc_t(C.Structure):
     _fields_ = [("B", C.c_int32), ("H_q", C.c_int32), ("H_kv", C.c_int32), ("L_q", C.c_int32), ("L_k", C.c_int32), ("D_qk", C.c_int32),
                 ("D_v", C.c_int32), ("scale", C.c_float), ("cap", C.c_float), ("slopes", C.POINTER(C.c_float)), ("mask", C.c_int),
                 ("window", C.c_int32), ("out_dtype", C.c_int), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
-                ("v_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3)]
+                ("v_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3), ("kv_splits", C.c_int32)]
 
 
 _lib.ae_span_create.argtypes = [C.POINTER(ae_span_desc_t), C.POINTER(C.c_void_p)]
 _lib.ae_span_create.restype = C.c_int
 _lib.ae_span_forward.argtypes = [C.c_void_p] * 6 + [C.c_int64] + [C.c_void_p] * 3
 _lib.ae_span_forward.restype = C.c_int
+_lib.ae_span_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+_lib.ae_span_workspace_bytes.restype = C.c_int
+_lib.ae_span_forward_split.argtypes = [C.c_void_p] * 6 + [C.c_int64] + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]
+_lib.ae_span_forward_split.restype = C.c_int
 _lib.ae_span_backward_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
 _lib.ae_span_backward_workspace_bytes.restype = C.c_int
 _lib.ae_span_backward.argtypes = ([C.c_void_p] * 6 + [C.c_int64] + [C.c_void_p] * 2 + [C.POINTER(C.c_int64)] + [C.c_void_p] * 4
@@ -1327,14 +1331,14 @@ _lib.ae_span_documents.restype = C.c_int
 
 def ae_span_create(*, B: int, H_q: int, H_kv: int, L_q: int, L_k: int, D_qk: int, D_v: int, scale: float, cap: float = 0.0,
                    slopes: Optional[Sequence[float]] = None, mask="causal", window: int = 0, out_dtype="f32", q_stride=(0, 0, 0),
-                   k_stride=(0, 0, 0), v_stride=(0, 0, 0), o_stride=(0, 0, 0)) -> int:
-    """Handle for softmax attention over a span of keys per query row; slopes: H_q host floats."""
+                   k_stride=(0, 0, 0), v_stride=(0, 0, 0), o_stride=(0, 0, 0), kv_splits: int = 0) -> int:
+    """Handle for softmax attention over a span of keys per query row; slopes: H_q host floats; kv_splits: of ae_span_forward_split."""
     if slopes is not None and len(slopes) != H_q:
         raise ValueError("slopes must hold a number for every query head")
     at, keep = _float_array(slopes)
     d = ae_span_desc_t(B=B, H_q=H_q, H_kv=H_kv, L_q=L_q, L_k=L_k, D_qk=D_qk, D_v=D_v, scale=float(scale), cap=float(cap), slopes=at,
                        mask=SPAN_MASKS[mask] if isinstance(mask, str) else int(mask), window=int(window),
-                       out_dtype=OUT_DTYPES[out_dtype] if isinstance(out_dtype, str) else int(out_dtype))
+                       out_dtype=OUT_DTYPES[out_dtype] if isinstance(out_dtype, str) else int(out_dtype), kv_splits=int(kv_splits))
     for name, val in (("q_stride", q_stride), ("k_stride", k_stride), ("v_stride", v_stride), ("o_stride", o_stride)):
         setattr(d, name, _strides_t(*[int(x) for x in val]))
     h = C.c_void_p()
@@ -1346,6 +1350,18 @@ def ae_span_forward(handle: int, Q: int, K: int, V: int, key_begin: int, key_end
                     stream: int = 0) -> None:
     """Device addresses; key_begin and key_end are 0 but for the mask "spans", stats may be 0."""
     _check(_lib.ae_span_forward(handle, Q, K, V, key_begin, key_end, span_stride, O, stats, stream))
+
+
+def ae_span_workspace_bytes(handle: int) -> int:
+    n = C.c_size_t()
+    _check(_lib.ae_span_workspace_bytes(handle, C.byref(n)))
+    return n.value
+
+
+def ae_span_forward_split(handle: int, Q: int, K: int, V: int, key_begin: int, key_end: int, span_stride: int, O: int, stats: int, workspace: int,
+                          workspace_bytes: int, stream: int = 0) -> None:
+    """ae_span_forward with the keys cut into ranges where the handle's ae_span_workspace_bytes is not 0."""
+    _check(_lib.ae_span_forward_split(handle, Q, K, V, key_begin, key_end, span_stride, O, stats, workspace, workspace_bytes, stream))
 
 
 def ae_span_backward_workspace_bytes(handle: int) -> int:
@@ -1376,9 +1392,10 @@ class SpanAttentionPlan:
     V [B, H_kv, L_k, D_v] (bf16) and out [B, H_q, L_q, D_v] (bf16 or fp32), last dimension contiguous, give shapes, strides and device.
     cap: scores are bent to cap tanh(s / cap) (0: not); slopes: a host number per query head, times the distance between query and key
     taken off the score; mask: "none", "causal", "sliding_window" (window keys) or "spans", the key span of every query row given with each call
-    (document_spans makes them for packed documents).  Calls of one plan may run at the same time."""
+    (document_spans makes them for packed documents); kv_splits: ranges of keys that the forward pass walks apart (0: the library chooses, 1: none).
+    Calls of one plan may run at the same time."""
 
-    def __init__(self, Q, K, V, out, *, scale, cap=0.0, slopes=None, mask="causal", window=0):
+    def __init__(self, Q, K, V, out, *, scale, cap=0.0, slopes=None, mask="causal", window=0, kv_splits=0):
         import torch
 
         self.handle = None
@@ -1395,12 +1412,21 @@ class SpanAttentionPlan:
         _no_overlap(out)
         self.handle = ae_span_create(B=B, H_q=H_q, H_kv=H_kv, L_q=L_q, L_k=L_k, D_qk=D_qk, D_v=D_v, scale=scale, cap=cap, slopes=slopes, mask=mask,
                                      window=window, out_dtype="bf16" if out.dtype == torch.bfloat16 else "f32", q_stride=Q.stride()[:3],
-                                     k_stride=K.stride()[:3], v_stride=V.stride()[:3], o_stride=out.stride()[:3])
+                                     k_stride=K.stride()[:3], v_stride=V.stride()[:3], o_stride=out.stride()[:3], kv_splits=kv_splits)
         self.device, self._given, self._rows = Q.device, mask in ("spans", 3), (B, H_q, L_q)
         self._specs = [_shape_of(t) for t in (Q, K, V, out)]
         self._grad_shapes = [tuple(t.shape) for t in (Q, K, V)]
         self._types = (torch.bfloat16, torch.float32, torch.int32, torch.uint8)
-        self.workspace_bytes = ae_span_backward_workspace_bytes(self.handle)
+        self.workspace_bytes, self.split_bytes = ae_span_backward_workspace_bytes(self.handle), ae_span_workspace_bytes(self.handle)
+
+    def _workspace(self, size, stream):
+        """Allocated on the stream that the call is on."""
+        import torch
+
+        if stream is None:
+            return torch.empty(size, dtype=self._types[3], device=self.device)
+        with _memory_of(stream):
+            return torch.empty(size, dtype=self._types[3], device=self.device)
 
     def _spans(self, spans):
         if (spans is not None) != self._given:
@@ -1424,15 +1450,17 @@ class SpanAttentionPlan:
         """Writes and returns out; spans: (begin, end), int32 [B, L_q] or [L_q]; stats: fp32 [B, H_q, L_q] that receives ln sum exp."""
         if [_shape_of(t) for t in (Q, K, V, out)] != self._specs:
             raise ValueError("a tensor differs from the plan's in shape, strides, type or device")
-        _enqueue(ae_span_forward, self.device, stream, self.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), *self._spans(spans), out.data_ptr(),
-                 0 if stats is None else self._check_stats(stats))
+        args = (self.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), *self._spans(spans), out.data_ptr(), 0 if stats is None else self._check_stats(stats))
+        if self.split_bytes:
+            ws = self._workspace(self.split_bytes, stream)
+            _enqueue(ae_span_forward_split, self.device, stream, *args, ws.data_ptr(), self.split_bytes)
+        else:
+            _enqueue(ae_span_forward, self.device, stream, *args)
         return out
 
     def backward(self, Q, K, V, out, dO, stats, dQ, dK, dV, *, spans=None, stream=None):
         """Gradients for those of the output, dO bf16 [B, H_q, L_q, D_v] (last dimension contiguous); out and stats are what forward() wrote; dQ, dK,
         dV: contiguous, all fp32 or all bf16.  The workspace is allocated on the stream that the call is on."""
-        import torch
-
         if [_shape_of(t) for t in (Q, K, V, out)] != self._specs:
             raise ValueError("a tensor differs from the plan's in shape, strides, type or device")
         if dO.dtype != self._types[0] or dO.shape != out.shape or dO.device != self.device or dO.stride(3) != 1:
@@ -1442,11 +1470,7 @@ class SpanAttentionPlan:
             if tuple(t.shape) != shape or t.dtype != dQ.dtype or t.dtype not in self._types[:2] or not t.is_contiguous() or t.device != self.device:
                 raise ValueError("dQ, dK and dV must be contiguous device tensors of the shapes of Q, K and V, all fp32 or all bf16")
         given, at = self._spans(spans), self._check_stats(stats)
-        if stream is None:
-            ws = torch.empty(self.workspace_bytes, dtype=self._types[3], device=self.device)
-        else:
-            with _memory_of(stream):
-                ws = torch.empty(self.workspace_bytes, dtype=self._types[3], device=self.device)
+        ws = self._workspace(self.workspace_bytes, stream)
         _enqueue(ae_span_backward, self.device, stream, self.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), *given, out.data_ptr(), dO.data_ptr(),
                  dO.stride()[:3], at, dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), 1 if dQ.dtype == self._types[0] else 0, ws.data_ptr(),
                  self.workspace_bytes)
@@ -1459,18 +1483,18 @@ class SpanAttentionPlan:
 
 
 def span_attention_forward(Q, K, V, *, scale, cap=0.0, slopes=None, mask="causal", window=0, spans=None, out=None, out_dtype=None, stats=None,
-                           stream=None):
+                           stream=None, kv_splits=0):
     """Softmax attention on bf16 device tensors Q [B, H_q, L_q, D_qk], K, V [B, H_kv, L_k, D] (last dimension contiguous), every query row over a span of
     keys; scores scale q k, capped by cap tanh(s / cap) where cap > 0, less slopes[h] |i + L_k - L_q - j| where slopes (H_q host
     numbers) are given.  mask: "none", "causal", "sliding_window" with window, or "spans" with spans = (begin, end), int32 [B, L_q] or [L_q]: row i
     sees begin <= j < end.  Returns O [B, H_q, L_q, D_v], fp32 or bf16 (out / out_dtype); stats: optional fp32 [B, H_q, L_q] that receives
-    ln sum exp, which span_attention_backward needs."""
+    ln sum exp, which span_attention_backward needs.  kv_splits: ranges of keys walked apart (0: the library chooses)."""
     import torch
 
     if out is None:
         with _memory_of(stream):
             out = torch.empty(Q.shape[:3] + V.shape[3:], dtype=out_dtype or torch.float32, device=Q.device)
-    plan = SpanAttentionPlan(Q, K, V, out, scale=scale, cap=cap, slopes=slopes, mask=mask, window=window)
+    plan = SpanAttentionPlan(Q, K, V, out, scale=scale, cap=cap, slopes=slopes, mask=mask, window=window, kv_splits=kv_splits)
     return plan.forward(Q, K, V, out, spans=spans, stats=stats, stream=stream)
 
 

@@ -15,6 +15,7 @@
 #include "dispatch.hpp"
 #include "attn_decode.hpp"
 #include "gated.hpp"
+#include "merge.hpp"
 #include "recurrent.hpp"
 #include "status.hpp"
 
@@ -74,15 +75,7 @@ void fill_strides(int64_t dst[3], const int64_t src[3], int H, int L, int D) {
 // normalised partial rows, O = sum_c exp(lse_c - LSE) O_c and LSE = ln sum_c exp(lse_c) (the
 // rule by which the online row-norm state of two key blocks is combined, Section 4.1).  A
 // split without a visible key has lse_c = -inf and weight 0.
-struct MergeParams {
-  const float* ws_o;    // [n_splits, rows, D_v]
-  const float* ws_lse;  // [n_splits, rows]
-  void* O;              // fp32 or bf16, strides os[] in elements
-  float* stats;         // optional [rows]
-  float bias;           // constant bias that the ranges' log-sum-exps leave out
-  int n_splits, B, H_q, L_q, D_v, out_bf16;
-  int64_t os[3];
-};
+using ae::MergeParams;
 // One wavefront per row, VEC = D_v / 64 consecutive columns per lane.  The kernel is two memory latencies long and
 // nothing else, so the first kBatch partial rows are requested together with the log-sum-exps that weigh them.  With the
 // rows requested behind the weights, and one column per lane after the other, a decoding step of 16 q heads on 8192 keys
@@ -176,6 +169,18 @@ void* static_scratch() {
 }
 
 }  // namespace
+
+hipError_t ae::launch_merge(const MergeParams& m, hipStream_t s) {
+  const int64_t workgroups = ((int64_t)m.B * m.H_q * m.L_q + 3) / 4;
+  if (!launch_fits(workgroups, 256)) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)workgroups);
+  switch (m.D_v / 64) {  // (head dims with split keys: D_v is 64, 128 or 256)
+    case 1: hipLaunchKernelGGL(attn_merge_kernel<1>, grid, dim3(256), 0, s, m); break;
+    case 2: hipLaunchKernelGGL(attn_merge_kernel<2>, grid, dim3(256), 0, s, m); break;
+    default: hipLaunchKernelGGL(attn_merge_kernel<4>, grid, dim3(256), 0, s, m); break;
+  }
+  return hipGetLastError();
+}
 
 struct ae_attn {
   ae_attn_desc_t desc;
@@ -513,13 +518,7 @@ static ae_status_t forward_impl(const ae_attn_t* h, const void* Q, const void* K
     m.out_bf16 = p.out_bf16;
     m.bias = decode && h->desc.score_mod == AE_MOD_BIAS ? h->desc.bias : 0.f;
     for (int a = 0; a < 3; ++a) m.os[a] = p.os[a];
-    const dim3 grid((unsigned)merge_grid);
-    switch (m.D_v / 64) {  // (head dims with split keys: D_v is 64, 128 or 256)
-      case 1: hipLaunchKernelGGL(attn_merge_kernel<1>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), m); break;
-      case 2: hipLaunchKernelGGL(attn_merge_kernel<2>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), m); break;
-      default: hipLaunchKernelGGL(attn_merge_kernel<4>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), m); break;
-    }
-    e = hipGetLastError();
+    e = ae::launch_merge(m, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(AE_ERR_HIP, "ae_attn_forward: merge launch failed: %s", hipGetErrorString(e));
   }
   return AE_OK;

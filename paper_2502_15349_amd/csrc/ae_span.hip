@@ -5,6 +5,7 @@
 #include <cmath>
 #include <new>
 
+#include "merge.hpp"
 #include "span_bwd.hpp"
 #include "span_documents.hpp"
 #include "span_launch.hpp"
@@ -18,6 +19,8 @@ struct ae_span {
   ae::DecayTable slopes;  // times log2(e)
   int mod;
   int64_t grid;
+  int n_splits;  // of ae_span_forward_split
+  size_t partial_bytes() const { return n_splits > 1 ? (size_t)n_splits * params.B * params.H_q * params.L_q * (desc.D_v + 1) * sizeof(float) : 0; }
 };
 
 namespace {
@@ -71,6 +74,28 @@ bool aliased(const void* const* ins, int n_in, const void* const* outs, int n_ou
   return false;
 }
 
+// Ranges of keys, by an estimate of the time in us: 5 for a launch and the ends of a walk, a tile of 64 keys 0.8, 1.06 or 1.25 (64/64, 128/128, 192/128), in
+// rounds of 256 workgroups; the second launch 5, and the partial results out and back at 4 TB/s.  Of given spans half of the keys are taken to be seen.
+// Measured, us, whole / cut: 1 x 16 heads of 128, 17 rows x 8192 143 / 23.6 (16 ranges), 512 rows x 4096 83 / 33 (6), 4 x 32/8 x 64 x 4096 79 / 57 (2; 3: 69);
+// not cut: 2 x 12 x 1023 29.1 (2 ranges: 37.4), 1 x 12 x 2048 causal 46.8 (43.5), 1 x 16 x 1024 unmasked 27.1 (35.0).
+int choose_splits(const ae_span& h) {
+  const ae::SpanParams& p = h.params;
+  const double tile_us = h.desc.D_qk == 64 ? 0.8 : h.desc.D_qk == 128 ? 1.06 : 1.25;
+  int64_t keys = p.L_k;
+  if (h.desc.mask == AE_SPAN_GIVEN) keys = (keys + 1) / 2;
+  if (h.desc.mask == AE_SPAN_WINDOW) keys = std::min<int64_t>(keys, (int64_t)p.span.window + ae::kSpanRows);
+  const int64_t tiles = (keys + 63) / 64, workgroups = (int64_t)p.n_groups * p.g * p.n_qtiles, rows = (int64_t)p.B * p.H_q * p.L_q;
+  auto us = [&](int64_t n) {
+    const double walk = (double)((workgroups * n + 255) / 256) * ((tiles + n - 1) / n) * tile_us;
+    return 5 + walk + (n > 1 ? 5 + 8.0 * rows * n * h.desc.D_v / 4e6 : 0.0);
+  };
+  int best = 1;
+  double least = 0.9 * us(1);  // (what ranges gain has to show)
+  for (int n : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
+    if (2 * n <= tiles && us(n) < least) best = n, least = us(n);
+  return best;
+}
+
 }  // namespace
 
 extern "C" {
@@ -86,6 +111,7 @@ ae_status_t ae_span_create(const ae_span_desc_t* d, ae_span_t** out) {
   if ((int)d->mask < AE_SPAN_ALL || (int)d->mask > AE_SPAN_GIVEN) return fail(AE_ERR_INVALID_ARG, "%s: unknown mask %d", who, (int)d->mask);
   if (d->mask == AE_SPAN_WINDOW && d->window < 1) return fail(AE_ERR_INVALID_ARG, "%s: the window must hold at least one key", who);
   if (d->out_dtype != AE_OUT_F32 && d->out_dtype != AE_OUT_BF16) return fail(AE_ERR_INVALID_ARG, "%s: unknown out_dtype %d", who, (int)d->out_dtype);
+  if (d->kv_splits < 0 || d->kv_splits > ae::kMaxMerged) return fail(AE_ERR_INVALID_ARG, "%s: kv_splits must be between 0 and %d", who, ae::kMaxMerged);
   const float log2e = 1.4426950408889634f;
   if (!std::isfinite(d->scale * log2e) || d->scale == 0.f) return fail(AE_ERR_INVALID_ARG, "%s: scale must be finite (its product with log2(e) too) and non-zero", who);
   ae::CapParams cap = {};
@@ -153,13 +179,20 @@ ae_status_t ae_span_create(const ae_span_desc_t* d, ae_span_t** out) {
     return fail(AE_ERR_UNSUPPORTED, "%s: the grid exceeds the launch limit", who);
   }
   p.base_grid = (int)h->grid;
+  h->n_splits = d->kv_splits > 0 ? d->kv_splits : choose_splits(*h);
+  if (h->grid * h->n_splits > 0x7fffffffLL || (double)h->n_splits * d->B * d->H_q * d->L_q * (d->D_v + 1) > 1e11) {
+    delete h;
+    return fail(AE_ERR_UNSUPPORTED, "%s: kv_splits: the grid exceeds the launch limit, or the partial results 4e11 bytes", who);
+  }
   *out = h;
   return AE_OK;
 }
 
-ae_status_t ae_span_forward(const ae_span_t* h, const void* Q, const void* K, const void* V, const int32_t* key_begin, const int32_t* key_end,
-                            int64_t span_stride, void* O, float* stats, hipStream_t stream) {
-  static const char who[] = "ae_span_forward";
+}  // extern "C"
+
+static ae_status_t span_forward(const ae_span_t* h, const void* Q, const void* K, const void* V, const int32_t* key_begin, const int32_t* key_end,
+                                int64_t span_stride, void* O, float* stats, bool split, void* workspace, size_t workspace_bytes, hipStream_t stream,
+                                const char* who) {
   if (!h) return fail(AE_ERR_INVALID_ARG, "%s: null handle", who);
   if (!Q || !K || !V || !O) return fail(AE_ERR_INVALID_ARG, "%s: null pointer", who);
   if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O) & 15 || (uintptr_t)stats & 3)
@@ -167,8 +200,11 @@ ae_status_t ae_span_forward(const ae_span_t* h, const void* Q, const void* K, co
   const ae_status_t st = check_spans(h, key_begin, key_end, span_stride, who);
   if (st != AE_OK) return st;
   const void* ins[] = {Q, K, V, key_begin, key_end};
-  const void* outs[] = {O, stats};
-  if (aliased(ins, 5, outs, 2)) return fail(AE_ERR_INVALID_ARG, "%s: an output aliases another tensor", who);
+  split = split && h->n_splits > 1;
+  if (split && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < h->partial_bytes()))
+    return fail(AE_ERR_INVALID_ARG, "%s: keys are cut: a 16-byte aligned workspace of %zu bytes is needed", who, h->partial_bytes());
+  const void* outs[] = {O, stats, split ? workspace : nullptr};
+  if (aliased(ins, 5, outs, 3)) return fail(AE_ERR_INVALID_ARG, "%s: an output aliases another tensor", who);
   ae::SpanParams p = h->params;
   p.Q = static_cast<const __bf16*>(Q);
   p.K = static_cast<const __bf16*>(K);
@@ -179,7 +215,32 @@ ae_status_t ae_span_forward(const ae_span_t* h, const void* Q, const void* K, co
   p.span.end = key_end;
   p.span.stride = span_stride;
   const auto launch = h->desc.D_qk == 64 ? ae::launch_span_64_64 : h->desc.D_qk == 128 ? ae::launch_span_128_128 : ae::launch_span_192_128;
-  return launched(launch(p, h->slopes, h->mod, h->grid, stream), who);
+  if (!split) return launched(launch(p, h->slopes, h->mod, h->grid, stream), who);
+  p.n_splits = h->n_splits;
+  p.ws_o = static_cast<float*>(workspace);
+  p.ws_lse = p.ws_o + (size_t)p.n_splits * p.B * p.H_q * p.L_q * h->desc.D_v;
+  const ae_status_t walked = launched(launch(p, h->slopes, h->mod, h->grid * p.n_splits, stream), who);
+  if (walked != AE_OK) return walked;
+  const ae::MergeParams m = {p.ws_o, p.ws_lse, O, stats, 0.f, p.n_splits, p.B, p.H_q, p.L_q, h->desc.D_v, p.out_bf16, {p.os[0], p.os[1], p.os[2]}};
+  return launched(ae::launch_merge(m, stream), who);
+}
+
+extern "C" {
+
+ae_status_t ae_span_forward(const ae_span_t* h, const void* Q, const void* K, const void* V, const int32_t* key_begin, const int32_t* key_end,
+                            int64_t span_stride, void* O, float* stats, hipStream_t stream) {
+  return span_forward(h, Q, K, V, key_begin, key_end, span_stride, O, stats, false, nullptr, 0, stream, "ae_span_forward");
+}
+
+ae_status_t ae_span_workspace_bytes(const ae_span_t* h, size_t* bytes) {
+  if (!h || !bytes) return fail(AE_ERR_INVALID_ARG, "ae_span_workspace_bytes: null argument");
+  *bytes = h->partial_bytes();
+  return AE_OK;
+}
+
+ae_status_t ae_span_forward_split(const ae_span_t* h, const void* Q, const void* K, const void* V, const int32_t* key_begin, const int32_t* key_end,
+                                  int64_t span_stride, void* O, float* stats, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return span_forward(h, Q, K, V, key_begin, key_end, span_stride, O, stats, true, workspace, workspace_bytes, stream, "ae_span_forward_split");
 }
 
 ae_status_t ae_span_backward_workspace_bytes(const ae_span_t* h, size_t* bytes) {

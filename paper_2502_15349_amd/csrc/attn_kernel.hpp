@@ -86,7 +86,7 @@ struct Params {
   int out_bf16;    // O holds bf16 instead of fp32
   int window;      // sliding-window kernels: key j is also hidden if j <= i + (L_k - L_q) - window
   // Split keys (n_splits > 1): the launch holds n_splits copies of the base_grid items; copy c
-  // walks key tiles [c * split_tiles, (c + 1) * split_tiles) only and writes its normalised
+  // walks key tiles [c * split_tiles, (c + 1) * split_tiles) only (spans: the c-th part of those that its rows see) and writes its normalised
   // partial rows (fp32, [split, B, H_q, L_q, D_v]) and their log-sum-exp ([split, B, H_q, L_q])
   // to the workspace instead of O / stats; attn_merge_kernel combines them.
   int n_splits, split_tiles, base_grid;
@@ -1118,7 +1118,7 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
   // (it would only wait at the barriers otherwise), which keeps its fragment ring, its LDS
   // addresses and its scores in step with the others.
   int jt0 = 0, jtm = 0, u_first = 0;
-  if (!C::WINDOW && p.n_splits > 1) {  // this workgroup's share of the key tiles
+  if (!C::WINDOW && !C::SPAN && p.n_splits > 1) {  // this workgroup's share of the key tiles
     jt0 = jtm = split * p.split_tiles;
     n_tiles = min(n_tiles, jt0 + p.split_tiles);
     n_vis = min(n_vis, 2 * n_tiles);
@@ -1131,6 +1131,12 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
   }
   if constexpr (C::SPAN) {  // the same walk: first the tiles behind every row's first key
     jt0 = lo_wg / C::BLOCK_N;
+    if (p.n_splits > 1) {  // this workgroup's share of its own key tiles
+      const int share = (max(n_tiles - jt0, 0) + p.n_splits - 1) / p.n_splits;
+      jt0 += split * share;
+      n_tiles = min(n_tiles, jt0 + share);
+      n_vis = min(n_vis, 2 * n_tiles);
+    }
     jtm = max(jt0, min((last_lo + C::BLOCK_N - 1) / C::BLOCK_N, n_tiles));
     u_first = lo_w / C::SUB_N;
   }

@@ -357,3 +357,60 @@ def test_refusals_of_the_binding(A):
         A.span_attention_backward(Q, K, V, O, Q, stats[:, :, :30], scale=1.0)
     with pytest.raises(A.AeAttnError):
         A.span_attention_forward(Q, K, V, scale=1.0, cap=-1.0)
+
+
+@pytest.mark.parametrize("dims", DIMS)
+@pytest.mark.parametrize("score", SCORES)
+@pytest.mark.parametrize("mask", ["none", "causal", "sliding_window", "unsorted"])
+@pytest.mark.parametrize("kv_splits", [2, 5, 256])
+def test_keys_in_ranges(A, dims, score, mask, kv_splits):
+    """Ranges with keys of some rows, of none, of all; more ranges than tiles; rows that see nothing."""
+    B, H_q, H_kv, L_q, L_k = 2, 4, 2, 70, 460
+    Q, K, V = rows(1, B, H_q, L_q, dims[0], 2.0), rows(2, B, H_kv, L_k, dims[0]), rows(3, B, H_kv, L_k, dims[1])
+    kw = dict(score, kv_splits=kv_splits)
+    if mask == "unsorted":
+        g = np.random.RandomState(7)
+        begin = g.randint(0, L_k, (B, L_q))
+        end = np.where(g.rand(B, L_q) < 0.2, begin, np.minimum(begin + g.randint(1, 300, (B, L_q)), L_k))
+    else:
+        kw.update(mask=mask, window=100 if mask == "sliding_window" else 0)
+        begin, end = spans_of(mask, B, L_q, L_k, kw["window"])
+    run_forward(A, Q, K, V, begin, end, out_dtype=torch.bfloat16 if kv_splits == 5 else torch.float32, **kw)
+
+
+def test_ranges_are_chosen_where_there_are_few_rows(A):
+    Q, K, V = rows(1, 1, 8, 3, 128, 2.0), rows(2, 1, 2, 5000, 128), rows(3, 1, 2, 5000, 128)
+    plan = A.SpanAttentionPlan(Q, K, V, torch.empty(1, 8, 3, 128, device="cuda"), scale=0.1)
+    assert plan.split_bytes > 0
+    begin, end = spans_of("causal", 1, 3, 5000)
+    a = run_forward(A, Q, K, V, begin, end, out_dtype=torch.float32, mask="causal", slopes=True)
+    b = run_forward(A, Q, K, V, begin, end, out_dtype=torch.float32, mask="causal", slopes=True)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    whole = A.SpanAttentionPlan(Q, K, V, torch.empty(1, 8, 3, 128, device="cuda"), scale=0.1, kv_splits=1)
+    assert whole.split_bytes == 0
+
+
+def test_ranges_on_two_streams_and_in_a_graph(A):
+    """Every call has partial results of its own."""
+    Q, K, V = rows(1, 1, 8, 40, 64, 2.0), rows(2, 1, 2, 3000, 64), rows(3, 1, 2, 3000, 64)
+    out = torch.empty(1, 8, 40, 64, device="cuda")
+    plan = A.SpanAttentionPlan(Q, K, V, out, scale=0.1, kv_splits=6)
+    want = plan.forward(Q, K, V, out).clone()
+    torch.cuda.synchronize()
+    results = []
+    for _ in range(2):
+        s, o = torch.cuda.Stream(), torch.empty_like(out)
+        torch.cuda.synchronize()
+        results.append(plan.forward(Q, K, V, o, stream=s))
+    torch.cuda.synchronize()
+    assert all(torch.equal(r, want) for r in results)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.forward(Q, K, V, out)
+    for n in range(3):
+        Q.copy_(rows(10 + n, 1, 8, 40, 64))
+        eager = plan.forward(Q, K, V, torch.empty_like(out))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)

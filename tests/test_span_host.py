@@ -145,3 +145,42 @@ def test_gradients_are_differences(kw):
                 f.append((span_attention(*x, begin, end, scale=0.7, **kw)[0] * dO).sum())
             want[at] = (f[0] - f[1]) / 2e-5
         assert np.abs(got[n] - want).max() < 1e-7
+
+
+@built
+def test_split_refusals(A):
+    for kw in (dict(kv_splits=-1), dict(kv_splits=257)):
+        refused(A, 1, A.ae_span_create, **{**SPAN, **kw})
+    refused(A, 2, A.ae_span_create, **{**SPAN, "L_q": 1 << 20, "H_q": 1 << 10, "kv_splits": 256})
+    p = 1 << 20
+    good = [p, 2 * p, 3 * p, 0, 0, 0, 6 * p, 7 * p]
+    h = A.ae_span_create(**SPAN, kv_splits=3)
+    need = A.ae_span_workspace_bytes(h)
+    assert need == 3 * 2 * 4 * 10 * 65 * 4
+    for ws, size in ((0, need), (8 * p, need - 1), (8 * p + 8, need), (6 * p, need), (p, need)):
+        refused(A, 1, A.ae_span_forward_split, h, *good, ws, size)
+    for n, bad in [(0, 0), (6, 0), (6, 2 * p), (7, 7 * p + 2)]:
+        a = list(good)
+        a[n] = bad
+        refused(A, 1, A.ae_span_forward_split, h, *a, 8 * p, need)
+    refused(A, 1, A.ae_span_forward_split, None, *good, 8 * p, need)
+    refused(A, 1, A.ae_span_workspace_bytes, None)
+    A.ae_span_destroy(h)
+
+
+@built
+def test_ranges_that_are_chosen(A):
+    """Few rows over many keys are cut, many rows are not."""
+    def ranges(**kw):
+        d = {**SPAN, "D_qk": 128, "D_v": 128, **kw}
+        h = A.ae_span_create(**d)
+        n = A.ae_span_workspace_bytes(h) / (d["B"] * d["H_q"] * d["L_q"] * 129 * 4)
+        A.ae_span_destroy(h)
+        return int(n)
+
+    assert ranges(B=1, H_q=16, H_kv=16, L_q=17, L_k=8192) >= 8
+    assert 4 <= ranges(B=1, H_q=16, H_kv=16, L_q=512, L_k=4096) <= 8
+    assert ranges(B=4, H_q=32, H_kv=8, L_q=64, L_k=4096) == 2
+    for kw in (dict(B=2, H_q=12, H_kv=12, L_q=1023, L_k=1023), dict(B=1, H_q=32, H_kv=8, L_q=8192, L_k=8192), dict(B=1, H_q=4, H_kv=4, L_q=10, L_k=100),
+               dict(B=1, H_q=16, H_kv=16, L_q=17, L_k=8192, mask="sliding_window", window=100), dict(B=1, H_q=16, H_kv=16, L_q=17, L_k=8192, kv_splits=1)):
+        assert ranges(**kw) == 0

@@ -19,37 +19,36 @@ constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
 // Digits of 11, 11 and 10 bits.  The first is the sign, the exponent and two bits of the mantissa, so that weights of one size spread over
 // dozens of bins: a wave's additions to LDS run one after the other where they meet in one.
 constexpr int kBins = 2048;
+constexpr int kLdsMoves = 2048;  // moves that are kept in LDS as well, where the workgroup itself reads them
 
-// Order of the entries as unsigned numbers: protected ones above all (and above infinity in the first digit, too), NaN below all, both
-// zeros alike.
-constexpr uint32_t kProtected = 0xffffffffu;
+// Order of the entries as unsigned numbers: protected ones above all, then numbers (both zeros alike), then NaN; 0 is left for what is behind a list.
 __device__ __forceinline__ uint32_t evict_key(float w, bool is_protected) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, w);
-  if (is_protected) return kProtected;
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
-  if (u == 0x80000000u) return u;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = __builtin_bit_cast(uint32_t, w + 0.f);
+  const uint32_t number = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return is_protected ? 0xffffffffu : (u & 0x7fffffffu) > 0x7f800000u ? 1u : number;
 }
 
-// Sums of per-wave counts over the workgroup, and over the waves in front.
-__device__ __forceinline__ void count_waves(int mine, int32_t* lds, int& all, int& front) {
+// Sums over the waves in front of per-wave counts; lane 0 of a wave has put its own into lds[wave] in front of a barrier.  all: of every wave.
+__device__ __forceinline__ int waves_in_front(const int32_t* lds, int& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  __syncthreads();
-  if (lane == 0) lds[wave] = mine;
-  __syncthreads();
   const int v = lane < kEvictWaves ? lds[lane] : 0;
+  int front = lane < wave ? v : 0;
   all = v;
-  front = lane < wave ? v : 0;
 #pragma unroll
   for (int s = 1; s < kEvictWaves; s *= 2) {
     all += __shfl_xor(all, s);
     front += __shfl_xor(front, s);
   }
   all = __builtin_amdgcn_readfirstlane(all);
-  front = __builtin_amdgcn_readfirstlane(front);
+  return __builtin_amdgcn_readfirstlane(front);
 }
+__device__ __forceinline__ int lanes_below(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
 
-__device__ __forceinline__ int load_or(const int32_t* at, bool there) { return there ? *at : -0x7fffffff - 1; }
+// Entry `at` of an array of a list (at most 2^30 entries: a 32-bit offset)
+template <class T>
+__device__ __forceinline__ T& entry(T* list, int at) {
+  return *reinterpret_cast<T*>((uintptr_t)list + (uint32_t)(at << 2));
+}
 
 // Copies a row of one list, 16 lanes a row; a row on a page outside the cache is left where it is.
 __device__ __forceinline__ void move_row(const EvictParams& p, const int32_t* table, int h, int src, int dst, int sub) {
@@ -69,7 +68,7 @@ __device__ __forceinline__ void move_row(const EvictParams& p, const int32_t* ta
 // the list, in order: entry i of lane l is piece + 64 i + l.
 template <int ITEMS>
 __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const EvictParams p) {
-  __shared__ int32_t hist[kBins], lds[kEvictWaves], found[3];
+  __shared__ int32_t hist[kBins], lds[2][kEvictWaves], found[3], move_lds[2][kLdsMoves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int list = blockIdx.x, b = list / p.H_kv, h = list % p.H_kv;
   const int len = max(0, min(scalar_load(p.lengths + b), p.max_length)), count = min(len, p.keep);
@@ -95,8 +94,8 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const int at = piece + 64 * i + lane;
-      pos[i] = load_or(positions + at, at < len);
-      w[i] = at < len ? weights[at] : 0.f;
+      pos[i] = at < len ? entry(positions, at) : -0x7fffffff - 1;
+      w[i] = at < len ? entry(weights, at) : 0.f;
     }
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) newest = max(newest, pos[i]);
@@ -105,14 +104,15 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
   }
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) newest = max(newest, __shfl_xor(newest, s));
-  if (lane == 0) lds[wave] = newest;
+  if (lane == 0) lds[0][wave] = newest;
   __syncthreads();
-  newest = lds[lane & (kEvictWaves - 1)];
+  newest = lds[0][lane & (kEvictWaves - 1)];
 #pragma unroll
   for (int s = 1; s < kEvictWaves; s *= 2) newest = max(newest, __shfl_xor(newest, s));
-  const int64_t from = (int64_t)newest - p.recent;  // positions beyond it are protected
-  // ---- keys; an entry behind the list has none (below every other: the list's own are raised by one) ----
-  auto key_from = [&](float weight, int position, int at) { return at < len ? max(evict_key(weight, position > from || position < p.sinks), 1u) : 0u; };
+  // ---- keys (positions lie at or below the newest one, at most 2^32 - 1 below) ----
+  auto key_from = [&](float weight, int position, int at) {
+    return at < len ? evict_key(weight, (uint32_t)newest - (uint32_t)position < (uint32_t)p.recent || position < p.sinks) : 0u;
+  };
   uint32_t key[ITEMS ? ITEMS : 1];
   if constexpr (ITEMS > 0) {
 #pragma unroll
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
   auto key_of = [&](int i) -> uint32_t {
     if constexpr (ITEMS > 0) return key[i];
     const int at = piece + 64 * i + lane;
-    return at < len ? key_from(weights[at], positions[at], at) : 0u;
+    return at < len ? key_from(entry(weights, at), entry(positions, at), at) : 0u;
   };
   auto each = [&](auto&& f) {
     if constexpr (ITEMS > 0) {
@@ -131,22 +131,16 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
       for (int i = 0; i < items; ++i) f(i);
     }
   };
-  // ---- digit by digit: of the keys that begin with `threshold`, `need` stay, of those above it all ----
-  int shift = 32, need = count, all, front, mine = 0;
+  // ---- digit by digit: of the keys that begin with `threshold`, `need` stay, of those above it all (what is behind the list is counted with
+  // the lowest ones; it comes last among them) ----
+  int shift = 32, need = count, all;
   uint32_t threshold = 0;
-  each([&](int i) { mine += __popcll(__builtin_amdgcn_ballot_w64(key_of(i) == kProtected)); });
-  count_waves(mine, lds, all, front);
-  if (all >= count) {  // only protected ones stay
-    shift = 0;
-    threshold = kProtected;
-  } else {
-    need -= all;
-  }
+  bool ties = true;
   while (shift > 0) {
     const int width = min(shift, 11), next = shift - width;
     each([&](int i) {
       const uint32_t k = key_of(i);
-      const bool in = k != kProtected && k != 0u && (shift == 32 || k >> (shift & 31) == threshold);
+      const bool in = shift == 32 || k >> (shift & 31) == threshold;
       const uint32_t digit = (k >> next) & ((1u << width) - 1);
       const uint64_t group = __builtin_amdgcn_ballot_w64(in);
       if (group == 0) return;
@@ -167,8 +161,9 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
       const int v = __shfl_up(sum, s);
       sum += lane >= s ? v : 0;
     }
-    count_waves(__builtin_amdgcn_readlane(sum, 63), lds, all, front);
-    const int above = front + sum - c1 - c0;
+    if (lane == 63) lds[1][wave] = sum;
+    __syncthreads();
+    const int above = waves_in_front(lds[1], all) + sum - c1 - c0;
     if (above < need && need <= above + c1 + c0) {  // of one thread
       const bool upper = need <= above + c1;
       found[0] = upper ? d : d - 1;
@@ -179,56 +174,95 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
     threshold = (shift == 32 ? 0u : threshold << width) | (uint32_t)__builtin_amdgcn_readfirstlane(found[0]);
     need = __builtin_amdgcn_readfirstlane(found[1]);
     shift = next;
-    if (need == __builtin_amdgcn_readfirstlane(found[2])) break;  // the whole bin stays
+    ties = need < __builtin_amdgcn_readfirstlane(found[2]);
+    if (!ties) break;  // the whole bin stays
   }
   // ---- of the keys that begin with the threshold the first `need` stay ----
-  mine = 0;
-  each([&](int i) { mine += __popcll(__builtin_amdgcn_ballot_w64(key_of(i) >> shift == threshold)); });
-  count_waves(mine, lds, all, front);
-  const int equal_front = front;
-  const uint64_t below = (1ull << lane) - 1;
-  auto walk = [&](auto&& f) {  // f(entry, whether it stays), in order
+  int equal_front = 0;
+  if (ties) {
+    int mine = 0;
+    each([&](int i) { mine += __popcll(__builtin_amdgcn_ballot_w64(key_of(i) >> shift == threshold)); });
+    if (lane == 0) lds[0][wave] = mine;
+    __syncthreads();
+    equal_front = waves_in_front(lds[0], all);
+    __syncthreads();
+  }
+  uint32_t kept = 0;  // ITEMS: bit i: entry i stays
+  auto walk = [&](bool again, auto&& f) {  // f(i, entry, lanes that move away, lanes that are moved to, whether it stays where it is), in order
     int equal = equal_front;
     each([&](int i) {
-      const uint32_t k = key_of(i) >> shift;
-      const uint64_t same = __builtin_amdgcn_ballot_w64(k == threshold);
-      const bool stays = k > threshold || (k == threshold && equal + __popcll(same & below) < need);
-      equal += __popcll(same);
-      f(piece + 64 * i + lane, stays, i);
+      const int first = piece + 64 * i, at = first + lane;
+      bool stays;
+      if (ITEMS > 0 && again) {
+        stays = (kept >> i) & 1;
+      } else {
+        const uint32_t k = key_of(i) >> shift;
+        stays = k >= threshold;
+        if (ties) {
+          const uint64_t same = __builtin_amdgcn_ballot_w64(k == threshold);
+          stays = k > threshold || (k == threshold && equal + lanes_below(same) < need);
+          equal += __popcll(same);
+        }
+        if (ITEMS > 0) kept |= (uint32_t)stays << i;
+      }
+      const uint64_t staying = __builtin_amdgcn_ballot_w64(stays);
+      const uint64_t low = first + 64 <= count ? ~0ull : first >= count ? 0ull : (1ull << (count - first)) - 1;  // the places below `count`
+      f(i, at, staying & ~low, ~staying & low, stays && at < count);
     });
   };
   int n_src = 0, n_dst = 0;
-  walk([&](int at, bool stays, int) {
-    n_src += __popcll(__builtin_amdgcn_ballot_w64(stays && at >= count));
-    n_dst += __popcll(__builtin_amdgcn_ballot_w64(!stays && at < count));
+  walk(false, [&](int, int, uint64_t src, uint64_t dst, bool) {
+    n_src += __popcll(src);
+    n_dst += __popcll(dst);
   });
-  int src_front, dst_front;
-  count_waves(n_src, lds, all, src_front);
-  const int n_moves = all;
+  if (lane == 0) {
+    lds[0][wave] = n_src;
+    lds[1][wave] = n_dst;
+  }
+  __syncthreads();
+  int n_moves;
+  int src_front = waves_in_front(lds[0], n_moves), dst_front = waves_in_front(lds[1], all);
+  const bool in_lds = n_moves <= kLdsMoves;
+  int32_t* sources = moves + 1;
+  int32_t* destinations = sources + p.most_moves;
   if (threadIdx.x == 0) moves[0] = n_moves;
-  count_waves(n_dst, lds, all, dst_front);
-  const bool copy_w = p.weights_out != p.weights, copy_p = p.positions_out != p.positions;
-  walk([&](int at, bool stays, int i) {
-    const uint64_t src = __builtin_amdgcn_ballot_w64(stays && at >= count), dst = __builtin_amdgcn_ballot_w64(!stays && at < count);
-    if (stays && at >= count) moves[1 + src_front + __popcll(src & below)] = at;
-    if (!stays && at < count) moves[1 + p.most_moves + dst_front + __popcll(dst & below)] = at;
-    if (stays && at < count) {
-      if (copy_w) p.weights_out[base + at] = ITEMS ? w[ITEMS ? i : 0] : weights[at];
-      if (copy_p) p.positions_out[base + at] = ITEMS ? pos[ITEMS ? i : 0] : positions[at];
+  float* weights_out = p.weights_out + base;
+  int32_t* positions_out = p.positions_out + base;
+  const bool copy_w = weights_out != weights, copy_p = positions_out != positions;
+  walk(true, [&](int i, int at, uint64_t src, uint64_t dst, bool stays) {
+    if (src != 0) {
+      const int n = src_front + lanes_below(src);
+      if ((src >> lane) & 1) {
+        if (in_lds) move_lds[0][n] = at;
+        if (!in_lds || !p.one_launch) entry(sources, n) = at;
+      }
+      src_front += __popcll(src);
     }
-    src_front += __popcll(src);
-    dst_front += __popcll(dst);
+    if (dst != 0) {
+      const int n = dst_front + lanes_below(dst);
+      if ((dst >> lane) & 1) {
+        if (in_lds) move_lds[1][n] = at;
+        if (!in_lds || !p.one_launch) entry(destinations, n) = at;
+      }
+      dst_front += __popcll(dst);
+    }
+    if (stays) {
+      if (copy_w) entry(weights_out, at) = ITEMS ? w[ITEMS ? i : 0] : entry(weights, at);
+      if (copy_p) entry(positions_out, at) = ITEMS ? pos[ITEMS ? i : 0] : entry(positions, at);
+    }
   });
   __threadfence_block();
   __syncthreads();
+  auto source = [&](int m) { return in_lds ? move_lds[0][m] : sources[m]; };
+  auto destination = [&](int m) { return in_lds ? move_lds[1][m] : destinations[m]; };
   for (int m = threadIdx.x; m < n_moves; m += kEvictThreads) {
-    const int src = moves[1 + m], dst = moves[1 + p.most_moves + m];
-    p.weights_out[base + dst] = weights[src];
-    p.positions_out[base + dst] = positions[src];
+    const int src = source(m), dst = destination(m);
+    entry(weights_out, dst) = entry(weights, src);
+    entry(positions_out, dst) = entry(positions, src);
   }
   if (p.one_launch) {
     const int32_t* table = p.table + (int64_t)b * p.table_width;
-    for (int m = threadIdx.x / 16; m < n_moves; m += kEvictThreads / 16) move_row(p, table, h, moves[1 + m], moves[1 + p.most_moves + m], threadIdx.x % 16);
+    for (int m = threadIdx.x / 16; m < n_moves; m += kEvictThreads / 16) move_row(p, table, h, source(m), destination(m), threadIdx.x % 16);
   }
 }
 

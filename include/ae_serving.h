@@ -204,7 +204,7 @@ ae_status_t ae_cached_destroy(ae_cached_t *h); /* NULL is allowed */
  * they are.  weights_out may be weights itself.  An entry on a page number outside the cache receives nothing; a row with the
  * statistic -inf gives nothing.  Sums are fp32, in an order that does not change.
  *   Q, stats   as in ae_cached_forward; new_positions  device, int32, [B, n_new], batch entries new_stride apart (0: shared).
- * At most 2^24 query rows, n_new (H_q / H_kv)^2 < 2^32 (AE_ERR_UNSUPPORTED beyond).                                             */
+ * At most 2^24 query rows (AE_ERR_UNSUPPORTED beyond).                                                                          */
 typedef struct ae_weigh ae_weigh_t;
 typedef struct {
   int32_t B, H_q, n_new;

@@ -599,9 +599,7 @@ ae_status_t ae_weigh_create(const ae_cache_t* cache, const ae_weigh_desc_t* d, a
   if (d->H_q % cd.H_kv != 0) return fail(AE_ERR_INVALID_ARG, "%s: H_q (%d) is not a multiple of H_kv (%d)", who, d->H_q, cd.H_kv);
   if (!std::isfinite(d->scale * 1.4426950408889634f) || d->scale == 0.f)
     return fail(AE_ERR_INVALID_ARG, "%s: scale must be finite (its product with log2(e) too) and non-zero", who);
-  const int64_t g = d->H_q / cd.H_kv;
-  if ((double)d->B * d->H_q * d->n_new > 1 << 24 || g * g * d->n_new >= 1ll << 32)
-    return fail(AE_ERR_UNSUPPORTED, "%s: at most 2^24 query rows, and fewer than 2^32 / (H_q / H_kv) of a k/v head", who);
+  if ((double)d->B * d->H_q * d->n_new > 1 << 24) return fail(AE_ERR_UNSUPPORTED, "%s: at most 2^24 query rows", who);
   ae::CapParams cap;
   st = check_cap(d->scale, d->cap, &cap, who);
   if (st != AE_OK) return st;
@@ -619,7 +617,6 @@ ae_status_t ae_weigh_create(const ae_cache_t* cache, const ae_weigh_desc_t* d, a
   p.H_q = d->H_q;
   p.H_kv = cd.H_kv;
   p.g = d->H_q / cd.H_kv;
-  p.g_inverse = 0xffffffffu / (uint32_t)p.g + 1;
   p.n = d->n_new;
   p.page_shift = cache->page_shift;
   p.n_pages = cd.n_pages;

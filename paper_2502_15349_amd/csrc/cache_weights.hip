@@ -6,11 +6,12 @@
 // rows] = K Q^T by MFMA 16x16x32 with the keys in the order of cached_attn.hip, so that a lane holds 8 neighbouring keys of one
 // row.  The weights are summed in its registers over the row tiles and over the 16 lanes of a group at the end, in a fixed order; every
 // entry is written once, by one wavefront.  One tile of rows comes straight from memory, more through LDS, 64 rows at a time, where the four wavefronts
-// of a workgroup share them (each for itself: the L2 serves 2 GB for 500 tokens of 4 x 16/16 heads x 8000 keys of 128, 237 us instead of 138 in 8 bits with a cap).
+// of a workgroup share them.  (Each for itself, the L2 serves 2 GB for 500 tokens of 4 x 16/16 heads x 8000 keys of 128: 237 us in 8 bits with a cap.)
 //
-// Bound by the reading of the keys for a few rows (16 x 32/8 x 2048, one token: 12.9 us, 3.2 TB/s; 8 tokens 15.4), by vector instructions for many (an
-// exponential, a multiply-add, an addition and, with a cap, eight more for every score; 500 tokens as above: 98 us, 0.65 PFLOP/s; capped 138).  64 keys a wavefront, with half
-// the reads of the rows: 106 and 147, and a third slower where there are fewer keys than compute units take (1 x 32/8 x 200 of 3000: 21.6 -> 32.4).
+// Bound by the reading of the keys for a few rows (16 x 32/8 x 2048, one token: 12.3 us, 3.4 TB/s; 8 tokens 15.4), by vector instructions for many (an
+// exponential, a multiply-add, an addition and, with a cap, seven more for every score; 500 tokens as above: 93 us, 0.68 PFLOP/s; in 8 bits with a cap 116).  64 keys a
+// wavefront, with half the reads of the rows, took 7 % longer there, and half as long again where there are fewer keys than compute units take (1 x 32/8 x
+// 200 of 3000: 21.6 -> 32.4).  Divisions for the rows' places instead of steps, and scores moved out of accumulation registers: 121 instead of 116.
 #include "cache_weights.hpp"
 
 #include "cached_attn.hpp"
@@ -26,11 +27,13 @@ constexpr int kWeighKeys = 128;  // of a workgroup: four wavefronts of 32
 constexpr int kWeighRows = 64;  // query rows in LDS at a time (twice: the next ones arrive meanwhile)
 
 // SHARED: rows go through LDS.
+// (The second bound keeps the scores out of accumulation registers, from which every one would have to be moved first.)
 template <int DQK, bool E4M3, bool SHARED>
-__global__ __launch_bounds__(256) void weigh_kernel(const WeighParams p) {
+__global__ __launch_bounds__(256, DQK == 192 ? 3 : 4) void weigh_kernel(const WeighParams p) {
   constexpr int KS = DQK / 32, RB = DQK * (E4M3 ? 1 : 2);
   // Rows in LDS are 16 bytes apart from each other's end: 16 rows' chunks of 16 bytes lie in different banks.
-  constexpr int PITCH = 2 * DQK + 16, CHUNKS = DQK / 8, COPIES = kWeighRows * CHUNKS / 256;
+  constexpr int PITCH = 2 * DQK + 16, CHUNKS = DQK / 8;
+  constexpr int PASS_ROWS = DQK == 192 ? 8 : 256 / CHUNKS, COPIES = kWeighRows / PASS_ROWS, COPIERS = PASS_ROWS * CHUNKS;  // a pass copies a chunk a thread
   __shared__ __attribute__((aligned(16))) char row_lds[SHARED ? 2 * kWeighRows * PITCH : 16];
   __shared__ float nl_lds[SHARED ? 2 * kWeighRows : 1];
   __shared__ int lim_lds[SHARED ? 2 * kWeighRows : 1];
@@ -129,43 +132,56 @@ __global__ __launch_bounds__(256) void weigh_kernel(const WeighParams p) {
   // rows of earlier tokens see none of the keys
   if constexpr (SHARED) {
     const int c0 = (int)((int64_t)max(0, tile * kWeighKeys - first_new) * p.g / kWeighRows), n_c = (rows + kWeighRows - 1) / kWeighRows;
+    // Rows follow each other by a fixed number of tokens and heads, and a token more where the heads run over: no divisions on the way.
+    struct At {
+      int t, h;
+      int64_t q;
+    };
+    const int64_t next_token = p.qs[2] - p.g * p.qs[1];
+    auto start = [&](int r) { return At{r / p.g, r % p.g, r / p.g * p.qs[2] + r % p.g * p.qs[1]}; };
+    auto advance = [&](At& at, const At& by) {
+      at.t += by.t;
+      at.h += by.h;
+      at.q += by.q;
+      if (at.h >= p.g) {
+        at.h -= p.g;
+        at.q += next_token;
+        ++at.t;
+      }
+    };
+    const int row = threadIdx.x / CHUNKS, chunk = threadIdx.x % CHUNKS;
+    const bool copies = COPIERS == 256 || (int)threadIdx.x < COPIERS;
+    const At by_pass = start(PASS_ROWS), by_buffer = start(kWeighRows);
+    At at_copy = start(kWeighRows * c0 + row), at_state = start(kWeighRows * c0 + threadIdx.x);
     u32x4 got[COPIES];
     float nl = 0.f;
     int lim = -1;
-    auto place = [&](int r, int& t, int& h) {
-      r = min(r, rows - 1);
-      t = p.g == 1 ? r : (int)__umulhi((uint32_t)r, p.g_inverse);  // (exact: r g < 2^32)
-      h = r - t * p.g;
-    };
-    auto request = [&](int c) {
-      int t, h;
+    auto request = [&]() {
 #pragma unroll
-      for (int i = 0; i < COPIES; ++i) {
-        const int n = 256 * i + threadIdx.x;
-        place(kWeighRows * c + n / CHUNKS, t, h);
-        got[i] = *reinterpret_cast<const u32x4*>(q0 + h * p.qs[1] + t * p.qs[2] + n % CHUNKS * 8);
+      for (int i = 0; i < COPIES; ++i) {  // (a row that there is not: the first one)
+        if (copies) got[i] = *reinterpret_cast<const u32x4*>(q0 + (at_copy.t < p.n ? at_copy.q : 0) + 8 * chunk);
+        advance(at_copy, by_pass);
       }
       if (threadIdx.x < kWeighRows) {
-        const int r = kWeighRows * c + threadIdx.x;
-        place(r, t, h);
-        row_state(r < rows, t, h, nl, lim);
+        const bool there = at_state.t < p.n;
+        row_state(there, there ? at_state.t : 0, at_state.h, nl, lim);
+        advance(at_state, by_buffer);
       }
     };
-    request(c0);
+    request();
     for (int c = c0; c < n_c; ++c) {
       const int buf = c & 1;
       char* to = row_lds + buf * kWeighRows * PITCH;
+      if (copies) {
 #pragma unroll
-      for (int i = 0; i < COPIES; ++i) {
-        const int n = 256 * i + threadIdx.x;
-        *reinterpret_cast<u32x4*>(to + n / CHUNKS * PITCH + n % CHUNKS * 16) = got[i];
+        for (int i = 0; i < COPIES; ++i) *reinterpret_cast<u32x4*>(to + (PASS_ROWS * i + row) * PITCH + 16 * chunk) = got[i];
       }
       if (threadIdx.x < kWeighRows) {
         nl_lds[buf * kWeighRows + threadIdx.x] = nl;
         lim_lds[buf * kWeighRows + threadIdx.x] = lim;
       }
       __syncthreads();  // (the other buffer was read in front of it)
-      if (c + 1 < n_c) request(c + 1);
+      if (c + 1 < n_c) request();
       const int tiles = min(kWeighRows / 16, (rows - kWeighRows * c + 15) / 16);
       if (j0 >= len) continue;
       for (int rt = 0; rt < tiles; ++rt) {

@@ -18,7 +18,6 @@ struct WeighParams {
   int32_t* positions;            // [B, H_kv, capacity], or null
   const int32_t* new_positions;  // [B, n], new_stride apart
   int64_t new_stride, capacity;
-  uint32_t g_inverse;  // 2^32 / g, rounded up
   int B, H_q, H_kv, g, n, page_shift, n_pages, table_width, max_length;
   float c;  // scale * log2(e)
   int capped;

@@ -209,18 +209,22 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
 #pragma unroll
   for (int s = 0; s < (C::E4M3 ? C::KS / 2 : C::KS); ++s) kaddr[s] = lds0 + krow * C::RBK + (((4 * s + hi) ^ row_swizzle<C::CPRK>(krow)) << 4);
   const int vrow = C::E4M3 ? 8 * hi + (ql >> 1) : 8 * hi + (ql >> 2);
-  uint32_t vaddr[C::DB];
+  // With modified scores in 8 bits, where registers are short (a spill's reload waits for every copy in flight: 32 x 32/8 x 5003 58.9 us instead of 55), the
+  // blocks' addresses are formed from the first one's as they are used: rows are 64 or 128 bytes, so a block is a bit pattern of the address.
+  constexpr bool kFormed = C::SCORED && C::E4M3;
+  static_assert(!kFormed || C::STAGE % 128 == 0, "");
+  uint32_t vaddr[kFormed ? 1 : C::DB];
 #pragma unroll
-  for (int d = 0; d < C::DB; ++d)
+  for (int d = 0; d < (kFormed ? 1 : C::DB); ++d)
     vaddr[d] = lds0 + C::K_BYTES + vrow * C::RBV +
                (C::E4M3 ? ((d ^ tr_swizzle<C::CPRV, true>(vrow)) << 4) + 8 * (ql & 1)
                         : (((2 * d + ((ql & 3) >> 1)) ^ tr_swizzle<C::CPRV, false>(vrow)) << 4) + 8 * (ql & 1));
   auto read_v = [&](int d) -> bf16x8 {
     if constexpr (C::E4M3) {
-      const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(uintptr_t)vaddr[d]);
+      const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(uintptr_t)(kFormed ? vaddr[0] ^ (uint32_t)(d << 4) : vaddr[kFormed ? 0 : d]));
       return widen8(v[0], v[1], 1.f);
     } else {
-      return read_v_frag(vaddr[d], 4 * C::RBV);
+      return read_v_frag(vaddr[kFormed ? 0 : d], 4 * C::RBV);
     }
   };
 
@@ -332,6 +336,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
       for (int e = 0; e < 8; ++e) pb[rt][e] = (__bf16)x[e];
     }
     await_values();
+    if constexpr (kFormed) asm volatile("" : "+v"(vaddr[0]));  // (or the compiler forms all of them in front of the walk after all)
     // Rows that are not there are made zero: a weight of zero does not do away with a NaN.  Nor for the rows that only some of the
     // newest tokens see: NaN and infinities in those count as zero here, and reach the rows that see them at the end.
     if (!masked) {

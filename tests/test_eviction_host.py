@@ -62,7 +62,7 @@ def test_scored_handles(A, cache):
     (dict(B=0), 1), (dict(H_q=0), 1), (dict(H_q=7), 1), (dict(n_new=0), 1), (dict(table_width=0), 1), (dict(max_length=0), 1), (dict(max_length=129), 1),
     (dict(capacity=99), 1), (dict(scale=0.0), 1), (dict(scale=float("inf")), 1), (dict(scale=float("nan")), 1), (dict(cap=-1.0), 1), (dict(cap=float("nan")), 1),
     (dict(q_stride=(1024, 128, 4)), 1), (dict(q_stride=(-8, 8, 8)), 1), (dict(B=1 << 22), 2), (dict(B=1 << 23, H_q=2, n_new=2), 2),
-    (dict(table_width=1 << 26, max_length=(1 << 30) + 1, capacity=1 << 31), 2), (dict(B=1, H_q=1 << 17, n_new=1), 2), (dict(B=1, H_q=1 << 12, n_new=1 << 10), 2),
+    (dict(table_width=1 << 26, max_length=(1 << 30) + 1, capacity=1 << 31), 2), (dict(B=1, H_q=1 << 14, n_new=1 << 11), 2),
 ])
 def test_weigh_refusals(A, cache, patch, status):
     refused(A, status, A.ae_weigh_create, cache[0], **{**WEIGH, **patch})

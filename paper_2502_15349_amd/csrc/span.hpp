@@ -55,22 +55,20 @@ __device__ __forceinline__ void cap_scores(S& s, const CapParams& c, F&& add) {
     }
   }
 }
+__device__ __forceinline__ float cap_tanh_series(float s, const CapParams& c) {
+  const float y = s * c.k;
+  return y * cap_poly(y * y, kCapPoly[0], kCapPoly[1], kCapPoly[2], kCapPoly[3], kCapPoly[4]);
+}
 // N raw scores of a lane -> tanh(y), from which the score, times unit, and its derivative by scale s, 1 - tanh^2, follow.
 template <int N, class S>
 __device__ __forceinline__ void cap_tanh(S& s, const CapParams& c) {
   if (beyond_series<N>(s, c)) {
 #pragma unroll
-    for (int r = 0; r < N; ++r) {
-      const float y = s[r] * c.k;
-      s[r] = __builtin_fabsf(y) <= kCapSeries ? y * cap_poly(y * y, kCapPoly[0], kCapPoly[1], kCapPoly[2], kCapPoly[3], kCapPoly[4])
-                                              : __builtin_fmaf(-2.f, cap_fraction(s[r], c), 1.f);
-    }
+    for (int r = 0; r < N; ++r)
+      s[r] = __builtin_fabsf(s[r] * c.k) <= kCapSeries ? cap_tanh_series(s[r], c) : __builtin_fmaf(-2.f, cap_fraction(s[r], c), 1.f);
   } else {
 #pragma unroll
-    for (int r = 0; r < N; ++r) {
-      const float y = s[r] * c.k;
-      s[r] = y * cap_poly(y * y, kCapPoly[0], kCapPoly[1], kCapPoly[2], kCapPoly[3], kCapPoly[4]);
-    }
+    for (int r = 0; r < N; ++r) s[r] = cap_tanh_series(s[r], c);
   }
 }
 __device__ __forceinline__ float cap_slope(float t) { return __builtin_fmaf(-t, t, 1.f); }

@@ -1237,7 +1237,8 @@ class CacheWeightsPlan:
 class CacheEvictionPlan:
     """A handle for the eviction of cached entries by weight, for lists of one shape, with its workspace.  weights [B, H_kv, capacity] fp32 gives
     shapes and device.  Of every list `keep` entries stay, for each k/v head its own: those of the newest `recent` positions and of positions below `sinks`
-    first, then those with the most weight (equal ones from the list's front).  Calls of one plan must not overlap; of a captured graph, the
+    first, then those with the most weight (equal ones from the list's front).  Calls of one plan must not overlap (they share its workspace, which belongs
+    to the stream that is current when the plan is made: another stream waits for that one before its first call); of a captured graph, the
     plan has to outlive it."""
 
     def __init__(self, cache, weights, *, keep, max_length, table_width, recent=0, sinks=0):
@@ -1392,7 +1393,7 @@ class SpanAttentionPlan:
     V [B, H_kv, L_k, D_v] (bf16) and out [B, H_q, L_q, D_v] (bf16 or fp32), last dimension contiguous, give shapes, strides and device.
     cap: scores are bent to cap tanh(s / cap) (0: not); slopes: a host number per query head, times the distance between query and key
     taken off the score; mask: "none", "causal", "sliding_window" (window keys) or "spans", the key span of every query row given with each call
-    (document_spans makes them for packed documents); kv_splits: ranges of keys that the forward pass walks apart (0: the library chooses, 1: none).
+    (document_spans makes them for packed documents); inputs are finite, rows that nothing sees included; kv_splits: ranges of keys that the forward pass walks apart (0: the library chooses, 1: none).
     Calls of one plan may run at the same time."""
 
     def __init__(self, Q, K, V, out, *, scale, cap=0.0, slopes=None, mask="causal", window=0, kv_splits=0):

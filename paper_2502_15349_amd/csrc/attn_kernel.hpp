@@ -838,8 +838,11 @@ struct KeyLoop {
     mx = max_halves(mx);
     const bool unset = st.m == -INFINITY, moved = unset ? mx > -INFINITY : mx > kLazyLog2;
     if (__builtin_amdgcn_ballot_w64(moved) != 0) {
-      const float d = moved ? mx + kAhead : 0.f, alpha = moved && !unset ? fast_exp2(-d) : 1.f;  // (a row without a reference has nothing to rescale)
-      if (moved) st.m = unset ? d : st.m + d;
+      // (what the reference has moved by is taken after its rounding: far from zero, under a slope, the two differ.  A row without a reference has
+      // nothing to rescale.)
+      const float to = unset ? mx + kAhead : st.m + (mx + kAhead);
+      const float d = !moved ? 0.f : unset ? to : to - st.m, alpha = moved && !unset ? fast_exp2(-d) : 1.f;
+      if (moved) st.m = to;
       st.l *= alpha;
 #pragma unroll
       for (int db = 0; db < C::DB; ++db)

@@ -45,13 +45,18 @@ ae_status_t launched(hipError_t e, const char* who) {
 }
 
 size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
+// Whether the backward pass can put its tiles in an order (spans of the other masks have one)
+bool tiles_ordered(const ae_span_desc_t& d) {
+  return d.mask == AE_SPAN_GIVEN && (d.L_q + 127) / 128 <= ae::kMostOrdered && (d.L_k + 127) / 128 <= ae::kMostOrdered;
+}
 struct Workspace {
-  size_t delta, rows, blocks;  // bytes of each piece: delta; begin and end, each; blocks
-  size_t all() const { return delta + 2 * rows + blocks; }
+  size_t delta, rows, blocks, order;  // bytes of each piece: delta; begin and end, each; blocks; order
+  size_t all() const { return delta + 2 * rows + blocks + order; }
 };
 Workspace backward_workspace(const ae_span_desc_t& d) {
   return {round_up((size_t)d.B * d.H_q * d.L_q * 4), round_up((size_t)d.B * d.L_q * 4),
-          round_up((size_t)d.B * ((d.L_q + 31) / 32) * sizeof(ae::SpanBlock))};
+          round_up((size_t)d.B * ((d.L_q + 31) / 32) * sizeof(ae::SpanBlock)),
+          tiles_ordered(d) ? round_up((size_t)d.B * ((d.L_q + 127) / 128 + (d.L_k + 127) / 128) * 4) : 0};
 }
 
 ae_status_t check_spans(const ae_span* h, const int32_t* begin, const int32_t* end, int64_t stride, const char* who) {
@@ -288,6 +293,7 @@ ae_status_t ae_span_backward(const ae_span_t* h, const void* Q, const void* K, c
   p.O = O;
   p.lse = stats;
   p.delta = reinterpret_cast<float*>(ws);
+  w.order = nullptr;
   p.begin = w.begin;
   p.end = w.end;
   p.blocks = w.blocks;
@@ -311,6 +317,8 @@ ae_status_t ae_span_backward(const ae_span_t* h, const void* Q, const void* K, c
   const int64_t tiles_q = part((int64_t)((d.L_q + 127) / 128) * p.g), tiles_kv = part((d.L_k + 127) / 128), rounds = ((n << p.cut) + 7) / 8;
   p.together[0] = (int)std::max<int64_t>(1, std::min(std::max<int64_t>(4, (64 + tiles_q - 1) / tiles_q), rounds));
   p.together[1] = (int)std::max<int64_t>(1, std::min(std::max<int64_t>(4, (32 + tiles_kv - 1) / tiles_kv), rounds));
+  if (tiles_ordered(d) && !ae::span_halved(rounds * tiles_kv, d.D_qk)) w.order = reinterpret_cast<int32_t*>(ws + need.delta + 2 * need.rows + need.blocks);
+  p.order = w.order;
   int var = ae::BWD_SPAN;
   if (h->mod == ae::MOD_CAP || h->mod == ae::MOD_CAP_SLOPE) var |= ae::BWD_CAP;
   if (h->mod == ae::MOD_SLOPE || h->mod == ae::MOD_CAP_SLOPE) var |= ae::BWD_SLOPE;

@@ -89,6 +89,7 @@ struct BwdSpanParams : BwdParams {
   CapParams cap;
   int64_t dos[3];              // element strides {batch, head, row} of dO
   int grad_bf16;               // dQ, dK and dV are bf16
+  const int32_t* order;        // [B, key tiles + query tiles] of 128 rows: each side's tiles, those with the longest walks first (null: as they come)
 };
 
 // Chunk swizzle of the backward tiles.  A tile row is read both ways -- 128-bit row
@@ -186,6 +187,17 @@ __device__ __forceinline__ SpanBlock load_block(const SpanBlock* at) {
   const i32x4 v = *reinterpret_cast<const __attribute__((address_space(4))) i32x4*>((uintptr_t)uniform_ptr(at));
   return {v[0], v[1], v[2], v[3]};
 }
+// The n-th of the tiles of own rows that is walked: those with the longest walks first, as the causal mask has them by themselves.
+template <class C>
+__device__ __forceinline__ int own_tile(const typename C::P& p, int b, int n, int n_tiles) {
+  if constexpr (C::SPAN && C::OWN == 128)
+    if (p.order != nullptr) {
+      const int key_tiles = (p.L_k + 127) / 128, query_tiles = (p.L_q + 127) / 128;
+      const int32_t* at = p.order + (int64_t)b * (key_tiles + query_tiles) + (C::KV_SIDE ? 0 : key_tiles) + n;
+      return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uintptr_t)uniform_ptr(at));
+    }
+  return C::KV_SIDE ? n : n_tiles - 1 - n;
+}
 // Tiles of TILE other rows that own rows [own0, own0 + OWN) need: queries whose span has one of these keys (key side), keys of their
 // spans (query side).  Spans need not be sorted; the walk takes the tiles between the first and the last one.  Every wave forms them.
 template <class C>
@@ -280,7 +292,7 @@ __device__ __forceinline__ void bwd_single_walk(const typename C::P& p, const De
   int group, item;
   if (!place_in_group(block, p.B * p.H_kv, C::KV_SIDE ? n_own_tiles : n_own_tiles * p.g, p.together[C::KV_SIDE ? 1 : 0], p.cut, group, item)) return;
   const int b = group / p.H_kv, hk = group % p.H_kv;
-  int ot = C::KV_SIDE ? item : n_own_tiles - 1 - item / p.g;
+  int ot = own_tile<C>(p, b, C::KV_SIDE ? item : item / p.g, n_own_tiles);
   const int ho = C::KV_SIDE ? hk : hk * p.g + item % p.g;  // ho: k/v head (key side) or q head (query side)
   const int own0 = ot * C::OWN, ow0 = own0 + (C::SPLIT ? wave & 1 : wave) * 32;  // first own row of the workgroup / of this wave
   const int own = ow0 + ln;                              // this lane's own row (column of S, dP, G^T)
@@ -886,7 +898,7 @@ __device__ __forceinline__ void bwd_pair_walk(const typename C::P& p, const Deca
   int group, item;
   if (!place_in_group(block, p.B * p.H_kv, C::KV_SIDE ? n_own_tiles : n_own_tiles * p.g, p.together[C::KV_SIDE ? 1 : 0], p.cut, group, item)) return;
   const int b = group / p.H_kv, hk = group % p.H_kv;
-  const int ot = C::KV_SIDE ? item : n_own_tiles - 1 - item / p.g;
+  const int ot = own_tile<C>(p, b, C::KV_SIDE ? item : item / p.g, n_own_tiles);
   const int ho = C::KV_SIDE ? hk : hk * p.g + item % p.g;  // ho: k/v head (key side) or q head (query side)
   const int own0 = ot * C::OWN, ow0 = own0 + w4 * 32;
   const int own = ow0 + ln;

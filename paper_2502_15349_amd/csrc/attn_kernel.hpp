@@ -139,7 +139,7 @@ struct Cfg {
   static_assert(!FOLD || ((NORM_ == NORM_SOFTMAX || NORM_ == NORM_SIGMOID) && MOD_ == MOD_PLAIN), "FOLD: softmax or sigmoid, no bias tensor");
   static constexpr int MASK = MASK_;
   static constexpr bool CAUSAL = MASK_ == 1 || MASK_ == 2, WINDOW = MASK_ == 2, SPAN = MASK_ == MASK_SPAN;
-  static constexpr bool ROTATED = WINDOW || SPAN;  // (see the walk over the key tiles)
+  static constexpr bool ROTATED = WINDOW;  // (see the walk over the key tiles)
   static constexpr bool CAPPED = MOD_ == MOD_CAP || MOD_ == MOD_CAP_SLOPE, SLOPED = MOD_ == MOD_SLOPE || MOD_ == MOD_CAP_SLOPE;
   static constexpr bool FINAL = CAPPED || SLOPED;  // the modified scores, in powers of two, are formed in front of mask and row maximum
   static_assert(!FINAL || (SPAN && NORM_ == NORM_SOFTMAX), "capped and distance-biased scores: softmax over spans");
@@ -177,12 +177,12 @@ struct Cfg {
   // LDS fragment reads kept in flight ahead of their MFMA: a ring of PF register quads.  It must divide the MFMAs of
   // an iteration, 4 (DB + T), and fit either block of a sub-step.  Four cover an LDS latency of 128 clocks at one
   // MFMA per 32; under the load of eight wavefronts and the tile copies the latency is longer, and eight measured
-  // 1-3 % faster where the registers are there (128/128 and 192/128; the sliding-window kernels have none to spare).
+  // 1-3 % faster where the registers are there (128/128 and 192/128; the sliding-window kernels have none to spare, and spans did not gain).
 #ifndef AE_TUNE_PF
 #define AE_TUNE_PF 8
 #endif
   static constexpr int PF = (4 * (DV / 32 + DQK / 16)) % AE_TUNE_PF == 0 && AE_TUNE_PF <= DQK / 16 && AE_TUNE_PF <= 2 * (DV / 32) &&
-                                    DQK + DV <= 320 && !ROTATED && MOD_ != MOD_BIAS_T
+                                    DQK + DV <= 320 && !ROTATED && !SPAN && MOD_ != MOD_BIAS_T
                                 ? AE_TUNE_PF : 4;
   // A copy instruction that finds the CU's vector memory queue full blocks the wave
   // that issues it, and with it everything behind it in program order.  Where the
@@ -1055,9 +1055,9 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
     kmax_w = max(0, min(p.L_k, iw0 + 32 + off));
   }
   // Spans: the lane's own row's; the keys that some row of the wave sees, [lo_w, kmax_w), and that all do, [all_lo, all_hi); the first and the
-  // last one that a row of the workgroup sees, [lo_wg, kmax), and the last beginning of a row's.  Rows that see nothing count in
+  // last one that a row of the workgroup sees, [lo_wg, kmax).  Rows that see nothing count in
   // all_hi alone (0), rows behind the last one not at all.
-  int span_lo = 0, span_hi = 0, lo_w = 0, all_lo = 0, all_hi = 0, lo_wg = 0, last_lo = 0;
+  int span_lo = 0, span_hi = 0, lo_w = 0, all_lo = 0, all_hi = 0, lo_wg = 0;
   if constexpr (C::SPAN) {
     constexpr int kNone = 0x7fffffff;
     span_of(p.span, b, min(i, p.L_q - 1), off, p.L_k, span_lo, span_hi);
@@ -1070,9 +1070,9 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
         span_of(p.span, b, min(max(r0, -off), r1), off, p.L_k, lo_first, unused);
         if (lo_first >= unused) lo_first = kNone;
       };
-      int unused;
+      int u0, u1;
       bounds(iw0, iw0 + 31, lo_w, kmax_w, all_lo, all_hi);
-      bounds(i_wg, i_wg + C::BLOCK_M - 1, lo_wg, kmax, last_lo, unused);
+      bounds(i_wg, i_wg + C::BLOCK_M - 1, lo_wg, kmax, u0, u1);
     } else {
       const bool sees = span_lo < span_hi;
       lo_w = sees ? span_lo : kNone;
@@ -1082,14 +1082,12 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
       // (two lanes hold a row of the wave; the workgroup's other rows are read again, by every wave, which needs no barrier)
       lo_wg = lo_w;
       kmax = span_hi;
-      last_lo = span_lo;
 #pragma unroll
       for (int k = 0; k < C::BLOCK_M / 64; ++k) {
         int lo, hi;
         span_of(p.span, b, min(i_wg + 64 * k + lane, p.L_q - 1), off, p.L_k, lo, hi);
         lo_wg = min(lo_wg, lo < hi ? lo : kNone);
         kmax = max(kmax, hi);
-        last_lo = max(last_lo, lo);
       }
 #pragma unroll
       for (int s = 1; s < 64; s *= 2) {
@@ -1099,10 +1097,9 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
         all_hi = min(all_hi, __shfl_xor(all_hi, s));
         lo_wg = min(lo_wg, __shfl_xor(lo_wg, s));
         kmax = max(kmax, __shfl_xor(kmax, s));
-        last_lo = max(last_lo, __shfl_xor(last_lo, s));
       }
       auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };
-      scalar(lo_w), scalar(kmax_w), scalar(all_lo), scalar(all_hi), scalar(lo_wg), scalar(kmax), scalar(last_lo);
+      scalar(lo_w), scalar(kmax_w), scalar(all_lo), scalar(all_hi), scalar(lo_wg), scalar(kmax);
     }
     if (lo_wg == kNone) lo_wg = 0;
   }
@@ -1132,7 +1129,9 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
     jtm = max(jt0, min(jtm, n_tiles));
     u_first = max(0, iw0 + off - p.window + 1) / C::SUB_N;
   }
-  if constexpr (C::SPAN) {  // the same walk: first the tiles behind every row's first key
+  // Spans are walked in order, with the short form in the middle: a wave whose rows begin later than others' has weights of zero until then, one whose
+  // rows have ended has nothing more to do.  (Rotated as above, 1 x 32/8 x 8192 of 128 in documents that begin inside tiles took 182 us, 169 with this; 2 x 16 x 2500 of 192/128 in a window of 1000 59.7, 57.5.)
+  if constexpr (C::SPAN) {
     jt0 = lo_wg / C::BLOCK_N;
     if (p.n_splits > 1) {  // this workgroup's share of its own key tiles
       const int share = (max(n_tiles - jt0, 0) + p.n_splits - 1) / p.n_splits;
@@ -1140,7 +1139,7 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
       n_tiles = min(n_tiles, jt0 + share);
       n_vis = min(n_vis, 2 * n_tiles);
     }
-    jtm = max(jt0, min((last_lo + C::BLOCK_N - 1) / C::BLOCK_N, n_tiles));
+    jtm = jt0;
     u_first = lo_w / C::SUB_N;
   }
   const int n_walk = max(n_tiles - jt0, 0), n_lead = n_tiles - jtm;  // positions in the walk; those before the rotation
@@ -1384,8 +1383,8 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
       const int u = 2 * jt;
       // sub-tiles the wave runs its phases for / has weights of its own in / scores ahead
       const bool vis0 = FAST || C::ROTATED || u < n_vis, vis1 = FAST || C::ROTATED || u + 1 < n_vis;
-      const bool real0 = FAST || !C::ROTATED || (u >= u_first && u < n_vis);
-      const bool real1 = FAST || !C::ROTATED || (u + 1 >= u_first && u + 1 < n_vis);
+      const bool real0 = FAST || !(C::ROTATED || C::SPAN) || (u >= u_first && u < n_vis);
+      const bool real1 = FAST || !(C::ROTATED || C::SPAN) || (u + 1 >= u_first && u + 1 < n_vis);
       const bool sc0 = FAST || C::ROTATED || u + 1 < n_vis;
       const bool sc1 = FAST || (C::ROTATED ? pos + 1 < n_walk : u + 2 < n_vis);
       const bool more = FAST || pos + 2 < n_walk;  // there is a tile two positions on to copy
@@ -1453,26 +1452,35 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
       buf = nb;
     };
 
-    // Positions pos < n_fast of this wave take the short form (tile jt = jtm + pos): sub-tiles
+    // Positions pos < n_fast (spans: from first_fast on) of this wave take the short form (tile jt = jtm + pos): sub-tiles
     // 2jt, 2jt+1 and 2jt+2 are visible, no key of tile jt is hidden from any of its rows
     // (neither by the diagonal, nor by the end of the keys, nor -- from jtm on -- by the lower
     // edge of a window), and the tile two positions on is a whole tile before the rotation.
     int m1 = min((n_vis - 1) / 2, min(p.L_k / C::BLOCK_N, n_tiles) - 2);
     if (C::CAUSAL) m1 = min(m1, (iw0 + off + 1) / C::BLOCK_N);
     if (C::SPAN) m1 = min(m1, all_hi / C::BLOCK_N);
-    const int n_fast = max(m1 - jtm, 0);
+    const int first_fast = C::SPAN ? max((all_lo + C::BLOCK_N - 1) / C::BLOCK_N - jtm, 0) : 0, n_fast = max(m1 - jtm, 0);
 
     if (trailing) phase_barrier();
-    kcp = kbase + (jtm + 2) * ktile_step;  // the first tile the short form copies
-    vcp = vbase + (jtm + 2) * vtile_step;
+    kcp = kbase + (jtm + first_fast + 2) * ktile_step;  // the first tile the short form copies
+    vcp = vbase + (jtm + first_fast + 2) * vtile_step;
     int pos = 0;
     // The loop's place in memory must not depend on the length of the code in front of it.  192/128: of twelve places tried, 1 x 128
     // heads x 8192, causal, took 2112 to 2126 us; longer address arithmetic of the prologue had moved it to one of the slow ones (2254 us
     // became 2271, on another card 2144 became 2162; with this 2145).  128/128, sigmoid: 1 x 16 x 2048 causal 50.1 had become 50.7, so 50.2;
     // 1 x 16 x 1000 unmasked 29.0, 29.4, 29.0.  The other kernels showed no difference.
     if constexpr (C::DQK == 192 || (C::DQK == 128 && C::DV == 128 && C::NORM == NORM_SIGMOID)) asm volatile(".p2align 7");
-    for (; pos < n_fast; ++pos) iteration(std::true_type{}, pos);
-    for (; pos < n_walk; ++pos) iteration(std::false_type{}, pos);
+    if constexpr (C::SPAN) {  // (twice round at most: either form is in the program once)
+      int stop = first_fast < n_fast ? first_fast : n_walk;
+      while (pos < n_walk) {
+        for (; pos < stop; ++pos) iteration(std::false_type{}, pos);
+        for (; pos < n_fast; ++pos) iteration(std::true_type{}, pos);
+        stop = n_walk;
+      }
+    } else {
+      for (; pos < n_fast; ++pos) iteration(std::true_type{}, pos);
+      for (; pos < n_walk; ++pos) iteration(std::false_type{}, pos);
+    }
     if (!trailing) phase_barrier();  // both halves are at the same point again
   }
   // No copy is in flight (the last iterations issue none) and every wave is past its

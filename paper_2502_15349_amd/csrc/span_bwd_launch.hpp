@@ -41,7 +41,7 @@ hipError_t launch_span_var(const BwdSpanParams& p, const DecayTable& dt, hipStre
   // 300 (48) 63.8 / 73.7, 1 x 16 x 4000 (64) 89.2 / 89.8, 4 x 16 x 2048 (128) 96 / 111.  Larger heads have pairs of wavefronts to walk faster: 128/128 causal 1 x 16 x
   // 512 (8) 29.3 / 26.0, 1 x 32/8 x 1024 (8) 124 / 108, x 2048 (16) 234 / 222, but 1 x 16 x 1024 unmasked (16) 44.5 / 62.6; 192/128 1 x 16 x 512 (8) 32.3 / 30.8,
   // 1 x 32/8 x 1024 (8) 135 / 125, x 2048 (16) 259 / 265.
-  if (key_wgs <= (DQK == 64 ? 32 : 8)) return launch_span_sides<K0, Q0>(p, dt, s, true);
+  if (span_halved(key_wgs, DQK)) return launch_span_sides<K0, Q0>(p, dt, s, true);
   if constexpr (DQK == 64) return launch_span_sides<K1, Q1>(p, dt, s, walked_keys<true>(p) < 750000 || key_wgs < 128);
   else if constexpr (DQK == 128) return launch_span_sides<K2, Q1>(p, dt, s, key_wgs <= (p.g == 1 ? 48 : 32));
   else return launch_span_sides<K2, Q2>(p, dt, s, walked_keys<true>(p) < 700000 || key_wgs < 64);

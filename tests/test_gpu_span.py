@@ -414,3 +414,33 @@ def test_ranges_on_two_streams_and_in_a_graph(A):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
+
+
+@pytest.mark.parametrize("dims,B,H_q,H_kv,L", [((64, 64), 4, 16, 16, 600), ((128, 128), 4, 16, 16, 300), ((192, 128), 3, 24, 12, 515)])
+@pytest.mark.parametrize("kind", ["documents", "unsorted", "some_empty"])
+def test_many_workgroups_with_walks_of_unequal_length(A, dims, B, H_q, H_kv, L, kind):
+    """Backward calls whose tiles are put in an order, another one for each batch entry."""
+    Q, K, V, dO = rows(91, B, H_q, L, dims[0]), rows(92, B, H_kv, L, dims[0]), rows(93, B, H_kv, L, dims[1]), rows(94, B, H_q, L, dims[1])
+    if kind == "documents":
+        begin, end = document_spans(documents(95, B, L, 400, padding=7), L)
+    else:
+        g = np.random.RandomState(96)
+        begin = g.randint(0, L, (B, L))
+        end = begin + g.randint(0, 80, (B, L))
+        if kind == "some_empty":
+            end[:, 100:400] = begin[:, 100:400]
+    run_forward(A, Q, K, V, begin, end)
+    run_backward(A, Q, K, V, dO, begin, end)
+
+
+@pytest.mark.parametrize("B,H_q,H_kv,L_q,L_k", [(2, 32, 8, 1500, 1500), (1, 64, 16, 700, 2000), (1, 16, 16, 2000, 700), (1, 4, 2, 16385, 16385), (1, 16, 16, 16384, 300)])
+def test_an_order_of_tiles_changes_nothing(A, B, H_q, H_kv, L_q, L_k):
+    """Given spans that are the causal mask, whose own order needs no other, at sizes on both sides of the largest order."""
+    Q, K, V, dO = rows(97, B, H_q, L_q, 128), rows(98, B, H_kv, L_k, 128), rows(99, B, H_kv, L_k, 128), rows(100, B, H_q, L_q, 128)
+    stats = torch.empty(B, H_q, L_q, device="cuda")
+    O = A.span_attention_forward(Q, K, V, scale=0.09, stats=stats)
+    end = (torch.arange(L_q, device="cuda", dtype=torch.int32) + (L_k - L_q + 1)).clamp(min=0)
+    spans = torch.zeros_like(end), end
+    want = A.span_attention_backward(Q, K, V, O, dO, stats, scale=0.09)
+    got = A.span_attention_backward(Q, K, V, O, dO, stats, scale=0.09, mask="spans", spans=spans)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))

@@ -1235,25 +1235,18 @@ __device__ __forceinline__ void bwd_pair_walk(const typename C::P& p, const Deca
         static_for<0, T1 + AHEAD>(product);
         if constexpr (C::LIN) read_rows(nl4, nl_own, 0);  // (here: 16 registers less during the products)
         float x[16];
-        // Exponents.  Capped scores cost as much as the exponentials: where all are in the series and no entry is hidden they are formed a few at
-        // a time between the products of dP, like the weights (2 x 32/8 x 4096 causal, 128/128, key side alone: 706 -> XXX us).
-        const float d0 = (float)(C::KV_SIDE ? o0 + off - own + 4 * half : own + off - o0 - 4 * half);  // slopes: query less key, register 0
-        auto exponent = [&](int r) {
+        // (Capped scores formed a few at a time between the products of dP, like the weights, took longer: 2 x 32/8 x 4096 causal with a cap, whole
+        // backward pass, 128/128 1126 -> 1142 us, 192/128 1391 -> 1427.)
+        if constexpr (C::CAPPED) cap_tanh<16>(s, p.cap);  // (kept: the cap's derivative follows from them)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
           if constexpr (C::CAPPED) x[r] = __builtin_fmaf(s[r], p.cap.unit, nl4[r / 4][r % 4]);
           else x[r] = __builtin_fmaf(s[r], p.c2, C::NORM == NORM_SOFTMAX ? nl4[r / 4][r % 4] : p.b2);
-          if constexpr (C::SLOPED) x[r] = __builtin_fmaf(-sl, __builtin_fabsf(C::KV_SIDE ? d0 + (float)key_offset(r) : d0 - (float)key_offset(r)), x[r]);
-        };
-        bool lazy = false;
-        if constexpr (C::CAPPED) {
-          lazy = full && !beyond_series<16>(s, p.cap);
-          if (!lazy) {
-            cap_tanh<16>(s, p.cap);  // (kept: the cap's derivative follows from them)
+        }
+        if constexpr (C::SLOPED) {
+          const float d0 = (float)(C::KV_SIDE ? o0 + off - own + 4 * half : own + off - o0 - 4 * half);  // query less key, register 0
 #pragma unroll
-            for (int r = 0; r < 16; ++r) exponent(r);
-          }
-        } else {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) exponent(r);
+          for (int r = 0; r < 16; ++r) x[r] = __builtin_fmaf(-sl, __builtin_fabsf(C::KV_SIDE ? d0 + (float)key_offset(r) : d0 - (float)key_offset(r)), x[r]);
         }
         if constexpr (C::BIAS) {
           // register r = 4 q4 + e is (query, key) = (own row, key 8 q4 + 4 half + e of the tile) on the query side,
@@ -1333,14 +1326,6 @@ __device__ __forceinline__ void bwd_pair_walk(const typename C::P& p, const Deca
         };
         static_for<T1 + AHEAD, M>([&](auto nc) {
           constexpr int k = decltype(nc)::value - T1 - AHEAD, K = T2 - AHEAD;
-          if constexpr (C::CAPPED)
-            if (lazy) {
-#pragma unroll
-              for (int r = 16 * k / K; r < 16 * (k + 1) / K; ++r) {
-                s[r] = cap_tanh_series(s[r], p.cap);
-                exponent(r);
-              }
-            }
 #pragma unroll
           for (int r = 16 * k / K; r < 16 * (k + 1) / K; ++r) weight(r);
           sched_fence();

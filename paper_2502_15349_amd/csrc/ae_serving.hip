@@ -443,9 +443,7 @@ static ae_status_t check_cap(float scale, float cap, ae::CapParams* out, const c
   if (cap == 0.f) return AE_OK;
   if (!(cap > 0.f) || !std::isfinite(cap)) return fail(AE_ERR_INVALID_ARG, "%s: cap must be 0 or positive and finite", who);
   *out = ae::cap_params(scale, cap);
-  const float all[] = {out->k, out->unit, out->e, out->poly[4]};
-  for (float x : all)
-    if (!std::isnormal(x)) return fail(AE_ERR_INVALID_ARG, "%s: cap and scale / cap must be in the range of 32-bit numbers", who);
+  if (!ae::cap_ok(scale, cap)) return fail(AE_ERR_INVALID_ARG, "%s: cap and scale / cap must be in the range of 32-bit numbers", who);
   return AE_OK;
 }
 

@@ -123,9 +123,7 @@ ae_status_t ae_span_create(const ae_span_desc_t* d, ae_span_t** out) {
   if (d->cap != 0.f) {
     if (!(d->cap > 0.f) || !std::isfinite(d->cap)) return fail(AE_ERR_INVALID_ARG, "%s: cap must be 0 or positive and finite", who);
     cap = ae::cap_params(d->scale, d->cap);
-    const float all[] = {cap.k, cap.unit, cap.e, cap.poly[4]};
-    for (float x : all)
-      if (!std::isnormal(x)) return fail(AE_ERR_INVALID_ARG, "%s: cap and scale / cap must be in the range of 32-bit numbers", who);
+    if (!ae::cap_ok(d->scale, d->cap)) return fail(AE_ERR_INVALID_ARG, "%s: cap and scale / cap must be in the range of 32-bit numbers", who);
   }
   if ((int64_t)d->B * d->H_kv > (1 << 24) || d->L_q > (1 << 28) || d->L_k > (1 << 28)) return fail(AE_ERR_UNSUPPORTED, "%s: problem too large for 32-bit tile indices", who);
   if (d->slopes) {
@@ -162,6 +160,7 @@ ae_status_t ae_span_create(const ae_span_desc_t* d, ae_span_t** out) {
   p.out_bf16 = d->out_dtype == AE_OUT_BF16;
   p.n_splits = 1;
   p.cap = d->cap != 0.f ? ae::cap_params(std::fabs(d->scale), d->cap) : cap;  // (the sign is on the queries)
+  p.reference = d->cap != 0.f && !d->slopes ? ae::capped_reference(p.cap.unit) : -INFINITY;
   p.span.kind = (int)d->mask;
   p.span.window = d->mask == AE_SPAN_WINDOW ? (int)std::min<int64_t>(d->window, (int64_t)d->L_q + d->L_k) : 0;
   if (d->slopes)

@@ -104,6 +104,7 @@ struct Params {
 struct SpanParams : Params {
   SpanRows span;
   CapParams cap;
+  float reference;  // of every row, from the start, where the cap bounds the scores closely enough (see capped_reference); else -infinity
 };
 
 struct DecayTable {
@@ -829,9 +830,21 @@ struct KeyLoop {
   // Capped and distance-biased scores, as exponents relative to the row's reference (to zero while it has none): where one is above it by
   // more than kLazyLog2 the reference moves, and the exponents, the sum and the output with it.  Under a slope the scores rise from tile to tile
   // (by 46 powers of two in 32 keys at a slope of one), so there it moves kAhead powers of two beyond them, which spares most of the moves that would follow:
-  // weights of 2^-40 leave 86 more in 32 bits, and a common factor of all weights of a row is no error.
-  static constexpr float kAhead = C::SLOPED ? 40.f : 0.f;
+  // weights of 2^-80 leave 46 more in 32 bits, and a common factor of all weights of a row is no error.
+  static constexpr float kAhead = C::SLOPED ? 80.f : 0.f;
   __device__ __forceinline__ void final_weights(f32x16& s, float& acc) {
+    if (C::SLOPED || p.reference == -INFINITY) follow_maximum(s);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float x0 = fast_exp2(s[2 * q]), x1 = fast_exp2(s[2 * q + 1]);
+      acc += x0 + x1;
+      bf16x2 pr;
+      pr[0] = (__bf16)x0;
+      pr[1] = (__bf16)x1;
+      pk[q / 4][q % 4] = __builtin_bit_cast(uint32_t, pr);
+    }
+  }
+  __device__ __forceinline__ void follow_maximum(f32x16& s) {
     float mx = -INFINITY;
 #pragma unroll
     for (int q = 0; q < 8; ++q) mx = max3(mx, s[2 * q], s[2 * q + 1]);
@@ -850,15 +863,6 @@ struct KeyLoop {
         for (int r = 0; r < 16; ++r) st.o[db][r] *= alpha;
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] -= d;
-    }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const float x0 = fast_exp2(s[2 * q]), x1 = fast_exp2(s[2 * q + 1]);
-      acc += x0 + x1;
-      bf16x2 pr;
-      pr[0] = (__bf16)x0;
-      pr[1] = (__bf16)x1;
-      pk[q / 4][q % 4] = __builtin_bit_cast(uint32_t, pr);
     }
   }
 
@@ -1040,6 +1044,7 @@ __global__ __launch_bounds__(C::THREADS) void attn_fwd_kernel(const typename C::
 
   RowState<C> st;
   st.m = -INFINITY;
+  if constexpr (C::CAPPED && !C::SLOPED) st.m = p.reference;
   st.l = 0.f;
   st.thr = -1.f;
 #pragma unroll

@@ -444,3 +444,24 @@ def test_an_order_of_tiles_changes_nothing(A, B, H_q, H_kv, L_q, L_k):
     want = A.span_attention_backward(Q, K, V, O, dO, stats, scale=0.09)
     got = A.span_attention_backward(Q, K, V, O, dO, stats, scale=0.09, mask="spans", spans=spans)
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("cap", [1e-20, 1e-6, 1e-3, 3e3, 1e5, 1e9, 1e14, 1e30])
+def test_caps_whose_series_is_cut_or_left_out(A, cap):
+    Q, K, V, dO = rows(1, 1, 2, 100, 64, 3.0), rows(2, 1, 2, 100, 64), rows(3, 1, 2, 100, 64), rows(4, 1, 2, 100, 64)
+    begin, end = spans_of("causal", 1, 100, 100)
+    run_forward(A, Q, K, V, begin, end, mask="causal", scale=0.3, cap=cap)
+    run_backward(A, Q, K, V, dO, begin, end, mask="causal", scale=0.3, cap=cap)
+
+
+@pytest.mark.parametrize("cap", [30.0, 50.0, 51.0])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_rows_whose_scores_are_all_at_the_cap(A, cap, sign):
+    """Every score far beyond the cap on one side, or, in the later rows, on both."""
+    Q, V, dO = rows(1, 1, 2, 150, 64).abs() + 0.5, rows(3, 1, 2, 150, 64), rows(4, 1, 2, 150, 64)
+    K = sign * (rows(2, 1, 2, 150, 64).abs() + 0.5)
+    K[:, :, 100::3] *= -1
+    begin, end = spans_of("causal", 1, 150, 150)
+    run_forward(A, Q, K, V * 2.0 ** -20, begin, end, mask="causal", scale=30.0, cap=cap)
+    run_forward(A, Q, K, V * 2.0 ** 20, begin, end, mask="causal", scale=30.0, cap=cap)
+    run_backward(A, Q, K, V, dO, begin, end, mask="causal", scale=30.0, cap=cap)

@@ -51,7 +51,7 @@ typedef struct {
   int32_t D_qk, D_v;              /* 64/64, 128/128 or 192/128 */
   float scale;                    /* finite and non-zero */
   float cap;                      /* 0: none; else positive, with cap and scale / cap in the range of 32-bit numbers */
-  const float *slopes;            /* host, [H_q] finite numbers, copied by create; NULL: none.  H_q <= AE_MAX_SLOPE_HEADS, L_q + L_k <= 2^24 */
+  const float *slopes;            /* host, [H_q] finite numbers below 10^30 times the scale, copied by create; NULL: none.  H_q <= AE_MAX_SLOPE_HEADS, L_q + L_k <= 2^24 */
   ae_span_mask_t mask;
   int32_t window;                 /* AE_SPAN_WINDOW: >= 1 */
   ae_out_dtype_t out_dtype;       /* of O */

@@ -131,6 +131,8 @@ ae_status_t ae_span_create(const ae_span_desc_t* d, ae_span_t** out) {
     if ((int64_t)d->L_q + d->L_k > (1 << 24)) return fail(AE_ERR_UNSUPPORTED, "%s: slopes come with L_q + L_k up to 2^24", who);
     for (int k = 0; k < d->H_q; ++k)
       if (!std::isfinite(d->slopes[k] * log2e * (1 << 24))) return fail(AE_ERR_INVALID_ARG, "%s: slopes[%d] must be finite, and 2^24 times it", who, k);
+    for (int k = 0; k < d->H_q; ++k)
+      if (!(std::fabs((double)d->slopes[k] / d->scale) < 1e30)) return fail(AE_ERR_INVALID_ARG, "%s: slopes[%d] must be below 10^30 times the scale", who, k);
   }
   ae_span* h = new (std::nothrow) ae_span();
   if (!h) return fail(AE_ERR_NOMEM, "%s: out of host memory", who);

@@ -184,3 +184,10 @@ def test_ranges_that_are_chosen(A):
     for kw in (dict(B=2, H_q=12, H_kv=12, L_q=1023, L_k=1023), dict(B=1, H_q=32, H_kv=8, L_q=8192, L_k=8192), dict(B=1, H_q=4, H_kv=4, L_q=10, L_k=100),
                dict(B=1, H_q=16, H_kv=16, L_q=17, L_k=8192, mask="sliding_window", window=100), dict(B=1, H_q=16, H_kv=16, L_q=17, L_k=8192, kv_splits=1)):
         assert ranges(**kw) == 0
+
+
+@built
+def test_slopes_far_above_the_scale_are_refused(A):
+    for slopes in ([0.0, 1e2, 0.0, 0.0], [-1e2] * 4):
+        refused(A, 1, A.ae_span_create, **{**SPAN, "scale": 1e-29, "slopes": slopes})
+    A.ae_span_destroy(A.ae_span_create(**{**SPAN, "scale": 1e-27, "slopes": [1e2] * 4}))

@@ -318,7 +318,7 @@ ae_status_t ae_span_backward(const ae_span_t* h, const void* Q, const void* K, c
   const int64_t tiles_q = part((int64_t)((d.L_q + 127) / 128) * p.g), tiles_kv = part((d.L_k + 127) / 128), rounds = ((n << p.cut) + 7) / 8;
   p.together[0] = (int)std::max<int64_t>(1, std::min(std::max<int64_t>(4, (64 + tiles_q - 1) / tiles_q), rounds));
   p.together[1] = (int)std::max<int64_t>(1, std::min(std::max<int64_t>(4, (32 + tiles_kv - 1) / tiles_kv), rounds));
-  if (tiles_ordered(d) && !ae::span_halved(rounds * tiles_kv, d.D_qk)) w.order = reinterpret_cast<int32_t*>(ws + need.delta + 2 * need.rows + need.blocks);
+  if (tiles_ordered(d) && !ae::span_halved(rounds * tiles_kv, d.D_qk, p.g)) w.order = reinterpret_cast<int32_t*>(ws + need.delta + 2 * need.rows + need.blocks);
   p.order = w.order;
   int var = ae::BWD_SPAN;
   if (h->mod == ae::MOD_CAP || h->mod == ae::MOD_CAP_SLOPE) var |= ae::BWD_CAP;

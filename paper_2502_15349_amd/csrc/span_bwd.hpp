@@ -12,7 +12,7 @@ struct SpanPrepare {
   int32_t* order;  // BwdSpanParams::order; null: not wanted
 };
 // Whether the walks are halved, with 64 rows a workgroup: rule and measurements at launch_span_var.
-inline bool span_halved(int64_t key_workgroups_per_xcd, int dqk) { return key_workgroups_per_xcd <= (dqk == 64 ? 32 : 8); }
+inline bool span_halved(int64_t key_workgroups_per_xcd, int dqk, int heads_per_group) { return key_workgroups_per_xcd <= (dqk == 64 ? 32 : heads_per_group >= 4 ? 16 : 8); }
 // Most tiles of a side that are put in an order.
 constexpr int kMostOrdered = 128;
 // var: BWD_SPAN with BWD_CAP, BWD_SLOPE

@@ -40,8 +40,10 @@ hipError_t launch_span_var(const BwdSpanParams& p, const DecayTable& dt, hipStre
   // (4) 61.5 / 44.8, x 2048 (16) 213 / 147, 2 x 12 x 1023 (24) 41.7 / 33.6, 1 x 16 x 2048 (32) 68 / 56, documents 1 x 32/8 x 4096 (32) 222 / 156, but 16 x 32/8 x
   // 300 (48) 63.8 / 73.7, 1 x 16 x 4000 (64) 89.2 / 89.8, 4 x 16 x 2048 (128) 96 / 111.  Larger heads have pairs of wavefronts to walk faster: 128/128 causal 1 x 16 x
   // 512 (8) 29.3 / 26.0, 1 x 32/8 x 1024 (8) 124 / 108, x 2048 (16) 234 / 222, but 1 x 16 x 1024 unmasked (16) 44.5 / 62.6; 192/128 1 x 16 x 512 (8) 32.3 / 30.8,
-  // 1 x 32/8 x 1024 (8) 135 / 125, x 2048 (16) 259 / 265.
-  if (span_halved(key_wgs, DQK)) return launch_span_sides<K0, Q0>(p, dt, s, true);
+  // 1 x 32/8 x 1024 (8) 135 / 125, x 2048 (16) 259 / 265.  A key-side workgroup walks the query heads of its group one after the other, so larger groups gain
+  // longer; causal with a cap: 128/128 3 x 32/8 x 448 (12) 84.3 / 69.8, 1 x 64/8 x 1500 (12) 438 / 362, 2 x 64/4 x 2048 (16) 1158 / 1067, but 3 x 64/8 x 800 (21)
+  // 256 / 326; 192/128 88.5 / 83.2, 461 / 426, 1223 / 1200, 268 / 376.  64/64: 6 x 64/8 x 1002 (48) 398 / 451, 3 x 12 x 1344 (49) 87 / 95.
+  if (span_halved(key_wgs, DQK, p.g)) return launch_span_sides<K0, Q0>(p, dt, s, true);
   if constexpr (DQK == 64) return launch_span_sides<K1, Q1>(p, dt, s, walked_keys<true>(p) < 750000 || key_wgs < 128);
   else if constexpr (DQK == 128) return launch_span_sides<K2, Q1>(p, dt, s, key_wgs <= (p.g == 1 ? 48 : 32));
   else return launch_span_sides<K2, Q2>(p, dt, s, walked_keys<true>(p) < 700000 || key_wgs < 64);

@@ -162,7 +162,6 @@ ae_status_t ae_span_create(const ae_span_desc_t* d, ae_span_t** out) {
   p.out_bf16 = d->out_dtype == AE_OUT_BF16;
   p.n_splits = 1;
   p.cap = d->cap != 0.f ? ae::cap_params(std::fabs(d->scale), d->cap) : cap;  // (the sign is on the queries)
-  p.reference = d->cap != 0.f && !d->slopes ? ae::capped_reference(p.cap.unit) : -INFINITY;
   p.span.kind = (int)d->mask;
   p.span.window = d->mask == AE_SPAN_WINDOW ? (int)std::min<int64_t>(d->window, (int64_t)d->L_q + d->L_k) : 0;
   if (d->slopes)

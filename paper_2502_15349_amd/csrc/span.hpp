@@ -44,10 +44,6 @@ inline CapParams cap_params(float scale, float cap) {
   c.limit = (float)std::fmin(limit / std::fabs(k), 1e18);  // (its square is a number)
   return c;
 }
-// Capped scores lie within +-unit powers of two: up to a cap of 50 one reference serves every row, from which the least weight there can be is 2^-90 and the
-// greatest at most 2^56, so that a row's maximum need not be followed (values from 2^-36 to 2^40 have room beside them; without a cap, or with a larger one,
-// weights lie below 2^8).  Forward, causal with a cap of 50, maximum followed / not: 2 x 32/8 x 4096 of 128/128 355 / 332 us, 192/128 383 / 368, 4 x 16 x 4096 of 64/64 286 / 255.
-inline float capped_reference(float unit) { return unit <= 73.f ? std::fmin(unit, 90.f - unit) : -INFINITY; }
 inline bool cap_ok(float scale, float cap) {  // of a positive, finite cap: whether the constants are in the range of 32-bit numbers
   const float k = (float)((double)scale / cap), unit = (float)(cap * 1.4426950408889634);
   return std::isnormal(k) && std::isnormal(k * 3.f) && std::isnormal(unit);

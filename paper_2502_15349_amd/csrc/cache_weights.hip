@@ -9,7 +9,7 @@
 // of a workgroup share them.  (Each for itself, the L2 serves 2 GB for 500 tokens of 4 x 16/16 heads x 8000 keys of 128: 237 us in 8 bits with a cap.)
 //
 // Bound by the reading of the keys for a few rows (16 x 32/8 x 2048, one token: 12.3 us, 3.4 TB/s; 8 tokens 15.4), by vector instructions for many (an
-// exponential, a multiply-add, an addition and, with a cap, seven more for every score; 500 tokens as above: 93 us, 0.68 PFLOP/s; in 8 bits with a cap 116).  64 keys a
+// exponential, a multiply-add, an addition and, with a cap, six more for every score; 500 tokens as above: 93 us, 0.68 PFLOP/s; in 8 bits with a cap 110).  64 keys a
 // wavefront, with half the reads of the rows, took 7 % longer there, and half as long again where there are fewer keys than compute units take (1 x 32/8 x
 // 200 of 3000: 21.6 -> 32.4).  Divisions for the rows' places instead of steps, and scores moved out of accumulation registers: 121 instead of 116.
 #include "cache_weights.hpp"

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
     lim[rt] = pt.causal ? len - p.n + 1 + t : len;
     if constexpr (C::SCORED) {
       const CachedPart& own = p.part[0];
-      slope[rt] = p.slopes[h];
+      slope[rt] = p.slopes[min(h, kMaxSlopeHeads - 1)];  // (more heads come without slopes: all of the table is 0)
       at[rt] = (float)(pt.causal ? len - p.n + t : len + max(0, min(own.lengths[b], own.max_length)) - p.n + t);
     }
   }

@@ -222,3 +222,20 @@ def test_refusals_of_the_binding(A):
         A.attention_cached(Q, c, t.cuda(), ints([40]), scale=0.1, slopes=[1.0])
     with pytest.raises(A.AeAttnError):
         A.attention_cached(Q, c, t.cuda(), ints([40]), scale=0.1, cap=-2.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("H_q,H_kv,n,prefix", [(264, 1, 1, 0), (320, 8, 2, 0), (1024, 16, 1, 0), (512, 16, 1, 100)])
+def test_a_cap_with_more_heads_than_a_table_of_slopes_has(A, dtype, H_q, H_kv, n, prefix):
+    """Caps come with any number of heads; the statistics of all of them are the definition's too, and what the entries receive by them adds up."""
+    lengths, page = [150, 33], 32
+    c, t, pre = setup(A, 17, H_kv, page, lengths, 64, 64, dtype, extra=-(-prefix // page))
+    Q, L = queries(18, 2, H_q, n, 64), ints(lengths)
+    kw = dict(scale=0.125, cap=8.0)
+    S = torch.full((2, H_q, n), float("nan"), device="cuda")
+    O = A.attention_cached(Q, c, t.cuda(), L, stats=S, prefix_table=pre.cuda() if prefix else None, prefix_length=prefix, **kw)
+    keys, vals = ([np.concatenate([rows_of(x, pre.tolist(), prefix), rows_of(x, t[b].tolist(), lengths[b])], 2) for b in range(2)] for x in values(c))
+    check(O, S, Q, keys, vals, **kw)
+    if not prefix:  # g n rows of probabilities that sum to 1; score and statistic are within e each, 64 2^-24 of 0.125 * 64 * 8 * 4, so 2e-3 together
+        W = A.cache_weights(Q, c, t.cuda(), L, S, torch.zeros(2, H_kv, 160, device="cuda"), **kw)
+        assert torch.allclose(W.sum(-1), torch.full((2, H_kv), float(H_q // H_kv * n), device="cuda"), rtol=2.0 ** -8, atol=0)

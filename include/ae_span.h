@@ -73,7 +73,8 @@ ae_status_t ae_span_create(const ae_span_desc_t *desc, ae_span_t **out);
  * Precision: scores, their modification, softmax, sums and accumulators are fp32; a weight is rounded once to bf16 for the
  * product with the values, while the sum that divides the row is that of the unrounded weights: an output is within 2^-8
  * sum_j p_j |v_j| of the exact one, and a bf16 output is rounded once more.  A capped score has a relative error of 3e-7 up to 0.6
- * of the cap (0.2, 0.1, 0.03 and 5e-4 of it where |scale| / cap is below 1.2e-4, 8e-6, 6e-8 and 7e-13) and an absolute one of 2e-7 of the cap beyond.  With
+ * of the cap (0.2, 0.1, 0.03 and 5e-4 of it where |scale| / cap is below 1.2e-4, 8e-6, 6e-8 and 7e-13) and an absolute one of 2e-7 of the cap beyond, or
+ * everywhere where |scale| / cap is above 4e3 (caps up to 10^6; with larger ones sooner) and where |q . k| is above 10^18.  With
  * slopes a row's weights may be held at 2^-80 of their size: products with values below 2^-40 in magnitude can be lost then.          */
 ae_status_t ae_span_forward(const ae_span_t *h, const void *Q, const void *K, const void *V, const int32_t *key_begin,
                             const int32_t *key_end, int64_t span_stride, void *O, float *stats, hipStream_t stream);

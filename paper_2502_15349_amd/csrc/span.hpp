@@ -34,8 +34,8 @@ inline CapParams cap_params(float scale, float cap) {
       c.limit = -1.f;
       return c;
     }
-    if (least < 1e-37) {  // a huge cap: without this term and those behind it, as far as they are below 1e-7
-      if (i > 0) limit = std::fmin(limit, std::pow(1e-7 / std::fabs(kCapPoly[i]), 0.5 / i));
+    if (i > 0 && least < 1e-37) {  // a huge cap: without this term and those behind it, as far as they are below 1e-7.  (The first one is the score itself.)
+      limit = std::fmin(limit, std::pow(1e-7 / std::fabs(kCapPoly[i]), 0.5 / i));
       break;
     }
     c.poly[i] = (float)(t * unit);

@@ -239,3 +239,21 @@ def test_a_cap_with_more_heads_than_a_table_of_slopes_has(A, dtype, H_q, H_kv, n
     if not prefix:  # g n rows of probabilities that sum to 1; score and statistic are within e each, 64 2^-24 of 0.125 * 64 * 8 * 4, so 2e-3 together
         W = A.cache_weights(Q, c, t.cuda(), L, S, torch.zeros(2, H_kv, 160, device="cuda"), **kw)
         assert torch.allclose(W.sum(-1), torch.full((2, H_kv), float(H_q // H_kv * n), device="cuda"), rtol=2.0 ** -8, atol=0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("cap", [2e36, 1e37])
+def test_the_largest_caps_leave_the_scores(A, dtype, cap):
+    """Scale / cap next to the smallest 32-bit number with all its bits: as without a cap, also for what the entries receive."""
+    lengths, page = [300, 70], 32
+    c, t, _ = setup(A, 19, 2, page, lengths, 64, 64, dtype)
+    Q, L, got = queries(20, 2, 8, 2, 64), ints(lengths), []
+    for x in (0.0, cap):
+        S = torch.empty(2, 8, 2, device="cuda")
+        O = A.attention_cached(Q, c, t.cuda(), L, scale=0.125, stats=S, cap=x)
+        keys, vals = ([rows_of(y, t[b].tolist(), lengths[b]) for b in range(2)] for y in values(c))
+        check(O, S, Q, keys, vals, 0.125, cap=x)
+        got.append((S, A.cache_weights(Q, c, t.cuda(), L, S, torch.zeros(2, 2, 320, device="cuda"), scale=0.125, cap=x)))
+    # scores up to 20 or so, 3e-7 of which the cap's constants are off, and the roundings of the statistic
+    assert (got[0][0] - got[1][0]).abs().max() <= 20 * 3e-7 + 2.0 ** -19 * 20
+    assert torch.allclose(got[0][1], got[1][1], rtol=1e-4, atol=0)

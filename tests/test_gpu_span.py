@@ -465,3 +465,14 @@ def test_rows_whose_scores_are_all_at_the_cap(A, cap, sign):
     run_forward(A, Q, K, V * 2.0 ** -20, begin, end, mask="causal", scale=30.0, cap=cap)
     run_forward(A, Q, K, V * 2.0 ** 20, begin, end, mask="causal", scale=30.0, cap=cap)
     run_backward(A, Q, K, V, dO, begin, end, mask="causal", scale=30.0, cap=cap)
+
+
+@pytest.mark.parametrize("cap", [2e36, 1e37, 2e38])
+def test_the_largest_caps_leave_the_scores(A, cap):
+    """Scale / cap next to the smallest 32-bit number with all its bits: the series is its first term."""
+    Q, K, V, dO = rows(1, 1, 2, 100, 64, 3.0), rows(2, 1, 2, 100, 64), rows(3, 1, 2, 100, 64), rows(4, 1, 2, 100, 64)
+    begin, end = spans_of("causal", 1, 100, 100)
+    scale = 0.3 if cap < 1e38 else 3.0
+    run_forward(A, Q, K, V, begin, end, mask="causal", scale=scale, cap=cap)
+    run_forward(A, Q, K, V, begin, end, mask="causal", scale=-scale, cap=cap, slopes=True)
+    run_backward(A, Q, K, V, dO, begin, end, mask="causal", scale=scale, cap=cap)

@@ -2,6 +2,8 @@
 import ctypes
 import os
 import re
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -191,3 +193,54 @@ def test_slopes_far_above_the_scale_are_refused(A):
     for slopes in ([0.0, 1e2, 0.0, 0.0], [-1e2] * 4):
         refused(A, 1, A.ae_span_create, **{**SPAN, "scale": 1e-29, "slopes": slopes})
     A.ae_span_destroy(A.ae_span_create(**{**SPAN, "scale": 1e-27, "slopes": [1e2] * 4}))
+
+
+CAP_PARAMS = """
+#include <stdio.h>
+#include <stdlib.h>
+#include "%s"
+int main(int n, char** a) {
+  for (int i = 1; i + 1 < n; i += 2) {
+    const float scale = strtof(a[i], nullptr), cap = strtof(a[i + 1], nullptr);
+    const ae::CapParams c = ae::cap_params(scale, cap);
+    printf("%%d %%.9g %%.9g %%.9g", (int)ae::cap_ok(scale, cap), c.limit, c.unit, c.e);
+    for (float x : c.poly) printf(" %%.9g", x);
+    for (float x : c.tanh) printf(" %%.9g", x);
+    printf("\\n");
+  }
+}
+"""
+
+
+def test_constants_of_accepted_caps(tmp_path):
+    """Over all accepted magnitudes of cap and scale the capped score that the kernels' constants stand for, evaluated in 64 bits: where the series holds, the
+    definition's to 3e-7 of itself, a term of it that is left out included; where it does not, the exact form's constants are there."""
+    hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+    if not os.path.exists(hipcc):
+        pytest.skip("hipcc is not there")
+    src, out = tmp_path / "cap.hip", str(tmp_path / "cap")
+    src.write_text(CAP_PARAMS % os.path.join(ROOT, "paper_2502_15349_amd", "csrc", "span.hpp"))
+    subprocess.run([hipcc, "--offload-host-only", "-O1", "-std=c++17", str(src), "-o", out], check=True, capture_output=True)
+    pairs = [(s, c) for s in (0.125, -0.125, 1.0, 1e-3, 1e3, 1e-30, 1e-37, 1e30) for c in [10.0 ** n for n in range(-37, 38)] + [50.0, 2e36, 1.5e38]]
+    got = subprocess.run([out, *[repr(x) for p in pairs for x in p]], check=True, capture_output=True, text=True).stdout.split("\n")[:-1]
+    assert len(got) == len(pairs)
+    accepted = 0
+    for (scale, cap), line in zip(pairs, got):
+        ok, limit, unit, e, *rest = (float(x) for x in line.split())
+        scale, cap = float(np.float32(scale)), float(np.float32(cap))
+        if not ok:
+            continue
+        accepted += 1
+        poly, tanh, k = np.array(rest[:5]), np.array(rest[5:]), scale / cap
+        # (constants below 2^-126 have fewer bits; unit log2(e) rounded twice)
+        assert abs(unit - cap / np.log(2)) <= 2e-7 * unit and abs(e - 2 * k / np.log(2)) <= 2e-7 * abs(e) + 1e-44
+        if limit < 0:
+            assert (poly == 0).all() and (tanh == 0).all()
+            continue
+        assert abs(tanh[0] - k) <= 2e-7 * abs(k) and abs(poly[0] - scale / np.log(2)) <= 2e-7 * abs(scale) + 1e-44, (scale, cap)
+        s = limit * np.array([1.0, 0.99, 0.5, 1e-2, 1e-6])
+        y = k * s
+        for c, want in ((tanh, np.tanh(y)), (poly, cap / np.log(2) * np.tanh(y))):
+            value = s * sum(x * (s * s) ** n for n, x in enumerate(c))
+            assert np.all(np.abs(value - want) <= 3e-7 * np.abs(want) + 1e-44 * s), (scale, cap)
+    assert accepted > 400

@@ -292,13 +292,21 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_EU) void cached_attn_kernel(co
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = s[e / 4][rt][e % 4];
       if constexpr (C::SCORED) {  // in powers of two from here on
-        const float base = -slope[rt] * (at[rt] - (float)(j0 + 8 * hi));  // (no key is behind its token)
+        const float base = -slope[rt] * (at[rt] - (float)(j0 + 8 * hi));
         auto far = [&](int e) { return __builtin_fmaf(slope[rt], (float)e, base); };
         if (p.capped) {
           cap_scores<8>(x, p.cap, far);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(x[e], c, far(e));
+        }
+        // No key that is seen is behind its token, but for the keys of a prefix and tokens that their own list is too short for.
+        if (!pt.causal && __builtin_amdgcn_ballot_w64(at[rt] < (float)(j0 + 31)) != 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float behind = fmaxf((float)(j0 + 8 * hi + e) - at[rt], 0.f);
+            x[e] = __builtin_fmaf(-slope[rt], behind, __builtin_fmaf(-slope[rt], behind, x[e]));  // (in this form nothing is kept in registers for it)
+          }
         }
       }
       if (masked) {

@@ -257,3 +257,24 @@ def test_the_largest_caps_leave_the_scores(A, dtype, cap):
     # scores up to 20 or so, 3e-7 of which the cap's constants are off, and the roundings of the statistic
     assert (got[0][0] - got[1][0]).abs().max() <= 20 * 3e-7 + 2.0 ** -19 * 20
     assert torch.allclose(got[0][1], got[1][1], rtol=1e-4, atol=0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("H_q,H_kv,n,lengths,prefix", [(8, 2, 3, [0, 1, 2, 3, 50], 100), (4, 4, 8, [2, 0], 5), (16, 1, 2, [0, 300], 700)])
+def test_tokens_that_their_list_is_too_short_for(A, dtype, H_q, H_kv, n, lengths, prefix):
+    """Behind a prefix they see all of it, from places inside it or in front of it: keys on both sides."""
+    page = 16
+    c, t, pre = setup(A, 21, H_kv, page, lengths, 64, 64, dtype, extra=-(-prefix // page))
+    Q, B = queries(22, len(lengths), H_q, n, 64), len(lengths)
+    keys, vals = ([np.concatenate([rows_of(x, pre.tolist(), prefix), rows_of(x, t[b].tolist(), lengths[b])], 2) for b in range(B)] for x in values(c))
+    for kw in (dict(slopes=slopes_of(H_q)), dict(slopes=[1.5 - h for h in range(H_q)]), dict(cap=4.0, slopes=slopes_of(H_q))):
+        S = torch.empty(B, H_q, n, device="cuda")
+        O = A.attention_cached(Q, c, t.cuda(), ints(lengths), scale=0.1, stats=S, prefix_table=pre.cuda(), prefix_length=prefix, **kw)
+        for b in range(B):
+            q, L = Q[b: b + 1].cpu().double().numpy(), prefix + lengths[b]
+            seen = np.zeros((1, n), int), np.maximum(prefix, L - n + 1 + np.arange(n))[None]
+            ref, lse, mag = span_attention(q, keys[b], vals[b], *seen, scale=0.1, **kw)
+            most = 0.1 * float(np.abs(q).max((0, 1, 2)) @ np.abs(keys[b]).max((0, 1, 2)))
+            e = 64 * 2.0 ** -24 * most + 4e-7 * min(kw.get("cap", 0.0), most) + 2.0 ** -22 * max(map(abs, kw["slopes"])) * (L + n) + 2.0 ** -21
+            assert np.all(np.abs(O[b: b + 1].cpu().double().numpy() - ref) <= (2.0 ** -8 + 2 * e + 2.0 ** -20) * mag), b
+            assert np.all(np.abs(S[b: b + 1].cpu().double().numpy() - lse) <= e + 2.0 ** -20 * (1 + np.abs(lse))), b

@@ -1438,7 +1438,7 @@ class SpanAttentionPlan:
         B, _, L_q = self._rows
         for t in (begin, end):
             if (t.dtype != self._types[2] or t.device != self.device or tuple(t.shape) not in ((L_q,), (B, L_q)) or t.shape != begin.shape
-                    or (L_q > 1 and t.stride(-1) != 1) or t.stride() != begin.stride()):
+                    or (L_q > 1 and t.stride(-1) != 1) or (t.dim() == 2 and B > 1 and t.stride(0) != begin.stride(0))):
                 raise ValueError("spans must be a pair of int32 device tensors [L_q] or [B, L_q] of the same strides, with contiguous rows")
         return begin.data_ptr(), end.data_ptr(), begin.stride(0) if begin.dim() == 2 else 0
 

@@ -476,3 +476,18 @@ def test_the_largest_caps_leave_the_scores(A, cap):
     run_forward(A, Q, K, V, begin, end, mask="causal", scale=scale, cap=cap)
     run_forward(A, Q, K, V, begin, end, mask="causal", scale=-scale, cap=cap, slopes=True)
     run_backward(A, Q, K, V, dO, begin, end, mask="causal", scale=scale, cap=cap)
+
+
+def test_strides_of_spans_that_do_not_matter(A):
+    """Rows of one batch entry, or of one query, have no distance: any stride will do, and two different ones."""
+    Q, K, V, dO = rows(1, 1, 2, 40, 64), rows(2, 1, 2, 40, 64), rows(3, 1, 2, 40, 64), rows(4, 1, 2, 40, 64)
+    begin, end = spans_tensor(*spans_of("causal", 1, 40, 40))
+    odd = torch.stack([end[0], end[0]])[1:].as_strided((1, 40), (7, 1))
+    want = A.span_attention_forward(Q, K, V, scale=0.1, mask="spans", spans=(begin, end))
+    assert torch.equal(A.span_attention_forward(Q, K, V, scale=0.1, mask="spans", spans=(begin, odd)), want)
+    one = torch.stack([end[0, 20:22], end[0, 20:22]], 1)[:1, :1].as_strided((1, 1), (1, 2))
+    got = A.span_attention_forward(Q[:, :, 20:21], K, V, scale=0.1, mask="spans", spans=(begin[:, :1], one))
+    assert got.shape == (1, 2, 1, 64) and torch.isfinite(got).all()
+    two = spans_tensor(*spans_of("causal", 2, 40, 40))
+    with pytest.raises(ValueError):  # where they matter they have to be the same
+        A.span_attention_forward(*(t.expand(2, -1, -1, -1) for t in (Q, K, V)), scale=0.1, mask="spans", spans=(two[0], two[1][:1].expand(2, 40)))

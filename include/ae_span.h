@@ -37,6 +37,7 @@ typedef enum {
 } ae_span_mask_t;
 
 #define AE_MAX_SLOPE_HEADS AE_MAX_DECAY_HEADS
+#define AE_MAX_SLOPE 128 /* (where the keys next to a key weigh 2^-184 of it) */
 
 /*
  * Layouts (bf16 inputs, fp32 or bf16 output, last dimension contiguous):
@@ -51,7 +52,8 @@ typedef struct {
   int32_t D_qk, D_v;              /* 64/64, 128/128 or 192/128 */
   float scale;                    /* finite and non-zero */
   float cap;                      /* 0: none; else positive, with cap and scale / cap in the range of 32-bit numbers */
-  const float *slopes;            /* host, [H_q] finite numbers below 10^30 times the scale, copied by create; NULL: none.  H_q <= AE_MAX_SLOPE_HEADS, L_q + L_k <= 2^24 */
+  const float *slopes;            /* host, [H_q] finite numbers below 10^30 times the scale, copied by create; NULL: none.  AE_ERR_UNSUPPORTED beyond AE_MAX_SLOPE in
+                                   * magnitude, AE_MAX_SLOPE_HEADS heads or L_q + L_k = 2^24 */
   ae_span_mask_t mask;
   int32_t window;                 /* AE_SPAN_WINDOW: >= 1 */
   ae_out_dtype_t out_dtype;       /* of O */

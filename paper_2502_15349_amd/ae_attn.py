@@ -1391,7 +1391,7 @@ def ae_span_documents(B: int, L: int, n_docs: int, offsets: int, offset_stride: 
 class SpanAttentionPlan:
     """A handle for span attention, for calls of one shape: the layers of a model keep it.  Q [B, H_q, L_q, D_qk], K [B, H_kv, L_k, D_qk],
     V [B, H_kv, L_k, D_v] (bf16) and out [B, H_q, L_q, D_v] (bf16 or fp32), last dimension contiguous, give shapes, strides and device.
-    cap: scores are bent to cap tanh(s / cap) (0: not); slopes: a host number per query head, times the distance between query and key
+    cap: scores are bent to cap tanh(s / cap) (0: not); slopes: a host number per query head, at most 128 in magnitude, times the distance between query and key
     taken off the score; mask: "none", "causal", "sliding_window" (window keys) or "spans", the key span of every query row given with each call
     (document_spans makes them for packed documents); inputs are finite, rows that nothing sees included; kv_splits: ranges of keys that the forward pass walks apart (0: the library chooses, 1: none).
     Calls of one plan may run at the same time."""

@@ -131,6 +131,11 @@ ae_status_t ae_span_create(const ae_span_desc_t* d, ae_span_t** out) {
     if ((int64_t)d->L_q + d->L_k > (1 << 24)) return fail(AE_ERR_UNSUPPORTED, "%s: slopes come with L_q + L_k up to 2^24", who);
     for (int k = 0; k < d->H_q; ++k)
       if (!std::isfinite(d->slopes[k] * log2e * (1 << 24))) return fail(AE_ERR_INVALID_ARG, "%s: slopes[%d] must be finite, and 2^24 times it", who, k);
+    // The forward pass forms exponents from terms of up to 31 slopes, of either sign, that cancel for near keys.  Measured, a statistic is then off by up to 48 x 2^-22
+    // times the slope (slopes alone at 64/64 and 128/128; elsewhere 12): 1.5e-3 at a slope of 128, 8e-2 at 10^4, where the backward pass, whose distances are
+    // exact, would take weights of 1 for 0.93.
+    for (int k = 0; k < d->H_q; ++k)
+      if (std::fabs(d->slopes[k]) > AE_MAX_SLOPE) return fail(AE_ERR_UNSUPPORTED, "%s: slopes[%d] must not exceed %d in magnitude", who, k, AE_MAX_SLOPE);
     for (int k = 0; k < d->H_q; ++k)
       if (!(std::fabs((double)d->slopes[k] / d->scale) < 1e30)) return fail(AE_ERR_INVALID_ARG, "%s: slopes[%d] must be below 10^30 times the scale", who, k);
   }

@@ -491,3 +491,20 @@ def test_strides_of_spans_that_do_not_matter(A):
     two = spans_tensor(*spans_of("causal", 2, 40, 40))
     with pytest.raises(ValueError):  # where they matter they have to be the same
         A.span_attention_forward(*(t.expand(2, -1, -1, -1) for t in (Q, K, V)), scale=0.1, mask="spans", spans=(two[0], two[1][:1].expand(2, 40)))
+
+
+@pytest.mark.parametrize("dims", DIMS)
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("L_q,L_k", [(300, 300), (90, 333)])
+def test_the_steepest_slopes(A, dims, cap, L_q, L_k):
+    """Every row sees its own key, which (and the nearest ones) has the weight: the statistic is off by 2^-22 of the slope times 128 at most, and of
+    slope times distance, 40 for the keys that weigh more than e^-40 with the scores' own differences."""
+    slopes = [128.0, 31.0, 4.0, 0.5]
+    Q, K, V, dO = rows(1, 1, 4, L_q, dims[0]), rows(2, 1, 2, L_k, dims[0]), rows(3, 1, 2, L_k, dims[1]), rows(4, 1, 4, L_q, dims[1])
+    for mask in ("causal", "none"):
+        begin, end = spans_of(mask, 1, L_q, L_k)
+        _, stats = run_forward(A, Q, K, V, begin, end, mask=mask, cap=cap, slopes=slopes, out_dtype=torch.float32)
+        _, lse, _ = span_attention(host(Q), host(K), host(V), begin, end, scale=dims[0] ** -0.5, cap=cap, slopes=slopes)
+        e = score_error(Q, K, dims[0] ** -0.5, cap, None, 0) + 2.0 ** -22 * (128 * np.array(slopes) + 40)
+        assert np.all(np.abs(host(stats) - lse) <= (e[:, None] + 2.0 ** -20 * (1 + np.abs(lse))))
+        run_backward(A, Q, K, V, dO, begin, end, mask=mask, cap=cap, slopes=slopes)

@@ -244,3 +244,10 @@ def test_constants_of_accepted_caps(tmp_path):
             value = s * sum(x * (s * s) ** n for n, x in enumerate(c))
             assert np.all(np.abs(value - want) <= 3e-7 * np.abs(want) + 1e-44 * s), (scale, cap)
     assert accepted > 400
+
+
+@built
+def test_steep_slopes_are_refused(A):
+    for slopes in ([0.0, 128.5, 0.0, 0.0], [-1e3] * 4, [0.0, 0.0, 0.0, 1e20]):
+        refused(A, 2, A.ae_span_create, **{**SPAN, "slopes": slopes})
+    A.ae_span_destroy(A.ae_span_create(**{**SPAN, "slopes": [128.0, -128.0, 0.0, 1.0]}))

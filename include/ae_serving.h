@@ -179,7 +179,8 @@ ae_status_t ae_cached_create(const ae_cache_t *cache, const ae_cached_desc_t *de
  * 32-bit numbers; 0: no cap), less slopes[h] times the distance |place of the token - place of the key| in the list (a prefix in front of it; token t
  * of the newest is at place prefix_length + lengths[b] - n_new + t, also where lengths[b] < n_new puts that into the prefix or in front of it)
  * where slopes (host, [H_q] finite numbers, copied; H_q <= 256; max_length + prefix_length <= 2^24) are given.  They are formed in fp32: a capped score
- * has a relative error of 3e-7 up to 0.6 of the cap (less of it where |scale| / cap is below 1.2e-4, as in ae_span_forward) and an absolute one of 2e-7 of the cap beyond.  A prefix is walked in the own keys' launch here: AE_ERR_UNSUPPORTED where a
+ * has a relative error of 3e-7 up to 0.6 of the cap (less of it where |scale| / cap is below 1.2e-4, as in ae_span_forward, or everywhere one of the cap's size) and an absolute one of 2e-7 of the cap beyond; with slopes the score of a key at distance x carries an
+ * error of up to 2^-21 |slope| x besides, which counts where far keys have weight: under a negative slope.  A prefix is walked in the own keys' launch here: AE_ERR_UNSUPPORTED where a
  * sequence has more than 32 rows for a k/v head (n_new * H_q / H_kv) or the batch more than 2048; name the prefix's pages in every list then. */
 ae_status_t ae_cached_create_scored(const ae_cache_t *cache, const ae_cached_desc_t *desc, float cap, const float *slopes, ae_cached_t **out);
 ae_status_t ae_cached_workspace_bytes(const ae_cached_t *h, size_t *bytes);

@@ -77,7 +77,10 @@ ae_status_t ae_span_create(const ae_span_desc_t *desc, ae_span_t **out);
  * sum_j p_j |v_j| of the exact one, and a bf16 output is rounded once more.  A capped score has a relative error of 3e-7 up to 0.6
  * of the cap (0.2, 0.1, 0.03 and 5e-4 of it where |scale| / cap is below 1.2e-4, 8e-6, 6e-8 and 7e-13) and an absolute one of 2e-7 of the cap beyond, or
  * everywhere where |scale| / cap is above 4e3 (caps up to 10^6; with larger ones sooner) and where |q . k| is above 10^18.  With
- * slopes a row's weights may be held at 2^-80 of their size: products with values below 2^-40 in magnitude can be lost then.          */
+ * slopes the score of a key at distance x carries an error of up to 2^-21 |slope| (64 + x) besides, its weight as much of itself, and the statistic that of the keys
+ * with most weight: an output is within (2^-8 + 2^-20 |slope| (64 + x)) sum_j p_j |v_j|.  For near keys that is next to nothing at usual slopes (3e-5 at 1) and 2^-8 at the
+ * steepest; where rows see far keys alone, or the slope is negative, far keys count (measured at slope 1 and x = 65536: statistics are off by up to 8e-3, a quarter of that bound).
+ * And a row's weights may be held at 2^-80 of their size with slopes: products with values below 2^-40 in magnitude can be lost then.          */
 ae_status_t ae_span_forward(const ae_span_t *h, const void *Q, const void *K, const void *V, const int32_t *key_begin,
                             const int32_t *key_end, int64_t span_stride, void *O, float *stats, hipStream_t stream);
 
@@ -97,6 +100,7 @@ ae_status_t ae_span_forward_split(const ae_span_t *h, const void *Q, const void 
  *   dQ, dK, dV device, contiguous, fp32 or bf16 (grad_dtype), 16-byte aligned, every element is written;
  *   workspace  device, 16-byte aligned, ae_span_backward_workspace_bytes, needs no initialisation.  Calls that share it must not overlap.
  * Two or three launches.  P and dS are rounded once to bf16 for the products.
+ * With slopes P carries the relative error of the statistic that the forward pass wrote and of its own scores, each as above.
  * With O in bf16 its rounding enters dO . O: where a row sees few keys, dP - dO . O is a small difference of larger numbers, so
  * keep O in fp32 where such rows' gradients matter.                                                                    */
 ae_status_t ae_span_backward_workspace_bytes(const ae_span_t *h, size_t *bytes);

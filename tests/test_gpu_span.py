@@ -508,3 +508,16 @@ def test_the_steepest_slopes(A, dims, cap, L_q, L_k):
         e = score_error(Q, K, dims[0] ** -0.5, cap, None, 0) + 2.0 ** -22 * (128 * np.array(slopes) + 40)
         assert np.all(np.abs(host(stats) - lse) <= (e[:, None] + 2.0 ** -20 * (1 + np.abs(lse))))
         run_backward(A, Q, K, V, dO, begin, end, mask=mask, cap=cap, slopes=slopes)
+
+
+@pytest.mark.parametrize("dims", DIMS)
+@pytest.mark.parametrize("score", [dict(), dict(cap=12.0)])
+def test_rows_that_see_far_keys_alone(A, dims, score):
+    """Spans 65536 keys away, next to each other and not, under slopes: errors of 2^-22 slope (L_q + L_k) of a score, as the bounds above have it."""
+    L_q, L_k = 70, 66000
+    Q, K, V, dO = rows(1, 1, 2, L_q, dims[0]), rows(2, 1, 1, L_k, dims[0]), rows(3, 1, 1, L_k, dims[1]), rows(4, 1, 2, L_q, dims[1])
+    begin = np.where(np.arange(L_q) % 2, 100, 20)[None]
+    end = begin + 1 + 3 * np.arange(L_q)
+    kw = dict(score, slopes=[1.0, -0.25])
+    run_forward(A, Q, K, V, begin, end, out_dtype=torch.float32, **kw)
+    run_backward(A, Q, K, V, dO, begin, end, **kw)

@@ -5,7 +5,9 @@
 //
 // A workgroup has a list: the least key that stays is found digit by digit from the top, by histograms in LDS, and the moves are
 // written down.  Rows are then copied by the same workgroup, or, where there can be many for each of a few lists, by a second launch.
-// (Bit by bit with counts in registers, two barriers a bit: the selection 19.6 us instead of 11 for 128 lists of 1100 entries, 47.6 instead of 28 for 64 of 16384.)
+// (Bit by bit with counts in registers, two barriers a bit: the selection 19.6 us instead of 11 for 128 lists of 1100 entries, 47.6 instead of 28 for 64 of 16384,
+// 24 by now.  With sixteen entries a thread the unrolled ballots need more scalar registers than there are, 119 of them go through the lanes of a vector register; longer
+// lists are read again for every digit and walk: 8 lists of 65536 to 8192 in bf16 187 us with their moves, of 16384 to 2048 25.)
 #include "cache_weights.hpp"
 
 #include "cached_attn.hpp"

@@ -18,9 +18,10 @@ struct CapParams {
 };
 // |y| up to kCapSeries: tanh(y) = y P(y^2), P of degree four, least largest relative error (7.3e-8, less than an ulp of the result).  With the powers of
 // scale / cap in the coefficients it is a chain of six multiplications and additions, the last one with what is added to the score; the exact form, 1 - 2 / (1 +
-// e^(2 y)), has two instructions at a quarter of the rate (44 clocks a wavefront against 24) and an error of 1e-7 of the cap rather than of the score.  Scores
-// beyond 0.6 of the cap are rare in what it is for.  (With y formed first, an instruction more: backward 2 x 32/8 x 4096
-// causal, 128/128 1135 us for 1115; forward 361 for 353.)
+// e^(2 y)), has two instructions at a quarter of the rate (44 clocks a wavefront against 24) and an error of 1e-7 of the cap rather than of the score.  Where one score of a
+// sub-tile is beyond 0.6 of the cap, all of its scores take both forms.  Causal 2 x 32/8 x 4096 of 128/128 with a cap of 50, us, forward and backward: no score beyond
+// 374, 1181; one key in 32 with most of its scores beyond 607, 1456; nearly all scores beyond 619, 1519; without a cap 284, 991.  (With y formed first, an instruction
+// more: backward 1135 for 1115; forward 361 for 353, on another card.)
 constexpr float kCapSeries = 0.6f;
 constexpr float kCapPoly[5] = {0.9999999268711602f, -0.33332309980430974f, 0.1331017369802445f, -0.05210148086945954f, 0.015475427532193886f};
 inline CapParams cap_params(float scale, float cap) {
